@@ -56,6 +56,7 @@ extern "C" {
 #define ZIPVL_OP_DECODE_Q       6  /* dims->n = cap_hi + cap_lo + cap_tail */
 #define ZIPVL_OP_SCORE_ALL_ROWS 7
 #define ZIPVL_OP_DECODE_STEP    8  /* dims->n = cap */
+#define ZIPVL_OP_DECODE_PAGED   9  /* dims->n = table_pages * page, m = prefix_pages * page (0: no prefixes) */
 
 /* flags of zipvl_sparse_prefill */
 #define ZIPVL_OUT_FULL            0  /* O is [B,Hq,n,d]; rows of dropped tokens are written as zeros */
@@ -296,6 +297,87 @@ int zipvl_decode_attn_q(const void* q, const zipvl_qtensor* Kq, const zipvl_qten
                         const int32_t* len_hi, const int32_t* len_lo, int32_t cap_hi, int32_t cap_lo,
                         const void* K_tail, const void* V_tail, const int32_t* len_tail, int32_t cap_tail,
                         const zipvl_dims* dims, float softmax_scale, void* o, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rotary positions with one or several axes (one for text; frame, row and column for images and video), in front of
+ * zipvl_score: pair i of a row's channels is turned by the angle pos[axis[i], b, t] * freq[i],
+ *   (x, y) -> (x cos - y sin, x sin + y cos),
+ * channels that no pair has (from 2 * pairs) are copied.  [host], read before the call returns.
+ */
+#define ZIPVL_MAX_AXES  4
+#define ZIPVL_MAX_PAIRS 64
+#define ZIPVL_ROPE_HALVES     0   /* pair i = channels i and i + pairs */
+#define ZIPVL_ROPE_NEIGHBOURS 1   /* pair i = channels 2 i and 2 i + 1 */
+typedef struct zipvl_rope {
+    int32_t axes;                     /* rows of pos: 1 .. ZIPVL_MAX_AXES */
+    int32_t pairs;                    /* a multiple of 8, 2 * pairs <= d */
+    int32_t layout;                   /* ZIPVL_ROPE_HALVES | ZIPVL_ROPE_NEIGHBOURS */
+    int32_t reserved;                 /* 0 */
+    double  freq[ZIPVL_MAX_PAIRS];    /* radians a position, within 2 pi of zero */
+    int32_t axis[ZIPVL_MAX_PAIRS];    /* the row of pos that pair i goes by */
+} zipvl_rope;
+
+/* flag of zipvl_rotate */
+#define ZIPVL_ROTATE_INVERSE 1        /* by the opposite angles: takes a rotation back; also its gradient */
+
+/*
+ * The queries and keys of a layer, rotated.  Q [B,Hq,n,d] by dims->q_strides, K [B,Hkv,n,d] by dims->k_strides; one of the two may be NULL
+ * (and its output with it).  Qo, Ko are laid out by the q_strides and k_strides of `out` (its other fields are not looked at; NULL = as Q and K):
+ * no element twice.  Qo may be Q and Ko may be K (with the same strides); outputs that overlap inputs in any other way are not.
+ * pos [device] [axes, B, n] int32 contiguous, any values.  B * n < 2^30.
+ * Numerics: angles are good to 2e-9 radians plus 1e-9 of a position beyond 2^24 (whole turns are dropped before anything is rounded), sines and
+ * cosines to 1e-7, products and sums in fp32, one rounding at the end.
+ */
+int zipvl_rotate(const void* Q, const void* K, const zipvl_dims* dims, const int32_t* pos, const zipvl_rope* rope, int flags,
+                 void* Qo, void* Ko, const zipvl_dims* out, void* stream);
+
+/*
+ * A KV cache in pages.  K, V [device] [num_pages, page, d] contiguous, 16-byte aligned; page = 16, 32, 64, 128 or 256 rows.  A page holds rows
+ * of one unit, or of one (prefix, KV head); row r of it stands in page table[r / page] at r % page.  A table is [device] int32 [units, table_pages]
+ * contiguous.  Entries of a table outside [0, num_pages) stand for no page: their rows are not written and not attended to.
+ */
+typedef struct zipvl_pages {
+    void* K;
+    void* V;
+    int32_t num_pages;
+    int32_t page;
+} zipvl_pages;
+
+/*
+ * Rows into a paged cache, the keys (and queries) rotated on the way: zipvl_kv_append and zipvl_compact_kv for pages, for one new token of
+ * every batch element, pieces of prompts, or the tokens that a layer keeps.
+ * Unit u = b*Hkv + g brings c = k[u] rows (k NULL: all n; clamped to [0, n]); row i is token t = idx[u, i] (idx NULL: t = i; idx needs k) and
+ * becomes row start[u] + i of the unit:
+ *   K row <- rotate(K[b,g,t]) at pos[:, b, t] (rope NULL: as it is, pos is then not looked at),  V row <- V[b,g,t]
+ *   len[u] = min(start[u] + c, table_pages * page)
+ * Rows behind the table's end are not written; start is clamped to [0, table_pages * page].  len may be start itself.
+ * Q (may be NULL; not with idx): Qo[b,h,i] = rotate(Q[b,h,i]) for i < c of the unit of head h; Qo [B,Hq,n,d] contiguous, may be Q; rows from c are left
+ * as they are.
+ * K, V, Q by dims' strides; start, len [device] int32 [B*Hkv]; flags: 0 or ZIPVL_T_PER_BATCH (idx [B,n], k [B]).  Two units whose new
+ * rows fall into one page's same rows race.  B * n < 2^30.  Numerics of the rotation as for zipvl_rotate; V and unrotated K are bit copies.
+ * One launch; two where len is start and n > 1.
+ */
+int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, const int32_t* idx, const int32_t* k,
+                       const int32_t* pos, const zipvl_rope* rope, const zipvl_pages* pages, const int32_t* table, int32_t table_pages,
+                       const int32_t* start, int32_t* len, const void* Q, void* Qo, int flags, void* stream);
+
+/*
+ * Decode attention (Eq. (5) / Algorithm 2) over pages, for a batch whose elements share long prefixes (questions about one image or video):
+ *   o[b,h] = softmax( q[b,h] . [Kp ; Ko]^T * softmax_scale ) [Vp ; Vo]
+ * with Ko, Vo the first len[u] rows of the unit u = b*Hkv + g by table [B*Hkv, table_pages], and Kp, Vp the first prefix_len[p*Hkv + g] rows
+ * by prefix_table [groups*Hkv, prefix_pages] of the group p that b is in.  Group p is the batch elements group_begin[p] .. group_begin[p+1] - 1
+ * (group_begin [device] int32 [groups + 1], ascending within [0, B]); elements in no group have no prefix.  The rows of a prefix are
+ * read once for all queries of a group (once for every 64 of them, where there are more).
+ * groups = 0: nothing is shared (prefix_table, prefix_len, group_begin are not looked at).  groups <= B.
+ * Lengths are clamped to [0, pages of the table * page]; a head without any row gets zeros.  Nothing behind a length is read.
+ * q, o [device] [B*Hq, d] contiguous; G = Hq/Hkv <= 32.  Rows that are attended to must be finite.
+ * ws [device] zipvl_workspace_bytes(ZIPVL_OP_DECODE_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that
+ * overlap on one workspace race).
+ */
+int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len,
+                            const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len,
+                            const int32_t* group_begin, int32_t groups, const zipvl_dims* dims, float softmax_scale,
+                            void* o, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

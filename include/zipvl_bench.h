@@ -41,7 +41,12 @@ extern "C" {
 #define ZIPVL_K_PROBE_READ     18
 #define ZIPVL_K_DECODE_STEP    19
 #define ZIPVL_K_SELECT_HIST    20
-#define ZIPVL_K_COUNT          21
+#define ZIPVL_K_ROTATE         21
+#define ZIPVL_K_PAGED_APPEND   22
+#define ZIPVL_K_PAGED_ADVANCE  23
+#define ZIPVL_K_PAGED_PARTIAL  24
+#define ZIPVL_K_PAGED_COMBINE  25
+#define ZIPVL_K_COUNT          26
 int zipvl_timing_enable(int on);
 int zipvl_timing_read(int kernel_id, double* total_ms, int* launches);
 

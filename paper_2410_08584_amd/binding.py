@@ -17,10 +17,14 @@ _LIB_NAME = "libzipvl.so"
 OUT_FULL, OUT_COMPACT, KV_ALREADY_COMPACT, T_PER_BATCH = 0, 1, 2, 4
 SCORE_PER_QHEAD = 1
 SELECT_NEGATIVE, SELECT_NONFINITE, SELECT_OVERFLOW = 1, 2, 4
-OP_SCORE, OP_SELECT, OP_SPARSE_PREFILL, OP_DECODE, OP_QUANTIZE_KV, OP_DECODE_Q, OP_SCORE_ALL_ROWS, OP_DECODE_STEP = 1, 2, 3, 4, 5, 6, 7, 8
+OP_SCORE, OP_SELECT, OP_SPARSE_PREFILL, OP_DECODE, OP_QUANTIZE_KV, OP_DECODE_Q, OP_SCORE_ALL_ROWS, OP_DECODE_STEP, OP_DECODE_PAGED = 1, 2, 3, 4, 5, 6, 7, 8, 9
+ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
+ROTATE_INVERSE = 1
+MAX_AXES, MAX_PAIRS = 4, 64
 
 EXPORTS = ("zipvl_version", "zipvl_last_error", "zipvl_workspace_bytes", "zipvl_score", "zipvl_select",
            "zipvl_score_all_rows", "zipvl_share_scores", "zipvl_quantize_kv", "zipvl_decode_attn_q", "zipvl_sparse_prefill", "zipvl_compact_kv", "zipvl_kv_append", "zipvl_decode_attn", "zipvl_decode_attn_static", "zipvl_decode_step",
+           "zipvl_rotate", "zipvl_paged_append", "zipvl_decode_attn_paged",
            "zipvl_timing_enable", "zipvl_timing_read", "zipvl_probe_mfma", "zipvl_probe_stream_read")
 
 
@@ -39,6 +43,34 @@ class Dims(C.Structure):
 class QTensor(C.Structure):
     """zipvl_qtensor: one tensor (K or V) of the mixed-precision cache."""
     _fields_ = [("hi_codes", C.c_void_p), ("hi_params", C.c_void_p), ("lo_codes", C.c_void_p), ("lo_params", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    """zipvl_rope: which channels are pairs, and how far a position turns each.  freqs: radians a position of every pair (a multiple of 8 of them, at
+    most d / 2); axes: the row of pos that each pair goes by (None: one axis for all); layout: pair i = channels i and i + pairs
+    (ROPE_HALVES) or 2 i and 2 i + 1 (ROPE_NEIGHBOURS)."""
+    _fields_ = [("axes", C.c_int32), ("pairs", C.c_int32), ("layout", C.c_int32), ("reserved", C.c_int32),
+                ("freq", C.c_double * MAX_PAIRS), ("axis", C.c_int32 * MAX_PAIRS)]
+
+    def __init__(self, freqs: Sequence[float], axes: Optional[Sequence[int]] = None, layout: int = ROPE_HALVES):
+        freqs = [float(f) for f in freqs]
+        axes = [0] * len(freqs) if axes is None else [int(a) for a in axes]
+        if not 0 < len(freqs) <= MAX_PAIRS or len(axes) != len(freqs):
+            raise ZipvlError(-2, f"a rope of {len(freqs)} frequencies and {len(axes)} axes (as many of both, 1 to {MAX_PAIRS})")
+        if min(axes) < 0 or max(axes) >= MAX_AXES:
+            raise ZipvlError(-1, f"axes of a rope are 0 to {MAX_AXES - 1}, got {min(axes)} to {max(axes)}")
+        super().__init__(max(axes) + 1, len(freqs), int(layout), 0, (C.c_double * MAX_PAIRS)(*freqs), (C.c_int32 * MAX_PAIRS)(*axes))
+
+    @classmethod
+    def of_sections(cls, sections: Sequence[int], theta: float = 10000.0, layout: int = ROPE_HALVES) -> "Rope":
+        """Frequencies theta^(-i / pairs) of pairs = sum(sections) pairs, the first sections[0] of them by axis 0, the next by axis 1, ..."""
+        pairs = sum(sections)
+        return cls([theta ** (-i / pairs) for i in range(pairs)], [a for a, s in enumerate(sections) for _ in range(s)], layout)
+
+
+class Pages(C.Structure):
+    """zipvl_pages"""
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("num_pages", C.c_int32), ("page", C.c_int32)]
 
 
 _lib = None
@@ -104,7 +136,12 @@ def load_library():
     lib.zipvl_timing_read.argtypes = [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]
     lib.zipvl_timing_enable.restype = C.c_int
     lib.zipvl_timing_read.restype = C.c_int
-    for name in ("zipvl_score", "zipvl_score_all_rows", "zipvl_select", "zipvl_share_scores", "zipvl_quantize_kv",
+    lib.zipvl_rotate.argtypes = [vp, vp, C.POINTER(Dims), i32p, C.POINTER(Rope), C.c_int, vp, vp, C.POINTER(Dims), vp]
+    lib.zipvl_paged_append.argtypes = [vp, vp, C.POINTER(Dims), i32p, i32p, i32p, C.POINTER(Rope), C.POINTER(Pages), i32p, C.c_int32,
+                                       i32p, i32p, vp, vp, C.c_int, vp]
+    lib.zipvl_decode_attn_paged.argtypes = [vp, C.POINTER(Pages), i32p, C.c_int32, i32p, i32p, C.c_int32, i32p, i32p, C.c_int32,
+                                            C.POINTER(Dims), C.c_float, vp, vp, C.c_size_t, vp]
+    for name in ("zipvl_rotate", "zipvl_paged_append", "zipvl_decode_attn_paged", "zipvl_score", "zipvl_score_all_rows", "zipvl_select", "zipvl_share_scores", "zipvl_quantize_kv",
                  "zipvl_decode_attn_q", "zipvl_sparse_prefill", "zipvl_compact_kv", "zipvl_kv_append", "zipvl_decode_attn",
                  "zipvl_decode_step"):
         getattr(lib, name).restype = C.c_int
@@ -466,10 +503,199 @@ def zipvl_decode_attn_q(q: torch.Tensor, cache: QCache, softmax_scale: float, *,
     return o
 
 
+# ---------------------------------------------------------------- positions and pages
+def _expect(name: str, t: torch.Tensor, shape, dtype=torch.int32):
+    """A contiguous tensor of this shape and type."""
+    if tuple(t.shape) != tuple(shape):
+        raise ZipvlError(-2, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise ZipvlError(-5, f"{name} is {t.dtype}, expected {dtype}")
+    _dense(t)
+
+
+def _rows_like(name: str, t: torch.Tensor, shape, dtype):
+    if tuple(t.shape) != tuple(shape):
+        raise ZipvlError(-2, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise ZipvlError(-5, f"{name} is {t.dtype}, expected {dtype}")
+
+
+def _row_strides(t: Optional[torch.Tensor]) -> Tuple[int, int, int]:
+    """(batch, head, token) strides; an axis of one element has any stride in torch, and here that of a contiguous tensor."""
+    if t is None:
+        return (0, 0, 0)
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ZipvlError(-1, "expected a [B,H,n,d] view with a contiguous last dimension")
+    out, inner = [0, 0, 0], t.shape[3]
+    for a in (2, 1, 0):
+        out[a] = t.stride(a) if t.shape[a] != 1 else inner
+        inner *= t.shape[a]
+    return tuple(out)
+
+
+def _dims_rows(Q, K, V, *, B, Hq, Hkv, n, d, dtype) -> Dims:
+    return Dims.from_buffer_copy(_pack_dims(B, Hq, Hkv, n, d, dtype, *_row_strides(Q), *_row_strides(K), *_row_strides(V)))
+
+
+def _on_device(call, *tensors):
+    """`call(stream)` on the device that all tensors are on, with torch's current stream there."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ZipvlError(-1, f"expected tensors on one GPU, got {sorted(str(x) for x in devices)}")
+    device = next(iter(devices))
+    if device.index == torch.cuda.current_device():
+        _check(call(_stream()))
+    else:
+        with torch.cuda.device(device):
+            _check(call(_stream()))
+
+
+def zipvl_rotate(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], pos: torch.Tensor, rope: Rope, flags: int = 0, *,
+                 Qo: Optional[torch.Tensor] = None, Ko: Optional[torch.Tensor] = None):
+    """(Qo, Ko): Q [B,Hq,n,d] and K [B,Hkv,n,d] (either may be None) turned by pos [axes,B,n]; flags: 0 or ROTATE_INVERSE.  Qo may be Q, Ko may be K."""
+    lib = load_library()
+    ref = Q if Q is not None else K
+    if ref is None:
+        raise ZipvlError(-1, "zipvl_rotate: Q and K are None")
+    if ref.dim() != 4:
+        raise ZipvlError(-2, f"zipvl_rotate: expected [B,H,n,d], got shape {tuple(ref.shape)}")
+    B, _, n, d = ref.shape
+    if Q is not None and K is not None:
+        _rows_like("K", K, (B, K.shape[1], n, d), Q.dtype)
+    _expect("pos", pos, (rope.axes, B, n))
+    if Q is not None and Qo is None:
+        Qo = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if K is not None and Ko is None:
+        Ko = torch.empty(K.shape, dtype=K.dtype, device=K.device)
+    for name, t, like in (("Qo", Qo, Q), ("Ko", Ko, K)):
+        if t is not None and like is not None:
+            _rows_like(name, t, like.shape, like.dtype)
+    Hkv = K.shape[1] if K is not None else Q.shape[1]
+    size = dict(B=B, Hq=Q.shape[1] if Q is not None else Hkv, Hkv=Hkv, n=n, d=d, dtype=_dtype_code(ref))
+    dm, out = _dims_rows(Q, K, None, **size), _dims_rows(Qo, Ko, None, **size)
+    _on_device(lambda stream: lib.zipvl_rotate(_ptr(Q), _ptr(K), C.byref(dm), _ptr(pos), C.byref(rope), int(flags), _ptr(Qo), _ptr(Ko),
+                                               C.byref(out), stream), Q, K, pos, Qo, Ko)
+    return Qo, Ko
+
+
+class PagedCache:
+    """A KV cache in pages: K, V [num_pages, page, d].  Which pages hold the rows of a unit stands in a table, int32 [units, table_pages]."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor):
+        if K.dim() != 3:
+            raise ZipvlError(-2, f"pages of shape {tuple(K.shape)}, expected [num_pages, page, d]")
+        _expect("V", V, K.shape, K.dtype)
+        _dense(K)
+        _dtype_code(K)
+        self.K, self.V = K, V
+        if K.device != V.device:
+            raise ZipvlError(-1, f"pages of K on {K.device}, of V on {V.device}")
+        self.num_pages, self.page, self.d = K.shape
+
+    @classmethod
+    def empty(cls, num_pages: int, page: int, d: int, dtype: torch.dtype, device) -> "PagedCache":
+        return cls(*(torch.empty((num_pages, page, d), dtype=dtype, device=device) for _ in range(2)))
+
+    def struct(self) -> Pages:
+        return Pages(self.K.data_ptr(), self.V.data_ptr(), self.num_pages, self.page)
+
+
+def zipvl_paged_append(K: torch.Tensor, V: torch.Tensor, cache: PagedCache, table: torch.Tensor, start: torch.Tensor, *,
+                       idx: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                       rope: Optional[Rope] = None, Q: Optional[torch.Tensor] = None, Qo: Optional[torch.Tensor] = None,
+                       length: Optional[torch.Tensor] = None, flags: int = 0):
+    """(length, Qo): rows of K, V [B,Hkv,n,d] behind row start[u] of every unit, K (and Q, into Qo) turned by pos [axes,B,n] where rope is given.
+    k: how many rows a unit brings (None: n); idx: which tokens (None: the first k).  length None: start itself is moved on."""
+    lib = load_library()
+    if K.dim() != 4:
+        raise ZipvlError(-2, f"zipvl_paged_append: expected K [B,Hkv,n,d], got shape {tuple(K.shape)}")
+    B, Hkv, n, d = K.shape
+    units = B * Hkv
+    _rows_like("V", V, K.shape, K.dtype)
+    if cache.d != d or cache.K.dtype != K.dtype:
+        raise ZipvlError(-2, f"rows of {d} {K.dtype} into pages of {cache.d} {cache.K.dtype}")
+    if table.dim() != 2:
+        raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [{units}, table_pages]")
+    _expect("table", table, (units, table.shape[1]))
+    if length is None:
+        length = start
+    _expect("start", start, (units,))
+    _expect("length", length, (units,))
+    rows = B if flags & T_PER_BATCH else units
+    if k is not None:
+        _expect("k", k, (rows,))
+    if idx is not None:
+        _expect("idx", idx, (rows, n))
+    if rope is not None:
+        if pos is None:
+            raise ZipvlError(-1, "zipvl_paged_append: rope is given without pos")
+        _expect("pos", pos, (rope.axes, B, n))
+    if Q is not None:
+        if Q.dim() != 4:
+            raise ZipvlError(-2, f"zipvl_paged_append: expected Q [B,Hq,n,d], got shape {tuple(Q.shape)}")
+        _rows_like("Q", Q, (B, Q.shape[1], n, d), K.dtype)
+        if Qo is None:
+            Qo = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        _expect("Qo", Qo, Q.shape, Q.dtype)
+    else:
+        Qo = None
+    dm = _dims_rows(Q, K, V, B=B, Hq=Hkv if Q is None else Q.shape[1], Hkv=Hkv, n=n, d=d, dtype=_dtype_code(K))
+    pages = cache.struct()
+    _on_device(lambda stream: lib.zipvl_paged_append(
+        _ptr(K), _ptr(V), C.byref(dm), _ptr(idx), _ptr(k), _ptr(pos), None if rope is None else C.byref(rope), C.byref(pages), _ptr(table),
+        table.shape[1], _ptr(start), _ptr(length), _ptr(Q), _ptr(Qo), int(flags), stream), K, V, cache.K, table, start, length, idx, k, pos, Q, Qo)
+    return length, Qo
+
+
+def decode_paged_workspace(cache: PagedCache, table: torch.Tensor, prefix_table: Optional[torch.Tensor] = None, *, B: int, Hq: int, Hkv: int) -> torch.Tensor:
+    """A workspace for zipvl_decode_attn_paged over tables of these widths."""
+    dm = dims_of(None, None, None, B=B, Hq=Hq, Hkv=Hkv, n=table.shape[1] * cache.page, d=cache.d, dtype=_dtype_code(cache.K))
+    return _workspace(workspace_bytes(OP_DECODE_PAGED, dm, 0 if prefix_table is None else prefix_table.shape[1] * cache.page), cache.K.device)
+
+
+def zipvl_decode_attn_paged(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, length: torch.Tensor, softmax_scale: float, *,
+                            B: int, Hq: int, Hkv: int, prefix_table: Optional[torch.Tensor] = None, prefix_len: Optional[torch.Tensor] = None,
+                            group_begin: Optional[torch.Tensor] = None, o: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """o [B*Hq, d]: one query per head against the prefix of its batch element's group (prefix_table [groups*Hkv, prefix_pages], prefix_len
+    [groups*Hkv], group_begin [groups+1]; all None: nothing is shared) and the first length[u] rows by table [B*Hkv, table_pages]."""
+    lib = load_library()
+    d, units = cache.d, B * Hkv
+    if table.dim() != 2:
+        raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [{units}, table_pages]")
+    _expect("table", table, (units, table.shape[1]))
+    _expect("length", length, (units,))
+    for name, t in (("q", q), ("o", o)):
+        if t is not None:
+            if t.numel() != B * Hq * d or t.dtype != cache.K.dtype:
+                raise ZipvlError(-2, f"{name} has {t.numel()} elements of {t.dtype}, expected [{B * Hq}, {d}] of {cache.K.dtype}")
+            _dense(t)
+    groups = 0
+    if any(t is not None for t in (prefix_table, prefix_len, group_begin)):
+        if any(t is None for t in (prefix_table, prefix_len, group_begin)):
+            raise ZipvlError(-1, "prefix_table, prefix_len and group_begin must all be given or all be None")
+        groups = group_begin.numel() - 1
+        if prefix_table.dim() != 2:
+            raise ZipvlError(-2, f"prefix_table has shape {tuple(prefix_table.shape)}, expected [{groups * Hkv}, prefix_pages]")
+        _expect("group_begin", group_begin, (groups + 1,))
+        _expect("prefix_table", prefix_table, (groups * Hkv, prefix_table.shape[1]))
+        _expect("prefix_len", prefix_len, (groups * Hkv,))
+    dm = dims_of(None, None, None, B=B, Hq=Hq, Hkv=Hkv, n=max(1, table.shape[1] * cache.page), d=d, dtype=_dtype_code(cache.K))
+    if o is None:
+        o = torch.empty((B * Hq, d), dtype=q.dtype, device=q.device)
+    if ws is None:
+        ws = decode_paged_workspace(cache, table, prefix_table, B=B, Hq=Hq, Hkv=Hkv)
+    pages = cache.struct()
+    _on_device(lambda stream: lib.zipvl_decode_attn_paged(
+        _ptr(q), C.byref(pages), _ptr(table), table.shape[1], _ptr(length), _ptr(prefix_table), 0 if prefix_table is None else prefix_table.shape[1],
+        _ptr(prefix_len), _ptr(group_begin), groups, C.byref(dm), float(softmax_scale), _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), stream),
+        q, cache.K, table, length, prefix_table, prefix_len, group_begin, o, ws)
+    return o
+
+
 KERNELS = ("score_rowstats", "score_colsum", "select", "compact_kv", "kv_append", "zero_fill",
            "pack_kv", "flash_kept", "decode_partial", "decode_combine", "score_rowfinal", "share_scores",
            "token_slots", "quantize_rows", "decode_q_partial", "allrows_lse", "allrows_colsum", "probe_mfma", "probe_read",
-           "decode_step", "select_hist")
+           "decode_step", "select_hist", "rotate", "paged_append", "paged_advance", "paged_partial", "paged_combine")
 
 
 def zipvl_probe_peaks(device="cuda:0", iters: int = 4096, read_mib: int = 4096):

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libzipvl.so")
 PYCALL = os.path.join(HERE, "_pycall.so")          # extension module over libzipvl.so: the calls of a layer without ctypes
-SOURCES = ["zipvl_api.hip", "score.hip", "select.hip", "attn.hip", "compact.hip", "decode.hip", "quant.hip", "allrows.hip", "peaks.hip"]
+SOURCES = ["zipvl_api.hip", "score.hip", "select.hip", "attn.hip", "compact.hip", "decode.hip", "quant.hip", "allrows.hip", "rotate.hip", "paged.hip", "peaks.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          # packed fp32 vector instructions off.  The switch reaches both passes of hipcc (-Xarch_device does not
          # forward options that take an argument); the host pass answers with a harmless "not a recognized

@@ -61,6 +61,17 @@ int launch_decode_attn_q(const void* q, const zipvl_qtensor& Kq, const zipvl_qte
                          const int32_t* len_lo, int32_t cap_hi, int32_t cap_lo, const void* Kt, const void* Vt,
                          const int32_t* len_t, int32_t cap_t, const zipvl_dims& d, float scale, void* o, void* ws, size_t ws_bytes, hipStream_t st);
 
+int launch_rotate(const void* Q, const void* K, const zipvl_dims& d, const int32_t* pos, const zipvl_rope& rope, int flags, void* Qo, void* Ko,
+                  const zipvl_dims& out, hipStream_t st);
+int launch_paged_append(const void* K, const void* V, const zipvl_dims& d, const int32_t* idx, const int32_t* k, const int32_t* pos,
+                        const zipvl_rope* rope, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* start,
+                        int32_t* len, const void* Q, void* Qo, int flags, hipStream_t st);
+
+size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix);       // rows of the tables
+int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* len,
+                             const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin,
+                             int32_t groups, const zipvl_dims& d, float scale, void* o, void* ws, hipStream_t st);
+
 int launch_probe_mfma(int iters, int workgroups, float* out, hipStream_t st);
 int launch_probe_read(const void* src, size_t bytes, int workgroups, uint32_t* out, hipStream_t st);
 

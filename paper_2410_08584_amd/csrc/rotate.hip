@@ -1,0 +1,202 @@
+// Rotary positions of a layer's queries and keys, and the rows that go into a paged cache with the rotation on the way.
+// Both read every row once and write it once: memory, or latency for a few tokens.
+//
+// D / 16 threads have a row, two runs of eight channels each, so that a pair of channels meets in one thread and a rotated row
+// needs nothing from other lanes.  A thread stays with a token while it goes through heads: angles depend on the token alone.
+#include <algorithm>
+#include <cmath>
+
+#include "launch.h"
+#include "rotary.h"
+
+namespace zipvl {
+
+struct Rows { char* base; int64_t b, h, t; };                // a tensor [B, H, n, d]: strides in bytes
+struct RowsIn { const char* base; int64_t b, h, t; };
+
+// Tokens of all batch elements follow each other.  A workgroup has 256 D^-1 16 rows a turn: `tokens` of them (a power of two) of as many
+// heads as that leaves, and goes through the heads from its first in steps of `step`.
+struct Walk {
+    int n, total, tokens_log2, step;                         // total = B n
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void rotate_kernel(RowsIn Q, RowsIn K, Rows Qo, Rows Ko, int Hq, int heads, Walk w,
+                                                     const int32_t* __restrict__ pos, Turns turns)
+{
+    constexpr int kThreads = D / 16;
+    const int slot = threadIdx.x / kThreads, c = threadIdx.x % kThreads;
+    const int token = (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
+    if (token >= w.total) return;
+    const int b = token / w.n, t = token - b * w.n;
+    const Runs runs(c, turns.pairs, turns.neighbours);
+    Angles at;
+    if (runs.first >= 0) at.set(turns, runs.first, pos + token, (int64_t)w.total);
+    for (int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2); h < heads; h += w.step) {
+        const bool query = h < Hq;
+        const int hh = query ? h : h - Hq;
+        const RowsIn& in = query ? Q : K;
+        const Rows& out = query ? Qo : Ko;
+        const T* src = reinterpret_cast<const T*>(in.base + b * in.b + hh * in.h + t * in.t);
+        T* dst = reinterpret_cast<T*>(out.base + b * out.b + hh * out.h + t * out.t);
+        Run<T> ra = load_run(src + runs.a), rb = load_run(src + runs.b);
+        if (runs.first >= 0) turn_runs(ra, rb, at, turns.neighbours);
+        store_run(dst + runs.a, ra);
+        store_run(dst + runs.b, rb);
+    }
+}
+
+struct PagedRows {
+    char *K, *V;
+    int num_pages, page_log2, width;                         // width: pages in a unit's row of the table
+    const int32_t* table;
+    const int32_t* start;
+    int32_t* len;                                            // NULL: another launch leaves it (advance_kernel)
+    const int32_t *idx, *k;
+    int per_batch;
+};
+
+__device__ __forceinline__ int paged_start(const PagedRows& p, int u) { return max(0, min(p.start[u], p.width << p.page_log2)); }
+__device__ __forceinline__ int paged_count(const PagedRows& p, int u, int b, int n) { return p.k ? max(0, min(p.k[p.per_batch ? b : u], n)) : n; }
+__device__ __forceinline__ int paged_len(const PagedRows& p, int start, int count) { return (int)min((int64_t)start + count, (int64_t)p.width << p.page_log2); }
+
+// Heads [0, Hkv) are those of K and V, [Hkv, heads) of Q (as many as are given).
+template <typename T, int D, bool TURN>
+__global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, RowsIn Q, Rows Qo, int Hkv, int G, int heads, Walk w, PagedRows p,
+                                                           const int32_t* __restrict__ pos, Turns turns)
+{
+    constexpr int kThreads = D / 16;
+    const int slot = threadIdx.x / kThreads, c = threadIdx.x % kThreads;
+    const int token = (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
+    if (token >= w.total) return;
+    const int b = token / w.n, i = token - b * w.n;          // row i of what a unit brings
+    const Runs runs(c, TURN ? turns.pairs : 0, TURN ? turns.neighbours : 0);
+    Angles at;
+    bool have = false;
+    for (int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2); h < heads; h += w.step) {
+        const bool query = h >= Hkv;
+        const int g = query ? (h - Hkv) / G : h, u = b * Hkv + g;
+        const int count = paged_count(p, u, b, w.n);
+        const int start = query ? 0 : paged_start(p, u);     // only the threads of a row of K may read it: len may stand there
+        if (!query && i == 0 && c == 0 && p.len) p.len[u] = paged_len(p, start, count);
+        if (i >= count) continue;
+        const int t = p.idx ? max(0, min(p.idx[(int64_t)(p.per_batch ? b : u) * w.n + i], w.n - 1)) : i;
+        if (TURN && runs.first >= 0 && (p.idx || !have)) {
+            at.set(turns, runs.first, pos + (int64_t)b * w.n + t, (int64_t)w.total);
+            have = true;
+        }
+        if (query) {
+            const T* src = reinterpret_cast<const T*>(Q.base + b * Q.b + (h - Hkv) * Q.h + t * Q.t);
+            T* dst = reinterpret_cast<T*>(Qo.base + b * Qo.b + (h - Hkv) * Qo.h + t * Qo.t);
+            Run<T> ra = load_run(src + runs.a), rb = load_run(src + runs.b);
+            if (TURN && runs.first >= 0) turn_runs(ra, rb, at, turns.neighbours);
+            store_run(dst + runs.a, ra);
+            store_run(dst + runs.b, rb);
+            continue;
+        }
+        const int64_t row = (int64_t)start + i;
+        if (row >> p.page_log2 >= p.width) continue;         // behind the table
+        const int page = p.table[(int64_t)u * p.width + (row >> p.page_log2)];
+        if ((unsigned)page >= (unsigned)p.num_pages) continue;
+        const int64_t at_row = (((int64_t)page << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * D;
+        const T* ks = reinterpret_cast<const T*>(K.base + b * K.b + g * K.h + t * K.t);
+        const T* vs = reinterpret_cast<const T*>(V.base + b * V.b + g * V.h + t * V.t);
+        Run<T> ra = load_run(ks + runs.a), rb = load_run(ks + runs.b);
+        const Run<T> va = load_run(vs + runs.a), vb = load_run(vs + runs.b);
+        if (TURN && runs.first >= 0) turn_runs(ra, rb, at, turns.neighbours);
+        T *kd = reinterpret_cast<T*>(p.K) + at_row, *vd = reinterpret_cast<T*>(p.V) + at_row;
+        store_run(kd + runs.a, ra);
+        store_run(kd + runs.b, rb);
+        store_run(vd + runs.a, va);
+        store_run(vd + runs.b, vb);
+    }
+}
+
+// len of every unit, where it stands in the place of start and several workgroups of the append read that
+__global__ __launch_bounds__(256) void advance_kernel(PagedRows p, int32_t* len, int units, int Hkv, int n) {
+    const int u = blockIdx.x * 256 + threadIdx.x;
+    if (u < units) len[u] = paged_len(p, paged_start(p, u), paged_count(p, u, u / Hkv, n));
+}
+
+static Turns turns_of(const zipvl_rope* r, bool inverse) {
+    Turns t = {};
+    if (!r) return t;
+    t.pairs = r->pairs;
+    t.neighbours = r->layout == ZIPVL_ROPE_NEIGHBOURS;
+    t.backwards = inverse ? 0x80000000u : 0u;
+    for (int i = 0; i < r->pairs; ++i) {
+        const long double turns = (long double)r->freq[i] / 6.283185307179586476925286766559005768L;
+        const long double part = turns - floorl(turns);                              // [0, 1]
+        t.turn[i] = part < 1.0L ? (uint64_t)(part * 18446744073709551616.0L) : 0;
+        t.axis[i] = (uint8_t)r->axis[i];
+    }
+    return t;
+}
+
+static RowsIn rows_in(const void* p, const int64_t (&s)[3], int e) { return {(const char*)p, s[0] * e, s[1] * e, s[2] * e}; }
+static Rows rows_out(void* p, const int64_t (&s)[3], int e) { return {(char*)p, s[0] * e, s[1] * e, s[2] * e}; }
+
+static dim3 walk_of(const zipvl_dims& d, int heads, Walk& w) {
+    const int rows = 4096 / d.d;                             // of a workgroup, a turn
+    w.n = d.n;
+    w.total = d.B * d.n;
+    w.tokens_log2 = 0;
+    while ((1 << w.tokens_log2) < rows && (1 << w.tokens_log2) < w.total) ++w.tokens_log2;
+    const int lanes = rows >> w.tokens_log2, tiles = (w.total + (1 << w.tokens_log2) - 1) >> w.tokens_log2;
+    const int most = (heads + lanes - 1) / lanes;
+    const int parts = std::max(1, std::min(most, (2048 + tiles - 1) / tiles));
+    w.step = parts * lanes;
+    return dim3(tiles, parts);
+}
+
+int launch_rotate(const void* Q, const void* K, const zipvl_dims& d, const int32_t* pos, const zipvl_rope& rope, int flags, void* Qo, void* Ko,
+                  const zipvl_dims& out, hipStream_t st)
+{
+    const int e = d.dtype == ZIPVL_BF16 ? 2 : 4;
+    const int Hq = Q ? d.Hq : 0, heads = Hq + (K ? d.Hkv : 0);
+    Walk w;
+    const dim3 grid = walk_of(d, heads, w);
+    const Turns turns = turns_of(&rope, flags & ZIPVL_ROTATE_INVERSE);
+    KernelTimer tm(ZIPVL_K_ROTATE, st);
+#define ZIPVL_ROTATE(T, D)                                                                                                         \
+    hipLaunchKernelGGL((rotate_kernel<T, D>), grid, dim3(256), 0, st, rows_in(Q, d.q_strides, e), rows_in(K, d.k_strides, e), \
+                       rows_out(Qo, out.q_strides, e), rows_out(Ko, out.k_strides, e), Hq, heads, w, pos, turns)
+    if (d.dtype == ZIPVL_BF16) { if (d.d == 128) ZIPVL_ROTATE(__bf16, 128); else ZIPVL_ROTATE(__bf16, 64); }
+    else { if (d.d == 128) ZIPVL_ROTATE(float, 128); else ZIPVL_ROTATE(float, 64); }
+#undef ZIPVL_ROTATE
+    return check_launch("rotate");
+}
+
+int launch_paged_append(const void* K, const void* V, const zipvl_dims& d, const int32_t* idx, const int32_t* k, const int32_t* pos,
+                        const zipvl_rope* rope, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* start,
+                        int32_t* len, const void* Q, void* Qo, int flags, hipStream_t st)
+{
+    const int e = d.dtype == ZIPVL_BF16 ? 2 : 4;
+    const int heads = d.Hkv + (Q ? d.Hq : 0);
+    Walk w;
+    const dim3 grid = walk_of(d, heads, w);
+    const Turns turns = turns_of(rope, false);
+    const bool in_place = len == start && d.n > 1;           // one token: the threads that read a start are one wave, and its store comes after
+    PagedRows p = {(char*)pages.K, (char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table_pages, table, start, in_place ? nullptr : len,
+                   idx, k, (flags & ZIPVL_T_PER_BATCH) ? 1 : 0};
+    const int64_t qo[3] = {(int64_t)d.Hq * d.n * d.d, (int64_t)d.n * d.d, d.d};
+    {
+        KernelTimer tm(ZIPVL_K_PAGED_APPEND, st);
+#define ZIPVL_APPEND(T, D, TURN)                                                                                                           \
+    hipLaunchKernelGGL((paged_append_kernel<T, D, TURN>), grid, dim3(256), 0, st, rows_in(K, d.k_strides, e), rows_in(V, d.v_strides, e),  \
+                       rows_in(Q, d.q_strides, e), rows_out(Qo, qo, e), d.Hkv, d.Hq / d.Hkv, heads, w, p, pos, turns)
+#define ZIPVL_APPEND_T(T, D) do { if (rope) ZIPVL_APPEND(T, D, true); else ZIPVL_APPEND(T, D, false); } while (0)
+        if (d.dtype == ZIPVL_BF16) { if (d.d == 128) ZIPVL_APPEND_T(__bf16, 128); else ZIPVL_APPEND_T(__bf16, 64); }
+        else { if (d.d == 128) ZIPVL_APPEND_T(float, 128); else ZIPVL_APPEND_T(float, 64); }
+#undef ZIPVL_APPEND_T
+#undef ZIPVL_APPEND
+    }
+    const int rc = check_launch("paged_append");
+    if (rc || !in_place) return rc;
+    const int units = d.B * d.Hkv;
+    KernelTimer tm(ZIPVL_K_PAGED_ADVANCE, st);
+    hipLaunchKernelGGL(advance_kernel, dim3((units + 255) / 256), dim3(256), 0, st, p, len, units, d.Hkv, d.n);
+    return check_launch("paged_append lengths");
+}
+
+}  // namespace zipvl

@@ -1,6 +1,8 @@
 // C ABI: argument validation and dispatch.  Nothing here touches device data;
 // every check is on the host-visible arguments, and a rejected call launches
 // nothing.
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <mutex>
@@ -112,6 +114,9 @@ size_t zipvl_workspace_bytes(int op, const zipvl_dims* dims, int m) {
         case ZIPVL_OP_DECODE_Q: return decode_workspace_bytes(*dims, dims->n);
         case ZIPVL_OP_SCORE_ALL_ROWS: return allrows_workspace_bytes(*dims);
         case ZIPVL_OP_DECODE_STEP: return decode_step_workspace_bytes(*dims, dims->n);
+        case ZIPVL_OP_DECODE_PAGED:
+            if (m < 0) { set_error(ZIPVL_EINVAL, "zipvl_workspace_bytes: m = %d is negative", m); return 0; }
+            return decode_paged_workspace_bytes(*dims, dims->n, m);
         default: set_error(ZIPVL_EUNSUPPORTED, "zipvl_workspace_bytes: unknown op %d", op); return 0;
     }
 }
@@ -357,6 +362,143 @@ int zipvl_decode_attn_q(const void* q, const zipvl_qtensor* Kq, const zipvl_qten
     if (!aligned16(ws)) return set_error(ZIPVL_EALIGN, "%s: ws is not 16-byte aligned", fn);
     return launch_decode_attn_q(q, *Kq, *Vq, len_hi, len_lo, cap_hi, cap_lo, K_tail, V_tail, len_tail, cap_tail,
                                 *dims, softmax_scale, o, ws, ws_bytes, (hipStream_t)stream);
+}
+
+static int check_rope(const char* fn, const zipvl_rope* r, int d) {
+    if (!r) return set_error(ZIPVL_EINVAL, "%s: rope is NULL", fn);
+    if (r->axes < 1 || r->axes > ZIPVL_MAX_AXES) return set_error(ZIPVL_EINVAL, "%s: rope has %d axes (1 to %d)", fn, r->axes, ZIPVL_MAX_AXES);
+    if (r->pairs < 8 || r->pairs % 8 || 2 * r->pairs > d) return set_error(ZIPVL_ESHAPE, "%s: rope has %d pairs (a multiple of 8 up to d / 2 = %d)", fn, r->pairs, d / 2);
+    if (r->layout != ZIPVL_ROPE_HALVES && r->layout != ZIPVL_ROPE_NEIGHBOURS) return set_error(ZIPVL_EUNSUPPORTED, "%s: unknown layout %d of rope", fn, r->layout);
+    if (r->reserved) return set_error(ZIPVL_EUNSUPPORTED, "%s: reserved field of rope is %d", fn, r->reserved);
+    for (int i = 0; i < r->pairs; ++i) {
+        if (!(std::fabs(r->freq[i]) <= 6.283185307179587)) return set_error(ZIPVL_EINVAL, "%s: freq[%d] = %g is not within 2 pi of zero", fn, i, r->freq[i]);
+        if (r->axis[i] < 0 || r->axis[i] >= r->axes) return set_error(ZIPVL_EINVAL, "%s: axis[%d] = %d is outside [0, %d)", fn, i, r->axis[i], r->axes);
+    }
+    return ZIPVL_OK;
+}
+
+// An output of `sizes` rows of d elements: no element twice (every stride goes past all that the smaller ones cover).
+static int check_apart(const char* fn, const char* what, const int64_t* strides, const int (&sizes)[3], int d) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return strides[a] < strides[b]; });
+    int64_t covered = d;
+    for (int a : order) {
+        if (sizes[a] == 1) continue;
+        if (strides[a] < covered) return set_error(ZIPVL_EINVAL, "%s: rows of %s overlap (stride %lld)", fn, what, (long long)strides[a]);
+        covered = strides[a] * (sizes[a] - 1) + covered;
+    }
+    return ZIPVL_OK;
+}
+
+static int check_tokens(const char* fn, const zipvl_dims& d) {
+    if ((int64_t)d.B * d.n >= (1 << 30)) return set_error(ZIPVL_ESHAPE, "%s: B*n = %lld is not below 2^30", fn, (long long)d.B * d.n);
+    return ZIPVL_OK;
+}
+
+int zipvl_rotate(const void* Q, const void* K, const zipvl_dims* dims, const int32_t* pos, const zipvl_rope* rope, int flags,
+                 void* Qo, void* Ko, const zipvl_dims* out, void* stream)
+{
+    const char* fn = "zipvl_rotate";
+    int rc = check_dims(fn, dims, Q != nullptr, K != nullptr, false);
+    if (rc || (rc = check_tokens(fn, *dims)) || (rc = check_rope(fn, rope, dims->d))) return rc;
+    if (!Q && !K) return set_error(ZIPVL_EINVAL, "%s: Q and K are NULL", fn);
+    if ((Q == nullptr) != (Qo == nullptr) || (K == nullptr) != (Ko == nullptr))
+        return set_error(ZIPVL_EINVAL, "%s: Q and Qo, K and Ko must both be given or both be NULL", fn);
+    for (const void* p : {Q, K, (const void*)Qo, (const void*)Ko})
+        if (!aligned16(p)) return set_error(ZIPVL_EALIGN, "%s: Q, K, Qo or Ko is not 16-byte aligned", fn);
+    if (!pos) return set_error(ZIPVL_EINVAL, "%s: pos is NULL", fn);
+    if (reinterpret_cast<uintptr_t>(pos) & 3u) return set_error(ZIPVL_EALIGN, "%s: pos is not 4-byte aligned", fn);
+    if (flags & ~ZIPVL_ROTATE_INVERSE) return set_error(ZIPVL_EUNSUPPORTED, "%s: unknown flags 0x%x", fn, flags);
+    zipvl_dims o = *dims;
+    if (out) {
+        std::copy(out->q_strides, out->q_strides + 3, o.q_strides);
+        std::copy(out->k_strides, out->k_strides + 3, o.k_strides);
+        if ((rc = check_dims(fn, &o, Q != nullptr, K != nullptr, false))) return rc;
+    }
+    if (Q && (rc = check_apart(fn, "Qo", o.q_strides, {o.B, o.Hq, o.n}, o.d))) return rc;
+    if (K && (rc = check_apart(fn, "Ko", o.k_strides, {o.B, o.Hkv, o.n}, o.d))) return rc;
+    auto same = [](const int64_t* a, const int64_t* b) { return std::equal(a, a + 3, b); };
+    if ((Q && Qo == Q && !same(o.q_strides, dims->q_strides)) || (K && Ko == K && !same(o.k_strides, dims->k_strides)))
+        return set_error(ZIPVL_EINVAL, "%s: an output in the place of its input must have its strides", fn);
+    return launch_rotate(Q, K, *dims, pos, *rope, flags, Qo, Ko, o, (hipStream_t)stream);
+}
+
+static int check_pages(const char* fn, const zipvl_pages* p) {
+    if (!p) return set_error(ZIPVL_EINVAL, "%s: pages is NULL", fn);
+    if (!p->K || !p->V) return set_error(ZIPVL_EINVAL, "%s: an array of pages is NULL", fn);
+    if (!aligned16(p->K) || !aligned16(p->V)) return set_error(ZIPVL_EALIGN, "%s: an array of pages is not 16-byte aligned", fn);
+    if (p->num_pages < 1) return set_error(ZIPVL_EINVAL, "%s: num_pages = %d must be positive", fn, p->num_pages);
+    if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1))) return set_error(ZIPVL_ESHAPE, "%s: pages of %d rows (16, 32, 64, 128 or 256)", fn, p->page);
+    return ZIPVL_OK;
+}
+
+static int check_table(const char* fn, const char* what, const int32_t* table, int32_t width, int page) {
+    if (!table) return set_error(ZIPVL_EINVAL, "%s: %s is NULL", fn, what);
+    if (reinterpret_cast<uintptr_t>(table) & 3u) return set_error(ZIPVL_EALIGN, "%s: %s is not 4-byte aligned", fn, what);
+    if (width < 1) return set_error(ZIPVL_EINVAL, "%s: %s of %d pages a unit", fn, what, width);
+    if ((int64_t)width * page > (1 << 24)) return set_error(ZIPVL_ESHAPE, "%s: %s holds %lld rows a unit, more than 2^24", fn, what, (long long)width * page);
+    return ZIPVL_OK;
+}
+
+int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, const int32_t* idx, const int32_t* k, const int32_t* pos,
+                       const zipvl_rope* rope, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* start,
+                       int32_t* len, const void* Q, void* Qo, int flags, void* stream)
+{
+    const char* fn = "zipvl_paged_append";
+    int rc = check_dims(fn, dims, Q != nullptr, true, true);
+    if (rc || (rc = check_tokens(fn, *dims)) || (rc = check_pages(fn, pages)) || (rc = check_table(fn, "table", table, table_pages, pages->page))) return rc;
+    ZIPVL_REQUIRE_PTR(fn, K);
+    ZIPVL_REQUIRE_PTR(fn, V);
+    if (!start || !len) return set_error(ZIPVL_EINVAL, "%s: start / len is NULL", fn);
+    if (rope && (rc = check_rope(fn, rope, dims->d))) return rc;
+    if (rope && !pos) return set_error(ZIPVL_EINVAL, "%s: pos is NULL", fn);
+    if (idx && !k) return set_error(ZIPVL_EINVAL, "%s: idx is given without k", fn);
+    if ((Q == nullptr) != (Qo == nullptr)) return set_error(ZIPVL_EINVAL, "%s: Q and Qo must both be given or both be NULL", fn);
+    if (!aligned16(Q) || !aligned16(Qo)) return set_error(ZIPVL_EALIGN, "%s: Q or Qo is not 16-byte aligned", fn);
+    if (Q && idx) return set_error(ZIPVL_EUNSUPPORTED, "%s: Q together with idx", fn);
+    if (Q && !rope) return set_error(ZIPVL_EINVAL, "%s: Q is given without rope", fn);
+    if (Q && Qo == Q) {
+        const int64_t dense[3] = {(int64_t)dims->Hq * dims->n * dims->d, (int64_t)dims->n * dims->d, dims->d};
+        const int sizes[3] = {dims->B, dims->Hq, dims->n};
+        for (int a = 0; a < 3; ++a)
+            if (sizes[a] > 1 && dims->q_strides[a] != dense[a]) return set_error(ZIPVL_EINVAL, "%s: Qo in the place of a Q that is not contiguous", fn);
+    }
+    if (flags & ~ZIPVL_T_PER_BATCH) return set_error(ZIPVL_EUNSUPPORTED, "%s: unknown flags 0x%x", fn, flags);
+    if ((reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(rope ? pos : nullptr) |
+         reinterpret_cast<uintptr_t>(start) | reinterpret_cast<uintptr_t>(len)) & 3u)
+        return set_error(ZIPVL_EALIGN, "%s: idx, k, pos, start or len is not 4-byte aligned", fn);
+    return launch_paged_append(K, V, *dims, idx, k, pos, rope, *pages, table, table_pages, start, len, Q, Qo, flags, (hipStream_t)stream);
+}
+
+int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len,
+                            const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin,
+                            int32_t groups, const zipvl_dims* dims, float softmax_scale, void* o, void* ws, size_t ws_bytes, void* stream)
+{
+    const char* fn = "zipvl_decode_attn_paged";
+    zipvl_dims d = dims ? *dims : zipvl_dims{};
+    d.n = 1;                                                 // not looked at
+    int rc = check_dims(fn, dims ? &d : nullptr, false, false, false);
+    if (rc || (rc = check_pages(fn, pages)) || (rc = check_table(fn, "table", table, table_pages, pages->page))) return rc;
+    if (d.Hq / d.Hkv > 32) return set_error(ZIPVL_ESHAPE, "%s: %d query heads per KV head (up to 32)", fn, d.Hq / d.Hkv);
+    ZIPVL_REQUIRE_PTR(fn, q);
+    ZIPVL_REQUIRE_PTR(fn, o);
+    if (!len) return set_error(ZIPVL_EINVAL, "%s: len is NULL", fn);
+    if (groups < 0 || groups > d.B) return set_error(ZIPVL_EINVAL, "%s: %d groups of %d batch elements", fn, groups, d.B);
+    if (groups) {
+        if ((rc = check_table(fn, "prefix_table", prefix_table, prefix_pages, pages->page))) return rc;
+        if (!prefix_len || !group_begin) return set_error(ZIPVL_EINVAL, "%s: prefix_len / group_begin is NULL", fn);
+    } else {
+        prefix_table = prefix_len = group_begin = nullptr;
+        prefix_pages = 0;
+    }
+    if ((reinterpret_cast<uintptr_t>(len) | reinterpret_cast<uintptr_t>(prefix_len) | reinterpret_cast<uintptr_t>(group_begin)) & 3u)
+        return set_error(ZIPVL_EALIGN, "%s: len, prefix_len or group_begin is not 4-byte aligned", fn);
+    if (!(softmax_scale > 0.f) || !(softmax_scale < 1e30f)) return set_error(ZIPVL_EINVAL, "%s: softmax_scale must be positive and finite", fn);
+    const size_t need = decode_paged_workspace_bytes(d, table_pages * pages->page, prefix_pages * pages->page);
+    if (!ws || ws_bytes < need) return set_error(ZIPVL_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+    if (!aligned16(ws)) return set_error(ZIPVL_EALIGN, "%s: ws is not 16-byte aligned", fn);
+    return launch_decode_attn_paged(q, *pages, table, table_pages, len, prefix_table, prefix_pages, prefix_len, group_begin, groups, d,
+                                    softmax_scale, o, ws, (hipStream_t)stream);
 }
 
 int zipvl_probe_mfma(int iters, int workgroups, float* out, void* stream)
