@@ -554,6 +554,8 @@ def zipvl_rotate(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], pos: torc
                  Qo: Optional[torch.Tensor] = None, Ko: Optional[torch.Tensor] = None):
     """(Qo, Ko): Q [B,Hq,n,d] and K [B,Hkv,n,d] (either may be None) turned by pos [axes,B,n]; flags: 0 or ROTATE_INVERSE.  Qo may be Q, Ko may be K."""
     lib = load_library()
+    if (Q is None or Qo is not None) and (K is None or Ko is not None) and _called(_native.rotate(Q, K, pos, rope, flags, Qo, Ko)):
+        return Qo, Ko
     ref = Q if Q is not None else K
     if ref is None:
         raise ZipvlError(-1, "zipvl_rotate: Q and K are None")
@@ -607,6 +609,11 @@ def zipvl_paged_append(K: torch.Tensor, V: torch.Tensor, cache: PagedCache, tabl
     """(length, Qo): rows of K, V [B,Hkv,n,d] behind row start[u] of every unit, K (and Q, into Qo) turned by pos [axes,B,n] where rope is given.
     k: how many rows a unit brings (None: n); idx: which tokens (None: the first k).  length None: start itself is moved on."""
     lib = load_library()
+    if length is None:
+        length = start
+    if (Q is None or Qo is not None) and _called(
+            _native.paged_append(K, V, cache, table, start, idx, k, pos, rope, Q, Qo if Q is not None else None, length, flags)):
+        return length, Qo if Q is not None else None
     if K.dim() != 4:
         raise ZipvlError(-2, f"zipvl_paged_append: expected K [B,Hkv,n,d], got shape {tuple(K.shape)}")
     B, Hkv, n, d = K.shape
@@ -617,8 +624,6 @@ def zipvl_paged_append(K: torch.Tensor, V: torch.Tensor, cache: PagedCache, tabl
     if table.dim() != 2:
         raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [{units}, table_pages]")
     _expect("table", table, (units, table.shape[1]))
-    if length is None:
-        length = start
     _expect("start", start, (units,))
     _expect("length", length, (units,))
     rows = B if flags & T_PER_BATCH else units
@@ -659,6 +664,9 @@ def zipvl_decode_attn_paged(q: torch.Tensor, cache: PagedCache, table: torch.Ten
     """o [B*Hq, d]: one query per head against the prefix of its batch element's group (prefix_table [groups*Hkv, prefix_pages], prefix_len
     [groups*Hkv], group_begin [groups+1]; all None: nothing is shared) and the first length[u] rows by table [B*Hkv, table_pages]."""
     lib = load_library()
+    if o is not None and ws is not None and _called(
+            _native.decode_attn_paged(q, cache, table, length, softmax_scale, B, Hq, Hkv, prefix_table, prefix_len, group_begin, o, ws)):
+        return o
     d, units = cache.d, B * Hkv
     if table.dim() != 2:
         raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [{units}, table_pages]")

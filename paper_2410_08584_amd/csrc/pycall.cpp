@@ -8,14 +8,15 @@
 #include <Python.h>
 
 #include <climits>
+#include <cstring>
 
 #include "zipvl.h"
 
 namespace {
 
 PyObject *s_data_ptr, *s_shape, *s_dtype, *s_stride, *s_numel, *s_is_contiguous, *s_hi_codes, *s_hi_params, *s_lo_codes, *s_lo_params, *s_K, *s_V,
-    *s_len_hi, *s_len_lo, *s_cap_hi, *s_cap_lo, *s_d;
-PyObject *g_tensor, *g_f32, *g_bf16, *g_is_initialized, *g_get_device, *g_get_stream;
+    *s_len_hi, *s_len_lo, *s_cap_hi, *s_cap_lo, *s_d, *s_on_device;
+PyObject *g_tensor, *g_f32, *g_bf16, *g_i32, *g_u8, *g_is_initialized, *g_get_device, *g_get_stream;
 
 // An owned reference.
 struct Ref {
@@ -118,12 +119,90 @@ struct Args {
         d.n = narrow(n); d.d = narrow(dim); d.dtype = code;
         return d;
     }
-    void* stream() {                                         // torch's current one
+    // The tensors of positions and pages, which have to be on the current device: an address, with the shape, the type and contiguity checked.
+    long on = -2;                                            // the device of those seen so far
+    void* placed(PyObject* t) {
+        void* v = address(t);
+        if (!ok) return nullptr;
+        Ref r(method(t, s_on_device));
+        const long at = r.p && PyLong_CheckExact(r.p) ? PyLong_AsLong(r.p) : -1;
+        if (at < 0 || (on != -2 && on != at)) ok = false;
+        on = at;
+        return v;
+    }
+    void typed(PyObject* t, PyObject* dtype) {
+        if (!tensor(t)) return;
+        Ref r(PyObject_GetAttr(t, s_dtype));
+        if (r.p != dtype) ok = false;
+    }
+    template <int N> void* array(PyObject* t, PyObject* dtype, const int64_t (&want)[N]) {
+        int64_t s[N] = {};
+        shape(t, s);
+        for (int i = 0; i < N; ++i)
+            if (s[i] != want[i]) ok = false;
+        typed(t, dtype);
+        dense(t);
+        return placed(t);
+    }
+    template <int N> void* ints(PyObject* t, const int64_t (&want)[N]) { return array(t, g_i32, want); }
+    template <int N> void* ints_or_null(PyObject* t, const int64_t (&want)[N]) { return t == Py_None ? nullptr : ints(t, want); }
+    void* table(PyObject* t, int64_t units, int32_t& width) {
+        int64_t s[2] = {};
+        shape(t, s);
+        width = narrow(s[1]);
+        return ints(t, {units, s[1]});
+    }
+    void* rows(PyObject* t, PyObject* dtype, int64_t B, int64_t H, int64_t n, int64_t d, int64_t (&st)[3]) {     // [B, H, n, d], contiguous rows
+        int64_t s[4] = {}, all[4] = {};
+        shape(t, s);
+        if (s[0] != B || s[1] != H || s[2] != n || s[3] != d) ok = false;
+        typed(t, dtype);
+        if (!ok) return nullptr;
+        Ref r(method(t, s_stride));
+        extents(r.p, all);
+        if (all[3] != 1) ok = false;
+        int64_t inner = d;                                   // an axis of one element has any stride in torch, and here that of a contiguous tensor
+        for (int a = 2; a >= 0; --a) {
+            st[a] = s[a] == 1 ? inner : all[a];
+            inner *= s[a];
+        }
+        return placed(t);
+    }
+    zipvl_rope rope(PyObject* o) {                           // a ctypes structure
+        zipvl_rope r = {};
+        Py_buffer b;
+        if (!ok || PyObject_GetBuffer(o, &b, PyBUF_SIMPLE)) { ok = false; return r; }
+        if (b.len == (Py_ssize_t)sizeof r) memcpy(&r, b.buf, sizeof r);
+        else ok = false;
+        PyBuffer_Release(&b);
+        return r;
+    }
+    struct Pool { zipvl_pages pages; int64_t d; PyObject* dtype; };
+    Pool pool(PyObject* cache) {                             // a PagedCache
+        Pool x = {};
+        Ref K(PyObject_GetAttr(cache, s_K)), V(PyObject_GetAttr(cache, s_V));
+        if (!K.p || !V.p) { ok = false; return x; }
+        int64_t s[3] = {};
+        shape(K.p, s);
+        if (!ok) return x;
+        Ref t(PyObject_GetAttr(K.p, s_dtype));
+        if (t.p != g_f32 && t.p != g_bf16) { ok = false; return x; }
+        x.dtype = t.p == g_f32 ? g_f32 : g_bf16;
+        dense(K.p);
+        x.pages.K = placed(K.p);
+        x.pages.V = array(V.p, x.dtype, s);
+        x.pages.num_pages = narrow(s[0]);
+        x.pages.page = narrow(s[1]);
+        x.d = s[2];
+        return x;
+    }
+    void* stream_there() { return stream(true); }            // the current device's, if the tensors are on it
+    void* stream(bool there = false) {                       // torch's current one
         if (!ok) return nullptr;
         Ref up(PyObject_CallNoArgs(g_is_initialized));
         if (up.p != Py_True) { ok = false; return nullptr; }
         Ref device(PyObject_CallNoArgs(g_get_device));
-        if (!device.p) { ok = false; return nullptr; }
+        if (!device.p || (there && PyLong_AsLong(device.p) != on)) { ok = false; return nullptr; }
         Ref s(PyObject_CallOneArg(g_get_stream, device.p));
         if (!s.p) { ok = false; return nullptr; }
         void* v = PyLong_AsVoidPtr(s.p);
@@ -281,9 +360,109 @@ PyObject* decode_attn_q(PyObject*, PyObject* const* a, Py_ssize_t na) {
     });
 }
 
+// (Q, K, pos, rope, flags, Qo, Ko); Q with Qo or K with Ko may be None
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t na) {
+    if (!count_is(na, 7)) return general_way();
+    Args x{a};
+    const bool q = a[0] != Py_None, k = a[1] != Py_None;
+    if ((!q && !k) || q != (a[5] != Py_None) || k != (a[6] != Py_None)) return general_way();
+    zipvl_dims d = {}, out = {};
+    int64_t s[4] = {}, sk[4] = {};
+    x.shape(a[q ? 0 : 1], s);
+    if (k) x.shape(a[1], sk);
+    d.B = x.narrow(s[0]); d.n = x.narrow(s[2]); d.d = x.narrow(s[3]);
+    d.Hkv = x.narrow(k ? sk[1] : s[1]);
+    d.Hq = x.narrow(s[1]);
+    d.dtype = x.dtype(a[q ? 0 : 1]);
+    PyObject* type = d.dtype ? g_bf16 : g_f32;
+    out = d;
+    void *Q = q ? x.rows(a[0], type, s[0], s[1], s[2], s[3], d.q_strides) : nullptr, *Qo = q ? x.rows(a[5], type, s[0], s[1], s[2], s[3], out.q_strides) : nullptr;
+    void *K = k ? x.rows(a[1], type, s[0], sk[1], s[2], s[3], d.k_strides) : nullptr, *Ko = k ? x.rows(a[6], type, s[0], sk[1], s[2], s[3], out.k_strides) : nullptr;
+    const zipvl_rope rope = x.rope(a[3]);
+    void* pos = x.ints(a[2], {(int64_t)rope.axes, s[0], s[2]});
+    const int flags = x.int32(a[4]);
+    void* st = x.stream_there();
+    return finish(x, [&] { return zipvl_rotate(Q, K, &d, (int32_t*)pos, &rope, flags, Qo, Ko, &out, st); });
+}
+
+// (K, V, cache, table, start, idx, k, pos, rope, Q, Qo, length, flags)
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t na) {
+    if (!count_is(na, 13)) return general_way();
+    Args x{a};
+    const bool q = a[9] != Py_None, turned = a[8] != Py_None;
+    if (q != (a[10] != Py_None)) return general_way();
+    zipvl_dims d = {};
+    int64_t s[4] = {}, sq[4] = {};
+    x.shape(a[0], s);
+    if (q) x.shape(a[9], sq);
+    d.B = x.narrow(s[0]); d.Hkv = x.narrow(s[1]); d.n = x.narrow(s[2]); d.d = x.narrow(s[3]);
+    d.Hq = q ? x.narrow(sq[1]) : d.Hkv;
+    d.dtype = x.dtype(a[0]);
+    PyObject* type = d.dtype ? g_bf16 : g_f32;
+    const Args::Pool pool = x.pool(a[2]);
+    if (pool.dtype != type || pool.d != s[3]) return general_way();
+    void *K = x.rows(a[0], type, s[0], s[1], s[2], s[3], d.k_strides), *V = x.rows(a[1], type, s[0], s[1], s[2], s[3], d.v_strides);
+    const int flags = x.int32(a[12]);
+    const int64_t units = s[0] * s[1], sets = flags & ZIPVL_T_PER_BATCH ? s[0] : units;
+    int32_t width = 0;
+    void *table = x.table(a[3], units, width), *start = x.ints(a[4], {units}), *len = a[11] == a[4] ? start : x.ints(a[11], {units});
+    void *idx = x.ints_or_null(a[5], {sets, s[2]}), *k = x.ints_or_null(a[6], {sets});
+    zipvl_rope rope = {};
+    if (turned) rope = x.rope(a[8]);
+    void* pos = turned ? x.ints(a[7], {(int64_t)rope.axes, s[0], s[2]}) : nullptr;
+    void *Q = nullptr, *Qo = nullptr;
+    if (q) {
+        Q = x.rows(a[9], type, s[0], sq[1], s[2], s[3], d.q_strides);
+        Qo = x.array(a[10], type, {s[0], sq[1], s[2], s[3]});
+    }
+    void* st = x.stream_there();
+    return finish(x, [&] {
+        return zipvl_paged_append(K, V, &d, (int32_t*)idx, (int32_t*)k, (int32_t*)pos, turned ? &rope : nullptr, &pool.pages, (int32_t*)table, width,
+                                  (int32_t*)start, (int32_t*)len, Q, Qo, flags, st);
+    });
+}
+
+// (q, cache, table, length, scale, B, Hq, Hkv, prefix_table, prefix_len, group_begin, o, ws)
+PyObject* decode_attn_paged(PyObject*, PyObject* const* a, Py_ssize_t na) {
+    if (!count_is(na, 13)) return general_way();
+    Args x{a};
+    const Args::Pool pool = x.pool(a[1]);
+    const zipvl_dims d = x.step(a[5], a[6], a[7], 1, pool.d, pool.dtype == g_bf16);
+    const float scale = (float)x.real(a[4]);
+    auto heads = [&](PyObject* t) {                          // any contiguous shape of B Hq rows
+        if ((int64_t)x.bytes(t) != (int64_t)d.B * d.Hq * d.d) x.ok = false;
+        x.typed(t, pool.dtype);
+        x.dense(t);
+        return x.placed(t);
+    };
+    void *q = heads(a[0]), *o = heads(a[11]);
+    const int64_t units = (int64_t)d.B * d.Hkv;
+    int32_t width = 0, prefix_width = 0, groups = 0;
+    void *table = x.table(a[2], units, width), *len = x.ints(a[3], {units}), *prefix_table = nullptr, *prefix_len = nullptr, *begin = nullptr;
+    if (a[8] != Py_None || a[9] != Py_None || a[10] != Py_None) {
+        int64_t s[1] = {};
+        x.shape(a[10], s);
+        groups = x.narrow(s[0] - 1);
+        if (groups < 1) x.ok = false;
+        prefix_table = x.table(a[8], (int64_t)groups * d.Hkv, prefix_width);
+        prefix_len = x.ints(a[9], {(int64_t)groups * d.Hkv});
+        begin = x.ints(a[10], {(int64_t)groups + 1});
+    }
+    x.typed(a[12], g_u8);
+    x.dense(a[12]);
+    void* ws = x.placed(a[12]);
+    const size_t ws_bytes = x.bytes(a[12]);
+    void* st = x.stream_there();
+    return finish(x, [&] {
+        return zipvl_decode_attn_paged(q, &pool.pages, (int32_t*)table, width, (int32_t*)len, (int32_t*)prefix_table, prefix_width, (int32_t*)prefix_len,
+                                       (int32_t*)begin, groups, &d, scale, o, ws, ws_bytes, st);
+    });
+}
+
 #define ZIPVL_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ZIPVL_METHOD(score), ZIPVL_METHOD(select), ZIPVL_METHOD(compact_kv), ZIPVL_METHOD(sparse_prefill), ZIPVL_METHOD(kv_append),
-                         ZIPVL_METHOD(decode_step), ZIPVL_METHOD(decode_attn_q), {nullptr, nullptr, 0, nullptr}};
+                         ZIPVL_METHOD(decode_step), ZIPVL_METHOD(decode_attn_q), ZIPVL_METHOD(rotate), ZIPVL_METHOD(paged_append),
+                         ZIPVL_METHOD(decode_attn_paged), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", "Calls of libzipvl.so on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -292,13 +471,13 @@ PyMODINIT_FUNC PyInit__pycall(void) {
     struct { PyObject** at; const char* text; } names[] = {
         {&s_data_ptr, "data_ptr"}, {&s_shape, "shape"}, {&s_dtype, "dtype"}, {&s_stride, "stride"}, {&s_numel, "numel"}, {&s_is_contiguous, "is_contiguous"},
         {&s_hi_codes, "hi_codes"}, {&s_hi_params, "hi_params"}, {&s_lo_codes, "lo_codes"}, {&s_lo_params, "lo_params"}, {&s_K, "K"}, {&s_V, "V"},
-        {&s_len_hi, "len_hi"}, {&s_len_lo, "len_lo"}, {&s_cap_hi, "cap_hi"}, {&s_cap_lo, "cap_lo"}, {&s_d, "d"}};
+        {&s_len_hi, "len_hi"}, {&s_len_lo, "len_lo"}, {&s_cap_hi, "cap_hi"}, {&s_cap_lo, "cap_lo"}, {&s_d, "d"}, {&s_on_device, "get_device"}};
     for (auto& n : names)
         if (!(*n.at = PyUnicode_InternFromString(n.text))) return nullptr;
     Ref torch(PyImport_ImportModule("torch"));
     if (!torch.p) return nullptr;
     struct { PyObject** at; const char *in, *name; } objects[] = {
-        {&g_tensor, nullptr, "Tensor"}, {&g_f32, nullptr, "float32"}, {&g_bf16, nullptr, "bfloat16"}, {&g_is_initialized, "cuda", "is_initialized"},
+        {&g_tensor, nullptr, "Tensor"}, {&g_f32, nullptr, "float32"}, {&g_bf16, nullptr, "bfloat16"}, {&g_i32, nullptr, "int32"}, {&g_u8, nullptr, "uint8"}, {&g_is_initialized, "cuda", "is_initialized"},
         {&g_get_device, "_C", "_cuda_getDevice"}, {&g_get_stream, "_C", "_cuda_getCurrentRawStream"}};
     for (auto& o : objects) {
         Ref in(o.in ? PyObject_GetAttrString(torch.p, o.in) : nullptr);

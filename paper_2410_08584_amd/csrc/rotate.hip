@@ -4,7 +4,6 @@
 // D / 16 threads have a row, two runs of eight channels each, so that a pair of channels meets in one thread and a rotated row
 // needs nothing from other lanes.  A thread stays with a token while it goes through heads: angles depend on the token alone.
 #include <algorithm>
-#include <cmath>
 
 #include "launch.h"
 #include "rotary.h"
@@ -124,9 +123,9 @@ static Turns turns_of(const zipvl_rope* r, bool inverse) {
     t.pairs = r->pairs;
     t.neighbours = r->layout == ZIPVL_ROPE_NEIGHBOURS;
     t.backwards = inverse ? 0x80000000u : 0u;
-    for (int i = 0; i < r->pairs; ++i) {
-        const long double turns = (long double)r->freq[i] / 6.283185307179586476925286766559005768L;
-        const long double part = turns - floorl(turns);                              // [0, 1]
+    for (int i = 0; i < r->pairs; ++i) {                     // in 64-bit significands; a division and floorl of each are 2 us of a call's 4
+        long double part = (long double)r->freq[i] * 0.159154943091895335768883763372514362L;      // 1 / (2 pi); within a turn of zero
+        if (part < 0.0L) part += 1.0L;
         t.turn[i] = part < 1.0L ? (uint64_t)(part * 18446744073709551616.0L) : 0;
         t.axis[i] = (uint8_t)r->axis[i];
     }
