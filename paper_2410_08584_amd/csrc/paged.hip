@@ -1,15 +1,14 @@
 // Decode attention over pages, with prefixes that several batch elements share (Eq. (5); Algorithm 2).
 //
 // Memory-bound for as long as few queries meet a row.  An item is a unit (batch element, KV head) with its own rows and the G queries of its
-// group of heads, or a (prefix, KV head) with the G queries of every batch element that shares it, in blocks of 32: a row of a prefix is read once
-// for 32 queries instead of once for every batch element.  Both are the same work: 32 columns of queries (those that an item lacks are
-// zero) against tiles of 32 rows, S^T = K Q^T and O^T += V^T P^T on 32x32 matrix tiles, so that a lane has one query and the softmax
-// statistics are scalars of a lane.
+// group of heads, or a (prefix, KV head) with the G queries of every batch element that shares it, in blocks of 128: a row of a prefix comes from
+// memory once for 128 queries instead of once for every batch element.  Both are the same work: columns of 32 queries (those that an item
+// lacks are zero) against tiles of 32 rows, S^T = K Q^T and O^T += V^T P^T on 32x32 matrix tiles, so that a lane has one query and the
+// softmax statistics are scalars of a lane.  A wave has 32 columns and tiles of its own in LDS: four waves take four tiles in turn (up to 32
+// queries), two and two the same two (up to 64), or all the same one, which comes from L2 for all but the first.
 //
-// How the work is cut up is decided on the device, where the lengths are: every item weighs its tiles and a little for its start, the weights of all
-// items follow each other on a line, and the workgroups take equal pieces of that line.  However unequal the lengths, no workgroup has more than
-// another; a long item gets many workgroups and several short ones share one.  Every workgroup sums up the weights by itself (B Hkv +
-// groups Hkv lengths, a microsecond), nothing is read back and no launch is spent on it.
+// How the work is cut up is decided on the device, where the lengths are (Line).  Nothing is read back and no launch is spent on it: every
+// workgroup goes over the B Hkv + groups Hkv lengths by itself, a microsecond.
 // Parts (max, sum, weighted sum of rows) of an item that was cut are joined by a second launch.
 #include <algorithm>
 #include <atomic>
@@ -19,10 +18,10 @@
 
 namespace zipvl {
 
-constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4;
-constexpr int kStart = 2;            // what starting an item weighs, in tiles: its queries, its first rows, its part
+constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4, kBlock = kCols * kPartWaves;
+constexpr int kStartPrefix = 8, kStartOwn = 3;       // what starting an item weighs: its queries, its first rows, its part
 constexpr int kLeast = 8;            // weight below which a workgroup is not worth its part
-constexpr int kSolo = 4;             // tiles up to which one wave takes an item alone
+constexpr int kLeastFew = 4;         // the same where every item has workgroups of its own
 constexpr int kPartGrid = 512;       // two workgroups a CU
 constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
 
@@ -33,21 +32,26 @@ struct PagedRead {
     const int32_t* prefix_table; int prefix_width; const int32_t* prefix_len;
     const int32_t* group_begin; int groups;
     int B, Hq, Hkv, G;
+    uint32_t inv_Hkv, inv_G;
+    __device__ __forceinline__ int prefixes() const { return groups * Hkv; }
+    __device__ __forceinline__ int items() const { return (groups + B) * Hkv; }
 };
 
-// Parts: a record is D floats and (max, sum).  Records 2 (b Hq + h) + {0: prefix, 1: own} are those of items that one workgroup had whole;
-// behind them every workgroup has 32 for the piece of an item that began before it and 32 for one that goes on after it.  `pieces` says of
-// every own item and every block of a prefix which workgroups had it.
+// Parts: a record is D floats and (max, sum).  Records 2 (b Hq + h) + {0: prefix, 1: own} are those of items that were not cut.  Behind them are those
+// of pieces: for every workgroup `cols` of a prefix that began before it and as many of one that goes on after it, then for every
+// wave G and G of own items in the same way.  `pieces` says of every own item and every block of a prefix from which to which
+// workgroup, or wave, its pieces are.
 struct Parts {
-    float* o; float* ml; int2* pieces; int rows;             // rows = B Hq
-    __device__ __forceinline__ int64_t whole(int row, int own) const { return 2 * (int64_t)row + own; }
-    __device__ __forceinline__ int64_t piece(int wg, int begins, int col) const { return 2 * (int64_t)rows + ((int64_t)wg * 2 + begins) * kCols + col; }
+    float* o; float* ml; int2* pieces; int rows, cols, G;    // rows = B Hq
+    __device__ __forceinline__ int whole(int row, int own) const { return 2 * row + own; }
+    __device__ __forceinline__ int piece(int own, int who, int begins, int col) const {      // below 2^20
+        return 2 * rows + (own ? 2 * kPartGrid * cols + (who * 2 + begins) * G : (who * 2 + begins) * cols) + col;
+    }
 };
-// Blocks of a prefix are counted from begin G / 32 + p: no two groups meet, and B G / 32 + groups + 1 are enough.
-__host__ __device__ __forceinline__ int piece_slots(const PagedRead& p) { return (int)((int64_t)p.B * p.G / kCols) + p.groups + 1; }
+// Blocks of a prefix are counted from begin G / kBlock + p: no two groups meet, and B G / kBlock + groups + 1 are enough.
 __device__ __forceinline__ int piece_own(const PagedRead& p, int u) { return u; }
 __device__ __forceinline__ int piece_prefix(const PagedRead& p, int group, int begin, int block, int g) {
-    return p.B * p.Hkv + (begin * p.G / kCols + group + block) * p.Hkv + g;
+    return p.B * p.Hkv + (begin * p.G / kBlock + group + block) * p.Hkv + g;
 }
 
 __device__ __forceinline__ int clamped(int v, int low, int high) { return max(low, min(v, high)); }
@@ -59,19 +63,53 @@ __device__ __forceinline__ Group group_of(const PagedRead& p, int i) {
 __device__ __forceinline__ int own_rows(const PagedRead& p, int u) { return clamped(p.len[u], 0, p.width << p.page_log2); }
 __device__ __forceinline__ int prefix_rows(const PagedRead& p, int i) { return clamped(p.prefix_len[i], 0, p.prefix_width << p.page_log2); }
 
-// Items: (prefix, KV head) first, then (batch element, KV head).
+// Items: (prefix, KV head) first, then (batch element, KV head).  A wave's tile is one unit of weight: a tile of a block weighs 1, 2 or 4 by
+// the waves that have it.
 struct Item {
-    int rows, blocks, begin;                                 // rows of the cache; blocks of queries; first batch element
+    int rows;                                                // of the cache
+    uint32_t who;                                            // queries | first batch element << 16: both below 2^16
+    __device__ __forceinline__ int cols() const { return who & 0xFFFF; }
+    __device__ __forceinline__ int begin() const { return who >> 16; }
     __device__ __forceinline__ int tiles() const { return (rows + kTileRows - 1) / kTileRows; }
-    __device__ __forceinline__ int weight_of_block() const { return rows ? tiles() + kStart : 0; }
-    __device__ __forceinline__ double weight() const { return (double)blocks * weight_of_block(); }       // whole numbers below 2^53
+    __device__ __forceinline__ int blocks() const { return rows ? (cols() + kBlock - 1) / kBlock : 0; }
+    __device__ __forceinline__ int factor(int block) const {
+        const int left = cols() - block * kBlock;
+        return left <= kCols ? 1 : left <= 2 * kCols ? 2 : 4;
+    }
+    __device__ __forceinline__ int weight_of_full_block() const { return 4 * tiles() + kStartPrefix; }
+    __device__ __forceinline__ int weight(bool own) const {  // below 2^31: at most 512 blocks of 2^19 tiles
+        const int n = blocks();
+        return n ? (n - 1) * weight_of_full_block() + factor(n - 1) * tiles() + (own ? kStartOwn : kStartPrefix) : 0;
+    }
 };
-__device__ __forceinline__ Item item_of(const PagedRead& p, int i) {
-    const int prefixes = p.groups * p.Hkv;
-    if (i >= prefixes + p.B * p.Hkv) return {0, 0, 0};
-    if (i >= prefixes) return {own_rows(p, i - prefixes), 1, (i - prefixes) / p.Hkv};
-    const Group g = group_of(p, i / p.Hkv);
-    return {prefix_rows(p, i), ((g.end - g.begin) * p.G + kCols - 1) / kCols, g.begin};
+// Sizes of items first, first + 1, ... first + N - 1 below `end`: all lengths are asked for at once.
+template <int N>
+__device__ __forceinline__ void items_of(const PagedRead& p, int first, int end, Item (&it)[N]) {
+    const int prefixes = p.prefixes();
+    int length[N], g0[N], g1[N];
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+        const int i = min(first + x, p.items() - 1);
+        length[x] = i < prefixes ? p.prefix_len[i] : p.len[i - prefixes];
+    }
+    if (p.groups) {
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            const int group = min(divided(first + x, p.Hkv, p.inv_Hkv), p.groups - 1);
+            g0[x] = p.group_begin[group];
+            g1[x] = p.group_begin[group + 1];
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+        const int i = first + x;
+        if (i >= end) it[x] = {0, 0};
+        else if (i >= prefixes) it[x] = {clamped(length[x], 0, p.width << p.page_log2), (uint32_t)p.G | (uint32_t)divided(i - prefixes, p.Hkv, p.inv_Hkv) << 16};
+        else {
+            const int begin = clamped(g0[x], 0, p.B), members = clamped(g1[x], begin, p.B) - begin;
+            it[x] = {clamped(length[x], 0, p.prefix_width << p.page_log2), (uint32_t)(members * p.G) | (uint32_t)begin << 16};
+        }
+    }
 }
 
 // sums of lanes 0 ... own
@@ -98,7 +136,7 @@ struct PartCfg {
     static constexpr int NL = TILE / 1024, RPL = 1024 / RB;  // loads of 1 KiB per tile, rows per load
     static constexpr int WAVE = 2 * TILE;                    // a wave's LDS: a tile of K, one of V
     static constexpr int CH = D / Elem<T>::kPerChunk, ODB = D / 32;
-    static constexpr int MB = WAVE >= 2 * 32 * 33 * 4 ? 2 : 1;       // blocks of 32 channels joined at a time
+    static_assert(WAVE >= D * kCols * 4, "room for a wave's sums");
     static constexpr int LDS = kPartWaves * WAVE;
     static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
     // swizzle of row r's 16-byte chunks: K is read 32 rows at a time at one chunk, V of bf16 by transposing reads
@@ -252,6 +290,7 @@ struct WavePart {
             const int t = first + min(from + lane, n - 1) * step;
             e0 = table[t * kTileRows >> p.page_log2];
             if (small) e1 = t * kTileRows + 16 < rows ? table[2 * t + 1] : -1;
+            asm volatile("" : "+v"(e0), "+v"(e1));           // here they are waited for, and not, with all requested rows, where a tile looks at them
         };
         int at = -1;
         auto next = [&](Tile& x) {                           // the next tile of which there is a row; false: none
@@ -306,180 +345,338 @@ struct WavePart {
     }
 };
 
+// The line of work.  Many items: their weights follow each other and the workgroups take equal pieces, so that however unequal the lengths, no
+// workgroup has more than another; a long item gets many workgroups and several short ones share one.  The waves of a workgroup share
+// the pieces of prefixes, which many queries see; a piece of own items is cut again into equal ones for each wave, which then wait for
+// nobody.  Few items: each has workgroups of its own, a whole number by its weight, as many as the chip has room for: a workgroup that ends
+// one item and starts another does so one after the other, and where the work is small that is what lasts.
+struct Line {
+    int item;                                                // of the workgroup's first position
+    int64_t start;                                           // of that item on the line
+    int64_t lo, hi;                                          // the workgroup's piece
+    int64_t own;                                             // where own items begin
+    int each;                                                // few items: weight for which an item has a workgroup; 0: many
+};
+
+struct LineShared {
+    double sums[kPartWaves], own[kPartWaves], base;
+    int item;
+    int2 few[kPartWaves];
+};
+constexpr int kSeen = 1024;          // items whose sizes are left in LDS
+
+__device__ __forceinline__ int workgroups_of_block(const Item& it, int block, int each) { return (it.factor(block) * it.tiles() + each - 1) / each; }
+__device__ __forceinline__ int workgroups_of(const Item& it, int each) {
+    const int n = it.blocks();
+    return n ? (n - 1) * ((4 * it.tiles() + each - 1) / each) + workgroups_of_block(it, n - 1, each) : 0;
+}
+
+__device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, Item* seen, Line& line) {
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+    const int items = p.items(), prefixes = p.prefixes(), per = (items + 255) / 256, from = tid * per, end = min(items, from + per);
+    double sum = 0.0, before = 0.0;                          // of all of the thread's items, of those that are prefixes
+    Item first = {0, 0};
+    int blocks = 0;
+    if (per == 1) {
+        Item it[1];
+        items_of(p, from, end, it);
+        first = it[0];
+        sum = first.weight(from >= prefixes);
+        before = from < prefixes ? sum : 0.0;
+        blocks = first.blocks();
+        seen[tid] = first;
+    } else {
+        for (int x0 = from; x0 < end; x0 += 8) {
+            Item it[8];
+            items_of(p, x0, end, it);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int weight = it[x].weight(x0 + x >= prefixes);
+                sum += weight;
+                if (x0 + x < prefixes) before += weight;
+                blocks += it[x].blocks();
+                if (x0 + x < min(end, kSeen)) seen[x0 + x] = it[x];
+            }
+        }
+    }
+    const double upto = wave_scan(sum), wave_before = wave_sum(before);
+    const int wave_blocks = wave_sum(blocks);
+    if (lane == 63) {
+        sh.sums[w] = upto;
+        sh.own[w] = wave_before;
+        sh.few[w].x = wave_blocks;
+    }
+    if (tid == 0) sh.item = items;
+    __syncthreads();
+    double total = 0.0, base = upto - sum, own = 0.0;
+    int all_blocks = 0;
+    for (int x = 0; x < kPartWaves; ++x) {
+        if (x < w) base += sh.sums[x];
+        total += sh.sums[x];
+        own += sh.own[x];
+        all_blocks += sh.few[x].x;
+    }
+    if (total == 0.0) return false;
+    line.each = 0;
+    line.own = (int64_t)own;
+    if (per == 1 && 2 * all_blocks <= (int)gridDim.x) {      // few: the line again, in workgroups
+        const int room = gridDim.x - all_blocks;
+        line.each = (int)fmax((double)kLeastFew, ceil(total / room));        // no more than there is room for: starts are counted too
+        const int mine = workgroups_of(first, line.each);
+        const double many = wave_scan((double)mine);
+        if (lane == 63) sh.few[w].y = (int)many;
+        __syncthreads();
+        base = many - mine;
+        sum = mine;
+        int all = 0;
+        for (int x = 0; x < kPartWaves; ++x) {
+            if (x < w) base += sh.few[x].y;
+            all += sh.few[x].y;
+        }
+        if ((int)blockIdx.x >= all) return false;
+        line.lo = blockIdx.x;
+        line.hi = line.lo + 1;
+    } else {
+        const int wgs = (int)fmax(1.0, fmin((double)gridDim.x, floor(total / kLeast)));  // a piece is longer than a tile of any item: none is without a tile
+        if ((int)blockIdx.x >= wgs) return false;
+        const double step = total / wgs;                     // borders are whole numbers, and the same ones for the workgroups on both sides
+        line.lo = (int64_t)floor(blockIdx.x * step);
+        line.hi = (int)blockIdx.x == wgs - 1 ? (int64_t)total : (int64_t)floor((blockIdx.x + 1) * step);
+    }
+    if (base <= (double)line.lo && (double)line.lo < base + sum) {
+        sh.item = from;
+        sh.base = base;
+    }
+    __syncthreads();
+    line.item = __builtin_amdgcn_readfirstlane(sh.item);
+    line.start = (int64_t)sh.base;
+    return true;
+}
+
+// What a workgroup, or a wave, has of an item.
+struct Piece { int item, block, ta, tb; bool own; Item it; };
+
+// The pieces on [pos, hi) of the line one after the other, from `item`, which starts at `start`.
+struct Walker {
+    const PagedRead& p;
+    const Item* in_lds;                                      // NULL: no longer
+    int item, window;
+    int64_t start, pos, hi;
+    Item seen;                                               // 64 items from `window`, one a lane
+    __device__ __forceinline__ void look() {
+        const int i = window + (int)(threadIdx.x & 63);
+        if (in_lds && p.items() <= kSeen) seen = i < p.items() ? in_lds[i] : Item{0, 0};
+        else {
+            Item it[1];
+            items_of(p, i, p.items(), it);
+            seen = it[0];
+        }
+    }
+    __device__ __forceinline__ bool next(Piece& x, int each) {
+        while (pos < hi && item < p.items()) {               // the items end where the line does, unless lengths change meanwhile
+            if (item >= window + 64) {
+                window = item;
+                look();
+            }
+            Item& it = x.it;
+            it.rows = __builtin_amdgcn_readlane(seen.rows, item - window);
+            it.who = __builtin_amdgcn_readlane(seen.who, item - window);
+            x.item = item;
+            x.own = item >= p.prefixes();
+            const int tiles = it.tiles(), n = it.blocks();
+            const int weight = each ? workgroups_of(it, each) : it.weight(x.own);
+            if (pos >= start + weight) { start += weight; ++item; continue; }
+            const int off = (int)(pos - start);
+            if (each) {
+                const int full = (4 * tiles + each - 1) / each;
+                x.block = n > 1 ? min(off / full, n - 1) : 0;
+                const int k = off - x.block * full, of = workgroups_of_block(it, x.block, each), some = tiles / of, more = tiles - some * of;
+                x.ta = k * some + min(k, more);
+                x.tb = x.ta + some + (k < more);
+                pos = hi;
+                return true;
+            }
+            const int full = it.weight_of_full_block();
+            x.block = n > 1 ? min(off / full, n - 1) : 0;
+            const int f = it.factor(x.block), x0 = off - x.block * full;
+            const int64_t block_start = start + (int64_t)x.block * full, block_end = x.block < n - 1 ? block_start + full : start + weight;
+            const int x1 = (int)(min(block_end, hi) - block_start);
+            pos = block_start + x1;
+            const int shift = f == 4 ? 2 : f - 1;
+            x.ta = min((x0 + f - 1) >> shift, tiles);        // a tile is whose piece it begins in
+            x.tb = min((x1 + f - 1) >> shift, tiles);
+            if (x.ta < x.tb) return true;                    // else: nothing but an item's start
+        }
+        return false;
+    }
+};
+
+// A lane's part to its record.
+template <typename T, int D>
+__device__ __forceinline__ void store_part(const Parts& out, int rec, const WavePart<T, D>& part, int h) {
+    float* dst = out.o + (int64_t)rec * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<floatx4*>(dst + 32 * db + 8 * x + 4 * h) = floatx4{part.o[db][4 * x], part.o[db][4 * x + 1], part.o[db][4 * x + 2], part.o[db][4 * x + 3]};
+    if (h == 0) *reinterpret_cast<float2*>(out.ml + 2 * (int64_t)rec) = make_float2(part.m, part.l);
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void paged_part_kernel(const T* __restrict__ q, PagedRead p, float c, Parts out) {
     using C = PartCfg<T, D>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ double sums[kPartWaves];
-    __shared__ double found_base;
-    __shared__ int found_item;
+    __shared__ LineShared sh;
     __shared__ float2 ml[kPartWaves][kCols];
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i = lane & 31, h = lane >> 5;
-    const int items = (p.groups + p.B) * p.Hkv, per = (items + 255) / 256;
     char* const mine = smem + w * C::WAVE;
+    Line line;
+    static_assert(kSeen * sizeof(Item) <= C::LDS, "the items' sizes stand where tiles come later");
+    if (!find_piece(p, sh, reinterpret_cast<Item*>(smem), line)) return;
+    Walker walk = {p, reinterpret_cast<const Item*>(smem), line.item, line.item, line.start, line.lo, line.each ? line.hi : min(line.hi, max(line.lo, line.own)), {0, 0}};
+    walk.look();
+    walk.in_lds = nullptr;
+    __syncthreads();                                         // tiles may come
 
-    // where on the line of weights this workgroup's piece is
-    double sum = 0.0;
-    for (int x = 0; x < per; ++x) sum += item_of(p, tid * per + x).weight();
-    const double upto = wave_scan(sum);
-    if (lane == 63) sums[w] = upto;
-    if (tid == 0) found_item = items;
-    __syncthreads();
-    double total = 0.0, base = upto - sum;
-    for (int x = 0; x < kPartWaves; ++x) {
-        if (x < w) base += sums[x];
-        total += sums[x];
-    }
-    const int64_t all = (int64_t)total;
-    const int64_t wgs = max((int64_t)1, min((int64_t)gridDim.x, all / kLeast));
-    if (blockIdx.x >= wgs || all == 0) return;
-    const int64_t lo = all * blockIdx.x / wgs, hi = all * (blockIdx.x + 1) / wgs;
-    if (base <= (double)lo && (double)lo < base + sum) { found_item = tid * per; found_base = base; }
-    __syncthreads();
-
-    int item = __builtin_amdgcn_readfirstlane(found_item), window = item;
-    int64_t pos = lo, start = (int64_t)found_base;           // start: of `item` on the line
-    Item seen = item_of(p, window + lane);                   // of 64 items, one a lane
-    int ordinal = 0;                                         // of short items, which the waves take in turn
-    while (pos < hi && item < items) {                       // the items end where the line does, unless lengths change meanwhile
-        if (item == window + 64) {
-            window = item;
-            seen = item_of(p, window + lane);
-        }
-        Item it;
-        it.rows = __builtin_amdgcn_readlane(seen.rows, item - window);
-        it.blocks = __builtin_amdgcn_readlane(seen.blocks, item - window);
-        it.begin = __builtin_amdgcn_readlane(seen.begin, item - window);
-        const int tiles = it.tiles(), wb = it.weight_of_block();
-        const int64_t weight = (int64_t)it.blocks * wb;
-        if (pos >= start + weight) { start += weight; ++item; continue; }
-        const int block = (int)(pos - start) / wb;            // an item weighs less than 2^31
-        const int64_t block_start = start + (int64_t)block * wb;
-        const int x0 = (int)(pos - block_start), x1 = (int)min((int64_t)wb, hi - block_start);
-        pos = block_start + x1;
-        const int ta = min(x0, tiles), tb = min(x1, tiles);
-        if (ta >= tb) continue;                              // nothing but the item's start
-        const bool own = item >= p.groups * p.Hkv, begins = ta == 0, ends = tb == tiles, whole = begins && ends;
-        const int unit = own ? item - p.groups * p.Hkv : item, g = unit % p.Hkv, group = own ? 0 : item / p.Hkv;
-        const Group members = own ? Group{it.begin, it.begin + 1} : group_of(p, group);
-        const int cols = min(kCols, (members.end - members.begin) * p.G - block * kCols);
-        int2* const piece = out.pieces + (own ? piece_own(p, unit) : piece_prefix(p, group, members.begin, block, g));
+    const int prefixes = p.prefixes();
+    Piece x;
+    while (walk.next(x, line.each)) {                        // of all waves
+        const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
+        const int unit = x.own ? x.item - prefixes : x.item, group = x.own ? 0 : divided(unit, p.Hkv, p.inv_Hkv);
+        const int g = x.own ? unit - x.it.begin() * p.Hkv : unit - group * p.Hkv;
+        const int cols = min(kBlock, x.it.cols() - x.block * kBlock), f = x.it.factor(x.block);
+        int2* const piece = out.pieces + (x.own ? piece_own(p, unit) : piece_prefix(p, group, x.it.begin(), x.block, g));
         if (tid == 0) {
             if (begins) piece->x = blockIdx.x;
             if (ends) piece->y = blockIdx.x;
         }
-        const bool solo = tb - ta <= kSolo;
-        if (solo && ordinal++ % kPartWaves != w) continue;
-
-        const int col = block * kCols + min(i, cols - 1);    // row of the output that lane i has
-        const int row = (members.begin + col / p.G) * p.Hq + g * p.G + col % p.G;
+        const int phases = kPartWaves / f, phase = w & (phases - 1), first_col = f == 1 ? 0 : f == 2 ? (w >> 1) * kCols : w * kCols;
+        const int in_wave = min(kCols, cols - first_col);    // columns; none where a block has three times 32
+        auto row_of = [&](int col) {                         // column of the block -> row of the output
+            const int r = x.block * kBlock + col, s = divided(r, p.G, p.inv_G);
+            return (x.it.begin() + s) * p.Hq + g * p.G + r - s * p.G;
+        };
+        const int row = row_of(first_col + max(0, min(i, in_wave - 1)));     // of this lane's query
         WavePart<T, D> part;
         part.reset();
-        part.load_queries(q + (int64_t)row * D, i < cols);
-        const int32_t* table = own ? p.table + (int64_t)unit * p.width : p.prefix_table + (int64_t)unit * p.prefix_width;
-        part.run(p, table, it.rows, solo ? ta : ta + w, solo ? 1 : kPartWaves, tb, c, mine);
+        part.load_queries(q + (int64_t)row * D, i < in_wave);
+        const int32_t* table = x.own ? p.table + (int64_t)unit * p.width : p.prefix_table + (int64_t)unit * p.prefix_width;
+        if (in_wave > 0) part.run(p, table, x.it.rows, x.ta + phase, phases, x.tb, c, mine);
         part.l += other_half(part.l);
-        auto record = [&](int of_col, int of_row) { return whole ? out.whole(of_row, own) : out.piece(blockIdx.x, begins, of_col); };
-        if (solo) {
-            if (i < cols) {
-                const int64_t rec = record(i, row);
-                float* dst = out.o + rec * D;
-#pragma unroll
-                for (int db = 0; db < C::ODB; ++db)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        *reinterpret_cast<floatx4*>(dst + 32 * db + 8 * x + 4 * h) = floatx4{part.o[db][4 * x], part.o[db][4 * x + 1], part.o[db][4 * x + 2], part.o[db][4 * x + 3]};
-                if (h == 0) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(part.m, part.l);
-            }
+        auto record = [&](int col) { return whole ? out.whole(row_of(col), x.own) : out.piece(x.own, blockIdx.x, begins, col); };
+        if (phases == 1) {
+            if (i < in_wave) store_part<T, D>(out, record(first_col + i), part, h);
             continue;
         }
-        // the waves' parts meet in LDS, a few channels at a time, rows of 33 so that both ways through are free of conflicts
+        // The parts of waves with the same columns meet in LDS: [channel][column], columns turned by the channel so that neither way through meets conflicts.
         if (h == 0) ml[w][i] = make_float2(part.m, part.l);
         __syncthreads();
         float M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int x = 0; x < kPartWaves; ++x) M = fmaxf(M, ml[x][i].x);
-#pragma unroll
-        for (int x = 0; x < kPartWaves; ++x) L += M > -INFINITY ? fast_exp2(ml[x][i].x - M) * ml[x][i].y : 0.f;
+        const int w0 = w - phase;
+        for (int y = 0; y < phases; ++y) M = fmaxf(M, ml[w0 + y][i].x);
+        for (int y = 0; y < phases; ++y) L += M > -INFINITY ? fast_exp2(ml[w0 + y][i].x - M) * ml[w0 + y][i].y : 0.f;
         const float a = M > -INFINITY ? fast_exp2(part.m - M) : 0.f;
-        if (w == 0 && h == 0 && i < cols) *reinterpret_cast<float2*>(out.ml + 2 * record(i, row)) = make_float2(M, L);
-        constexpr int kChannels = 32 * C::MB;
-        for (int pass = 0; pass < C::ODB / C::MB; ++pass) {
-            float* mo = reinterpret_cast<float*>(mine);
+        if (phase == 0 && h == 0 && i < in_wave) *reinterpret_cast<float2*>(out.ml + 2 * (int64_t)record(first_col + i)) = make_float2(M, L);
+        float* mo = reinterpret_cast<float*>(mine);
 #pragma unroll
-            for (int db = 0; db < C::ODB; ++db)
-                if (db / C::MB == pass)
+        for (int db = 0; db < C::ODB; ++db)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) mo[(32 * (db % C::MB) + acc_row(r, h)) * 33 + i] = part.o[db][r] * a;
-            __syncthreads();
-            for (int x = tid; x < cols * kChannels; x += 64 * kPartWaves) {
-                const int cc = x / kChannels, ch = x % kChannels;
-                float v = 0.f;
-#pragma unroll
-                for (int y = 0; y < kPartWaves; ++y) v += reinterpret_cast<const float*>(smem + y * C::WAVE)[ch * 33 + cc];
-                const int r = block * kCols + cc;
-                out.o[record(cc, (members.begin + r / p.G) * p.Hq + g * p.G + r % p.G) * D + pass * kChannels + ch] = v;
+            for (int r = 0; r < 16; ++r) {
+                const int ch = 32 * db + acc_row(r, h);
+                mo[ch * kCols + (i ^ (ch & 31))] = part.o[db][r] * a;
             }
-            __syncthreads();
+        __syncthreads();
+        for (int y = tid; y < cols * (D / 4); y += 64 * kPartWaves) {
+            const int cc = y / (D / 4), ch = y % (D / 4) * 4;
+            const char* base = smem + cc / kCols * phases * C::WAVE;
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+            for (int z = 0; z < phases; ++z)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += reinterpret_cast<const float*>(base + z * C::WAVE)[(ch + e) * kCols + ((cc % kCols) ^ ((ch + e) & 31))];
+            *reinterpret_cast<floatx4*>(out.o + (int64_t)record(cc) * D + ch) = v;
         }
+        __syncthreads();
+    }
+    if (line.each || line.hi <= line.own) return;
+
+    // Own items of a line of many.  Where fewer than kLeast are left to the workgroup (the first with own items) its last wave has them: the pieces of
+    // an item are those of waves that follow each other.
+    const int64_t from = max(line.lo, line.own), all = line.hi - from;
+    walk.pos = all < kLeast ? from : from + all * w / kPartWaves;
+    walk.hi = all < kLeast ? (w == kPartWaves - 1 ? line.hi : from) : from + all * (w + 1) / kPartWaves;
+    const int who = blockIdx.x * kPartWaves + w;
+    while (walk.next(x, 0)) {
+        const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
+        const int unit = x.item - prefixes, row = x.it.begin() * p.Hq + (unit - x.it.begin() * p.Hkv) * p.G + min(i, p.G - 1);
+        if (lane == 0) {
+            if (begins) out.pieces[piece_own(p, unit)].x = who;
+            if (ends) out.pieces[piece_own(p, unit)].y = who;
+        }
+        WavePart<T, D> part;
+        part.reset();
+        part.load_queries(q + (int64_t)row * D, i < p.G);
+        part.run(p, p.table + (int64_t)unit * p.width, x.it.rows, x.ta, 1, x.tb, c, mine);
+        part.l += other_half(part.l);
+        if (i < p.G) store_part<T, D>(out, whole ? out.whole(row, 1) : out.piece(1, who, begins, i), part, h);
     }
 }
 
-// The parts of one query head: those of its group's prefix, then its own -> its output row.
+// The parts of one query head: those of its group's prefix, then its own -> its output row.  A chain of loads, each for the address of the next:
+// groups, pieces (with the lengths), parts (maxima, sums and the first 64 parts' outputs at once).
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedRead p, Parts in, T* __restrict__ o, int wgs) {
-    constexpr int kPer = D / 4, kAt = 256 / kPer;            // threads per part, parts at a time
+__global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts in, T* __restrict__ o) {
+    constexpr int kPer = D / 4, kAt = 256 / kPer, kAtOnce = 64 / kAt;        // threads per part, parts at a time
     __shared__ floatx4 sum[256];
     const int row = blockIdx.x, b = row / p.Hq, head = row - b * p.Hq, g = head / p.G, u = b * p.Hkv + g;
     const int tid = threadIdx.x, lane = tid & 63;
-    int group = -1, begin = 0;
+    const int2 own_pieces = in.pieces[piece_own(p, u)];
+    const int own_len = own_rows(p, u);
+    int2 pre = {0, -1}, own = {0, -1};
+    int col = 0;
     for (int x = 0; x < p.groups; x += 64) {
         const Group m = x + lane < p.groups ? group_of(p, x + lane) : Group{0, 0};
         const uint64_t in_it = __ballot(m.begin <= b && b < m.end);
         if (in_it) {
-            const int who = __builtin_ctzll(in_it);
-            group = x + who;
-            begin = __shfl(m.begin, who);
+            const int who = __builtin_ctzll(in_it), group = x + who, begin = __builtin_amdgcn_readlane(m.begin, who);
+            col = (b - begin) * p.G + head - g * p.G;
+            const int2 pieces = in.pieces[piece_prefix(p, group, begin, col / kBlock, g)];
+            if (prefix_rows(p, group * p.Hkv + g) > 0) pre = pieces;
+            col %= kBlock;
             break;
         }
     }
-    int2 pre = {0, -1}, own = {0, -1};
-    int col = 0;
-    if (group >= 0 && prefix_rows(p, group * p.Hkv + g) > 0) {
-        col = (b - begin) * p.G + head - g * p.G;
-        pre = in.pieces[piece_prefix(p, group, begin, col / kCols, g)];
-        col %= kCols;
-    }
-    if (own_rows(p, u) > 0) own = in.pieces[piece_own(p, u)];
-    pre.x = max(pre.x, 0), pre.y = min(pre.y, wgs - 1), own.x = max(own.x, 0), own.y = min(own.y, wgs - 1);
+    if (own_len > 0) own = own_pieces;
+    pre.x = max(pre.x, 0), pre.y = min(pre.y, kPartGrid - 1), own.x = max(own.x, 0), own.y = min(own.y, kPartGrid * kPartWaves - 1);
     const int n_pre = max(0, pre.y - pre.x + 1), n = n_pre + max(0, own.y - own.x + 1);
     auto record = [&](int s) {
         const bool is_own = s >= n_pre;
         const int2 x = is_own ? own : pre;
-        const int wg = x.x + (is_own ? s - n_pre : s);
-        return x.x == x.y ? in.whole(row, is_own) : in.piece(wg, wg == x.x, is_own ? head - g * p.G : col);
+        const int who = x.x + (is_own ? s - n_pre : s);
+        return x.x == x.y ? in.whole(row, is_own) : in.piece(is_own, who, who == x.x, is_own ? head - g * p.G : col);
     };
     float M = -INFINITY, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < n; s0 += 64) {                     // 64 parts at a time, every wave all of their maxima and sums
         const int count = min(64, n - s0);
         float2 v = make_float2(-INFINITY, 0.f);
-        int64_t rec = 0;
-        if (lane < count) {
-            rec = record(s0 + lane);
-            v = *reinterpret_cast<const float2*>(in.ml + 2 * rec);
-        }
+        const int rec = record(s0 + min(lane, count - 1));
+        if (lane < count) v = *reinterpret_cast<const float2*>(in.ml + 2 * (int64_t)rec);
+        floatx4 part[kAtOnce];
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y)
+            if (y * kAt < count) part[y] = *reinterpret_cast<const floatx4*>(in.o + (int64_t)__shfl(rec, y * kAt + tid / kPer) * D + tid % kPer * 4);
         const float M_new = fmaxf(M, wave_max(v.x));
         const float a = M_new > -INFINITY ? fast_exp2(v.x - M_new) : 0.f, before = M_new > -INFINITY ? fast_exp2(M - M_new) : 0.f;
         L = L * before + wave_sum(a * v.y);
         acc *= before;
         M = M_new;
-        for (int x0 = 0; x0 < count; x0 += kAt) {            // all lanes to the end: a lane that has left answers no other
-            const int x = x0 + tid / kPer;
-            const float weight = __shfl(a, min(x, 63));
-            const int64_t r = __shfl(rec, min(x, 63));
-            if (x < count) acc += weight * *reinterpret_cast<const floatx4*>(in.o + r * D + tid % kPer * 4);
-        }
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y)
+            if (y * kAt < count) {                           // all lanes: a lane that is not there answers no other
+                const float weight = __shfl(a, y * kAt + tid / kPer);
+                if (y * kAt + tid / kPer < count) acc += weight * part[y];
+            }
     }
     sum[tid] = acc;
     __syncthreads();
@@ -492,30 +689,31 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedRead p, Parts in, 
     }
 }
 
-struct PagedLayout { size_t o, ml, pieces, total; };
-static PagedLayout paged_layout(const zipvl_dims& d, int groups) {
-    const size_t records = 2 * (size_t)d.B * d.Hq + 2 * (size_t)kPartGrid * kCols;
+struct PagedLayout { size_t o, ml, pieces, total; int cols; };
+static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes) {
+    const int G = d.Hq / d.Hkv;
     PagedLayout l;
+    l.cols = prefixes ? std::min(kBlock, (d.B * G + kCols - 1) / kCols * kCols) : kCols;     // that a workgroup may have
+    const size_t records = 2 * (size_t)d.B * d.Hq + 2 * (size_t)kPartGrid * (l.cols + kPartWaves * G);
     l.o = 0;
     l.ml = l.o + records * d.d * sizeof(float);
     l.pieces = l.ml + records * 2 * sizeof(float);
-    const size_t blocks = (size_t)d.B * (d.Hq / d.Hkv) / kCols + groups + 1;
+    const size_t blocks = prefixes ? (size_t)d.B * G / kBlock + d.B + 1 : 0;         // at most B groups
     l.total = l.pieces + ((size_t)d.B + blocks) * d.Hkv * sizeof(int2);
     return l;
 }
 
-// a call with a prefix has at most B groups
-size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) { return paged_layout(d, prefix ? d.B : 0).total; }
+size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) { return paged_layout(d, prefix > 0).total; }
 
 template <typename T, int D>
 static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, float scale, T* o, char* ws, hipStream_t st) {
     using C = PartCfg<T, D>;
-    const PagedLayout l = paged_layout(d, p.groups);
-    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq};
-    // what all lengths at their greatest would weigh
-    const int64_t own = (int64_t)d.B * d.Hkv * (((int64_t)p.width << p.page_log2) / kTileRows + 1 + kStart);
-    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kCols + p.groups) * d.Hkv * (((int64_t)p.prefix_width << p.page_log2) / kTileRows + 1 + kStart) : 0;
-    const int wgs = (int)std::max<int64_t>(1, std::min<int64_t>(kPartGrid, (own + pre) / kLeast));
+    const PagedLayout l = paged_layout(d, p.groups > 0);
+    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, p.G};
+    // no more workgroups than waves' tiles of all lengths at their greatest
+    const int64_t own = (int64_t)d.B * d.Hkv * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows);
+    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kCols + p.groups) * d.Hkv * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) : 0;
+    const int wgs = (int)std::min<int64_t>(kPartGrid, own + pre);
     static std::atomic<uint64_t> lds_set{0};                 // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return set_error(ZIPVL_EHIP, "decode_attn_paged: no current device");
@@ -531,7 +729,7 @@ static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, f
         if (rc) return rc;
     }
     KernelTimer tm(ZIPVL_K_PAGED_COMBINE, st);
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(d.B * d.Hq), dim3(256), 0, st, p, parts, o, wgs);
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(d.B * d.Hq), dim3(256), 0, st, p, parts, o);
     return check_launch("decode_attn_paged parts");
 }
 
@@ -540,7 +738,8 @@ int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int3
                              int32_t groups, const zipvl_dims& d, float scale, void* o, void* ws, hipStream_t st)
 {
     const PagedRead p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len,
-                         prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, d.Hq / d.Hkv};
+                         prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, d.Hq / d.Hkv,
+                         inverse(d.Hkv), inverse(d.Hq / d.Hkv)};
     if (d.dtype == ZIPVL_BF16)
         return d.d == 128 ? launch_paged_t<__bf16, 128>((const __bf16*)q, p, d, scale, (__bf16*)o, (char*)ws, st)
                           : launch_paged_t<__bf16, 64>((const __bf16*)q, p, d, scale, (__bf16*)o, (char*)ws, st);
