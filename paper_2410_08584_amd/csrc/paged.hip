@@ -21,9 +21,18 @@ namespace zipvl {
 constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4, kBlock = kCols * kPartWaves;
 constexpr int kStartPrefix = 8, kStartOwn = 3;       // what starting an item weighs: its queries, its first rows, its part
 constexpr int kLeast = 8;            // weight below which a workgroup is not worth its part
-constexpr int kLeastFew = 4;         // the same where every item has workgroups of its own
+// The same where every item has workgroups of its own.  A tile of fp32 rows is 2 us of a wave and more, and one for each is enough; of bf16 rows it
+// is 0.6, and half as many parts are worth it.  Two questions about an image of 576 rows, fp32: 14.1 us with 4, 17.3 with 8; eight about a video of 7200
+// rows, bf16: 22.6 and 19.3 (12: 19.7).
+template <typename T> constexpr int kLeastFew = sizeof(T) == 2 ? 8 : 4;
 constexpr int kPartGrid = 512;       // two workgroups a CU
 constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
+
+// a wave-uniform number in scalar registers
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t scalar(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
 
 struct PagedRead {
     const char *K, *V;
@@ -33,6 +42,7 @@ struct PagedRead {
     const int32_t* group_begin; int groups;
     int B, Hq, Hkv, G;
     uint32_t inv_Hkv, inv_G;
+    int least_few;
     __device__ __forceinline__ int prefixes() const { return groups * Hkv; }
     __device__ __forceinline__ int items() const { return (groups + B) * Hkv; }
 };
@@ -82,34 +92,18 @@ struct Item {
         return n ? (n - 1) * weight_of_full_block() + factor(n - 1) * tiles() + (own ? kStartOwn : kStartPrefix) : 0;
     }
 };
-// Sizes of items first, first + 1, ... first + N - 1 below `end`: all lengths are asked for at once.
-template <int N>
-__device__ __forceinline__ void items_of(const PagedRead& p, int first, int end, Item (&it)[N]) {
-    const int prefixes = p.prefixes();
-    int length[N], g0[N], g1[N];
-#pragma unroll
-    for (int x = 0; x < N; ++x) {
-        const int i = min(first + x, p.items() - 1);
-        length[x] = i < prefixes ? p.prefix_len[i] : p.len[i - prefixes];
-    }
-    if (p.groups) {
-#pragma unroll
-        for (int x = 0; x < N; ++x) {
-            const int group = min(divided(first + x, p.Hkv, p.inv_Hkv), p.groups - 1);
-            g0[x] = p.group_begin[group];
-            g1[x] = p.group_begin[group + 1];
-        }
-    }
-#pragma unroll
-    for (int x = 0; x < N; ++x) {
-        const int i = first + x;
-        if (i >= end) it[x] = {0, 0};
-        else if (i >= prefixes) it[x] = {clamped(length[x], 0, p.width << p.page_log2), (uint32_t)p.G | (uint32_t)divided(i - prefixes, p.Hkv, p.inv_Hkv) << 16};
-        else {
-            const int begin = clamped(g0[x], 0, p.B), members = clamped(g1[x], begin, p.B) - begin;
-            it[x] = {clamped(length[x], 0, p.prefix_width << p.page_log2), (uint32_t)(members * p.G) | (uint32_t)begin << 16};
-        }
-    }
+__device__ __forceinline__ Item own_item(const PagedRead& p, int u, int length) {
+    return {clamped(length, 0, p.width << p.page_log2), (uint32_t)p.G | (uint32_t)divided(u, p.Hkv, p.inv_Hkv) << 16};
+}
+__device__ __forceinline__ Item prefix_item(const PagedRead& p, int length, int g0, int g1) {
+    const int begin = clamped(g0, 0, p.B), members = clamped(g1, begin, p.B) - begin;
+    return {clamped(length, 0, p.prefix_width << p.page_log2), (uint32_t)(members * p.G) | (uint32_t)begin << 16};
+}
+__device__ __forceinline__ Item item_of(const PagedRead& p, int i) {
+    if (i >= p.items()) return {0, 0};
+    if (i >= p.prefixes()) return own_item(p, i - p.prefixes(), p.len[i - p.prefixes()]);
+    const int group = divided(i, p.Hkv, p.inv_Hkv);
+    return prefix_item(p, p.prefix_len[i], p.group_begin[group], p.group_begin[group + 1]);
 }
 
 // sums of lanes 0 ... own
@@ -283,6 +277,10 @@ struct WavePart {
     // Tiles first, first + step, ... below `end` of an item with `rows` rows and this row of a table.  K of the next tile is requested when K of this one
     // has been read, V of the next when V of this one has: a wave has one tile of each in LDS and one on the way at any time.
     __device__ __forceinline__ void run(const PagedRead& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine) {
+        first = scalar(first);
+        step = scalar(step);
+        end = scalar(end);
+        rows = scalar(rows);
         const int lane = threadIdx.x & 63, n = first < end ? (end - first + step - 1) / step : 0;
         const bool small = p.page_log2 == 4;                 // a tile is two pages
         int from = 0, e0 = -1, e1 = -1;                      // entries of the tiles from .. from + 63, one a lane
@@ -309,10 +307,10 @@ struct WavePart {
                     at1 = ((int64_t)((unsigned)b < (unsigned)p.num_pages ? b : 0) << 4) * C::RB;
                 } else if (!there) x.rows = 0;
                 if (x.rows == 0) continue;
-                x.k0 = scalar_ptr(p.K + at0);
-                x.k1 = scalar_ptr(p.K + at1);
-                x.v0 = scalar_ptr(p.V + at0);
-                x.v1 = scalar_ptr(p.V + at1);
+                x.k0 = p.K + at0;
+                x.k1 = p.K + at1;
+                x.v0 = p.V + at0;
+                x.v1 = p.V + at1;
                 x.rows = __builtin_amdgcn_readfirstlane(x.rows);
                 return true;
             }
@@ -345,6 +343,13 @@ struct WavePart {
     }
 };
 
+// a / b for 0 <= a < 2^22, b > 0: the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
+__device__ __forceinline__ int quotient(int a, int b) {
+    const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), left = a - q * b;
+    return q + (left >= b) - (left < 0);
+}
+
+
 // The line of work.  Many items: their weights follow each other and the workgroups take equal pieces, so that however unequal the lengths, no
 // workgroup has more than another; a long item gets many workgroups and several short ones share one.  The waves of a workgroup share
 // the pieces of prefixes, which many queries see; a piece of own items is cut again into equal ones for each wave, which then wait for
@@ -359,97 +364,119 @@ struct Line {
 };
 
 struct LineShared {
-    double sums[kPartWaves], own[kPartWaves], base;
+    double pre[kPartWaves], own[kPartWaves], base;
     int item;
     int2 few[kPartWaves];
 };
-constexpr int kSeen = 1024;          // items whose sizes are left in LDS
+constexpr int kSeen = 4096;          // items whose sizes are left in LDS
 
-__device__ __forceinline__ int workgroups_of_block(const Item& it, int block, int each) { return (it.factor(block) * it.tiles() + each - 1) / each; }
+__device__ __forceinline__ int workgroups_of_full_block(const Item& it, int each) { return quotient(4 * it.tiles() - 1, each) + 1; }
+__device__ __forceinline__ int workgroups_of_block(const Item& it, int block, int each) { return quotient(it.factor(block) * it.tiles() - 1, each) + 1; }
 __device__ __forceinline__ int workgroups_of(const Item& it, int each) {
     const int n = it.blocks();
-    return n ? (n - 1) * ((4 * it.tiles() + each - 1) / each) + workgroups_of_block(it, n - 1, each) : 0;
+    return n ? (n > 1 ? (n - 1) * workgroups_of_full_block(it, each) : 0) + workgroups_of_block(it, n - 1, each) : 0;
+}
+
+// What a thread has of a kind of items: `per` of them from `from`.
+struct Share { int from, end; };
+__device__ __forceinline__ Share share_of(int n) {
+    const int per = (n + 255) / 256, from = min(n, (int)threadIdx.x * per);
+    return {from, min(n, from + per)};
 }
 
 __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, Item* seen, Line& line) {
-    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
-    const int items = p.items(), prefixes = p.prefixes(), per = (items + 255) / 256, from = tid * per, end = min(items, from + per);
-    double sum = 0.0, before = 0.0;                          // of all of the thread's items, of those that are prefixes
-    Item first = {0, 0};
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, prefixes = p.prefixes();
+    const Share pre = share_of(prefixes), own = share_of(p.B * p.Hkv);
+    // whole numbers below 2^53
+    double pre_sum = 0.0, own_sum = 0.0;
     int blocks = 0;
-    if (per == 1) {
-        Item it[1];
-        items_of(p, from, end, it);
-        first = it[0];
-        sum = first.weight(from >= prefixes);
-        before = from < prefixes ? sum : 0.0;
-        blocks = first.blocks();
-        seen[tid] = first;
-    } else {
-        for (int x0 = from; x0 < end; x0 += 8) {
-            Item it[8];
-            items_of(p, x0, end, it);
+    Item first_pre = {0, 0}, first_own = {0, 0};
+    for (int i = pre.from; i < pre.end; ++i) {
+        const Item it = item_of(p, i);
+        if (i == pre.from) first_pre = it;
+        pre_sum += it.weight(false);
+        blocks += it.blocks();
+        if (i < kSeen) seen[i] = it;
+    }
+    for (int u0 = own.from; u0 < own.end; u0 += 4) {         // four lengths are asked for at once
+        int length[4];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const int weight = it[x].weight(x0 + x >= prefixes);
-                sum += weight;
-                if (x0 + x < prefixes) before += weight;
-                blocks += it[x].blocks();
-                if (x0 + x < min(end, kSeen)) seen[x0 + x] = it[x];
-            }
+        for (int x = 0; x < 4; ++x) length[x] = p.len[min(u0 + x, own.end - 1)];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            if (u0 + x >= own.end) break;
+            const Item it = own_item(p, u0 + x, length[x]);
+            if (u0 + x == own.from) first_own = it;
+            if (it.rows) { own_sum += it.tiles() + kStartOwn; ++blocks; }
+            if (prefixes + u0 + x < kSeen) seen[prefixes + u0 + x] = it;
         }
     }
-    const double upto = wave_scan(sum), wave_before = wave_sum(before);
+    const double pre_upto = wave_scan(pre_sum), own_upto = wave_scan(own_sum);
     const int wave_blocks = wave_sum(blocks);
     if (lane == 63) {
-        sh.sums[w] = upto;
-        sh.own[w] = wave_before;
+        sh.pre[w] = pre_upto;
+        sh.own[w] = own_upto;
         sh.few[w].x = wave_blocks;
     }
-    if (tid == 0) sh.item = items;
+    if (tid == 0) sh.item = p.items();
     __syncthreads();
-    double total = 0.0, base = upto - sum, own = 0.0;
+    double pre_base = pre_upto - pre_sum, own_base = own_upto - own_sum, pre_all = 0.0, own_all = 0.0;
     int all_blocks = 0;
     for (int x = 0; x < kPartWaves; ++x) {
-        if (x < w) base += sh.sums[x];
-        total += sh.sums[x];
-        own += sh.own[x];
+        if (x < w) { pre_base += sh.pre[x]; own_base += sh.own[x]; }
+        pre_all += sh.pre[x];
+        own_all += sh.own[x];
         all_blocks += sh.few[x].x;
     }
+    const double total = pre_all + own_all;
     if (total == 0.0) return false;
     line.each = 0;
-    line.own = (int64_t)own;
-    if (per == 1 && 2 * all_blocks <= (int)gridDim.x) {      // few: the line again, in workgroups
+    line.own = (int64_t)pre_all;
+    if (p.items() <= 256 && 2 * all_blocks <= (int)gridDim.x) {      // few: the line again, in workgroups
         const int room = gridDim.x - all_blocks;
-        line.each = (int)fmax((double)kLeastFew, ceil(total / room));        // no more than there is room for: starts are counted too
-        const int mine = workgroups_of(first, line.each);
-        const double many = wave_scan((double)mine);
-        if (lane == 63) sh.few[w].y = (int)many;
+        line.each = (int)fmax((double)p.least_few, ceil(total / room));      // no more than there is room for: starts are counted too
+        pre_sum = workgroups_of(first_pre, line.each);
+        own_sum = workgroups_of(first_own, line.each);
+        pre_base = wave_scan(pre_sum);
+        own_base = wave_scan(own_sum);
+        if (lane == 63) sh.few[w] = make_int2((int)pre_base, (int)own_base);
         __syncthreads();
-        base = many - mine;
-        sum = mine;
-        int all = 0;
+        pre_base -= pre_sum;
+        own_base -= own_sum;
+        int pre_n = 0, own_n = 0;
         for (int x = 0; x < kPartWaves; ++x) {
-            if (x < w) base += sh.few[x].y;
-            all += sh.few[x].y;
+            if (x < w) { pre_base += sh.few[x].x; own_base += sh.few[x].y; }
+            pre_n += sh.few[x].x;
+            own_n += sh.few[x].y;
         }
-        if ((int)blockIdx.x >= all) return false;
+        if ((int)blockIdx.x >= pre_n + own_n) return false;
+        own_base += pre_n;
         line.lo = blockIdx.x;
         line.hi = line.lo + 1;
     } else {
         const int wgs = (int)fmax(1.0, fmin((double)gridDim.x, floor(total / kLeast)));  // a piece is longer than a tile of any item: none is without a tile
         if ((int)blockIdx.x >= wgs) return false;
         const double step = total / wgs;                     // borders are whole numbers, and the same ones for the workgroups on both sides
+        own_base += pre_all;
         line.lo = (int64_t)floor(blockIdx.x * step);
         line.hi = (int)blockIdx.x == wgs - 1 ? (int64_t)total : (int64_t)floor((blockIdx.x + 1) * step);
     }
-    if (base <= (double)line.lo && (double)line.lo < base + sum) {
-        sh.item = from;
-        sh.base = base;
+    const double lo = (double)line.lo;
+    if (pre_base <= lo && lo < pre_base + pre_sum) {
+        sh.item = pre.from;
+        sh.base = pre_base;
+    }
+    if (own_base <= lo && lo < own_base + own_sum) {
+        sh.item = prefixes + own.from;
+        sh.base = own_base;
     }
     __syncthreads();
-    line.item = __builtin_amdgcn_readfirstlane(sh.item);
-    line.start = (int64_t)sh.base;
+    line.item = scalar(sh.item);
+    line.start = scalar((int64_t)sh.base);
+    line.lo = scalar(line.lo);
+    line.hi = scalar(line.hi);
+    line.own = scalar(line.own);
+    line.each = scalar(line.each);
     return true;
 }
 
@@ -466,11 +493,7 @@ struct Walker {
     __device__ __forceinline__ void look() {
         const int i = window + (int)(threadIdx.x & 63);
         if (in_lds && p.items() <= kSeen) seen = i < p.items() ? in_lds[i] : Item{0, 0};
-        else {
-            Item it[1];
-            items_of(p, i, p.items(), it);
-            seen = it[0];
-        }
+        else seen = item_of(p, i);
     }
     __device__ __forceinline__ bool next(Piece& x, int each) {
         while (pos < hi && item < p.items()) {               // the items end where the line does, unless lengths change meanwhile
@@ -488,9 +511,9 @@ struct Walker {
             if (pos >= start + weight) { start += weight; ++item; continue; }
             const int off = (int)(pos - start);
             if (each) {
-                const int full = (4 * tiles + each - 1) / each;
+                const int full = n > 1 ? workgroups_of_full_block(it, each) : 0;
                 x.block = n > 1 ? min(off / full, n - 1) : 0;
-                const int k = off - x.block * full, of = workgroups_of_block(it, x.block, each), some = tiles / of, more = tiles - some * of;
+                const int k = off - x.block * full, of = workgroups_of_block(it, x.block, each), some = quotient(tiles, of), more = tiles - some * of;
                 x.ta = k * some + min(k, more);
                 x.tb = x.ta + some + (k < more);
                 pos = hi;
@@ -587,6 +610,7 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
                 mo[ch * kCols + (i ^ (ch & 31))] = part.o[db][r] * a;
             }
         __syncthreads();
+#pragma unroll 2
         for (int y = tid; y < cols * (D / 4); y += 64 * kPartWaves) {
             const int cc = y / (D / 4), ch = y % (D / 4) * 4;
             const char* base = smem + cc / kCols * phases * C::WAVE;
@@ -683,9 +707,9 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
     if (tid < kPer) {
         for (int x = 1; x < min(kAt, n); ++x) acc += sum[x * kPer + tid];
         const float inv = L > 0.f ? 1.f / L : 0.f;
-        T* dst = o + (int64_t)row * D + tid * 4;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dst[e] = (T)(acc[e] * inv);
+        acc *= inv;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uintx2*>(o + (int64_t)row * D + tid * 4) = uintx2{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+        else *reinterpret_cast<floatx4*>(o + (int64_t)row * D + tid * 4) = acc;
     }
 }
 
@@ -739,7 +763,7 @@ int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int3
 {
     const PagedRead p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len,
                          prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, d.Hq / d.Hkv,
-                         inverse(d.Hkv), inverse(d.Hq / d.Hkv)};
+                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), d.dtype == ZIPVL_BF16 ? kLeastFew<__bf16> : kLeastFew<float>};
     if (d.dtype == ZIPVL_BF16)
         return d.d == 128 ? launch_paged_t<__bf16, 128>((const __bf16*)q, p, d, scale, (__bf16*)o, (char*)ws, st)
                           : launch_paged_t<__bf16, 64>((const __bf16*)q, p, d, scale, (__bf16*)o, (char*)ws, st);
