@@ -25,14 +25,12 @@ constexpr int kLeast = 8;            // weight below which a workgroup is not wo
 // is 0.6, and half as many parts are worth it.  Two questions about an image of 576 rows, fp32: 14.1 us with 4, 17.3 with 8; eight about a video of 7200
 // rows, bf16: 22.6 and 19.3 (12: 19.7).
 template <typename T> constexpr int kLeastFew = sizeof(T) == 2 ? 8 : 4;
+constexpr int kMostFew = 24;
 constexpr int kPartGrid = 512;       // two workgroups a CU
 constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
 
 // a wave-uniform number in scalar registers
 __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t scalar(int64_t v) {
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
 
 struct PagedRead {
     const char *K, *V;
@@ -107,13 +105,13 @@ __device__ __forceinline__ Item item_of(const PagedRead& p, int i) {
 }
 
 // sums of lanes 0 ... own
-__device__ __forceinline__ double wave_scan(double v) {
-    v += lane_moved<0x111, 0xF>(v, 0.0);
-    v += lane_moved<0x112, 0xF>(v, 0.0);
-    v += lane_moved<0x114, 0xF>(v, 0.0);
-    v += lane_moved<0x118, 0xF>(v, 0.0);
-    v += lane_moved<0x142, 0xA>(v, 0.0);
-    v += lane_moved<0x143, 0xC>(v, 0.0);
+__device__ __forceinline__ int wave_scan(int v) {
+    v += lane_moved<0x111, 0xF>(v, 0);
+    v += lane_moved<0x112, 0xF>(v, 0);
+    v += lane_moved<0x114, 0xF>(v, 0);
+    v += lane_moved<0x118, 0xF>(v, 0);
+    v += lane_moved<0x142, 0xA>(v, 0);
+    v += lane_moved<0x143, 0xC>(v, 0);
     return v;
 }
 
@@ -343,7 +341,7 @@ struct WavePart {
     }
 };
 
-// a / b for 0 <= a < 2^22, b > 0: the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
+// a / b for 0 <= a < 2^22, b > 0 (512 * 512 and four times the tiles of an item are less; kMostFew * 512 too): the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
 __device__ __forceinline__ int quotient(int a, int b) {
     const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), left = a - q * b;
     return q + (left >= b) - (left < 0);
@@ -357,16 +355,17 @@ __device__ __forceinline__ int quotient(int a, int b) {
 // one item and starts another does so one after the other, and where the work is small that is what lasts.
 struct Line {
     int item;                                                // of the workgroup's first position
-    int64_t start;                                           // of that item on the line
-    int64_t lo, hi;                                          // the workgroup's piece
-    int64_t own;                                             // where own items begin
+    int start;                                               // of that item on the line, which is shorter than 2^31
+    int lo, hi;                                              // the workgroup's piece
+    int own;                                                 // where own items begin
     int each;                                                // few items: weight for which an item has a workgroup; 0: many
+    int me;                                                  // the workgroup's number on the line
 };
 
 struct LineShared {
-    double pre[kPartWaves], own[kPartWaves], base;
-    int item;
+    int4 sums[kPartWaves];                                   // of prefixes, of own items; blocks
     int2 few[kPartWaves];
+    int item, base;
 };
 constexpr int kSeen = 4096;          // items whose sizes are left in LDS
 
@@ -387,10 +386,14 @@ __device__ __forceinline__ Share share_of(int n) {
 __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, Item* seen, Line& line) {
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, prefixes = p.prefixes();
     const Share pre = share_of(prefixes), own = share_of(p.B * p.Hkv);
-    // whole numbers below 2^53
-    double pre_sum = 0.0, own_sum = 0.0;
-    int blocks = 0;
+    int pre_sum = 0, own_sum = 0, blocks = 0;
     Item first_pre = {0, 0}, first_own = {0, 0};
+    int length[4];                                           // four are asked for at once, and the first four before those of prefixes are there
+    auto ask = [&](int u0) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) length[x] = p.len[clamped(u0 + x, 0, p.B * p.Hkv - 1)];
+    };
+    ask(own.from);
     for (int i = pre.from; i < pre.end; ++i) {
         const Item it = item_of(p, i);
         if (i == pre.from) first_pre = it;
@@ -398,10 +401,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
         blocks += it.blocks();
         if (i < kSeen) seen[i] = it;
     }
-    for (int u0 = own.from; u0 < own.end; u0 += 4) {         // four lengths are asked for at once
-        int length[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) length[x] = p.len[min(u0 + x, own.end - 1)];
+    for (int u0 = own.from; u0 < own.end; u0 += 4) {
+        if (u0 != own.from) ask(u0);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             if (u0 + x >= own.end) break;
@@ -411,72 +412,67 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
             if (prefixes + u0 + x < kSeen) seen[prefixes + u0 + x] = it;
         }
     }
-    const double pre_upto = wave_scan(pre_sum), own_upto = wave_scan(own_sum);
-    const int wave_blocks = wave_sum(blocks);
-    if (lane == 63) {
-        sh.pre[w] = pre_upto;
-        sh.own[w] = own_upto;
-        sh.few[w].x = wave_blocks;
-    }
+    const int pre_upto = wave_scan(pre_sum), own_upto = wave_scan(own_sum), wave_blocks = wave_sum(blocks);
+    if (lane == 63) sh.sums[w] = make_int4(pre_upto, own_upto, wave_blocks, 0);
     if (tid == 0) sh.item = p.items();
     __syncthreads();
-    double pre_base = pre_upto - pre_sum, own_base = own_upto - own_sum, pre_all = 0.0, own_all = 0.0;
-    int all_blocks = 0;
+    int pre_base = pre_upto - pre_sum, own_base = own_upto - own_sum, pre_all = 0, own_all = 0, all_blocks = 0;
+#pragma unroll
     for (int x = 0; x < kPartWaves; ++x) {
-        if (x < w) { pre_base += sh.pre[x]; own_base += sh.own[x]; }
-        pre_all += sh.pre[x];
-        own_all += sh.own[x];
-        all_blocks += sh.few[x].x;
+        const int4 v = sh.sums[x];
+        if (x < w) { pre_base += v.x; own_base += v.y; }
+        pre_all += v.x;
+        own_all += v.y;
+        all_blocks += v.z;
     }
-    const double total = pre_all + own_all;
-    if (total == 0.0) return false;
+    const int total = scalar(pre_all + own_all), grid = gridDim.x, room = grid - scalar(all_blocks);
+    if (total == 0) return false;
     line.each = 0;
-    line.own = (int64_t)pre_all;
-    if (p.items() <= 256 && 2 * all_blocks <= (int)gridDim.x) {      // few: the line again, in workgroups
-        const int room = gridDim.x - all_blocks;
-        line.each = (int)fmax((double)p.least_few, ceil(total / room));      // no more than there is room for: starts are counted too
+    line.me = blockIdx.x;
+    line.own = scalar(pre_all);
+    if (p.items() <= 256 && 2 * room >= grid && total <= kMostFew * room) {          // few: the line again, in workgroups
+        line.each = max(p.least_few, quotient(total - 1, room) + 1);     // no more than there is room for: starts are counted too
         pre_sum = workgroups_of(first_pre, line.each);
         own_sum = workgroups_of(first_own, line.each);
         pre_base = wave_scan(pre_sum);
         own_base = wave_scan(own_sum);
-        if (lane == 63) sh.few[w] = make_int2((int)pre_base, (int)own_base);
+        if (lane == 63) sh.few[w] = make_int2(pre_base, own_base);
         __syncthreads();
         pre_base -= pre_sum;
         own_base -= own_sum;
         int pre_n = 0, own_n = 0;
+#pragma unroll
         for (int x = 0; x < kPartWaves; ++x) {
-            if (x < w) { pre_base += sh.few[x].x; own_base += sh.few[x].y; }
-            pre_n += sh.few[x].x;
-            own_n += sh.few[x].y;
+            const int2 v = sh.few[x];
+            if (x < w) { pre_base += v.x; own_base += v.y; }
+            pre_n += v.x;
+            own_n += v.y;
         }
-        if ((int)blockIdx.x >= pre_n + own_n) return false;
+        if (line.me >= scalar(pre_n + own_n)) return false;
         own_base += pre_n;
-        line.lo = blockIdx.x;
-        line.hi = line.lo + 1;
+        line.lo = line.me;
+        line.hi = line.me + 1;
     } else {
-        const int wgs = (int)fmax(1.0, fmin((double)gridDim.x, floor(total / kLeast)));  // a piece is longer than a tile of any item: none is without a tile
-        if ((int)blockIdx.x >= wgs) return false;
-        const double step = total / wgs;                     // borders are whole numbers, and the same ones for the workgroups on both sides
-        own_base += pre_all;
-        line.lo = (int64_t)floor(blockIdx.x * step);
-        line.hi = (int)blockIdx.x == wgs - 1 ? (int64_t)total : (int64_t)floor((blockIdx.x + 1) * step);
+        const int wgs = max(1, min(grid, total / kLeast));   // a piece is longer than a tile of any item: none is without a tile
+        if (line.me >= wgs) return false;
+        const int each = scalar(total / wgs), more = total - each * wgs;
+        own_base += line.own;
+        line.lo = line.me * each + quotient(line.me * more, wgs);
+        line.hi = (line.me + 1) * each + quotient((line.me + 1) * more, wgs);
     }
-    const double lo = (double)line.lo;
-    if (pre_base <= lo && lo < pre_base + pre_sum) {
+    line.lo = scalar(line.lo);
+    line.hi = scalar(line.hi);
+    if (pre_base <= line.lo && line.lo < pre_base + pre_sum) {
         sh.item = pre.from;
         sh.base = pre_base;
     }
-    if (own_base <= lo && lo < own_base + own_sum) {
+    if (own_base <= line.lo && line.lo < own_base + own_sum) {
         sh.item = prefixes + own.from;
         sh.base = own_base;
     }
     __syncthreads();
     line.item = scalar(sh.item);
-    line.start = scalar((int64_t)sh.base);
-    line.lo = scalar(line.lo);
-    line.hi = scalar(line.hi);
-    line.own = scalar(line.own);
-    line.each = scalar(line.each);
+    line.start = scalar(sh.base);
     return true;
 }
 
@@ -488,7 +484,7 @@ struct Walker {
     const PagedRead& p;
     const Item* in_lds;                                      // NULL: no longer
     int item, window;
-    int64_t start, pos, hi;
+    int start, pos, hi;                                      // below 2^31
     Item seen;                                               // 64 items from `window`, one a lane
     __device__ __forceinline__ void look() {
         const int i = window + (int)(threadIdx.x & 63);
@@ -508,8 +504,8 @@ struct Walker {
             x.own = item >= p.prefixes();
             const int tiles = it.tiles(), n = it.blocks();
             const int weight = each ? workgroups_of(it, each) : it.weight(x.own);
-            if (pos >= start + weight) { start += weight; ++item; continue; }
-            const int off = (int)(pos - start);
+            if (pos - start >= weight) { start += weight; ++item; continue; }
+            const int off = pos - start;
             if (each) {
                 const int full = n > 1 ? workgroups_of_full_block(it, each) : 0;
                 x.block = n > 1 ? min(off / full, n - 1) : 0;
@@ -522,8 +518,7 @@ struct Walker {
             const int full = it.weight_of_full_block();
             x.block = n > 1 ? min(off / full, n - 1) : 0;
             const int f = it.factor(x.block), x0 = off - x.block * full;
-            const int64_t block_start = start + (int64_t)x.block * full, block_end = x.block < n - 1 ? block_start + full : start + weight;
-            const int x1 = (int)(min(block_end, hi) - block_start);
+            const int block_start = start + x.block * full, x1 = min((x.block < n - 1 ? full : weight - x.block * full), hi - block_start);
             pos = block_start + x1;
             const int shift = f == 4 ? 2 : f - 1;
             x.ta = min((x0 + f - 1) >> shift, tiles);        // a tile is whose piece it begins in
@@ -571,8 +566,8 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
         const int cols = min(kBlock, x.it.cols() - x.block * kBlock), f = x.it.factor(x.block);
         int2* const piece = out.pieces + (x.own ? piece_own(p, unit) : piece_prefix(p, group, x.it.begin(), x.block, g));
         if (tid == 0) {
-            if (begins) piece->x = blockIdx.x;
-            if (ends) piece->y = blockIdx.x;
+            if (begins) piece->x = line.me;
+            if (ends) piece->y = line.me;
         }
         const int phases = kPartWaves / f, phase = w & (phases - 1), first_col = f == 1 ? 0 : f == 2 ? (w >> 1) * kCols : w * kCols;
         const int in_wave = min(kCols, cols - first_col);    // columns; none where a block has three times 32
@@ -587,7 +582,7 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
         const int32_t* table = x.own ? p.table + (int64_t)unit * p.width : p.prefix_table + (int64_t)unit * p.prefix_width;
         if (in_wave > 0) part.run(p, table, x.it.rows, x.ta + phase, phases, x.tb, c, mine);
         part.l += other_half(part.l);
-        auto record = [&](int col) { return whole ? out.whole(row_of(col), x.own) : out.piece(x.own, blockIdx.x, begins, col); };
+        auto record = [&](int col) { return whole ? out.whole(row_of(col), x.own) : out.piece(x.own, line.me, begins, col); };
         if (phases == 1) {
             if (i < in_wave) store_part<T, D>(out, record(first_col + i), part, h);
             continue;
@@ -610,15 +605,20 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
                 mo[ch * kCols + (i ^ (ch & 31))] = part.o[db][r] * a;
             }
         __syncthreads();
-#pragma unroll 2
-        for (int y = tid; y < cols * (D / 4); y += 64 * kPartWaves) {
-            const int cc = y / (D / 4), ch = y % (D / 4) * 4;
-            const char* base = smem + cc / kCols * phases * C::WAVE;
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-            for (int z = 0; z < phases; ++z)
+        const int ch = tid % (D / 4) * 4, rec0 = whole ? 0 : out.piece(x.own, line.me, begins, 0);
+        int at[4];                                           // of channels ch .. ch + 3 in a column's place before it is turned
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += reinterpret_cast<const float*>(base + z * C::WAVE)[(ch + e) * kCols + ((cc % kCols) ^ ((ch + e) & 31))];
-            *reinterpret_cast<floatx4*>(out.o + (int64_t)record(cc) * D + ch) = v;
+        for (int e = 0; e < 4; ++e) at[e] = (ch + e) * kCols;
+#pragma unroll 4
+        for (int cc = tid / (D / 4); cc < cols; cc += 64 * kPartWaves / (D / 4)) {
+            const float* base = reinterpret_cast<const float*>(smem + cc / kCols * phases * C::WAVE);
+            floatx4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = base[at[e] + ((cc % kCols) ^ ((ch + e) & 31))];
+            for (int z = 1; z < phases; ++z)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += base[z * (C::WAVE / 4) + at[e] + ((cc % kCols) ^ ((ch + e) & 31))];
+            *reinterpret_cast<floatx4*>(out.o + (int64_t)(whole ? out.whole(row_of(cc), x.own) : rec0 + cc) * D + ch) = v;
         }
         __syncthreads();
     }
@@ -626,10 +626,10 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
 
     // Own items of a line of many.  Where fewer than kLeast are left to the workgroup (the first with own items) its last wave has them: the pieces of
     // an item are those of waves that follow each other.
-    const int64_t from = max(line.lo, line.own), all = line.hi - from;
-    walk.pos = all < kLeast ? from : from + all * w / kPartWaves;
-    walk.hi = all < kLeast ? (w == kPartWaves - 1 ? line.hi : from) : from + all * (w + 1) / kPartWaves;
-    const int who = blockIdx.x * kPartWaves + w;
+    const int from = max(line.lo, line.own), all = line.hi - from, quarter = all / kPartWaves, rest = all % kPartWaves;
+    walk.pos = all < kLeast ? from : from + w * quarter + min(w, rest);
+    walk.hi = all < kLeast ? (w == kPartWaves - 1 ? line.hi : from) : walk.pos + quarter + (w < rest);
+    const int who = line.me * kPartWaves + w;
     while (walk.next(x, 0)) {
         const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
         const int unit = x.item - prefixes, row = x.it.begin() * p.Hq + (unit - x.it.begin() * p.Hkv) * p.G + min(i, p.G - 1);
@@ -735,8 +735,10 @@ static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, f
     const PagedLayout l = paged_layout(d, p.groups > 0);
     const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, p.G};
     // no more workgroups than waves' tiles of all lengths at their greatest
-    const int64_t own = (int64_t)d.B * d.Hkv * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows);
-    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kCols + p.groups) * d.Hkv * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) : 0;
+    const int64_t own = (int64_t)d.B * d.Hkv * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows + kStartOwn);
+    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kBlock + p.groups) * d.Hkv * (4 * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartPrefix) : 0;
+    if (own + pre >= (int64_t)1 << 31)
+        return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^36)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
     const int wgs = (int)std::min<int64_t>(kPartGrid, own + pre);
     static std::atomic<uint64_t> lds_set{0};                 // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
