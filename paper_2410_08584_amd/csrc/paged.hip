@@ -25,6 +25,7 @@ constexpr int kLeast = 8;            // weight below which a workgroup is not wo
 // is 0.6, and half as many parts are worth it.  Two questions about an image of 576 rows, fp32: 14.1 us with 4, 17.3 with 8; eight about a video of 7200
 // rows, bf16: 22.6 and 19.3 (12: 19.7).
 template <typename T> constexpr int kLeastFew = sizeof(T) == 2 ? 8 : 4;
+constexpr int kCus = 256, kEarly = 17, kLate = 15;
 constexpr int kMostFew = 24;
 constexpr int kPartGrid = 512;       // two workgroups a CU
 constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
@@ -455,10 +456,13 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     } else {
         const int wgs = max(1, min(grid, total / kLeast));   // a piece is longer than a tile of any item: none is without a tile
         if (line.me >= wgs) return false;
-        const int each = scalar(total / wgs), more = total - each * wgs;
+        const bool first = line.me < kCus || wgs <= kCus;
+        const int early = wgs <= kCus ? total : scalar((int)((int64_t)total * (kEarly * kCus) / (kEarly * kCus + kLate * (wgs - kCus))));
+        const int n = first ? min(wgs, kCus) : wgs - kCus, me = first ? line.me : line.me - kCus, from = first ? 0 : early, share = first ? early : total - early;
+        const int each = scalar(share / n), more = share - each * n;
         own_base += line.own;
-        line.lo = line.me * each + quotient(line.me * more, wgs);
-        line.hi = (line.me + 1) * each + quotient((line.me + 1) * more, wgs);
+        line.lo = from + me * each + quotient(me * more, n);
+        line.hi = from + (me + 1) * each + quotient((me + 1) * more, n);
     }
     line.lo = scalar(line.lo);
     line.hi = scalar(line.hi);

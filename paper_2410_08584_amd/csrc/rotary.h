@@ -8,7 +8,7 @@ namespace zipvl {
 struct Turns {
     uint64_t turn[ZIPVL_MAX_PAIRS];          // of pair i, a position: freq / (2 pi) without whole turns, in 2^-64 of one
     uint8_t axis[ZIPVL_MAX_PAIRS];           // row of pos
-    int pairs, neighbours;
+    int axes, pairs, neighbours;
     uint32_t backwards;                      // the sign bit of the sines: 0x80000000 turns the other way
 };
 
@@ -30,12 +30,34 @@ __device__ __forceinline__ void turn_of(uint32_t pos, uint64_t turn, uint32_t ba
     cs = __uint_as_float(b ^ (((quarter + 1) & 2) << 30));
 }
 
-// Sines and cosines of the eight pairs of a thread at one position (pos[axis], axes `stride` apart).
+// A token's positions, and what a thread's eight pairs take of a turn a position: all of it is asked for at once, the axes' positions before it is known
+// which of them a pair goes by.
 struct Angles {
+    uint32_t pos[ZIPVL_MAX_AXES];
+    uint64_t turn[8], axis;                                  // a byte a pair
     float sn[8], cs[8];
-    __device__ __forceinline__ void set(const Turns& t, int first, const int32_t* pos, int64_t stride) {
+    __device__ __forceinline__ void ask(const Turns& t, int first, const int32_t* at, int64_t stride) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) turn_of((uint32_t)pos[t.axis[first + e] * stride], t.turn[first + e], t.backwards, sn[e], cs[e]);
+        for (int a = 0; a < ZIPVL_MAX_AXES; ++a) {
+            pos[a] = pos[0];
+            if (a < t.axes) pos[a] = (uint32_t)at[a * stride];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turn[e] = t.turn[first + e];
+        axis = *reinterpret_cast<const uint64_t*>(t.axis + first);
+    }
+    __device__ __forceinline__ void take(const Turns& t) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t a = (uint32_t)(axis >> (8 * e)) & 3;
+            uint32_t at = pos[0];
+            if (t.axes > 1) {
+                at = a == 1 ? pos[1] : at;
+                at = a == 2 ? pos[2] : at;
+                at = a == 3 ? pos[3] : at;
+            }
+            turn_of(at, turn[e], t.backwards, sn[e], cs[e]);
+        }
     }
 };
 

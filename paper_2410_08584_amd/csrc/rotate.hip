@@ -17,6 +17,7 @@ struct RowsIn { const char* base; int64_t b, h, t; };
 // heads as that leaves, and goes through the heads from its first in steps of `step`.
 struct Walk {
     int n, total, tokens_log2, step;                         // total = B n
+    uint32_t inv_n;
 };
 
 template <typename T, int D>
@@ -26,22 +27,29 @@ __global__ __launch_bounds__(256) void rotate_kernel(RowsIn Q, RowsIn K, Rows Qo
     constexpr int kThreads = D / 16;
     const int slot = threadIdx.x / kThreads, c = threadIdx.x % kThreads;
     const int token = (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
-    if (token >= w.total) return;
-    const int b = token / w.n, t = token - b * w.n;
+    const int first = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2);
+    if (token >= w.total || first >= heads) return;
+    const int b = divided(token, w.n, w.inv_n), t = token - b * w.n;
     const Runs runs(c, turns.pairs, turns.neighbours);
+    struct Row { Run<T> a, b; };
+    auto load = [&](int h) {
+        const RowsIn& in = h < Hq ? Q : K;
+        const T* src = reinterpret_cast<const T*>(in.base + b * in.b + (h < Hq ? h : h - Hq) * in.h + t * in.t);
+        return Row{load_run(src + runs.a), load_run(src + runs.b)};
+    };
     Angles at;
-    if (runs.first >= 0) at.set(turns, runs.first, pos + token, (int64_t)w.total);
-    for (int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2); h < heads; h += w.step) {
-        const bool query = h < Hq;
-        const int hh = query ? h : h - Hq;
-        const RowsIn& in = query ? Q : K;
-        const Rows& out = query ? Qo : Ko;
-        const T* src = reinterpret_cast<const T*>(in.base + b * in.b + hh * in.h + t * in.t);
-        T* dst = reinterpret_cast<T*>(out.base + b * out.b + hh * out.h + t * out.t);
-        Run<T> ra = load_run(src + runs.a), rb = load_run(src + runs.b);
-        if (runs.first >= 0) turn_runs(ra, rb, at, turns.neighbours);
-        store_run(dst + runs.a, ra);
-        store_run(dst + runs.b, rb);
+    if (runs.first >= 0) at.ask(turns, runs.first, pos + token, (int64_t)w.total);
+    Row row = load(first);                                   // while the angles are taken, and then a head ahead: no row overlaps another's output
+    if (runs.first >= 0) at.take(turns);
+    for (int h = first; h < heads; h += w.step) {
+        Row next = row;
+        if (h + w.step < heads) next = load(h + w.step);
+        const Rows& out = h < Hq ? Qo : Ko;
+        T* dst = reinterpret_cast<T*>(out.base + b * out.b + (h < Hq ? h : h - Hq) * out.h + t * out.t);
+        if (runs.first >= 0) turn_runs(row.a, row.b, at, turns.neighbours);
+        store_run(dst + runs.a, row.a);
+        store_run(dst + runs.b, row.b);
+        row = next;
     }
 }
 
@@ -59,31 +67,33 @@ __device__ __forceinline__ int paged_start(const PagedRows& p, int u) { return m
 __device__ __forceinline__ int paged_count(const PagedRows& p, int u, int b, int n) { return p.k ? max(0, min(p.k[p.per_batch ? b : u], n)) : n; }
 __device__ __forceinline__ int paged_len(const PagedRows& p, int start, int count) { return (int)min((int64_t)start + count, (int64_t)p.width << p.page_log2); }
 
-// Heads [0, Hkv) are those of K and V, [Hkv, heads) of Q (as many as are given).
+// Heads [0, Hkv) are those of K and V, [Hkv, heads) of Q (as many as are given).  A row's way is two round trips to memory: where a unit starts, how
+// much it brings and which token this is, all at once; then the row, and the page that it goes to.  Asking for the next head's row before
+// this one's is stored, as above, takes twice the registers and is slower (chunk of 5 x 777 tokens, 16 heads, fp32 10.9 -> 14.1 us).
 template <typename T, int D, bool TURN>
-__global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, RowsIn Q, Rows Qo, int Hkv, int G, int heads, Walk w, PagedRows p,
+__global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, RowsIn Q, Rows Qo, int Hkv, int G, uint32_t inv_G, int heads, Walk w, PagedRows p,
                                                            const int32_t* __restrict__ pos, Turns turns)
 {
     constexpr int kThreads = D / 16;
     const int slot = threadIdx.x / kThreads, c = threadIdx.x % kThreads;
     const int token = (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
     if (token >= w.total) return;
-    const int b = token / w.n, i = token - b * w.n;          // row i of what a unit brings
+    const int b = divided(token, w.n, w.inv_n), i = token - b * w.n;         // row i of what a unit brings
     const Runs runs(c, TURN ? turns.pairs : 0, TURN ? turns.neighbours : 0);
     Angles at;
-    bool have = false;
+    if (TURN && runs.first >= 0 && !p.idx) {
+        at.ask(turns, runs.first, pos + token, (int64_t)w.total);
+        at.take(turns);
+    }
     for (int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2); h < heads; h += w.step) {
         const bool query = h >= Hkv;
-        const int g = query ? (h - Hkv) / G : h, u = b * Hkv + g;
-        const int count = paged_count(p, u, b, w.n);
-        const int start = query ? 0 : paged_start(p, u);     // only the threads of a row of K may read it: len may stand there
+        const int g = query ? divided(h - Hkv, G, inv_G) : h, u = b * Hkv + g, set = p.per_batch ? b : u;
+        // only the threads of a row of K may read a start: len may stand there
+        const int brings = p.k ? p.k[set] : w.n, starts = query ? 0 : p.start[u];
+        const int which = p.idx ? p.idx[(int64_t)set * w.n + i] : i;
+        const int count = max(0, min(brings, w.n)), start = max(0, min(starts, p.width << p.page_log2)), t = max(0, min(which, w.n - 1));
         if (!query && i == 0 && c == 0 && p.len) p.len[u] = paged_len(p, start, count);
         if (i >= count) continue;
-        const int t = p.idx ? max(0, min(p.idx[(int64_t)(p.per_batch ? b : u) * w.n + i], w.n - 1)) : i;
-        if (TURN && runs.first >= 0 && (p.idx || !have)) {
-            at.set(turns, runs.first, pos + (int64_t)b * w.n + t, (int64_t)w.total);
-            have = true;
-        }
         if (query) {
             const T* src = reinterpret_cast<const T*>(Q.base + b * Q.b + (h - Hkv) * Q.h + t * Q.t);
             T* dst = reinterpret_cast<T*>(Qo.base + b * Qo.b + (h - Hkv) * Qo.h + t * Qo.t);
@@ -96,13 +106,19 @@ __global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, R
         const int64_t row = (int64_t)start + i;
         if (row >> p.page_log2 >= p.width) continue;         // behind the table
         const int page = p.table[(int64_t)u * p.width + (row >> p.page_log2)];
-        if ((unsigned)page >= (unsigned)p.num_pages) continue;
-        const int64_t at_row = (((int64_t)page << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * D;
         const T* ks = reinterpret_cast<const T*>(K.base + b * K.b + g * K.h + t * K.t);
         const T* vs = reinterpret_cast<const T*>(V.base + b * V.b + g * V.h + t * V.t);
         Run<T> ra = load_run(ks + runs.a), rb = load_run(ks + runs.b);
         const Run<T> va = load_run(vs + runs.a), vb = load_run(vs + runs.b);
-        if (TURN && runs.first >= 0) turn_runs(ra, rb, at, turns.neighbours);
+        if (TURN && runs.first >= 0) {
+            if (p.idx) {
+                at.ask(turns, runs.first, pos + (int64_t)b * w.n + t, (int64_t)w.total);
+                at.take(turns);
+            }
+            turn_runs(ra, rb, at, turns.neighbours);
+        }
+        if ((unsigned)page >= (unsigned)p.num_pages) continue;
+        const int64_t at_row = (((int64_t)page << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * D;
         T *kd = reinterpret_cast<T*>(p.K) + at_row, *vd = reinterpret_cast<T*>(p.V) + at_row;
         store_run(kd + runs.a, ra);
         store_run(kd + runs.b, rb);
@@ -120,6 +136,7 @@ __global__ __launch_bounds__(256) void advance_kernel(PagedRows p, int32_t* len,
 static Turns turns_of(const zipvl_rope* r, bool inverse) {
     Turns t = {};
     if (!r) return t;
+    t.axes = r->axes;
     t.pairs = r->pairs;
     t.neighbours = r->layout == ZIPVL_ROPE_NEIGHBOURS;
     t.backwards = inverse ? 0x80000000u : 0u;
@@ -135,6 +152,7 @@ static Turns turns_of(const zipvl_rope* r, bool inverse) {
 static RowsIn rows_in(const void* p, const int64_t (&s)[3], int e) { return {(const char*)p, s[0] * e, s[1] * e, s[2] * e}; }
 static Rows rows_out(void* p, const int64_t (&s)[3], int e) { return {(char*)p, s[0] * e, s[1] * e, s[2] * e}; }
 
+constexpr int kWalkGrid = 4096;
 static dim3 walk_of(const zipvl_dims& d, int heads, Walk& w) {
     const int rows = 4096 / d.d;                             // of a workgroup, a turn
     w.n = d.n;
@@ -143,8 +161,9 @@ static dim3 walk_of(const zipvl_dims& d, int heads, Walk& w) {
     while ((1 << w.tokens_log2) < rows && (1 << w.tokens_log2) < w.total) ++w.tokens_log2;
     const int lanes = rows >> w.tokens_log2, tiles = (w.total + (1 << w.tokens_log2) - 1) >> w.tokens_log2;
     const int most = (heads + lanes - 1) / lanes;
-    const int parts = std::max(1, std::min(most, (2048 + tiles - 1) / tiles));
+    const int parts = std::max(1, std::min(most, (kWalkGrid + tiles - 1) / tiles));
     w.step = parts * lanes;
+    w.inv_n = inverse(d.n);
     return dim3(tiles, parts);
 }
 
@@ -183,7 +202,7 @@ int launch_paged_append(const void* K, const void* V, const zipvl_dims& d, const
         KernelTimer tm(ZIPVL_K_PAGED_APPEND, st);
 #define ZIPVL_APPEND(T, D, TURN)                                                                                                           \
     hipLaunchKernelGGL((paged_append_kernel<T, D, TURN>), grid, dim3(256), 0, st, rows_in(K, d.k_strides, e), rows_in(V, d.v_strides, e),  \
-                       rows_in(Q, d.q_strides, e), rows_out(Qo, qo, e), d.Hkv, d.Hq / d.Hkv, heads, w, p, pos, turns)
+                       rows_in(Q, d.q_strides, e), rows_out(Qo, qo, e), d.Hkv, d.Hq / d.Hkv, inverse(d.Hq / d.Hkv), heads, w, p, pos, turns)
 #define ZIPVL_APPEND_T(T, D) do { if (rope) ZIPVL_APPEND(T, D, true); else ZIPVL_APPEND(T, D, false); } while (0)
         if (d.dtype == ZIPVL_BF16) { if (d.d == 128) ZIPVL_APPEND_T(__bf16, 128); else ZIPVL_APPEND_T(__bf16, 64); }
         else { if (d.d == 128) ZIPVL_APPEND_T(float, 128); else ZIPVL_APPEND_T(float, 64); }
