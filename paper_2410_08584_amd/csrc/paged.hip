@@ -12,6 +12,7 @@
 // Parts (max, sum, weighted sum of rows) of an item that was cut are joined by a second launch.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "launch.h"
 #include "ldsload.h"
@@ -40,7 +41,7 @@ struct PagedRead {
     const int32_t* prefix_table; int prefix_width; const int32_t* prefix_len;
     const int32_t* group_begin; int groups;
     int B, Hq, Hkv, G;
-    uint32_t inv_Hkv, inv_G;
+    uint32_t inv_Hkv, inv_G, inv_Hq;
     int least_few;
     __device__ __forceinline__ int prefixes() const { return groups * Hkv; }
     __device__ __forceinline__ int items() const { return (groups + B) * Hkv; }
@@ -116,10 +117,18 @@ __device__ __forceinline__ int wave_scan(int v) {
     return v;
 }
 
-__device__ __forceinline__ float other_half(float v) {
+// Over the groups of lanes that have one column each (lanes l and l ^ 32; for columns of 16 also l ^ 16), by register swaps.
+template <int COLS, typename F>
+__device__ __forceinline__ float over_groups(float v, F&& f) {
     const unsigned u = __float_as_uint(v);
     const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    if constexpr (COLS == 16) {
+        const unsigned x = __float_as_uint(v);
+        const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        v = f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    }
+    return v;
 }
 
 template <typename T, int D>
@@ -140,30 +149,54 @@ struct PartCfg {
     }
 };
 
-// A wave's queries against tiles of one item.
-template <typename T, int D>
+// A wave's queries, in 32 columns or in 16, against tiles of one item.  With 16 a tile is two of 16x16: half the matrix cycles and half the
+// exponentials, which is what a few tiles on their own last (fp32 products: 2 us a tile of d = 128, 4 with 32 columns).
+// Lane l has column l % COLS; the 64 / COLS groups of lanes share its keys and channels.
+template <typename T, int D, int COLS>
 struct WavePart {
     using C = PartCfg<T, D>;
-    uintx4 qf[C::CH];
-    floatx16 o[C::ODB];
-    float m, l;                                              // l: of the lane's half of the keys, until `finish`
+    static constexpr int kGroups = 64 / COLS, kFrags = C::RB / 16 / kGroups, kKeys = kTileRows / kGroups;
+    static constexpr int kPer = D / 16;                      // fp32, 16 columns: channels of a row that a lane has (weighted_rows)
+    static constexpr int kO = D / COLS;                      // blocks of COLS channels
+    using Acc = std::conditional_t<COLS == 32, floatx16, floatx4>;
+    uintx4 qf[kFrags];
+    Acc o[kO];
+    float m, l;                                              // l: of the lane's share of the keys while tiles come
 
     struct Tile { const char *k0, *k1, *v0, *v1; uint32_t rows; };      // of its first and second 16 rows; which of the 32 there are
+
+    // The lane, said anew: what follows from it is not worked out before the tiles and kept through them (it took 40 registers and spilled).
+    __device__ static __forceinline__ int here() {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
+        return lane;
+    }
+    __device__ static __forceinline__ int col() { return threadIdx.x & (COLS - 1); }
+    __device__ static __forceinline__ int group() { return (threadIdx.x & 63) / COLS; }
+    __device__ static __forceinline__ int key(int r) {      // of score r
+        if constexpr (COLS == 32) return acc_row(r, group());
+        else return 16 * (r >> 2) + 4 * group() + (r & 3);
+    }
+    static constexpr int kRegs = COLS == 32 ? 16 : 4;        // sums of a block in a lane
+    __device__ static __forceinline__ int channel(int b, int r, int group) {         // of o[b][r]
+        if constexpr (COLS == 32) return 32 * b + acc_row(r, group);
+        else if constexpr (sizeof(T) == 2) return 16 * b + 4 * group + r;
+        else return kPer * (4 * group + r) + b;
+    }
 
     __device__ __forceinline__ void reset() {
         m = -INFINITY;
         l = 0.f;
 #pragma unroll
-        for (int db = 0; db < C::ODB; ++db)
+        for (int b = 0; b < kO; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+            for (int r = 0; r < kRegs; ++r) o[b][r] = 0.f;
     }
-    __device__ __forceinline__ void load_queries(const T* row, bool there) {     // of column lane % 32
-        const int h = (threadIdx.x >> 5) & 1;
+    __device__ __forceinline__ void load_queries(const T* row, bool there) {     // of the lane's column
 #pragma unroll
-        for (int cc = 0; cc < C::CH; ++cc) {
+        for (int cc = 0; cc < kFrags; ++cc) {
             qf[cc] = uintx4{0, 0, 0, 0};
-            if (there) qf[cc] = load16(row + (2 * cc + h) * Elem<T>::kPerFrag);
+            if (there) qf[cc] = load16(row + (kGroups * cc + group()) * Elem<T>::kPerFrag);
         }
     }
 
@@ -189,87 +222,145 @@ struct WavePart {
         }
     }
 
-    __device__ __forceinline__ floatx16 scores(const char* kb) const {
-        const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
-        floatx16 s = {0};
+    __device__ static __forceinline__ floatx4 mma16(const uintx4& a, const uintx4& b, floatx4 acc) {
+        if constexpr (sizeof(T) == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+        else {
+            const floatx4 fa = __builtin_bit_cast(floatx4, a), fb = __builtin_bit_cast(floatx4, b);
 #pragma unroll
-        for (int cc = 0; cc < C::CH; ++cc) {
-            const uintx4 kf = *reinterpret_cast<const uintx4*>(kb + i * C::RB + swz_chunk(2 * cc + h, C::k_swizzle(i)));
-            s = mma_frag<T>(kf, qf[cc], s);
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], acc, 0, 0, 0);
+            return acc;
         }
-        return s;
+    }
+
+    __device__ __forceinline__ void scores(const char* kb, float (&s)[kKeys]) const {
+        const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
+        if constexpr (COLS == 32) {
+            floatx16 x = {0};
+#pragma unroll
+            for (int cc = 0; cc < kFrags; ++cc) {
+                const uintx4 kf = *reinterpret_cast<const uintx4*>(kb + i * C::RB + swz_chunk(2 * cc + group(), C::k_swizzle(i)));
+                x = mma_frag<T>(kf, qf[cc], x);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = x[r];
+        } else {
+            floatx4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+            for (int cc = 0; cc < kFrags; ++cc)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uintx4 kf = *reinterpret_cast<const uintx4*>(kb + (16 * t + i) * C::RB + swz_chunk(4 * cc + group(), C::k_swizzle(16 * t + i)));
+                    x[t] = mma16(kf, qf[cc], x[t]);
+                }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) s[r] = x[r >> 2][r & 3];
+        }
     }
 
     // scores -> weights; the offset m follows the running maximum lazily
-    __device__ __forceinline__ void weigh(floatx16& s, uint32_t rows, float c) {
-        const int h = (threadIdx.x >> 5) & 1;
+    __device__ __forceinline__ void weigh(float (&s)[kKeys], uint32_t rows, float c) {
         if (rows != 0xFFFFFFFFu) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (!(rows >> acc_row(r, h) & 1)) s[r] = -INFINITY;
+            for (int r = 0; r < kKeys; ++r)
+                if (!(rows >> key(r) & 1)) s[r] = -INFINITY;
         }
         float mx = s[0];
 #pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        for (int r = 1; r < kKeys; ++r) mx = fmaxf(mx, s[r]);
         mx *= c;
         if (__any(mx > m + kLazy)) {
-            mx = fmaxf(mx, other_half(mx));
+            mx = over_groups<COLS>(mx, [](float a, float b) { return fmaxf(a, b); });
             const float m_new = fmaxf(m, mx), a = m_new > -INFINITY ? fast_exp2(m - m_new) : 1.f;
             l *= a;
 #pragma unroll
-            for (int db = 0; db < C::ODB; ++db)
+            for (int b = 0; b < kO; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[db][r] *= a;
+                for (int r = 0; r < kRegs; ++r) o[b][r] *= a;
             m = m_new;
         }
         const float ms = m > -INFINITY ? m : 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < kKeys; ++r) {
             s[r] = fast_exp2(fmaf(s[r], c, -ms));
             l += s[r];
         }
     }
 
-    // O^T += V^T P^T.  The accumulators of S^T are the operand of P^T as they are (contraction slot t of a lane = key 16 s2 + 8 (t / 4) + 4 h + t % 4).
+    // O^T += V^T P^T.  A lane's weights are the operand of P^T as they are: contraction slot t of a lane = its key t.
     // bf16: the weights as two planes, 16 bits of each: one plane alone is off by 2^-9 of a weight, as much as the output's own rounding where a
     // few rows have all the weight, and costs as much memory time.
-    __device__ __forceinline__ void weighted_rows(const char* vb, const floatx16& s) {
-        const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    __device__ __forceinline__ void weighted_rows(const char* vb, const float (&s)[kKeys]) {
+        const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
         if constexpr (sizeof(T) == 2) {
             typedef short shortx4 __attribute__((ext_vector_type(4)));
             using lds_ptr = __attribute__((address_space(3))) shortx4*;
-            const int grp = (lane >> 4) & 1, e = (lane >> 2) & 3, q = lane & 3, row = 4 * h + e;
-            uintx4 hi[2], lo[2];
+            uintx4 hi[kKeys / 8], lo[kKeys / 8];
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2)
+            for (int y = 0; y < kKeys / 8; ++y)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float a = s[8 * s2 + 2 * x], b = s[8 * s2 + 2 * x + 1];
+                    const float a = s[8 * y + 2 * x], b = s[8 * y + 2 * x + 1];
                     const uint32_t w = pack_bf16x2(a, b);
-                    hi[s2][x] = w;
-                    lo[s2][x] = pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xFFFF0000u));
+                    hi[y][x] = w;
+                    lo[y][x] = pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xFFFF0000u));
                 }
+            // Channel l of four keys for every lane l of 16, which give the addresses of four consecutive channels each: lane 4 e + q of key e.
+            const int e = (lane >> 2) & 3, q = lane & 3, row = 4 * group() + e;
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2)
+            for (int y = 0; y < kKeys / 8; ++y)
 #pragma unroll
-                for (int db = 0; db < C::ODB; ++db) {
-                    const char* a0 = vb + (row + 16 * s2) * C::RB + swz_chunk(4 * db + 2 * grp + (q >> 1), C::v_swizzle(row)) + (q & 1) * 8;
+                for (int b = 0; b < kO; ++b) {
+                    const int chunk = COLS == 32 ? 4 * b + 2 * ((lane >> 4) & 1) + (q >> 1) : 2 * b + (q >> 1);
+                    const char* a0 = vb + (row + 16 * y) * C::RB + swz_chunk(chunk, C::v_swizzle(row)) + (q & 1) * 8;
                     const uintx2 f0 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)a0));
-                    const uintx2 f1 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a0 + 8 * C::RB)));
+                    const uintx2 f1 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a0 + (COLS == 32 ? 8 : 16) * C::RB)));
                     const uintx4 vf = {f0[0], f0[1], f1[0], f1[1]};
-                    o[db] = mma_frag<__bf16>(vf, lo[s2], o[db]);
-                    o[db] = mma_frag<__bf16>(vf, hi[s2], o[db]);
+                    if constexpr (COLS == 32) {
+                        o[b] = mma_frag<__bf16>(vf, lo[y], o[b]);
+                        o[b] = mma_frag<__bf16>(vf, hi[y], o[b]);
+                    } else {
+                        o[b] = mma16(vf, lo[y], o[b]);
+                        o[b] = mma16(vf, hi[y], o[b]);
+                    }
                 }
-        } else {
+        } else if constexpr (COLS == 32) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int key = acc_row(r, h);
+                const int k = key(r);
 #pragma unroll
-                for (int db = 0; db < C::ODB; ++db) {
-                    const float v = *reinterpret_cast<const float*>(vb + key * C::RB + swz_chunk(8 * db + (i >> 2), C::v_swizzle(key)) + (i & 3) * 4);
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], o[db], 0, 0, 0);
+                for (int b = 0; b < kO; ++b) {
+                    const float v = *reinterpret_cast<const float*>(vb + k * C::RB + swz_chunk(8 * b + (i >> 2), C::v_swizzle(k)) + (i & 3) * 4);
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], o[b], 0, 0, 0);
                 }
             }
+        } else {
+            // a lane reads its kPer channels of a row as they stand; channel kPer i + b is row i of block b
+#pragma unroll
+            for (int r = 0; r < kKeys; ++r) {
+                const int k = key(r);
+#pragma unroll
+                for (int x = 0; x < kPer / 4; ++x) {
+                    const floatx4 v = *reinterpret_cast<const floatx4*>(vb + k * C::RB + swz_chunk(kPer / 4 * i + x, C::v_swizzle(k)));
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) o[4 * x + y] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[y], s[r], o[4 * x + y], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // The lane's sums to a record of D floats.
+    __device__ __forceinline__ void store(float* dst) const {
+        const int group = here() / COLS;
+        if constexpr (COLS == 16 && sizeof(T) == 4) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int x = 0; x < kPer / 4; ++x) *reinterpret_cast<floatx4*>(dst + channel(4 * x, r, group)) = floatx4{o[4 * x][r], o[4 * x + 1][r], o[4 * x + 2][r], o[4 * x + 3][r]};
+        } else {
+#pragma unroll
+            for (int b = 0; b < kO; ++b)
+#pragma unroll
+                for (int r = 0; r < kRegs; r += 4) *reinterpret_cast<floatx4*>(dst + channel(b, r, group)) = floatx4{o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]};
         }
     }
 
@@ -327,7 +418,8 @@ struct WavePart {
         while (have) {
             const bool more = next(nxt);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::NL) : "memory");             // all but V of this tile
-            floatx16 s = scores(kb);
+            float s[kKeys];
+            scores(kb, s);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                       // K has been read
             if (more) fetch<false>(nxt.k0, nxt.k1, nxt.rows, klds);
             weigh(s, cur.rows, c);
@@ -339,6 +431,7 @@ struct WavePart {
             cur = nxt;
             have = more;
         }
+        l = over_groups<COLS>(l, [](float a, float b) { return a + b; });
     }
 };
 
@@ -533,26 +626,83 @@ struct Walker {
     }
 };
 
-// A lane's part to its record.
-template <typename T, int D>
-__device__ __forceinline__ void store_part(const Parts& out, int rec, const WavePart<T, D>& part, int h) {
-    float* dst = out.o + (int64_t)rec * D;
+// What the waves of a workgroup have of a block of queries: `phases` waves the same columns and every phases-th tile.
+struct Block {
+    int unit, g, first, block, cols;                         // first: batch element; of the group, if it is a prefix
+    int phases, phase, first_col;
+    bool own, begins, whole;
+};
+
+// All waves of the workgroup.
+template <typename T, int D, int COLS>
+__device__ __forceinline__ void shared_piece(const T* __restrict__ q, const PagedRead& p, float c, const Parts& out, const Piece& x, const Block& k, int me,
+                                             char* smem, float2 (&ml)[kPartWaves][kCols])
+{
+    using C = PartCfg<T, D>;
+    const int w = scalar(threadIdx.x >> 6);
+    char* const mine = smem + w * C::WAVE;
+    const int in_wave = min(COLS, k.cols - k.first_col);     // columns; none where a block has three times 32
+    auto row_of = [&](int col) {                             // column of the block -> row of the output
+        const int r = k.block * kBlock + col, s = divided(r, p.G, p.inv_G);
+        return (k.first + s) * p.Hq + k.g * p.G + r - s * p.G;
+    };
+    auto record = [&](int col) { return k.whole ? out.whole(row_of(col), k.own) : out.piece(k.own, me, k.begins, col); };
+    WavePart<T, D, COLS> part;
+    part.reset();
+    part.load_queries(q + (int64_t)row_of(k.first_col + max(0, min(part.col(), in_wave - 1))) * D, part.col() < in_wave);
+    const int32_t* table = k.own ? p.table + (int64_t)k.unit * p.width : p.prefix_table + (int64_t)k.unit * p.prefix_width;
+    if (in_wave > 0) part.run(p, table, x.it.rows, x.ta + k.phase, k.phases, x.tb, c, mine);
+    if (k.phases == 1) {
+        const int i = part.here() & (COLS - 1);
+        if (i < in_wave) {
+            const int64_t rec = record(k.first_col + i);
+            part.store(out.o + rec * D);
+            if (part.group() == 0) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(part.m, part.l);
+        }
+        return;
+    }
+    // The parts of waves with the same columns meet in LDS: [channel][column], columns turned by the channel so that neither way through meets conflicts.
+    const int lane = part.here(), i = lane & (COLS - 1), group = lane / COLS;
+    if (group == 0) ml[w][i] = make_float2(part.m, part.l);
+    __syncthreads();
+    float M = -INFINITY, L = 0.f;
+    const int w0 = w - k.phase;
+    for (int y = 0; y < k.phases; ++y) M = fmaxf(M, ml[w0 + y][i].x);
+    for (int y = 0; y < k.phases; ++y) L += M > -INFINITY ? fast_exp2(ml[w0 + y][i].x - M) * ml[w0 + y][i].y : 0.f;
+    const float a = M > -INFINITY ? fast_exp2(part.m - M) : 0.f;
+    if (k.phase == 0 && group == 0 && i < in_wave) *reinterpret_cast<float2*>(out.ml + 2 * (int64_t)record(k.first_col + i)) = make_float2(M, L);
+    float* mo = reinterpret_cast<float*>(mine);
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+    for (int b = 0; b < part.kO; ++b)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<floatx4*>(dst + 32 * db + 8 * x + 4 * h) = floatx4{part.o[db][4 * x], part.o[db][4 * x + 1], part.o[db][4 * x + 2], part.o[db][4 * x + 3]};
-    if (h == 0) *reinterpret_cast<float2*>(out.ml + 2 * (int64_t)rec) = make_float2(part.m, part.l);
+        for (int r = 0; r < part.kRegs; ++r) {
+            const int ch = part.channel(b, r, group);
+            mo[ch * kCols + (i ^ (ch & 31))] = part.o[b][r] * a;
+        }
+    __syncthreads();
+    const int tid = w * 64 + lane, ch = tid % (D / 4) * 4, rec0 = k.whole ? 0 : out.piece(k.own, me, k.begins, 0);
+#pragma unroll 4
+    for (int cc = tid / (D / 4); cc < k.cols; cc += 64 * kPartWaves / (D / 4)) {
+        const float* base = reinterpret_cast<const float*>(smem + cc / kCols * k.phases * C::WAVE);
+        floatx4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = base[(ch + e) * kCols + ((cc % kCols) ^ ((ch + e) & 31))];
+        for (int z = 1; z < k.phases; ++z)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += base[z * (C::WAVE / 4) + (ch + e) * kCols + ((cc % kCols) ^ ((ch + e) & 31))];
+        *reinterpret_cast<floatx4*>(out.o + (int64_t)(k.whole ? out.whole(row_of(cc), k.own) : rec0 + cc) * D + ch) = v;
+    }
+    __syncthreads();
 }
 
-template <typename T, int D>
+// OWN: columns for the queries of a group of heads.  With 16, blocks of up to 16 queries of a prefix have 16 too.
+template <typename T, int D, int OWN>
 __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void paged_part_kernel(const T* __restrict__ q, PagedRead p, float c, Parts out) {
     using C = PartCfg<T, D>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ LineShared sh;
     __shared__ float2 ml[kPartWaves][kCols];
-    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i = lane & 31, h = lane >> 5;
-    char* const mine = smem + w * C::WAVE;
+    const int tid = threadIdx.x, w = scalar(tid >> 6);
     Line line;
     static_assert(kSeen * sizeof(Item) <= C::LDS, "the items' sizes stand where tiles come later");
     if (!find_piece(p, sh, reinterpret_cast<Item*>(smem), line)) return;
@@ -564,67 +714,28 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
     const int prefixes = p.prefixes();
     Piece x;
     while (walk.next(x, line.each)) {                        // of all waves
-        const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
-        const int unit = x.own ? x.item - prefixes : x.item, group = x.own ? 0 : divided(unit, p.Hkv, p.inv_Hkv);
-        const int g = x.own ? unit - x.it.begin() * p.Hkv : unit - group * p.Hkv;
-        const int cols = min(kBlock, x.it.cols() - x.block * kBlock), f = x.it.factor(x.block);
-        int2* const piece = out.pieces + (x.own ? piece_own(p, unit) : piece_prefix(p, group, x.it.begin(), x.block, g));
+        const bool ends = x.tb == x.it.tiles();
+        Block k;
+        k.own = x.own;
+        k.begins = x.ta == 0;
+        k.whole = k.begins && ends;
+        k.unit = x.own ? x.item - prefixes : x.item;
+        const int group = x.own ? 0 : divided(k.unit, p.Hkv, p.inv_Hkv);
+        k.g = x.own ? k.unit - x.it.begin() * p.Hkv : k.unit - group * p.Hkv;
+        k.first = x.it.begin();
+        k.block = x.block;
+        k.cols = min(kBlock, x.it.cols() - x.block * kBlock);
+        const int f = x.it.factor(x.block);
+        k.phases = kPartWaves / f;
+        k.phase = w & (k.phases - 1);
+        k.first_col = f == 1 ? 0 : f == 2 ? (w >> 1) * kCols : w * kCols;
+        int2* const piece = out.pieces + (x.own ? piece_own(p, k.unit) : piece_prefix(p, group, k.first, x.block, k.g));
         if (tid == 0) {
-            if (begins) piece->x = line.me;
+            if (k.begins) piece->x = line.me;
             if (ends) piece->y = line.me;
         }
-        const int phases = kPartWaves / f, phase = w & (phases - 1), first_col = f == 1 ? 0 : f == 2 ? (w >> 1) * kCols : w * kCols;
-        const int in_wave = min(kCols, cols - first_col);    // columns; none where a block has three times 32
-        auto row_of = [&](int col) {                         // column of the block -> row of the output
-            const int r = x.block * kBlock + col, s = divided(r, p.G, p.inv_G);
-            return (x.it.begin() + s) * p.Hq + g * p.G + r - s * p.G;
-        };
-        const int row = row_of(first_col + max(0, min(i, in_wave - 1)));     // of this lane's query
-        WavePart<T, D> part;
-        part.reset();
-        part.load_queries(q + (int64_t)row * D, i < in_wave);
-        const int32_t* table = x.own ? p.table + (int64_t)unit * p.width : p.prefix_table + (int64_t)unit * p.prefix_width;
-        if (in_wave > 0) part.run(p, table, x.it.rows, x.ta + phase, phases, x.tb, c, mine);
-        part.l += other_half(part.l);
-        auto record = [&](int col) { return whole ? out.whole(row_of(col), x.own) : out.piece(x.own, line.me, begins, col); };
-        if (phases == 1) {
-            if (i < in_wave) store_part<T, D>(out, record(first_col + i), part, h);
-            continue;
-        }
-        // The parts of waves with the same columns meet in LDS: [channel][column], columns turned by the channel so that neither way through meets conflicts.
-        if (h == 0) ml[w][i] = make_float2(part.m, part.l);
-        __syncthreads();
-        float M = -INFINITY, L = 0.f;
-        const int w0 = w - phase;
-        for (int y = 0; y < phases; ++y) M = fmaxf(M, ml[w0 + y][i].x);
-        for (int y = 0; y < phases; ++y) L += M > -INFINITY ? fast_exp2(ml[w0 + y][i].x - M) * ml[w0 + y][i].y : 0.f;
-        const float a = M > -INFINITY ? fast_exp2(part.m - M) : 0.f;
-        if (phase == 0 && h == 0 && i < in_wave) *reinterpret_cast<float2*>(out.ml + 2 * (int64_t)record(first_col + i)) = make_float2(M, L);
-        float* mo = reinterpret_cast<float*>(mine);
-#pragma unroll
-        for (int db = 0; db < C::ODB; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int ch = 32 * db + acc_row(r, h);
-                mo[ch * kCols + (i ^ (ch & 31))] = part.o[db][r] * a;
-            }
-        __syncthreads();
-        const int ch = tid % (D / 4) * 4, rec0 = whole ? 0 : out.piece(x.own, line.me, begins, 0);
-        int at[4];                                           // of channels ch .. ch + 3 in a column's place before it is turned
-#pragma unroll
-        for (int e = 0; e < 4; ++e) at[e] = (ch + e) * kCols;
-#pragma unroll 4
-        for (int cc = tid / (D / 4); cc < cols; cc += 64 * kPartWaves / (D / 4)) {
-            const float* base = reinterpret_cast<const float*>(smem + cc / kCols * phases * C::WAVE);
-            floatx4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = base[at[e] + ((cc % kCols) ^ ((ch + e) & 31))];
-            for (int z = 1; z < phases; ++z)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += base[z * (C::WAVE / 4) + at[e] + ((cc % kCols) ^ ((ch + e) & 31))];
-            *reinterpret_cast<floatx4*>(out.o + (int64_t)(whole ? out.whole(row_of(cc), x.own) : rec0 + cc) * D + ch) = v;
-        }
-        __syncthreads();
+        if (OWN == 16 && k.cols <= 16) shared_piece<T, D, 16>(q, p, c, out, x, k, line.me, smem, ml);
+        else shared_piece<T, D, 32>(q, p, c, out, x, k, line.me, smem, ml);
     }
     if (line.each || line.hi <= line.own) return;
 
@@ -633,7 +744,7 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
     const int from = max(line.lo, line.own), all = line.hi - from, quarter = all / kPartWaves, rest = all % kPartWaves;
     walk.pos = all < kLeast ? from : from + w * quarter + min(w, rest);
     walk.hi = all < kLeast ? (w == kPartWaves - 1 ? line.hi : from) : walk.pos + quarter + (w < rest);
-    const int who = line.me * kPartWaves + w;
+    const int who = line.me * kPartWaves + w, i = tid & (OWN - 1), lane = tid & 63;
     while (walk.next(x, 0)) {
         const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
         const int unit = x.item - prefixes, row = x.it.begin() * p.Hq + (unit - x.it.begin() * p.Hkv) * p.G + min(i, p.G - 1);
@@ -641,23 +752,29 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
             if (begins) out.pieces[piece_own(p, unit)].x = who;
             if (ends) out.pieces[piece_own(p, unit)].y = who;
         }
-        WavePart<T, D> part;
+        WavePart<T, D, OWN> part;
         part.reset();
         part.load_queries(q + (int64_t)row * D, i < p.G);
-        part.run(p, p.table + (int64_t)unit * p.width, x.it.rows, x.ta, 1, x.tb, c, mine);
-        part.l += other_half(part.l);
-        if (i < p.G) store_part<T, D>(out, whole ? out.whole(row, 1) : out.piece(1, who, begins, i), part, h);
+        part.run(p, p.table + (int64_t)unit * p.width, x.it.rows, x.ta, 1, x.tb, c, smem + w * C::WAVE);
+        if (i < p.G) {
+            const int64_t rec = whole ? out.whole(row, 1) : out.piece(1, who, begins, i);
+            part.store(out.o + rec * D);
+            if (lane < OWN) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(part.m, part.l);
+        }
     }
 }
 
 // The parts of one query head: those of its group's prefix, then its own -> its output row.  A chain of loads, each for the address of the next:
-// groups, pieces (with the lengths), parts (maxima, sums and the first 64 parts' outputs at once).
-template <typename T, int D>
+// groups, pieces (with the lengths), parts (maxima, sums and the first parts' outputs at once).  WAVES waves have a row: all four where a row
+// may have many parts; one where rows are many, each has a few and dispatching a workgroup for it is what lasts (join_waves).
+template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts in, T* __restrict__ o) {
-    constexpr int kPer = D / 4, kAt = 256 / kPer, kAtOnce = 64 / kAt;        // threads per part, parts at a time
+    constexpr int kPer = D / 4, kAt = 64 * WAVES / kPer, kAtOnce = WAVES == 1 ? 4 : 64 / kAt;        // threads per part, parts at a time, loads on the way
     __shared__ floatx4 sum[256];
-    const int row = blockIdx.x, b = row / p.Hq, head = row - b * p.Hq, g = head / p.G, u = b * p.Hkv + g;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = WAVES == 1 ? lane : threadIdx.x;  // among the row's threads
+    const int row = scalar(WAVES == 1 ? (int)blockIdx.x * 4 + w : (int)blockIdx.x);
+    if (row >= in.rows) return;                              // of one wave a row: nobody waits
+    const int b = divided(row, p.Hq, p.inv_Hq), head = row - b * p.Hq, g = divided(head, p.G, p.inv_G), u = b * p.Hkv + g;
     const int2 own_pieces = in.pieces[piece_own(p, u)];
     const int own_len = own_rows(p, u);
     int2 pre = {0, -1}, own = {0, -1};
@@ -691,27 +808,40 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
         const int rec = record(s0 + min(lane, count - 1));
         if (lane < count) v = *reinterpret_cast<const float2*>(in.ml + 2 * (int64_t)rec);
         floatx4 part[kAtOnce];
+        auto ask = [&](int y0) {
 #pragma unroll
-        for (int y = 0; y < kAtOnce; ++y)
-            if (y * kAt < count) part[y] = *reinterpret_cast<const floatx4*>(in.o + (int64_t)__shfl(rec, y * kAt + tid / kPer) * D + tid % kPer * 4);
+            for (int y = 0; y < kAtOnce; ++y)
+                if ((y0 + y) * kAt < count) part[y] = *reinterpret_cast<const floatx4*>(in.o + (int64_t)__shfl(rec, (y0 + y) * kAt + tid / kPer) * D + tid % kPer * 4);
+        };
+        ask(0);
         const float M_new = fmaxf(M, wave_max(v.x));
         const float a = M_new > -INFINITY ? fast_exp2(v.x - M_new) : 0.f, before = M_new > -INFINITY ? fast_exp2(M - M_new) : 0.f;
         L = L * before + wave_sum(a * v.y);
         acc *= before;
         M = M_new;
+        for (int y0 = 0; y0 * kAt < count; y0 += kAtOnce) {
+            if (y0) ask(y0);
 #pragma unroll
-        for (int y = 0; y < kAtOnce; ++y)
-            if (y * kAt < count) {                           // all lanes: a lane that is not there answers no other
-                const float weight = __shfl(a, y * kAt + tid / kPer);
-                if (y * kAt + tid / kPer < count) acc += weight * part[y];
-            }
+            for (int y = 0; y < kAtOnce; ++y)
+                if ((y0 + y) * kAt < count) {                // all lanes: a lane that is not there answers no other
+                    const float weight = __shfl(a, (y0 + y) * kAt + tid / kPer);
+                    if ((y0 + y) * kAt + tid / kPer < count) acc += weight * part[y];
+                }
+        }
     }
-    sum[tid] = acc;
-    __syncthreads();
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int off = kPer; off < 64; off <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], off);
+    } else {
+        sum[tid] = acc;
+        __syncthreads();
+        if (tid < kPer)
+            for (int x = 1; x < min(kAt, n); ++x) acc += sum[x * kPer + tid];
+    }
     if (tid < kPer) {
-        for (int x = 1; x < min(kAt, n); ++x) acc += sum[x * kPer + tid];
-        const float inv = L > 0.f ? 1.f / L : 0.f;
-        acc *= inv;
+        acc *= L > 0.f ? 1.f / L : 0.f;
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uintx2*>(o + (int64_t)row * D + tid * 4) = uintx2{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
         else *reinterpret_cast<floatx4*>(o + (int64_t)row * D + tid * 4) = acc;
     }
@@ -733,7 +863,7 @@ static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes) {
 
 size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) { return paged_layout(d, prefix > 0).total; }
 
-template <typename T, int D>
+template <typename T, int D, int OWN>
 static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, float scale, T* o, char* ws, hipStream_t st) {
     using C = PartCfg<T, D>;
     const PagedLayout l = paged_layout(d, p.groups > 0);
@@ -748,18 +878,19 @@ static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, f
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return set_error(ZIPVL_EHIP, "decode_attn_paged: no current device");
     if (dev > 63 || !(lds_set.load(std::memory_order_relaxed) >> dev & 1)) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_part_kernel<T, D>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess)
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_part_kernel<T, D, OWN>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess)
             return set_error(ZIPVL_EHIP, "decode_attn_paged: %d bytes of LDS are refused", (int)C::LDS);
         if (dev <= 63) lds_set.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     {
         KernelTimer tm(ZIPVL_K_PAGED_PARTIAL, st);
-        hipLaunchKernelGGL((paged_part_kernel<T, D>), dim3(wgs), dim3(64 * kPartWaves), C::LDS, st, q, p, scale * kLog2e, parts);
+        hipLaunchKernelGGL((paged_part_kernel<T, D, OWN>), dim3(wgs), dim3(64 * kPartWaves), C::LDS, st, q, p, scale * kLog2e, parts);
         const int rc = check_launch("decode_attn_paged");
         if (rc) return rc;
     }
     KernelTimer tm(ZIPVL_K_PAGED_COMBINE, st);
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(d.B * d.Hq), dim3(256), 0, st, p, parts, o);
+    if (parts.rows >= 1536 && (p.groups ? p.groups : d.B) * d.Hkv >= 32) hipLaunchKernelGGL((paged_join_kernel<T, D, 1>), dim3((parts.rows + 3) / 4), dim3(256), 0, st, p, parts, o);
+    else hipLaunchKernelGGL((paged_join_kernel<T, D, 4>), dim3(parts.rows), dim3(256), 0, st, p, parts, o);
     return check_launch("decode_attn_paged parts");
 }
 
@@ -769,12 +900,14 @@ int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int3
 {
     const PagedRead p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len,
                          prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, d.Hq / d.Hkv,
-                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), d.dtype == ZIPVL_BF16 ? kLeastFew<__bf16> : kLeastFew<float>};
-    if (d.dtype == ZIPVL_BF16)
-        return d.d == 128 ? launch_paged_t<__bf16, 128>((const __bf16*)q, p, d, scale, (__bf16*)o, (char*)ws, st)
-                          : launch_paged_t<__bf16, 64>((const __bf16*)q, p, d, scale, (__bf16*)o, (char*)ws, st);
-    return d.d == 128 ? launch_paged_t<float, 128>((const float*)q, p, d, scale, (float*)o, (char*)ws, st)
-                      : launch_paged_t<float, 64>((const float*)q, p, d, scale, (float*)o, (char*)ws, st);
+                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), inverse(d.Hq), d.dtype == ZIPVL_BF16 ? kLeastFew<__bf16> : kLeastFew<float>};
+#define ZIPVL_PAGED(T, D)                                                                              \
+    return p.G <= 16 ? launch_paged_t<T, D, 16>((const T*)q, p, d, scale, (T*)o, (char*)ws, st)       \
+                     : launch_paged_t<T, D, 32>((const T*)q, p, d, scale, (T*)o, (char*)ws, st)
+    if (d.dtype == ZIPVL_BF16) { if (d.d == 128) ZIPVL_PAGED(__bf16, 128); ZIPVL_PAGED(__bf16, 64); }
+    if (d.d == 128) ZIPVL_PAGED(float, 128);
+    ZIPVL_PAGED(float, 64);
+#undef ZIPVL_PAGED
 }
 
 }  // namespace zipvl
