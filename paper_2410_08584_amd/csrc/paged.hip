@@ -28,7 +28,6 @@ constexpr int kLeast = 8;            // weight below which a workgroup is not wo
 template <typename T> constexpr int kLeastFew = sizeof(T) == 2 ? 8 : 4;
 constexpr int kCus = 256, kEarly = 17, kLate = 15;
 constexpr int kMostFew = 24;
-constexpr int kPartGrid = 512;       // two workgroups a CU
 constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
 
 // a wave-uniform number in scalar registers
@@ -42,7 +41,7 @@ struct PagedRead {
     const int32_t* group_begin; int groups;
     int B, Hq, Hkv, G;
     uint32_t inv_Hkv, inv_G, inv_Hq;
-    int least_few;
+    int least_few, wide;
     __device__ __forceinline__ int prefixes() const { return groups * Hkv; }
     __device__ __forceinline__ int items() const { return (groups + B) * Hkv; }
 };
@@ -52,10 +51,10 @@ struct PagedRead {
 // wave G and G of own items in the same way.  `pieces` says of every own item and every block of a prefix from which to which
 // workgroup, or wave, its pieces are.
 struct Parts {
-    float* o; float* ml; int2* pieces; int rows, cols, G;    // rows = B Hq
+    float* o; float* ml; int2* pieces; int rows, cols, G, grid;      // rows = B Hq
     __device__ __forceinline__ int whole(int row, int own) const { return 2 * row + own; }
     __device__ __forceinline__ int piece(int own, int who, int begins, int col) const {      // below 2^20
-        return 2 * rows + (own ? 2 * kPartGrid * cols + (who * 2 + begins) * G : (who * 2 + begins) * cols) + col;
+        return 2 * rows + (own ? 2 * grid * cols + (who * 2 + begins) * G : (who * 2 + begins) * cols) + col;
     }
 };
 // Blocks of a prefix are counted from begin G / kBlock + p: no two groups meet, and B G / kBlock + groups + 1 are enough.
@@ -74,7 +73,7 @@ __device__ __forceinline__ int own_rows(const PagedRead& p, int u) { return clam
 __device__ __forceinline__ int prefix_rows(const PagedRead& p, int i) { return clamped(p.prefix_len[i], 0, p.prefix_width << p.page_log2); }
 
 // Items: (prefix, KV head) first, then (batch element, KV head).  A wave's tile is one unit of weight: a tile of a block weighs 1, 2 or 4 by
-// the waves that have it.
+// the waves that have it; of fp32 rows twice that where it takes 32 columns, not 16 (`wide`: matrix time is what fp32 tiles last).
 struct Item {
     int rows;                                                // of the cache
     uint32_t who;                                            // queries | first batch element << 16: both below 2^16
@@ -82,14 +81,17 @@ struct Item {
     __device__ __forceinline__ int begin() const { return who >> 16; }
     __device__ __forceinline__ int tiles() const { return (rows + kTileRows - 1) / kTileRows; }
     __device__ __forceinline__ int blocks() const { return rows ? (cols() + kBlock - 1) / kBlock : 0; }
-    __device__ __forceinline__ int factor(int block) const {
+    __device__ __forceinline__ int waves_log2(int block) const {            // that have the same tile
         const int left = cols() - block * kBlock;
-        return left <= kCols ? 1 : left <= 2 * kCols ? 2 : 4;
+        return left <= kCols ? 0 : left <= 2 * kCols ? 1 : 2;
     }
-    __device__ __forceinline__ int weight_of_full_block() const { return 4 * tiles() + kStartPrefix; }
-    __device__ __forceinline__ int weight(bool own) const {  // below 2^31: at most 512 blocks of 2^19 tiles
+    __device__ __forceinline__ int tile_log2(int block, int wide) const {   // weight of a tile: up to 8
+        return waves_log2(block) + (cols() - block * kBlock > 16 ? wide : 0);
+    }
+    __device__ __forceinline__ int weight_of_full_block(int wide) const { return (tiles() << (2 + wide)) + kStartPrefix; }
+    __device__ __forceinline__ int weight(int start, int wide) const {
         const int n = blocks();
-        return n ? (n - 1) * weight_of_full_block() + factor(n - 1) * tiles() + (own ? kStartOwn : kStartPrefix) : 0;
+        return n ? (n - 1) * weight_of_full_block(wide) + (tiles() << tile_log2(n - 1, wide)) + start : 0;
     }
 };
 __device__ __forceinline__ Item own_item(const PagedRead& p, int u, int length) {
@@ -140,7 +142,8 @@ struct PartCfg {
     static constexpr int CH = D / Elem<T>::kPerChunk, ODB = D / 32;
     static_assert(WAVE >= D * kCols * 4, "room for a wave's sums");
     static constexpr int LDS = kPartWaves * WAVE;
-    static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
+    static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;           // workgroups, of bf16 rows of 64 channels too: three are up to 10 % slower
+    static constexpr int GRID = kCus * PER_CU;
     // swizzle of row r's 16-byte chunks: K is read 32 rows at a time at one chunk, V of bf16 by transposing reads
     __device__ static __forceinline__ int k_swizzle(int r) { return k_row_swizzle<RB>(r); }
     __device__ static __forceinline__ int v_swizzle(int r) {
@@ -435,7 +438,7 @@ struct WavePart {
     }
 };
 
-// a / b for 0 <= a < 2^22, b > 0 (512 * 512 and four times the tiles of an item are less; kMostFew * 512 too): the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
+// a / b for 0 <= a < 2^22, b > 0 (512 * 512 and eight times the tiles of an item are less; kMostFew * 512 too): the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
 __device__ __forceinline__ int quotient(int a, int b) {
     const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), left = a - q * b;
     return q + (left >= b) - (left < 0);
@@ -463,11 +466,11 @@ struct LineShared {
 };
 constexpr int kSeen = 4096;          // items whose sizes are left in LDS
 
-__device__ __forceinline__ int workgroups_of_full_block(const Item& it, int each) { return quotient(4 * it.tiles() - 1, each) + 1; }
-__device__ __forceinline__ int workgroups_of_block(const Item& it, int block, int each) { return quotient(it.factor(block) * it.tiles() - 1, each) + 1; }
-__device__ __forceinline__ int workgroups_of(const Item& it, int each) {
+// at most one a tile
+__device__ __forceinline__ int workgroups_of_block(const Item& it, int tile_log2, int each) { return min(quotient((it.tiles() << tile_log2) - 1, each) + 1, it.tiles()); }
+__device__ __forceinline__ int workgroups_of(const Item& it, int each, int wide) {
     const int n = it.blocks();
-    return n ? (n > 1 ? (n - 1) * workgroups_of_full_block(it, each) : 0) + workgroups_of_block(it, n - 1, each) : 0;
+    return n ? (n > 1 ? (n - 1) * workgroups_of_block(it, 2 + wide, each) : 0) + workgroups_of_block(it, it.tile_log2(n - 1, wide), each) : 0;
 }
 
 // What a thread has of a kind of items: `per` of them from `from`.
@@ -491,7 +494,7 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     for (int i = pre.from; i < pre.end; ++i) {
         const Item it = item_of(p, i);
         if (i == pre.from) first_pre = it;
-        pre_sum += it.weight(false);
+        pre_sum += it.weight(kStartPrefix, p.wide);
         blocks += it.blocks();
         if (i < kSeen) seen[i] = it;
     }
@@ -502,7 +505,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
             if (u0 + x >= own.end) break;
             const Item it = own_item(p, u0 + x, length[x]);
             if (u0 + x == own.from) first_own = it;
-            if (it.rows) { own_sum += it.tiles() + kStartOwn; ++blocks; }
+            own_sum += it.weight(kStartOwn, p.wide);
+            blocks += it.blocks();
             if (prefixes + u0 + x < kSeen) seen[prefixes + u0 + x] = it;
         }
     }
@@ -526,8 +530,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     line.own = scalar(pre_all);
     if (p.items() <= 256 && 2 * room >= grid && total <= kMostFew * room) {          // few: the line again, in workgroups
         line.each = max(p.least_few, quotient(total - 1, room) + 1);     // no more than there is room for: starts are counted too
-        pre_sum = workgroups_of(first_pre, line.each);
-        own_sum = workgroups_of(first_own, line.each);
+        pre_sum = workgroups_of(first_pre, line.each, p.wide);
+        own_sum = workgroups_of(first_own, line.each, p.wide);
         pre_base = wave_scan(pre_sum);
         own_base = wave_scan(own_sum);
         if (lane == 63) sh.few[w] = make_int2(pre_base, own_base);
@@ -600,26 +604,25 @@ struct Walker {
             x.item = item;
             x.own = item >= p.prefixes();
             const int tiles = it.tiles(), n = it.blocks();
-            const int weight = each ? workgroups_of(it, each) : it.weight(x.own);
+            const int weight = each ? workgroups_of(it, each, p.wide) : it.weight(x.own ? kStartOwn : kStartPrefix, p.wide);
             if (pos - start >= weight) { start += weight; ++item; continue; }
             const int off = pos - start;
             if (each) {
-                const int full = n > 1 ? workgroups_of_full_block(it, each) : 0;
+                const int full = n > 1 ? workgroups_of_block(it, 2 + p.wide, each) : 0;
                 x.block = n > 1 ? min(off / full, n - 1) : 0;
-                const int k = off - x.block * full, of = workgroups_of_block(it, x.block, each), some = quotient(tiles, of), more = tiles - some * of;
+                const int k = off - x.block * full, of = workgroups_of_block(it, it.tile_log2(x.block, p.wide), each), some = quotient(tiles, of), more = tiles - some * of;
                 x.ta = k * some + min(k, more);
                 x.tb = x.ta + some + (k < more);
                 pos = hi;
                 return true;
             }
-            const int full = it.weight_of_full_block();
+            const int full = it.weight_of_full_block(p.wide);
             x.block = n > 1 ? min(off / full, n - 1) : 0;
-            const int f = it.factor(x.block), x0 = off - x.block * full;
-            const int block_start = start + x.block * full, x1 = min((x.block < n - 1 ? full : weight - x.block * full), hi - block_start);
+            const int block_start = start + x.block * full, x0 = off - x.block * full, x1 = min((x.block < n - 1 ? full : weight - x.block * full), hi - block_start);
             pos = block_start + x1;
-            const int shift = f == 4 ? 2 : f - 1;
-            x.ta = min((x0 + f - 1) >> shift, tiles);        // a tile is whose piece it begins in
-            x.tb = min((x1 + f - 1) >> shift, tiles);
+            const int shift = it.tile_log2(x.block, p.wide), last = (1 << shift) - 1;
+            x.ta = min((x0 + last) >> shift, tiles);         // a tile is whose piece it begins in
+            x.tb = min((x1 + last) >> shift, tiles);
             if (x.ta < x.tb) return true;                    // else: nothing but an item's start
         }
         return false;
@@ -725,10 +728,10 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
         k.first = x.it.begin();
         k.block = x.block;
         k.cols = min(kBlock, x.it.cols() - x.block * kBlock);
-        const int f = x.it.factor(x.block);
-        k.phases = kPartWaves / f;
+        const int waves = x.it.waves_log2(x.block);
+        k.phases = kPartWaves >> waves;
         k.phase = w & (k.phases - 1);
-        k.first_col = f == 1 ? 0 : f == 2 ? (w >> 1) * kCols : w * kCols;
+        k.first_col = (w >> (2 - waves)) * kCols;
         int2* const piece = out.pieces + (x.own ? piece_own(p, k.unit) : piece_prefix(p, group, k.first, x.block, k.g));
         if (tid == 0) {
             if (k.begins) piece->x = line.me;
@@ -792,7 +795,7 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
         }
     }
     if (own_len > 0) own = own_pieces;
-    pre.x = max(pre.x, 0), pre.y = min(pre.y, kPartGrid - 1), own.x = max(own.x, 0), own.y = min(own.y, kPartGrid * kPartWaves - 1);
+    pre.x = max(pre.x, 0), pre.y = min(pre.y, in.grid - 1), own.x = max(own.x, 0), own.y = min(own.y, in.grid * kPartWaves - 1);
     const int n_pre = max(0, pre.y - pre.x + 1), n = n_pre + max(0, own.y - own.x + 1);
     auto record = [&](int s) {
         const bool is_own = s >= n_pre;
@@ -848,11 +851,11 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
 }
 
 struct PagedLayout { size_t o, ml, pieces, total; int cols; };
-static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes) {
+static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes, int grid) {
     const int G = d.Hq / d.Hkv;
     PagedLayout l;
     l.cols = prefixes ? std::min(kBlock, (d.B * G + kCols - 1) / kCols * kCols) : kCols;     // that a workgroup may have
-    const size_t records = 2 * (size_t)d.B * d.Hq + 2 * (size_t)kPartGrid * (l.cols + kPartWaves * G);
+    const size_t records = 2 * (size_t)d.B * d.Hq + 2 * (size_t)grid * (l.cols + kPartWaves * G);
     l.o = 0;
     l.ml = l.o + records * d.d * sizeof(float);
     l.pieces = l.ml + records * 2 * sizeof(float);
@@ -861,19 +864,23 @@ static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes) {
     return l;
 }
 
-size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) { return paged_layout(d, prefix > 0).total; }
+static int grid_of(const zipvl_dims& d) {
+    if (d.dtype == ZIPVL_BF16) return d.d == 128 ? PartCfg<__bf16, 128>::GRID : PartCfg<__bf16, 64>::GRID;
+    return d.d == 128 ? PartCfg<float, 128>::GRID : PartCfg<float, 64>::GRID;
+}
+size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) { return paged_layout(d, prefix > 0, grid_of(d)).total; }
 
 template <typename T, int D, int OWN>
 static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, float scale, T* o, char* ws, hipStream_t st) {
     using C = PartCfg<T, D>;
-    const PagedLayout l = paged_layout(d, p.groups > 0);
-    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, p.G};
-    // no more workgroups than waves' tiles of all lengths at their greatest
-    const int64_t own = (int64_t)d.B * d.Hkv * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows + kStartOwn);
-    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kBlock + p.groups) * d.Hkv * (4 * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartPrefix) : 0;
+    const PagedLayout l = paged_layout(d, p.groups > 0, C::GRID);
+    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, p.G, C::GRID};
+    // what all lengths at their greatest would weigh, and more: no more workgroups than that
+    const int64_t own = (int64_t)d.B * d.Hkv * (2 * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartOwn);
+    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kBlock + p.groups) * d.Hkv * (8 * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartPrefix) : 0;
     if (own + pre >= (int64_t)1 << 31)
-        return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^36)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
-    const int wgs = (int)std::min<int64_t>(kPartGrid, own + pre);
+        return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^33)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
+    const int wgs = (int)std::min<int64_t>(C::GRID, own + pre);
     static std::atomic<uint64_t> lds_set{0};                 // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return set_error(ZIPVL_EHIP, "decode_attn_paged: no current device");
@@ -900,7 +907,7 @@ int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int3
 {
     const PagedRead p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len,
                          prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, d.Hq / d.Hkv,
-                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), inverse(d.Hq), d.dtype == ZIPVL_BF16 ? kLeastFew<__bf16> : kLeastFew<float>};
+                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), inverse(d.Hq), d.dtype == ZIPVL_BF16 ? kLeastFew<__bf16> : kLeastFew<float>, d.dtype == ZIPVL_BF16 ? 0 : 1};
 #define ZIPVL_PAGED(T, D)                                                                              \
     return p.G <= 16 ? launch_paged_t<T, D, 16>((const T*)q, p, d, scale, (T*)o, (char*)ws, st)       \
                      : launch_paged_t<T, D, 32>((const T*)q, p, d, scale, (T*)o, (char*)ws, st)
