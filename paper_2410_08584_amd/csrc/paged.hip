@@ -20,14 +20,13 @@
 namespace zipvl {
 
 constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4, kBlock = kCols * kPartWaves;
-constexpr int kStartPrefix = 8, kStartOwn = 3;       // what starting an item weighs: its queries, its first rows, its part
+constexpr int kStartPrefix = 12, kStartOwn = 3;       // what starting an item weighs: its queries, its first rows, its part
 constexpr int kLeast = 8;            // weight below which a workgroup is not worth its part
 // The same where every item has workgroups of its own.  A tile of fp32 rows is 2 us of a wave and more, and one for each is enough; of bf16 rows it
 // is 0.6, and half as many parts are worth it.  Two questions about an image of 576 rows, fp32: 14.1 us with 4, 17.3 with 8; eight about a video of 7200
 // rows, bf16: 22.6 and 19.3 (12: 19.7).
 template <typename T> constexpr int kLeastFew = sizeof(T) == 2 ? 8 : 4;
-constexpr int kCus = 256, kEarly = 17, kLate = 15;
-constexpr int kMostFew = 24;
+constexpr int kCus = 256;
 constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
 
 // a wave-uniform number in scalar registers
@@ -438,7 +437,7 @@ struct WavePart {
     }
 };
 
-// a / b for 0 <= a < 2^22, b > 0 (512 * 512 and eight times the tiles of an item are less; kMostFew * 512 too): the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
+// a / b for 0 <= a < 2^22, b > 0 (512 * 512 and eight times the tiles of an item are less): the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
 __device__ __forceinline__ int quotient(int a, int b) {
     const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), left = a - q * b;
     return q + (left >= b) - (left < 0);
@@ -528,8 +527,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     line.each = 0;
     line.me = blockIdx.x;
     line.own = scalar(pre_all);
-    if (p.items() <= 256 && 2 * room >= grid && total <= kMostFew * room) {          // few: the line again, in workgroups
-        line.each = max(p.least_few, quotient(total - 1, room) + 1);     // no more than there is room for: starts are counted too
+    if (p.items() <= 256 && 2 * room >= grid) {          // few: the line again, in workgroups
+        line.each = max(p.least_few, (total - 1) / room + 1);    // no more than there is room for: starts are counted too
         pre_sum = workgroups_of(first_pre, line.each, p.wide);
         own_sum = workgroups_of(first_own, line.each, p.wide);
         pre_base = wave_scan(pre_sum);
@@ -553,13 +552,10 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     } else {
         const int wgs = max(1, min(grid, total / kLeast));   // a piece is longer than a tile of any item: none is without a tile
         if (line.me >= wgs) return false;
-        const bool first = line.me < kCus || wgs <= kCus;
-        const int early = wgs <= kCus ? total : scalar((int)((int64_t)total * (kEarly * kCus) / (kEarly * kCus + kLate * (wgs - kCus))));
-        const int n = first ? min(wgs, kCus) : wgs - kCus, me = first ? line.me : line.me - kCus, from = first ? 0 : early, share = first ? early : total - early;
-        const int each = scalar(share / n), more = share - each * n;
+        const int each = scalar(total / wgs), more = total - each * wgs;
         own_base += line.own;
-        line.lo = from + me * each + quotient(me * more, n);
-        line.hi = from + (me + 1) * each + quotient((me + 1) * more, n);
+        line.lo = line.me * each + quotient(line.me * more, wgs);
+        line.hi = (line.me + 1) * each + quotient((line.me + 1) * more, wgs);
     }
     line.lo = scalar(line.lo);
     line.hi = scalar(line.hi);
