@@ -416,6 +416,36 @@ def test_decode_attn_paged_long(dtype, d, groups):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", [  # B, Hq, Hkv, d, dtype, page, lens, groups, prefix: more items than workgroups of their own
+    (40, 16, 8, 64, "bf16", 16, [5, 40, 0, 33, 700, 64, 1], (17, 3, 20), [600, 0, 333, 1200]),
+    (33, 24, 8, 128, "bf16", 64, [90, 3, 0, 1500], (33,), [2000, 100]),
+    (80, 8, 4, 128, "f32", 32, [10, 0, 200, 31], (75, 5), [900, 33, 500]),
+    (130, 4, 2, 64, "f32", 16, [64, 7], (), []),
+    (45, 128, 8, 64, "bf16", 16, [20, 100], (30, 15), [300, 17]),
+    (35, 160, 8, 128, "bf16", 128, [33, 0, 260], (35,), [700]),
+    (200, 2, 2, 64, "bf16", 16, [3], tuple([1] * 150), [40, 16, 0]),
+], ids=lambda c: f"B{c[0]}Hq{c[1]}Hkv{c[2]}d{c[3]}{c[4]}P{len(c[7])}")
+def test_decode_attn_paged_of_many_items(case):
+    say(f"decode_attn_paged many {case[:6]}")
+    batch = Batch(*case, seed=28)
+    o = batch.run()
+    batch.check(o, which=list(range(0, batch.B, 3)) + [batch.B - 1])
+    assert torch.equal(o, batch.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[1, 0, 16, 17], [0], [0, 0, 0, 0, 0, 0, 5]])
+def test_decode_attn_paged_of_thousands_of_units(lens):
+    """More units than are looked at in LDS, most of them short or empty, one long."""
+    say(f"decode_attn_paged thousands {lens}")
+    B, Hq, Hkv = 700, 8, 8
+    lens = (lens * (B * Hkv))[:B * Hkv]
+    lens[3333] = 900
+    batch = Batch(B, Hq, Hkv, 64, "bf16", 16, lens, (300, 0, 400), [33], seed=29)
+    batch.check(batch.run(), which=[0, 1, 2, 150, 299, 300, 301, 416, 417, 500, 698, 699])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("gain,spike", [(20.0, 0.0), (1.0, 40.0), (1e-3, 0.0)])
 def test_decode_attn_paged_where_one_row_has_all_the_weight(dtype, d, gain, spike):
@@ -592,6 +622,79 @@ def test_decode_steps_as_a_graph_and_on_another_stream():
     for s in (captured, other):
         assert torch.equal(s["o"], eager["o"])
         assert s["cache"].K.view(torch.int16).equal(eager["cache"].K.view(torch.int16)) and s["cache"].V.view(torch.int16).equal(eager["cache"].V.view(torch.int16))
+
+
+@pytest.mark.gpu
+def test_calls_of_the_extension_module_are_the_general_ones(monkeypatch):
+    """Positions and pages through _pycall and through ctypes: the same bits; and tensors that it does not take are refused all the same."""
+    from paper_2410_08584_amd import binding
+    B, Hq, Hkv, n, d, page = 3, 8, 4, 20, 64, 16
+    rope = z.Rope.of_sections((8, 12, 12))
+    Q, K, V = layer(B, Hq, Hkv, n, d, "bf16", "token", 61)
+    pos = positions(3, B, n, 62)
+    batch = Batch(B, Hq, Hkv, d, "bf16", page, [3, 50, 16], (2, 1), [40, 77], seed=63)
+    taken = []
+
+    class Watched:
+        def __init__(self, inner):
+            self.inner = inner
+
+        def __getattr__(self, name):
+            def call(*args):
+                rc = getattr(self.inner, name)(*args)
+                taken.append((name, rc))
+                return rc
+            return call
+
+    def everything():
+        Qo, Ko = torch.zeros((B, Hq, n, d), dtype=Q.dtype, device=DEV), torch.zeros((B, Hkv, n, d), dtype=Q.dtype, device=DEV)
+        z.zipvl_rotate(Q, K, pos, rope, z.ROTATE_INVERSE, Qo=Qo, Ko=Ko)
+        cache = pools(60, page, d, "bf16", 64)
+        table = random_table(B * Hkv, 4, 60, 65)
+        start = torch.arange(B * Hkv, dtype=torch.int32, device=DEV)
+        k = torch.tensor([20, 3, 0], dtype=torch.int32, device=DEV)
+        Qa = torch.zeros((B, Hq, n, d), dtype=Q.dtype, device=DEV)
+        z.zipvl_paged_append(K, V, cache, table, start, k=k, pos=pos, rope=rope, Q=Q, Qo=Qa, flags=z.T_PER_BATCH)
+        o = torch.zeros((B * Hq, d), dtype=Q.dtype, device=DEV)
+        batch.run(o=o, ws=z.decode_paged_workspace(batch.cache, batch.table, batch.prefix_table, B=B, Hq=Hq, Hkv=Hkv))
+        return Qo, Ko, cache.K, cache.V, start, Qa, o
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_native", Watched(binding._native))
+        fast = everything()
+        assert [rc for name, rc in taken if name in ("rotate", "paged_append", "decode_attn_paged")] == [0, 0, 0]
+        with pytest.raises(z.ZipvlError, match="one GPU"):
+            z.zipvl_rotate(Q, K, pos.cpu(), rope, Qo=torch.empty_like(Q), Ko=torch.empty_like(K))
+        with pytest.raises(z.ZipvlError, match="pos has"):
+            z.zipvl_rotate(Q, K, pos[:2], rope, Qo=torch.empty_like(Q), Ko=torch.empty_like(K))
+        with pytest.raises(z.ZipvlError, match="contiguous"):
+            z.zipvl_rotate(Q, K, pos.transpose(1, 2).contiguous().transpose(1, 2), rope, Qo=torch.empty_like(Q), Ko=torch.empty_like(K))
+        assert [rc for name, rc in taken[-3:]] == [None] * 3
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_native", binding._NoExtension())
+        general = everything()
+    assert all(torch.equal(a, b) for a, b in zip(fast, general))
+
+
+@pytest.mark.gpu
+def test_rows_of_expanded_and_single_axes():
+    """Inputs whose axes have stride 0, or one element and torch's own idea of its stride, are taken as they are."""
+    d, page = 64, 16
+    rope = z.Rope(frequencies(32))
+    one = torch.randn((1, 1, 6, d), generator=torch.Generator().manual_seed(71)).to(DEV)
+    wide = one.expand(3, 4, 6, d)
+    pos = positions(1, 3, 6, 72)
+    Qo, _ = z.zipvl_rotate(wide, None, pos, rope)
+    assert torch.equal(Qo, z.zipvl_rotate(wide.contiguous(), None, pos, rope)[0])
+    with pytest.raises(z.ZipvlError, match="overlap"):
+        z.zipvl_rotate(wide, None, pos, rope, Qo=wide)
+    odd = torch.randn((2, 7, d), generator=torch.Generator().manual_seed(73)).to(DEV)[:, 3:4].unsqueeze(1)       # [2,1,1,d]
+    odd = odd.as_strided(odd.shape, (odd.stride(0), 5, 3, 1), odd.storage_offset())
+    pos = positions(1, 2, 1, 74)
+    assert torch.equal(z.zipvl_rotate(odd, None, pos, rope)[0], z.zipvl_rotate(odd.contiguous(), None, pos, rope)[0])
+    cache, table = pools(4, page, d, "f32", 75), torch.arange(2, dtype=torch.int32, device=DEV).view(2, 1)
+    length, _ = z.zipvl_paged_append(odd, odd, cache, table, torch.zeros((2,), dtype=torch.int32, device=DEV))
+    assert length.tolist() == [1, 1] and torch.equal(cache.V[:2, 0], odd[:, 0, 0])
 
 
 # ---------------------------------------------------------------- refusals, without a GPU
