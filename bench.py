@@ -25,6 +25,7 @@ if ROOT not in sys.path:
 MFMA_BF16_PEAK_TFLOPS = 2500.0      # MI355X dense bf16 matrix peak
 MFMA_FP32_PEAK_TFLOPS = 157.3
 HBM_PEAK_GBS = 8000.0
+PAGE = 64                # rows of a page of the paged caches (--paged)
 PREFILL_KERNELS = ("score_rowstats", "score_colsum", "select", "compact_kv", "pack_kv", "flash_kept")
 
 
@@ -164,7 +165,7 @@ def run_stack(args):
     lt = torch.empty((units,), dtype=torch.int32, device=dev)
     Kt4, Vt4 = Kt.view(B, H, n, d), Vt.view(B, H, n, d)
     ws_s = ws_p = None
-    caches, fulls, quants, kept, layer_ms, samples = [], [], [], [], [], []
+    caches, fulls, quants, paged, kept, layer_ms, samples = [], [], [], [], [], [], []
     kern_us = {}
     sample_layers = {0, (L - 1) // 2, L - 1}
     ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -216,6 +217,15 @@ def run_stack(args):
             quants.append((qc, torch.empty((units, cap_t, d), dtype=torch.bfloat16, device=dev),
                            torch.empty((units, cap_t, d), dtype=torch.bfloat16, device=dev),
                            torch.zeros((units,), dtype=torch.int32, device=dev)))
+        if args.paged:
+            # the same rows as a prefix in pages, and pages for what args.paged conversations about each prompt will say
+            own_pages = units * args.paged * (-(-(steps_dec + 8) // PAGE))
+            width = -(-int(k_h.max()) // PAGE)
+            cache = z.PagedCache.empty(units * width + own_pages, PAGE, d, torch.bfloat16, dev)
+            order = torch.randperm(cache.num_pages, device=dev, dtype=torch.int64).to(torch.int32)
+            ptable, otable = order[:units * width].view(units, width), order[units * width:].view(units * args.paged, -1)
+            plen, _ = z.zipvl_paged_append(K, V, cache, ptable, torch.zeros_like(k), idx=idx, k=k, length=torch.empty_like(k))
+            paged.append((cache, ptable, plen, otable, torch.zeros((units * args.paged,), dtype=torch.int32, device=dev)))
         del Q, K, V
     kept = np.stack(kept)
     gen = torch.Generator(device=dev); gen.manual_seed(12345)
@@ -314,6 +324,29 @@ def run_stack(args):
         res["quantised_4_2bit"] = entry(bytes_step, eager, graph,
                                         bits_per_element_incl_params=8.0 * (rows_hi * (d // 2 + 4) + rows_lo * (d // 4 + 4)) / ((rows_hi + rows_lo) * d),
                                         note="all prefill tokens stay in the cache (important ones 4 bit, the others 2 bit), appended rows bf16")
+    if args.paged:
+        # a decode step of B * args.paged conversations: query, key rotated, key and value into pages, attention over the prompt's prefix and their own
+        Bp = B * args.paged
+        rope = z.Rope.of_sections((d // 2 - 2 * (3 * d // 16), 3 * d // 16, 3 * d // 16))
+        begin = torch.arange(0, Bp + 1, args.paged, dtype=torch.int32, device=dev)
+        qp, kp, vp = (torch.randn((Bp, H, 1, d), generator=gen, device=dev).to(torch.bfloat16) for _ in range(3))
+        pos = torch.full((3, Bp, 1), n, dtype=torch.int32, device=dev)
+        qr = torch.empty_like(qp)
+        op = torch.empty((Bp * H, d), dtype=torch.bfloat16, device=dev)
+        o = op                                               # what the replay is compared by
+        ws_g = z.decode_paged_workspace(paged[0][0], paged[0][3], paged[0][1], B=Bp, Hq=H, Hkv=H)
+
+        def decode_paged(nsteps):
+            for _ in range(nsteps):
+                for (cache, ptable, plen, otable, olen) in paged:
+                    z.zipvl_paged_append(kp, vp, cache, otable, olen, pos=pos, rope=rope, Q=qp, Qo=qr)
+                    z.zipvl_decode_attn_paged(qr, cache, otable, olen, 1.0 / float(np.sqrt(d)), B=Bp, Hq=H, Hkv=H, prefix_table=ptable,
+                                              prefix_len=plen, group_begin=begin, o=op, ws=ws_g)
+                pos.add_(1)
+        eager, graph = timed_decode(decode_paged, [pp[4] for pp in paged] + [pos])
+        rows = sum(int(pp[2].sum().item()) for pp in paged) + L * H * Bp * (2 + (steps_dec - 2 + 1) / 2.0)
+        res["paged_shared_prefix"] = entry(2.0 * rows * d * e, eager, graph, conversations=Bp, page=PAGE,
+                                           note=f"{args.paged} conversations about each of the {B} prompts share its evicted cache, which is read once for all of them")
     ms_layer = float(np.mean(layer_ms))
     dense_flops = 2.0 * B * H * d * n * (n + 1)
     out = {
@@ -372,6 +405,8 @@ def main():
                          "selected from the head-averaged scores")
     ap.add_argument("--quantized", action="store_true",
                     help="shape 5: also decode against the mixed-precision cache (important tokens 4 bit, the others 2 bit)")
+    ap.add_argument("--paged", type=int, default=0, metavar="CONVERSATIONS",
+                    help="shape 5: also decode steps of that many conversations about each prompt, over paged caches that share the evicted prefix")
     ap.add_argument("--no-peaks", action="store_true", help="skip the two probe kernels (sustained bf16 MFMA rate, sustained read bandwidth)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-dense", action="store_true")
