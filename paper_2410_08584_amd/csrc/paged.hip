@@ -20,7 +20,8 @@
 namespace zipvl {
 
 constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4, kBlock = kCols * kPartWaves;
-constexpr int kStartPrefix = 12, kStartOwn = 3;       // what starting an item weighs: its queries, its first rows, its part
+constexpr int kStartPrefix = 12, kStartWave = 3;      // what starting an item weighs: its queries, its first rows, its part
+constexpr int kLight = 16;           // queries up to which waves cut a prefix
 constexpr int kLeast = 8;            // weight below which a workgroup is not worth its part
 // The same where every item has workgroups of its own.  A tile of fp32 rows is 2 us of a wave and more, and one for each is enough; of bf16 rows it
 // is 0.6, and half as many parts are worth it.  Two questions about an image of 576 rows, fp32: 14.1 us with 4, 17.3 with 8; eight about a video of 7200
@@ -47,15 +48,16 @@ struct PagedRead {
 
 // Parts: a record is D floats and (max, sum).  Records 2 (b Hq + h) + {0: prefix, 1: own} are those of items that were not cut.  Behind them are those
 // of pieces: for every workgroup `cols` of a prefix that began before it and as many of one that goes on after it, then for every
-// wave G and G of own items in the same way.  `pieces` says of every own item and every block of a prefix from which to which
+// wave `wave_cols` and as many in the same way.  `pieces` says of every own item and every block of a prefix from which to which
 // workgroup, or wave, its pieces are.
 struct Parts {
-    float* o; float* ml; int2* pieces; int rows, cols, G, grid;      // rows = B Hq
+    float* o; float* ml; int2* pieces; int rows, cols, wave_cols, grid;      // rows = B Hq
     __device__ __forceinline__ int whole(int row, int own) const { return 2 * row + own; }
-    __device__ __forceinline__ int piece(int own, int who, int begins, int col) const {      // below 2^20
-        return 2 * rows + (own ? 2 * grid * cols + (who * 2 + begins) * G : (who * 2 + begins) * cols) + col;
+    __device__ __forceinline__ int piece(int by_wave, int who, int begins, int col) const {  // below 2^20
+        return 2 * rows + (by_wave ? 2 * grid * cols + (who * 2 + begins) * wave_cols : (who * 2 + begins) * cols) + col;
     }
 };
+constexpr int kByWave = 1 << 30;     // on the numbers of a prefix's pieces, where waves had them
 // Blocks of a prefix are counted from begin G / kBlock + p: no two groups meet, and B G / kBlock + groups + 1 are enough.
 __device__ __forceinline__ int piece_own(const PagedRead& p, int u) { return u; }
 __device__ __forceinline__ int piece_prefix(const PagedRead& p, int group, int begin, int block, int g) {
@@ -88,9 +90,12 @@ struct Item {
         return waves_log2(block) + (cols() - block * kBlock > 16 ? wide : 0);
     }
     __device__ __forceinline__ int weight_of_full_block(int wide) const { return (tiles() << (2 + wide)) + kStartPrefix; }
-    __device__ __forceinline__ int weight(int start, int wide) const {
+    // Items of few queries are cut by waves (find_piece); the others' blocks by workgroups.
+    __device__ __forceinline__ bool light() const { return cols() <= kLight; }
+    __device__ __forceinline__ int weight(bool by_wave, int wide) const {
         const int n = blocks();
-        return n ? (n - 1) * weight_of_full_block(wide) + (tiles() << tile_log2(n - 1, wide)) + start : 0;
+        if (by_wave) return n ? (tiles() << (cols() > 16 ? wide : 0)) + kStartWave : 0;
+        return n ? (n - 1) * weight_of_full_block(wide) + (tiles() << tile_log2(n - 1, wide)) + kStartPrefix : 0;
     }
 };
 __device__ __forceinline__ Item own_item(const PagedRead& p, int u, int length) {
@@ -453,13 +458,13 @@ struct Line {
     int item;                                                // of the workgroup's first position
     int start;                                               // of that item on the line, which is shorter than 2^31
     int lo, hi;                                              // the workgroup's piece
-    int own;                                                 // where own items begin
+    int waves;                                               // where the items begin that waves cut
     int each;                                                // few items: weight for which an item has a workgroup; 0: many
     int me;                                                  // the workgroup's number on the line
 };
 
 struct LineShared {
-    int4 sums[kPartWaves];                                   // of prefixes, of own items; blocks
+    int4 sums[kPartWaves];                                   // of prefixes that workgroups cut, that waves cut, of own items; blocks
     int2 few[kPartWaves];
     int item, base;
 };
@@ -482,7 +487,7 @@ __device__ __forceinline__ Share share_of(int n) {
 __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, Item* seen, Line& line) {
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, prefixes = p.prefixes();
     const Share pre = share_of(prefixes), own = share_of(p.B * p.Hkv);
-    int pre_sum = 0, own_sum = 0, blocks = 0;
+    int pre_sum = 0, light_sum = 0, own_sum = 0, blocks = 0;
     Item first_pre = {0, 0}, first_own = {0, 0};
     int length[4];                                           // four are asked for at once, and the first four before those of prefixes are there
     auto ask = [&](int u0) {
@@ -493,7 +498,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     for (int i = pre.from; i < pre.end; ++i) {
         const Item it = item_of(p, i);
         if (i == pre.from) first_pre = it;
-        pre_sum += it.weight(kStartPrefix, p.wide);
+        if (it.light()) light_sum += it.weight(true, p.wide);
+        else pre_sum += it.weight(false, p.wide);
         blocks += it.blocks();
         if (i < kSeen) seen[i] = it;
     }
@@ -504,31 +510,33 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
             if (u0 + x >= own.end) break;
             const Item it = own_item(p, u0 + x, length[x]);
             if (u0 + x == own.from) first_own = it;
-            own_sum += it.weight(kStartOwn, p.wide);
+            own_sum += it.weight(true, p.wide);
             blocks += it.blocks();
             if (prefixes + u0 + x < kSeen) seen[prefixes + u0 + x] = it;
         }
     }
-    const int pre_upto = wave_scan(pre_sum), own_upto = wave_scan(own_sum), wave_blocks = wave_sum(blocks);
-    if (lane == 63) sh.sums[w] = make_int4(pre_upto, own_upto, wave_blocks, 0);
+    const int pre_upto = wave_scan(pre_sum), light_upto = wave_scan(light_sum), own_upto = wave_scan(own_sum), wave_blocks = wave_sum(blocks);
+    if (lane == 63) sh.sums[w] = make_int4(pre_upto, light_upto, own_upto, wave_blocks);
     if (tid == 0) sh.item = p.items();
     __syncthreads();
-    int pre_base = pre_upto - pre_sum, own_base = own_upto - own_sum, pre_all = 0, own_all = 0, all_blocks = 0;
+    int pre_base = pre_upto - pre_sum, light_base = light_upto - light_sum, own_base = own_upto - own_sum, pre_all = 0, light_all = 0, own_all = 0, all_blocks = 0;
 #pragma unroll
     for (int x = 0; x < kPartWaves; ++x) {
         const int4 v = sh.sums[x];
-        if (x < w) { pre_base += v.x; own_base += v.y; }
+        if (x < w) { pre_base += v.x; light_base += v.y; own_base += v.z; }
         pre_all += v.x;
-        own_all += v.y;
-        all_blocks += v.z;
+        light_all += v.y;
+        own_all += v.z;
+        all_blocks += v.w;
     }
-    const int total = scalar(pre_all + own_all), grid = gridDim.x, room = grid - scalar(all_blocks);
+    const int total = scalar(pre_all + light_all + own_all), grid = gridDim.x, room = grid - scalar(all_blocks);
     if (total == 0) return false;
     line.each = 0;
     line.me = blockIdx.x;
-    line.own = scalar(pre_all);
+    line.waves = scalar(pre_all);
     if (p.items() <= 256 && 2 * room >= grid) {          // few: the line again, in workgroups
         line.each = max(p.least_few, (total - 1) / room + 1);    // no more than there is room for: starts are counted too
+        light_sum = 0;
         pre_sum = workgroups_of(first_pre, line.each, p.wide);
         own_sum = workgroups_of(first_own, line.each, p.wide);
         pre_base = wave_scan(pre_sum);
@@ -553,7 +561,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
         const int wgs = max(1, min(grid, total / kLeast));   // a piece is longer than a tile of any item: none is without a tile
         if (line.me >= wgs) return false;
         const int each = scalar(total / wgs), more = total - each * wgs;
-        own_base += line.own;
+        light_base += pre_all;
+        own_base += pre_all + light_all;
         line.lo = line.me * each + quotient(line.me * more, wgs);
         line.hi = (line.me + 1) * each + quotient((line.me + 1) * more, wgs);
     }
@@ -562,6 +571,10 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     if (pre_base <= line.lo && line.lo < pre_base + pre_sum) {
         sh.item = pre.from;
         sh.base = pre_base;
+    }
+    if (light_base <= line.lo && line.lo < light_base + light_sum) {
+        sh.item = pre.from;
+        sh.base = light_base;
     }
     if (own_base <= line.lo && line.lo < own_base + own_sum) {
         sh.item = prefixes + own.from;
@@ -582,6 +595,7 @@ struct Walker {
     const Item* in_lds;                                      // NULL: no longer
     int item, window;
     int start, pos, hi;                                      // below 2^31
+    bool by_wave;                                            // among the items that waves cut; the others have no weight there
     Item seen;                                               // 64 items from `window`, one a lane
     __device__ __forceinline__ void look() {
         const int i = window + (int)(threadIdx.x & 63);
@@ -600,7 +614,7 @@ struct Walker {
             x.item = item;
             x.own = item >= p.prefixes();
             const int tiles = it.tiles(), n = it.blocks();
-            const int weight = each ? workgroups_of(it, each, p.wide) : it.weight(x.own ? kStartOwn : kStartPrefix, p.wide);
+            const int weight = each ? workgroups_of(it, each, p.wide) : (x.own || it.light()) == by_wave ? it.weight(by_wave, p.wide) : 0;
             if (pos - start >= weight) { start += weight; ++item; continue; }
             const int off = pos - start;
             if (each) {
@@ -705,7 +719,7 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
     Line line;
     static_assert(kSeen * sizeof(Item) <= C::LDS, "the items' sizes stand where tiles come later");
     if (!find_piece(p, sh, reinterpret_cast<Item*>(smem), line)) return;
-    Walker walk = {p, reinterpret_cast<const Item*>(smem), line.item, line.item, line.start, line.lo, line.each ? line.hi : min(line.hi, max(line.lo, line.own)), {0, 0}};
+    Walker walk = {p, reinterpret_cast<const Item*>(smem), line.item, line.item, line.start, line.lo, line.each ? line.hi : min(line.hi, max(line.lo, line.waves)), line.lo >= line.waves, {0, 0}};
     walk.look();
     walk.in_lds = nullptr;
     __syncthreads();                                         // tiles may come
@@ -736,27 +750,36 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
         if (OWN == 16 && k.cols <= 16) shared_piece<T, D, 16>(q, p, c, out, x, k, line.me, smem, ml);
         else shared_piece<T, D, 32>(q, p, c, out, x, k, line.me, smem, ml);
     }
-    if (line.each || line.hi <= line.own) return;
+    if (line.each || line.hi <= line.waves) return;
 
-    // Own items of a line of many.  Where fewer than kLeast are left to the workgroup (the first with own items) its last wave has them: the pieces of
+    // Items that waves cut.  Where fewer than kLeast are left to the workgroup (the first with such items) its last wave has them: the pieces of
     // an item are those of waves that follow each other.
-    const int from = max(line.lo, line.own), all = line.hi - from, quarter = all / kPartWaves, rest = all % kPartWaves;
+    const int from = max(line.lo, line.waves), all = line.hi - from, quarter = all / kPartWaves, rest = all % kPartWaves;
     walk.pos = all < kLeast ? from : from + w * quarter + min(w, rest);
     walk.hi = all < kLeast ? (w == kPartWaves - 1 ? line.hi : from) : walk.pos + quarter + (w < rest);
+    if (!walk.by_wave) {                                     // it stands behind the items that workgroups cut: back to the first item
+        walk.by_wave = true;
+        walk.item = walk.window = 0;
+        walk.start = line.waves;
+        walk.look();
+    }
     const int who = line.me * kPartWaves + w, i = tid & (OWN - 1), lane = tid & 63;
     while (walk.next(x, 0)) {
         const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
-        const int unit = x.item - prefixes, row = x.it.begin() * p.Hq + (unit - x.it.begin() * p.Hkv) * p.G + min(i, p.G - 1);
+        const int unit = x.own ? x.item - prefixes : x.item, group = x.own ? 0 : divided(unit, p.Hkv, p.inv_Hkv);
+        const int g = x.own ? unit - x.it.begin() * p.Hkv : unit - group * p.Hkv, cols = x.it.cols();
+        const int r = min(i, cols - 1), s = divided(r, p.G, p.inv_G), row = (x.it.begin() + s) * p.Hq + g * p.G + r - s * p.G;
         if (lane == 0) {
-            if (begins) out.pieces[piece_own(p, unit)].x = who;
-            if (ends) out.pieces[piece_own(p, unit)].y = who;
+            int2* const piece = out.pieces + (x.own ? piece_own(p, unit) : piece_prefix(p, group, x.it.begin(), 0, g));
+            if (begins) piece->x = x.own ? who : who | kByWave;
+            if (ends) piece->y = x.own ? who : who | kByWave;
         }
         WavePart<T, D, OWN> part;
         part.reset();
-        part.load_queries(q + (int64_t)row * D, i < p.G);
-        part.run(p, p.table + (int64_t)unit * p.width, x.it.rows, x.ta, 1, x.tb, c, smem + w * C::WAVE);
-        if (i < p.G) {
-            const int64_t rec = whole ? out.whole(row, 1) : out.piece(1, who, begins, i);
+        part.load_queries(q + (int64_t)row * D, i < cols);
+        part.run(p, x.own ? p.table + (int64_t)unit * p.width : p.prefix_table + (int64_t)unit * p.prefix_width, x.it.rows, x.ta, 1, x.tb, c, smem + w * C::WAVE);
+        if (i < cols) {
+            const int64_t rec = whole ? out.whole(row, x.own) : out.piece(1, who, begins, i);
             part.store(out.o + rec * D);
             if (lane < OWN) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(part.m, part.l);
         }
@@ -791,13 +814,15 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
         }
     }
     if (own_len > 0) own = own_pieces;
-    pre.x = max(pre.x, 0), pre.y = min(pre.y, in.grid - 1), own.x = max(own.x, 0), own.y = min(own.y, in.grid * kPartWaves - 1);
+    const bool waves_cut = pre.x & kByWave;                  // the prefix
+    pre.x &= ~kByWave, pre.y = pre.y < 0 ? -1 : pre.y & ~kByWave;
+    pre.x = max(pre.x, 0), pre.y = min(pre.y, in.grid * (waves_cut ? kPartWaves : 1) - 1), own.x = max(own.x, 0), own.y = min(own.y, in.grid * kPartWaves - 1);
     const int n_pre = max(0, pre.y - pre.x + 1), n = n_pre + max(0, own.y - own.x + 1);
     auto record = [&](int s) {
         const bool is_own = s >= n_pre;
         const int2 x = is_own ? own : pre;
         const int who = x.x + (is_own ? s - n_pre : s);
-        return x.x == x.y ? in.whole(row, is_own) : in.piece(is_own, who, who == x.x, is_own ? head - g * p.G : col);
+        return x.x == x.y ? in.whole(row, is_own) : in.piece(is_own || waves_cut, who, who == x.x, is_own ? head - g * p.G : col);
     };
     float M = -INFINITY, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -846,12 +871,13 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
     }
 }
 
-struct PagedLayout { size_t o, ml, pieces, total; int cols; };
+struct PagedLayout { size_t o, ml, pieces, total; int cols, wave_cols; };
 static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes, int grid) {
     const int G = d.Hq / d.Hkv;
     PagedLayout l;
     l.cols = prefixes ? std::min(kBlock, (d.B * G + kCols - 1) / kCols * kCols) : kCols;     // that a workgroup may have
-    const size_t records = 2 * (size_t)d.B * d.Hq + 2 * (size_t)grid * (l.cols + kPartWaves * G);
+    l.wave_cols = prefixes ? std::max(G, kLight) : G;
+    const size_t records = 2 * (size_t)d.B * d.Hq + 2 * (size_t)grid * (l.cols + kPartWaves * l.wave_cols);
     l.o = 0;
     l.ml = l.o + records * d.d * sizeof(float);
     l.pieces = l.ml + records * 2 * sizeof(float);
@@ -870,9 +896,9 @@ template <typename T, int D, int OWN>
 static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, float scale, T* o, char* ws, hipStream_t st) {
     using C = PartCfg<T, D>;
     const PagedLayout l = paged_layout(d, p.groups > 0, C::GRID);
-    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, p.G, C::GRID};
+    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, l.wave_cols, C::GRID};
     // what all lengths at their greatest would weigh, and more: no more workgroups than that
-    const int64_t own = (int64_t)d.B * d.Hkv * (2 * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartOwn);
+    const int64_t own = (int64_t)d.B * d.Hkv * (2 * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartWave);
     const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kBlock + p.groups) * d.Hkv * (8 * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartPrefix) : 0;
     if (own + pre >= (int64_t)1 << 31)
         return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^33)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
