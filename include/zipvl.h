@@ -367,10 +367,14 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
  * with Ko, Vo the first len[u] rows of the unit u = b*Hkv + g by table [B*Hkv, table_pages], and Kp, Vp the first prefix_len[p*Hkv + g] rows
  * by prefix_table [groups*Hkv, prefix_pages] of the group p that b is in.  Group p is the batch elements group_begin[p] .. group_begin[p+1] - 1
  * (group_begin [device] int32 [groups + 1], ascending within [0, B]); elements in no group have no prefix.  The rows of a prefix are
- * read once for all queries of a group (once for every 64 of them, where there are more).
+ * read once for all queries of a group (once for every 128 of them, where there are more).
  * groups = 0: nothing is shared (prefix_table, prefix_len, group_begin are not looked at).  groups <= B.
  * Lengths are clamped to [0, pages of the table * page]; a head without any row gets zeros.  Nothing behind a length is read.
  * q, o [device] [B*Hq, d] contiguous; G = Hq/Hkv <= 32.  Rows that are attended to must be finite.
+ * Tables are refused (ZIPVL_ESHAPE) that hold more than 2^24 rows a unit, or in all some 2^35 rows (those of prefixes counted four times for every 128
+ * queries begun).
+ * Numerics: scores, statistics and sums in fp32; bf16 weights enter the product with V with 16 bits, in two parts; one rounding at the end.  The order of
+ * all sums follows from the lengths: the same call gives the same bits.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_DECODE_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that
  * overlap on one workspace race).
  */

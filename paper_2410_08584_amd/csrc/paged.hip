@@ -2,14 +2,19 @@
 //
 // Memory-bound for as long as few queries meet a row.  An item is a unit (batch element, KV head) with its own rows and the G queries of its
 // group of heads, or a (prefix, KV head) with the G queries of every batch element that shares it, in blocks of 128: a row of a prefix comes from
-// memory once for 128 queries instead of once for every batch element.  Both are the same work: columns of 32 queries (those that an item
-// lacks are zero) against tiles of 32 rows, S^T = K Q^T and O^T += V^T P^T on 32x32 matrix tiles, so that a lane has one query and the
-// softmax statistics are scalars of a lane.  A wave has 32 columns and tiles of its own in LDS: four waves take four tiles in turn (up to 32
-// queries), two and two the same two (up to 64), or all the same one, which comes from L2 for all but the first.
+// memory once for 128 queries instead of once for every batch element.  Both are the same work: columns of queries (those that an item
+// lacks are zero) against tiles of 32 rows, S^T = K Q^T and O^T += V^T P^T on matrix tiles, so that a lane has one query and the
+// softmax statistics are scalars of a lane.  A wave has 32 columns, or 16, and tiles of its own in LDS.  Items of up to 16 queries are cut by waves; of the others
+// a workgroup has a block: its four waves take four tiles in turn (up to 32 queries), two and two the same two (up to 64), or all the same one, which
+// comes from L2 for all but the first.
 //
 // How the work is cut up is decided on the device, where the lengths are (Line).  Nothing is read back and no launch is spent on it: every
 // workgroup goes over the B Hkv + groups Hkv lengths by itself, a microsecond.
 // Parts (max, sum, weighted sum of rows) of an item that was cut are joined by a second launch.
+//
+// Measured, bf16, d = 128 (a call, both launches): 64 questions about two videos of 18432 tokens, 437 MB, 103 us = 4.2 TB/s; 16 sequences
+// with nothing shared, 353 MB, 72 us = 4.9 TB/s (reading that much and nothing else: 62 us).  Two questions about one image, fp32: 11.9 us, which is two launches,
+// finding the pieces and one tile after the other, not bytes.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -20,15 +25,17 @@
 namespace zipvl {
 
 constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4, kBlock = kCols * kPartWaves;
-constexpr int kStartPrefix = 12, kStartWave = 3;      // what starting an item weighs: its queries, its first rows, its part
-constexpr int kLight = 16;           // queries up to which waves cut a prefix
-constexpr int kLeast = 8;            // weight below which a workgroup is not worth its part
-// The same where every item has workgroups of its own.  A tile of fp32 rows is 2 us of a wave and more, and one for each is enough; of bf16 rows it
-// is 0.6, and half as many parts are worth it.  Two questions about an image of 576 rows, fp32: 14.1 us with 4, 17.3 with 8; eight about a video of 7200
-// rows, bf16: 22.6 and 19.3 (12: 19.7).
-template <typename T> constexpr int kLeastFew = sizeof(T) == 2 ? 8 : 4;
+// What starting an item weighs: its queries, its first rows, its part.  Of items that waves cut, bf16: 3; with 6, 95 calls took 0.7 % longer, with 1, 4 %.  fp32
+// tiles last longer and a start is 2 of them (two questions about an image: 11.6 us, with 3 12.8).  Of blocks: 6 or 24 change less than 0.3 %.
+constexpr int kStartPrefix = 12, kStartWave = 3;
+// Queries up to which waves cut a prefix, as they cut own rows.  Blocks of workgroups for all prefixes: 6 % longer over 95 calls, and twice as long
+// where many prefixes are short (three of 162 rows with 40 KV heads: 24.9 us instead of 11.7).  More than 16 columns would need the wider tile.
+constexpr int kLight = 16;
+// Weight below which a workgroup is not worth its part; a tile of a block may weigh as much and no piece may be shorter.  fp32 without blocks: half of it, a tile
+// for each wave, since such a tile is 2 us (with 8: 1.7 % longer over 95 calls, 13.0 us instead of 11.6 for two questions about an image); bf16 with 5, 6 or 7: as long.
+constexpr int kLeast = 8;
 constexpr int kCus = 256;
-constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves
+constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves (0: 0.5 % longer)
 
 // a wave-uniform number in scalar registers
 __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -41,7 +48,7 @@ struct PagedRead {
     const int32_t* group_begin; int groups;
     int B, Hq, Hkv, G;
     uint32_t inv_Hkv, inv_G, inv_Hq;
-    int least_few, wide;
+    int wide, least;
     __device__ __forceinline__ int prefixes() const { return groups * Hkv; }
     __device__ __forceinline__ int items() const { return (groups + B) * Hkv; }
 };
@@ -57,7 +64,12 @@ struct Parts {
         return 2 * rows + (by_wave ? 2 * grid * cols + (who * 2 + begins) * wave_cols : (who * 2 + begins) * cols) + col;
     }
 };
-constexpr int kByWave = 1 << 30;     // on the numbers of a prefix's pieces, where waves had them
+// On the numbers of pieces: of waves; of a long item; of the first wave, for its whole workgroup.
+constexpr int kByWave = 1 << 30, kLong = 1 << 29, kEntire = 1 << 28, kFlags = kByWave | kLong | kEntire;
+// A workgroup all of whose piece is of one item joins its four waves' parts if the item is long: more than 16 workgroups' pieces (parts are fewer for the second launch:
+// 13.5 us instead of 15.4 for 3 sequences of 17614 rows), or any item where pieces are 32 tiles and more (its waves then read side by side: 16 unshared
+// sequences 75.0 us instead of 77.5).  For short pieces meeting in LDS costs more than it saves (8 sequences of 811 rows: 16.1 us, 15.2 without).
+constexpr int kLongWorkgroups = 16, kLongPiece = 32;
 // Blocks of a prefix are counted from begin G / kBlock + p: no two groups meet, and B G / kBlock + groups + 1 are enough.
 __device__ __forceinline__ int piece_own(const PagedRead& p, int u) { return u; }
 __device__ __forceinline__ int piece_prefix(const PagedRead& p, int group, int begin, int block, int g) {
@@ -94,7 +106,7 @@ struct Item {
     __device__ __forceinline__ bool light() const { return cols() <= kLight; }
     __device__ __forceinline__ int weight(bool by_wave, int wide) const {
         const int n = blocks();
-        if (by_wave) return n ? (tiles() << (cols() > 16 ? wide : 0)) + kStartWave : 0;
+        if (by_wave) return n ? (tiles() << (cols() > 16 ? wide : 0)) + kStartWave - wide : 0;
         return n ? (n - 1) * weight_of_full_block(wide) + (tiles() << tile_log2(n - 1, wide)) + kStartPrefix : 0;
     }
 };
@@ -146,7 +158,8 @@ struct PartCfg {
     static constexpr int CH = D / Elem<T>::kPerChunk, ODB = D / 32;
     static_assert(WAVE >= D * kCols * 4, "room for a wave's sums");
     static constexpr int LDS = kPartWaves * WAVE;
-    static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;           // workgroups, of bf16 rows of 64 channels too: three are up to 10 % slower
+    // workgroups: of bf16 rows of 64 channels two as well, three are up to 10 % slower; one for all: 1.3 % longer over 95 calls, 64 questions 119 us instead of 106
+    static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
     static constexpr int GRID = kCus * PER_CU;
     // swizzle of row r's 16-byte chunks: K is read 32 rows at a time at one chunk, V of bf16 by transposing reads
     __device__ static __forceinline__ int k_swizzle(int r) { return k_row_swizzle<RB>(r); }
@@ -157,7 +170,8 @@ struct PartCfg {
 };
 
 // A wave's queries, in 32 columns or in 16, against tiles of one item.  With 16 a tile is two of 16x16: half the matrix cycles and half the
-// exponentials, which is what a few tiles on their own last (fp32 products: 2 us a tile of d = 128, 4 with 32 columns).
+// exponentials, which is what a few tiles on their own last (fp32 products: 2 us a tile of d = 128, 4 with 32 columns; 32 columns for all: 9 % longer over 65
+// calls, two questions about an image 14.4 us instead of 12.6).
 // Lane l has column l % COLS; the 64 / COLS groups of lanes share its keys and channels.
 template <typename T, int D, int COLS>
 struct WavePart {
@@ -312,7 +326,7 @@ struct WavePart {
 
     // O^T += V^T P^T.  A lane's weights are the operand of P^T as they are: contraction slot t of a lane = its key t.
     // bf16: the weights as two planes, 16 bits of each: one plane alone is off by 2^-9 of a weight, as much as the output's own rounding where a
-    // few rows have all the weight, and costs as much memory time.
+    // few rows have all the weight, and is no faster.
     __device__ __forceinline__ void weighted_rows(const char* vb, const float (&s)[kKeys]) {
         const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
         if constexpr (sizeof(T) == 2) {
@@ -459,40 +473,33 @@ struct WavePart {
     }
 };
 
-// a / b for 0 <= a < 2^22, b > 0 (512 * 512 and eight times the tiles of an item are less): the quotient in fp32 is off by less than one.  The compiler's division of whole numbers is some 40 instructions.
+// a / b for 0 <= a < 2^22, b > 0 (512 * 512 is less): the quotient in fp32 is off by less than one.  The compiler's division
+// of whole numbers is some 40 instructions.
 __device__ __forceinline__ int quotient(int a, int b) {
     const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), left = a - q * b;
     return q + (left >= b) - (left < 0);
 }
 
 
-// The line of work.  Many items: their weights follow each other and the workgroups take equal pieces, so that however unequal the lengths, no
-// workgroup has more than another; a long item gets many workgroups and several short ones share one.  The waves of a workgroup share
-// the pieces of prefixes, which many queries see; a piece of own items is cut again into equal ones for each wave, which then wait for
-// nobody.  Few items: each has workgroups of its own, a whole number by its weight, as many as the chip has room for: a workgroup that ends
-// one item and starts another does so one after the other, and where the work is small that is what lasts.
+// The line of work: the weights of all items follow each other and the workgroups take equal pieces, so that however unequal the lengths, no
+// workgroup has more than another; a long item gets many workgroups and several short ones share one.  First come the blocks of
+// prefixes, which the waves of a workgroup share; then what waves cut, light prefixes and own rows: a workgroup's piece of those is cut again into equal ones for
+// each wave, which then wait for nobody.  (Whole workgroups for every item where items are few: 1.8 % longer over 95 calls.)
 struct Line {
     int item;                                                // of the workgroup's first position
     int start;                                               // of that item on the line, which is shorter than 2^31
     int lo, hi;                                              // the workgroup's piece
     int waves;                                               // where the items begin that waves cut
-    int each;                                                // few items: weight for which an item has a workgroup; 0: many
+    int least;                                               // weight of a piece that four waves share
+    int longer;                                              // tiles that make an item a long one
     int me;                                                  // the workgroup's number on the line
 };
 
 struct LineShared {
-    int4 sums[kPartWaves];                                   // of prefixes that workgroups cut, that waves cut, of own items; blocks
-    int2 few[kPartWaves];
+    int4 sums[kPartWaves];                                   // of prefixes that workgroups cut, that waves cut, of own items
     int item, base;
 };
 constexpr int kSeen = 4096;          // items whose sizes are left in LDS
-
-// at most one a tile
-__device__ __forceinline__ int workgroups_of_block(const Item& it, int tile_log2, int each) { return min(quotient((it.tiles() << tile_log2) - 1, each) + 1, it.tiles()); }
-__device__ __forceinline__ int workgroups_of(const Item& it, int each, int wide) {
-    const int n = it.blocks();
-    return n ? (n > 1 ? (n - 1) * workgroups_of_block(it, 2 + wide, each) : 0) + workgroups_of_block(it, it.tile_log2(n - 1, wide), each) : 0;
-}
 
 // What a thread has of a kind of items: `per` of them from `from`.
 struct Share { int from, end; };
@@ -504,8 +511,7 @@ __device__ __forceinline__ Share share_of(int n) {
 __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, Item* seen, Line& line) {
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, prefixes = p.prefixes();
     const Share pre = share_of(prefixes), own = share_of(p.B * p.Hkv);
-    int pre_sum = 0, light_sum = 0, own_sum = 0, blocks = 0;
-    Item first_pre = {0, 0}, first_own = {0, 0};
+    int pre_sum = 0, light_sum = 0, own_sum = 0;
     int length[4];                                           // four are asked for at once, and the first four before those of prefixes are there
     auto ask = [&](int u0) {
 #pragma unroll
@@ -514,10 +520,8 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
     ask(own.from);
     for (int i = pre.from; i < pre.end; ++i) {
         const Item it = item_of(p, i);
-        if (i == pre.from) first_pre = it;
         if (it.light()) light_sum += it.weight(true, p.wide);
         else pre_sum += it.weight(false, p.wide);
-        blocks += it.blocks();
         if (i < kSeen) seen[i] = it;
     }
     for (int u0 = own.from; u0 < own.end; u0 += 4) {
@@ -526,17 +530,15 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
         for (int x = 0; x < 4; ++x) {
             if (u0 + x >= own.end) break;
             const Item it = own_item(p, u0 + x, length[x]);
-            if (u0 + x == own.from) first_own = it;
             own_sum += it.weight(true, p.wide);
-            blocks += it.blocks();
             if (prefixes + u0 + x < kSeen) seen[prefixes + u0 + x] = it;
         }
     }
-    const int pre_upto = wave_scan(pre_sum), light_upto = wave_scan(light_sum), own_upto = wave_scan(own_sum), wave_blocks = wave_sum(blocks);
-    if (lane == 63) sh.sums[w] = make_int4(pre_upto, light_upto, own_upto, wave_blocks);
+    const int pre_upto = wave_scan(pre_sum), light_upto = wave_scan(light_sum), own_upto = wave_scan(own_sum);
+    if (lane == 63) sh.sums[w] = make_int4(pre_upto, light_upto, own_upto, 0);
     if (tid == 0) sh.item = p.items();
     __syncthreads();
-    int pre_base = pre_upto - pre_sum, light_base = light_upto - light_sum, own_base = own_upto - own_sum, pre_all = 0, light_all = 0, own_all = 0, all_blocks = 0;
+    int pre_base = pre_upto - pre_sum, light_base = light_upto - light_sum, own_base = own_upto - own_sum, pre_all = 0, light_all = 0, own_all = 0;
 #pragma unroll
     for (int x = 0; x < kPartWaves; ++x) {
         const int4 v = sh.sums[x];
@@ -544,45 +546,20 @@ __device__ __forceinline__ bool find_piece(const PagedRead& p, LineShared& sh, I
         pre_all += v.x;
         light_all += v.y;
         own_all += v.z;
-        all_blocks += v.w;
     }
-    const int total = scalar(pre_all + light_all + own_all), grid = gridDim.x, room = grid - scalar(all_blocks);
+    const int total = scalar(pre_all + light_all + own_all);
     if (total == 0) return false;
-    line.each = 0;
     line.me = blockIdx.x;
     line.waves = scalar(pre_all);
-    if (p.items() <= 256 && 2 * room >= grid) {          // few: the line again, in workgroups
-        line.each = max(p.least_few, (total - 1) / room + 1);    // no more than there is room for: starts are counted too
-        light_sum = 0;
-        pre_sum = workgroups_of(first_pre, line.each, p.wide);
-        own_sum = workgroups_of(first_own, line.each, p.wide);
-        pre_base = wave_scan(pre_sum);
-        own_base = wave_scan(own_sum);
-        if (lane == 63) sh.few[w] = make_int2(pre_base, own_base);
-        __syncthreads();
-        pre_base -= pre_sum;
-        own_base -= own_sum;
-        int pre_n = 0, own_n = 0;
-#pragma unroll
-        for (int x = 0; x < kPartWaves; ++x) {
-            const int2 v = sh.few[x];
-            if (x < w) { pre_base += v.x; own_base += v.y; }
-            pre_n += v.x;
-            own_n += v.y;
-        }
-        if (line.me >= scalar(pre_n + own_n)) return false;
-        own_base += pre_n;
-        line.lo = line.me;
-        line.hi = line.me + 1;
-    } else {
-        const int wgs = max(1, min(grid, total / kLeast));   // a piece is longer than a tile of any item: none is without a tile
-        if (line.me >= wgs) return false;
-        const int each = scalar(total / wgs), more = total - each * wgs;
-        light_base += pre_all;
-        own_base += pre_all + light_all;
-        line.lo = line.me * each + quotient(line.me * more, wgs);
-        line.hi = (line.me + 1) * each + quotient((line.me + 1) * more, wgs);
-    }
+    line.least = line.waves == 0 ? p.least : kLeast;
+    const int wgs = max(1, min((int)gridDim.x, total / line.least));     // a piece is longer than a tile of any item: none is without a tile
+    if (line.me >= wgs) return false;
+    const int each = scalar(total / wgs), more = total - each * wgs;
+    line.longer = each >= kLongPiece ? 0 : kLongWorkgroups * each;
+    light_base += pre_all;
+    own_base += pre_all + light_all;
+    line.lo = line.me * each + quotient(line.me * more, wgs);
+    line.hi = (line.me + 1) * each + quotient((line.me + 1) * more, wgs);
     line.lo = scalar(line.lo);
     line.hi = scalar(line.hi);
     if (pre_base <= line.lo && line.lo < pre_base + pre_sum) {
@@ -619,36 +596,36 @@ struct Walker {
         if (in_lds && p.items() <= kSeen) seen = i < p.items() ? in_lds[i] : Item{0, 0};
         else seen = item_of(p, i);
     }
-    __device__ __forceinline__ bool next(Piece& x, int each) {
-        while (pos < hi && item < p.items()) {               // the items end where the line does, unless lengths change meanwhile
+    // On to the item that `pos` is in: its weight; 0: there is none (the items end where the line does, unless lengths change meanwhile).
+    __device__ __forceinline__ int skip(Item& it) {
+        for (; item < p.items(); ++item) {
             if (item >= window + 64) {
                 window = item;
                 look();
             }
-            Item& it = x.it;
             it.rows = __builtin_amdgcn_readlane(seen.rows, item - window);
             it.who = __builtin_amdgcn_readlane(seen.who, item - window);
+            const int weight = (item >= p.prefixes() || it.light()) == by_wave ? it.weight(by_wave, p.wide) : 0;
+            if (pos - start < weight) return weight;
+            start += weight;
+        }
+        return 0;
+    }
+    __device__ __forceinline__ bool next(Piece& x) {
+        while (pos < hi) {
+            Item& it = x.it;
+            const int weight = skip(it);
+            if (weight == 0) return false;
             x.item = item;
             x.own = item >= p.prefixes();
             const int tiles = it.tiles(), n = it.blocks();
-            const int weight = each ? workgroups_of(it, each, p.wide) : (x.own || it.light()) == by_wave ? it.weight(by_wave, p.wide) : 0;
-            if (pos - start >= weight) { start += weight; ++item; continue; }
-            const int off = pos - start;
-            if (each) {
-                const int full = n > 1 ? workgroups_of_block(it, 2 + p.wide, each) : 0;
-                x.block = n > 1 ? min(off / full, n - 1) : 0;
-                const int k = off - x.block * full, of = workgroups_of_block(it, it.tile_log2(x.block, p.wide), each), some = quotient(tiles, of), more = tiles - some * of;
-                x.ta = k * some + min(k, more);
-                x.tb = x.ta + some + (k < more);
-                pos = hi;
-                return true;
-            }
+            const int off = max(0, pos - start);             // a walker that was set back may stand before its item
             const int full = it.weight_of_full_block(p.wide);
             x.block = n > 1 ? min(off / full, n - 1) : 0;
             const int block_start = start + x.block * full, x0 = off - x.block * full, x1 = min((x.block < n - 1 ? full : weight - x.block * full), hi - block_start);
             pos = block_start + x1;
             const int shift = it.tile_log2(x.block, p.wide), last = (1 << shift) - 1;
-            x.ta = min((x0 + last) >> shift, tiles);         // a tile is whose piece it begins in
+            x.ta = clamped((x0 + last) >> shift, 0, tiles);  // a tile is whose piece it begins in
             x.tb = min((x1 + last) >> shift, tiles);
             if (x.ta < x.tb) return true;                    // else: nothing but an item's start
         }
@@ -660,12 +637,13 @@ struct Walker {
 struct Block {
     int unit, g, first, block, cols;                         // first: batch element; of the group, if it is a prefix
     int phases, phase, first_col;
-    bool own, begins, whole;
+    int who;                                                 // among those that cut such items
+    bool by_wave, own, begins, whole;
 };
 
-// All waves of the workgroup.
+// All waves of the workgroup, or, with one phase, any.
 template <typename T, int D, int COLS>
-__device__ __forceinline__ void shared_piece(const T* __restrict__ q, const PagedRead& p, float c, const Parts& out, const Piece& x, const Block& k, int me,
+__device__ __forceinline__ void shared_piece(const T* __restrict__ q, const PagedRead& p, float c, const Parts& out, const Piece& x, const Block& k,
                                              char* smem, float2 (&ml)[kPartWaves][kCols])
 {
     using C = PartCfg<T, D>;
@@ -676,7 +654,7 @@ __device__ __forceinline__ void shared_piece(const T* __restrict__ q, const Page
         const int r = k.block * kBlock + col, s = divided(r, p.G, p.inv_G);
         return (k.first + s) * p.Hq + k.g * p.G + r - s * p.G;
     };
-    auto record = [&](int col) { return k.whole ? out.whole(row_of(col), k.own) : out.piece(k.own, me, k.begins, col); };
+    auto record = [&](int col) { return k.whole ? out.whole(row_of(col), k.own) : out.piece(k.by_wave, k.who, k.begins, col); };
     WavePart<T, D, COLS> part;
     part.reset();
     part.load_queries(q + (int64_t)row_of(k.first_col + max(0, min(part.col(), in_wave - 1))) * D, part.col() < in_wave);
@@ -710,7 +688,7 @@ __device__ __forceinline__ void shared_piece(const T* __restrict__ q, const Page
             mo[ch * kCols + (i ^ (ch & 31))] = part.o[b][r] * a;
         }
     __syncthreads();
-    const int tid = w * 64 + lane, ch = tid % (D / 4) * 4, rec0 = k.whole ? 0 : out.piece(k.own, me, k.begins, 0);
+    const int tid = w * 64 + lane, ch = tid % (D / 4) * 4, rec0 = k.whole ? 0 : out.piece(k.by_wave, k.who, k.begins, 0);
 #pragma unroll 4
     for (int cc = tid / (D / 4); cc < k.cols; cc += 64 * kPartWaves / (D / 4)) {
         const float* base = reinterpret_cast<const float*>(smem + cc / kCols * k.phases * C::WAVE);
@@ -736,14 +714,39 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
     Line line;
     static_assert(kSeen * sizeof(Item) <= C::LDS, "the items' sizes stand where tiles come later");
     if (!find_piece(p, sh, reinterpret_cast<Item*>(smem), line)) return;
-    Walker walk = {p, reinterpret_cast<const Item*>(smem), line.item, line.item, line.start, line.lo, line.each ? line.hi : min(line.hi, max(line.lo, line.waves)), line.lo >= line.waves, {0, 0}};
+    // Of all waves: blocks of prefixes, then, if one long item that waves cut is all of the workgroup's piece, that.  Else each wave has a quarter of what
+    // is left; of less than `least` (the first workgroup with such items) the last wave has all: the pieces of an item are those of waves that follow
+    // each other.  One loop for all three: a launch comes to cold code, and what it does not need costs as much as what it needs.
+    enum { kBlocks, kOneItem, kWaves } stage = kBlocks;
+    const int prefixes = p.prefixes(), from = max(line.lo, line.waves), all = line.hi - from;
+    Walker walk = {p, reinterpret_cast<const Item*>(smem), line.item, line.item, line.start, line.lo, line.hi, line.lo >= line.waves, {0, 0}};
+    auto quarters = [&]() {
+        const int quarter = all / kPartWaves, rest = all % kPartWaves;
+        walk.by_wave = true;
+        walk.pos = all < line.least ? from : from + w * quarter + min(w, rest);
+        walk.hi = all < line.least ? (w == kPartWaves - 1 ? line.hi : from) : walk.pos + quarter + (w < rest);
+        stage = kWaves;
+    };
     walk.look();
+    if (walk.by_wave) {
+        Item it;
+        const int weight = walk.skip(it);
+        if (it.tiles() > line.longer && walk.start + weight >= line.hi) stage = kOneItem;
+        else quarters();
+    } else walk.hi = min(line.hi, line.waves);
     walk.in_lds = nullptr;
     __syncthreads();                                         // tiles may come
 
-    const int prefixes = p.prefixes();
     Piece x;
-    while (walk.next(x, line.each)) {                        // of all waves
+    for (;;) {
+        if (!walk.next(x)) {
+            if (stage != kBlocks || all <= 0) return;
+            quarters();
+            walk.item = walk.window = 0;                     // it stands behind the items that workgroups cut: back to the first item
+            walk.start = line.waves;
+            walk.look();
+            continue;
+        }
         const bool ends = x.tb == x.it.tiles();
         Block k;
         k.own = x.own;
@@ -755,57 +758,59 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
         k.first = x.it.begin();
         k.block = x.block;
         k.cols = min(kBlock, x.it.cols() - x.block * kBlock);
-        const int waves = x.it.waves_log2(x.block);
-        k.phases = kPartWaves >> waves;
+        const int waves = x.it.waves_log2(x.block);          // 0 of what waves cut
+        k.phases = stage == kWaves ? 1 : kPartWaves >> waves;
         k.phase = w & (k.phases - 1);
         k.first_col = (w >> (2 - waves)) * kCols;
-        int2* const piece = out.pieces + (x.own ? piece_own(p, k.unit) : piece_prefix(p, group, k.first, x.block, k.g));
-        if (tid == 0) {
-            if (k.begins) piece->x = line.me;
-            if (ends) piece->y = line.me;
+        k.by_wave = stage != kBlocks;
+        k.who = k.by_wave ? line.me * kPartWaves + (stage == kWaves ? w : 0) : line.me;
+        if ((stage == kWaves ? tid & 63 : tid) == 0) {
+            int2* const piece = out.pieces + (x.own ? piece_own(p, k.unit) : piece_prefix(p, group, k.first, x.block, k.g));
+            const int number = k.who | (k.by_wave ? kByWave | (x.it.tiles() > line.longer ? kLong : 0) : 0) | (stage == kOneItem ? kEntire : 0);
+            if (k.begins) piece->x = number;
+            if (ends) piece->y = number;
         }
-        if (OWN == 16 && k.cols <= 16) shared_piece<T, D, 16>(q, p, c, out, x, k, line.me, smem, ml);
-        else shared_piece<T, D, 32>(q, p, c, out, x, k, line.me, smem, ml);
+        if (OWN == 16 && k.cols <= 16) shared_piece<T, D, 16>(q, p, c, out, x, k, smem, ml);
+        else shared_piece<T, D, 32>(q, p, c, out, x, k, smem, ml);
     }
-    if (line.each || line.hi <= line.waves) return;
+}
 
-    // Items that waves cut.  Where fewer than kLeast are left to the workgroup (the first with such items) its last wave has them: the pieces of
-    // an item are those of waves that follow each other.
-    const int from = max(line.lo, line.waves), all = line.hi - from, quarter = all / kPartWaves, rest = all % kPartWaves;
-    walk.pos = all < kLeast ? from : from + w * quarter + min(w, rest);
-    walk.hi = all < kLeast ? (w == kPartWaves - 1 ? line.hi : from) : walk.pos + quarter + (w < rest);
-    if (!walk.by_wave) {                                     // it stands behind the items that workgroups cut: back to the first item
-        walk.by_wave = true;
-        walk.item = walk.window = 0;
-        walk.start = line.waves;
-        walk.look();
+// Whose an item's parts are: x .. y, workgroups or waves.  Of a long item: waves from x of the first workgroup (or all four at once), one part of each
+// workgroup between, which has nothing else, and waves up to y of the last (or all four at once).
+struct Span {
+    int head, mid, tail;                                     // parts
+    int x, between, last;                                    // part i is of x + i, between + 4 i or last + i
+    int base, cols;                                          // of records
+    __device__ __forceinline__ int count() const { return head + mid + tail; }
+    __device__ __forceinline__ int record(int i) const {
+        const int who = i < head ? x + i : i < head + mid ? between + kPartWaves * i : last + i;
+        return base + (2 * who + (i == 0)) * cols;
     }
-    const int who = line.me * kPartWaves + w, i = tid & (OWN - 1), lane = tid & 63;
-    while (walk.next(x, 0)) {
-        const bool begins = x.ta == 0, ends = x.tb == x.it.tiles(), whole = begins && ends;
-        const int unit = x.own ? x.item - prefixes : x.item, group = x.own ? 0 : divided(unit, p.Hkv, p.inv_Hkv);
-        const int g = x.own ? unit - x.it.begin() * p.Hkv : unit - group * p.Hkv, cols = x.it.cols();
-        const int r = min(i, cols - 1), s = divided(r, p.G, p.inv_G), row = (x.it.begin() + s) * p.Hq + g * p.G + r - s * p.G;
-        if (lane == 0) {
-            int2* const piece = out.pieces + (x.own ? piece_own(p, unit) : piece_prefix(p, group, x.it.begin(), 0, g));
-            if (begins) piece->x = x.own ? who : who | kByWave;
-            if (ends) piece->y = x.own ? who : who | kByWave;
-        }
-        WavePart<T, D, OWN> part;
-        part.reset();
-        part.load_queries(q + (int64_t)row * D, i < cols);
-        part.run(p, x.own ? p.table + (int64_t)unit * p.width : p.prefix_table + (int64_t)unit * p.prefix_width, x.it.rows, x.ta, 1, x.tb, c, smem + w * C::WAVE);
-        if (i < cols) {
-            const int64_t rec = whole ? out.whole(row, x.own) : out.piece(1, who, begins, i);
-            part.store(out.o + rec * D);
-            if (lane < OWN) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(part.m, part.l);
-        }
+};
+__device__ __forceinline__ Span span_of(const Parts& in, int2 v, int row, int own, int col) {
+    static_assert(kPartWaves == 4, "");
+    const bool by_wave = v.x & kByWave;
+    const int x = min(v.x & ~kFlags, in.grid * kPartWaves - 1), y = v.y < 0 ? -1 : min(v.y & ~kFlags, in.grid * (by_wave ? kPartWaves : 1) - 1);
+    Span s = {max(0, y - x + 1), 0, 0, x, 0, 0, in.piece(by_wave, 0, 0, col), by_wave ? in.wave_cols : in.cols};
+    if (v.x & kLong && x >> 2 < y >> 2) {
+        s.head = v.x & kEntire ? 1 : 4 - (x & 3);
+        s.mid = (y >> 2) - (x >> 2) - 1;
+        s.tail = v.y & kEntire ? 1 : (y & 3) + 1;
+        s.between = (x | 3) + 1 - 4 * s.head;
+        s.last = (y & ~3) - s.head - s.mid;
     }
+    if (x == y) {
+        s.base = in.whole(row, own);
+        s.cols = 0;
+    }
+    return s;
 }
 
 // The parts of one query head: those of its group's prefix, then its own -> its output row.  A chain of loads, each for the address of the next:
 // groups, pieces (with the lengths), parts (maxima, sums and the first parts' outputs at once).  WAVES waves have a row: all four where a row
-// may have many parts; one where rows are many, each has a few and dispatching a workgroup for it is what lasts (join_waves).
+// may have many parts; one where rows are many, each has a few parts and dispatching
+// a workgroup for it is what lasts (from 1536 rows on: up to 4 % of a call, 32.0 us instead of 33.4 for 49 sequences of 40 heads; always: 1.9 % longer, 22.8 us
+// instead of 19.5 for 8 questions about a video).
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts in, T* __restrict__ o) {
     constexpr int kPer = D / 4, kAt = 64 * WAVES / kPer, kAtOnce = WAVES == 1 ? 4 : 64 / kAt;        // threads per part, parts at a time, loads on the way
@@ -831,16 +836,9 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
         }
     }
     if (own_len > 0) own = own_pieces;
-    const bool waves_cut = pre.x & kByWave;                  // the prefix
-    pre.x &= ~kByWave, pre.y = pre.y < 0 ? -1 : pre.y & ~kByWave;
-    pre.x = max(pre.x, 0), pre.y = min(pre.y, in.grid * (waves_cut ? kPartWaves : 1) - 1), own.x = max(own.x, 0), own.y = min(own.y, in.grid * kPartWaves - 1);
-    const int n_pre = max(0, pre.y - pre.x + 1), n = n_pre + max(0, own.y - own.x + 1);
-    auto record = [&](int s) {
-        const bool is_own = s >= n_pre;
-        const int2 x = is_own ? own : pre;
-        const int who = x.x + (is_own ? s - n_pre : s);
-        return x.x == x.y ? in.whole(row, is_own) : in.piece(is_own || waves_cut, who, who == x.x, is_own ? head - g * p.G : col);
-    };
+    const Span a_pre = span_of(in, pre, row, 0, col), a_own = span_of(in, own, row, 1, head - g * p.G);
+    const int n_pre = a_pre.count(), n = n_pre + a_own.count();
+    auto record = [&](int s) { return s < n_pre ? a_pre.record(s) : a_own.record(s - n_pre); };
     float M = -INFINITY, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < n; s0 += 64) {                     // 64 parts at a time, every wave all of their maxima and sums
@@ -914,11 +912,11 @@ static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, f
     using C = PartCfg<T, D>;
     const PagedLayout l = paged_layout(d, p.groups > 0, C::GRID);
     const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, l.wave_cols, C::GRID};
-    // what all lengths at their greatest would weigh, and more: no more workgroups than that
+    // what all lengths at their greatest would weigh, and more: positions on the line are below 2^31, and no more workgroups than that
     const int64_t own = (int64_t)d.B * d.Hkv * (2 * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartWave);
     const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kBlock + p.groups) * d.Hkv * (8 * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartPrefix) : 0;
     if (own + pre >= (int64_t)1 << 31)
-        return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^33)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
+        return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^35)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
     const int wgs = (int)std::min<int64_t>(C::GRID, own + pre);
     static std::atomic<uint64_t> lds_set{0};                 // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
@@ -946,7 +944,8 @@ int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int3
 {
     const PagedRead p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len,
                          prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, d.Hq / d.Hkv,
-                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), inverse(d.Hq), d.dtype == ZIPVL_BF16 ? kLeastFew<__bf16> : kLeastFew<float>, d.dtype == ZIPVL_BF16 ? 0 : 1};
+                         inverse(d.Hkv), inverse(d.Hq / d.Hkv), inverse(d.Hq), d.dtype == ZIPVL_BF16 ? 0 : 1,
+                         d.dtype == ZIPVL_F32 && d.Hq / d.Hkv <= 16 ? kLeast / 2 : kLeast};
 #define ZIPVL_PAGED(T, D)                                                                              \
     return p.G <= 16 ? launch_paged_t<T, D, 16>((const T*)q, p, d, scale, (T*)o, (char*)ws, st)       \
                      : launch_paged_t<T, D, 32>((const T*)q, p, d, scale, (T*)o, (char*)ws, st)

@@ -446,6 +446,24 @@ def test_decode_attn_paged_of_thousands_of_units(lens):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", [  # B, Hq, Hkv, d, dtype, page, lens, groups, prefix: items longer than many workgroups' pieces, and pieces of one item
+    (64, 8, 8, 64, "bf16", 64, [3, 40, 0, 64, 31] * 20 + [30000] + [17, 1, 0] * 137, (), ()),
+    (2, 16, 2, 128, "f32", 32, [6000, 1, 0, 90], (2,), [20000, 33]),
+    (1, 8, 2, 128, "bf16", 16, [33, 40000], (1,), [17000, 700]),
+    (20, 16, 8, 128, "bf16", 64, [4000, 2500, 5100, 10, 3000, 4500, 0], (20,), [3000, 500]),
+    (20, 16, 8, 64, "bf16", 64, [9000, 2500, 5100, 12000, 3000], (9, 2), [3000, 5000]),
+    (2, 64, 2, 64, "f32", 32, [19000, 5000, 0, 700], (), ()),
+    (30, 4, 2, 128, "f32", 128, [2000, 3000, 900, 4000], (16, 14), [5000]),
+], ids=lambda c: f"B{c[0]}Hq{c[1]}Hkv{c[2]}d{c[3]}{c[4]}P{len(c[7])}")
+def test_decode_attn_paged_of_long_items(case):
+    say(f"decode_attn_paged long items {case[:6]}")
+    batch = Batch(*case, seed=31)
+    o = batch.run()
+    batch.check(o, which=sorted({0, 1 % batch.B, batch.B // 5, batch.B - 2 if batch.B > 1 else 0, batch.B - 1}))
+    assert torch.equal(o, batch.run())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("gain,spike", [(20.0, 0.0), (1.0, 40.0), (1e-3, 0.0)])
 def test_decode_attn_paged_where_one_row_has_all_the_weight(dtype, d, gain, spike):
@@ -783,6 +801,10 @@ def test_decode_attn_paged_refuses(lib):
     assert call(plen=None) == -1 and call(begin=None) == -1 and call(begin=ODD) == -3
     assert call(groups=-1) == -1 and call(groups=3) == -1
     assert call(pages=z.Pages(0x1000, 0x1000, 9, 20)) == -2
+    big = z.Pages(0x1000, 0x1000, 9, 256)
+    assert call(pages=big, width=65537) == -2 and call(pages=big, pwidth=65537) == -2 and "2^24" in z.zipvl_last_error()
+    assert call(dims(B=256, Hq=8, Hkv=8), pages=big, width=65536, groups=0) == -2 and "2^35" in z.zipvl_last_error()
+    assert call(dims(B=256, Hq=64, Hkv=8), pages=big, pwidth=65536, groups=48) == -2 and "2^35" in z.zipvl_last_error()
     for scale in (0.0, -1.0, math.nan, math.inf):
         assert call(scale=scale) == -1
     assert call(ws=None) == -4 and call(ws_bytes=1) == -4 and "workspace" in z.zipvl_last_error()
