@@ -1,5 +1,6 @@
 // Rotary positions of a layer's queries and keys, and the rows that go into a paged cache with the rotation on the way.
-// Both read every row once and write it once: memory, or latency for a few tokens.
+// Both read every row once and write it once: memory, or latency for a few tokens.  Measured: queries and keys of 18432 tokens, bf16, 302 MB, 61 us =
+// 4.9 TB/s; 8192 tokens of a stack into its pages, 1074 MB, 211 us = 5.1 TB/s (a large copy: 4.9 TB/s); one token for each of 8 sequences 3.3 us, a launch.
 //
 // D / 16 threads have a row, two runs of eight channels each, so that a pair of channels meets in one thread and a rotated row
 // needs nothing from other lanes.  A thread stays with a token while it goes through heads: angles depend on the token alone.
@@ -12,6 +13,7 @@ namespace zipvl {
 
 struct Rows { char* base; int64_t b, h, t; };                // a tensor [B, H, n, d]: strides in bytes
 struct RowsIn { const char* base; int64_t b, h, t; };
+template <typename R> __device__ __forceinline__ auto row_of(const R& r, int b, int h, int t) { return r.base + b * r.b + h * r.h + t * r.t; }
 
 // Tokens of all batch elements follow each other.  A workgroup has 256 D^-1 16 rows a turn: `tokens` of them (a power of two) of as many
 // heads as that leaves, and goes through the heads from its first in steps of `step`.
@@ -34,18 +36,20 @@ __global__ __launch_bounds__(256) void rotate_kernel(RowsIn Q, RowsIn K, Rows Qo
     struct Row { Run<T> a, b; };
     auto load = [&](int h) {
         const RowsIn& in = h < Hq ? Q : K;
-        const T* src = reinterpret_cast<const T*>(in.base + b * in.b + (h < Hq ? h : h - Hq) * in.h + t * in.t);
+        const T* src = reinterpret_cast<const T*>(row_of(in, b, h < Hq ? h : h - Hq, t));
         return Row{load_run(src + runs.a), load_run(src + runs.b)};
     };
     Angles at;
     if (runs.first >= 0) at.ask(turns, runs.first, pos + token, (int64_t)w.total);
-    Row row = load(first);                                   // while the angles are taken, and then a head ahead: no row overlaps another's output
+    // While the angles are taken, and then a head ahead: no row overlaps another's output.  (Without the latter: 63.5 us instead of 63.1 for 18432 tokens, and as
+    // long on average.)
+    Row row = load(first);
     if (runs.first >= 0) at.take(turns);
     for (int h = first; h < heads; h += w.step) {
         Row next = row;
         if (h + w.step < heads) next = load(h + w.step);
         const Rows& out = h < Hq ? Qo : Ko;
-        T* dst = reinterpret_cast<T*>(out.base + b * out.b + (h < Hq ? h : h - Hq) * out.h + t * out.t);
+        T* dst = reinterpret_cast<T*>(row_of(out, b, h < Hq ? h : h - Hq, t));
         if (runs.first >= 0) turn_runs(row.a, row.b, at, turns.neighbours);
         store_run(dst + runs.a, row.a);
         store_run(dst + runs.b, row.b);
@@ -68,8 +72,10 @@ __device__ __forceinline__ int paged_count(const PagedRows& p, int u, int b, int
 __device__ __forceinline__ int paged_len(const PagedRows& p, int start, int count) { return (int)min((int64_t)start + count, (int64_t)p.width << p.page_log2); }
 
 // Heads [0, Hkv) are those of K and V, [Hkv, heads) of Q (as many as are given).  A row's way is two round trips to memory: where a unit starts, how
-// much it brings and which token this is, all at once; then the row, and the page that it goes to.  Asking for the next head's row before
-// this one's is stored, as above, takes twice the registers and is slower (chunk of 5 x 777 tokens, 16 heads, fp32 10.9 -> 14.1 us).
+// much it brings, which token this is and its positions, all at once; then the row, and the page that it goes to, while the angles are taken.
+// Every head has threads of its own: going through heads as rotate_kernel does saves angles and costs 5 to 10 % (64 tokens of 64 sequences: 4.1 us
+// instead of 3.8, 777 tokens of 5 sequences, fp32 10.5 instead of 10.0, 8192 tokens of a stack 221 instead of 211; only where 0.4 of 18432 tokens
+// are kept it is 8.6 instead of 9.0, since threads of tokens that go are there for nothing).
 template <typename T, int D, bool TURN>
 __global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, RowsIn Q, Rows Qo, int Hkv, int G, uint32_t inv_G, int heads, Walk w, PagedRows p,
                                                            const int32_t* __restrict__ pos, Turns turns)
@@ -81,50 +87,52 @@ __global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, R
     const int b = divided(token, w.n, w.inv_n), i = token - b * w.n;         // row i of what a unit brings
     const Runs runs(c, TURN ? turns.pairs : 0, TURN ? turns.neighbours : 0);
     Angles at;
-    if (TURN && runs.first >= 0 && !p.idx) {
-        at.ask(turns, runs.first, pos + token, (int64_t)w.total);
-        at.take(turns);
-    }
-    for (int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2); h < heads; h += w.step) {
-        const bool query = h >= Hkv;
-        const int g = query ? divided(h - Hkv, G, inv_G) : h, u = b * Hkv + g, set = p.per_batch ? b : u;
-        // only the threads of a row of K may read a start: len may stand there
-        const int brings = p.k ? p.k[set] : w.n, starts = query ? 0 : p.start[u];
-        const int which = p.idx ? p.idx[(int64_t)set * w.n + i] : i;
-        const int count = max(0, min(brings, w.n)), start = max(0, min(starts, p.width << p.page_log2)), t = max(0, min(which, w.n - 1));
-        if (!query && i == 0 && c == 0 && p.len) p.len[u] = paged_len(p, start, count);
-        if (i >= count) continue;
-        if (query) {
-            const T* src = reinterpret_cast<const T*>(Q.base + b * Q.b + (h - Hkv) * Q.h + t * Q.t);
-            T* dst = reinterpret_cast<T*>(Qo.base + b * Qo.b + (h - Hkv) * Qo.h + t * Qo.t);
-            Run<T> ra = load_run(src + runs.a), rb = load_run(src + runs.b);
-            if (TURN && runs.first >= 0) turn_runs(ra, rb, at, turns.neighbours);
-            store_run(dst + runs.a, ra);
-            store_run(dst + runs.b, rb);
-            continue;
-        }
-        const int64_t row = (int64_t)start + i;
-        if (row >> p.page_log2 >= p.width) continue;         // behind the table
-        const int page = p.table[(int64_t)u * p.width + (row >> p.page_log2)];
-        const T* ks = reinterpret_cast<const T*>(K.base + b * K.b + g * K.h + t * K.t);
-        const T* vs = reinterpret_cast<const T*>(V.base + b * V.b + g * V.h + t * V.t);
-        Run<T> ra = load_run(ks + runs.a), rb = load_run(ks + runs.b);
-        const Run<T> va = load_run(vs + runs.a), vb = load_run(vs + runs.b);
-        if (TURN && runs.first >= 0) {
-            if (p.idx) {
-                at.ask(turns, runs.first, pos + (int64_t)b * w.n + t, (int64_t)w.total);
-                at.take(turns);
-            }
+    const bool turn = TURN && runs.first >= 0;
+    if (turn && !p.idx) at.ask(turns, runs.first, pos + token, (int64_t)w.total);
+    const int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2);
+    if (h >= heads) return;
+    const bool query = h >= Hkv;
+    const int g = query ? divided(h - Hkv, G, inv_G) : h, u = b * Hkv + g, set = p.per_batch ? b : u;
+    int brings = w.n, starts = 0, which = i;
+    if (p.k) brings = p.k[set];
+    if (!query) starts = p.start[u];                         // only the threads of a row of K may read it: len may stand there
+    if (p.idx) which = p.idx[(int64_t)set * w.n + i];
+    asm volatile("" : "+v"(brings), "+v"(starts), "+v"(which));              // here they are waited for, all three at once
+    const int count = max(0, min(brings, w.n)), start = max(0, min(starts, p.width << p.page_log2)), t = max(0, min(which, w.n - 1));
+    if (!query && i == 0 && c == 0 && p.len) p.len[u] = paged_len(p, start, count);
+    if (i >= count) return;
+    if (query) {
+        const T* src = reinterpret_cast<const T*>(row_of(Q, b, h - Hkv, t));
+        T* dst = reinterpret_cast<T*>(row_of(Qo, b, h - Hkv, t));
+        Run<T> ra = load_run(src + runs.a), rb = load_run(src + runs.b);
+        if (turn) {
+            at.take(turns);
             turn_runs(ra, rb, at, turns.neighbours);
         }
-        if ((unsigned)page >= (unsigned)p.num_pages) continue;
-        const int64_t at_row = (((int64_t)page << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * D;
-        T *kd = reinterpret_cast<T*>(p.K) + at_row, *vd = reinterpret_cast<T*>(p.V) + at_row;
-        store_run(kd + runs.a, ra);
-        store_run(kd + runs.b, rb);
-        store_run(vd + runs.a, va);
-        store_run(vd + runs.b, vb);
+        store_run(dst + runs.a, ra);
+        store_run(dst + runs.b, rb);
+        return;
     }
+    const int64_t row = (int64_t)start + i;
+    if (row >> p.page_log2 >= p.width) return;               // behind the table
+    if (turn && p.idx) at.ask(turns, runs.first, pos + (int64_t)b * w.n + t, (int64_t)w.total);
+    const int page = p.table[(int64_t)u * p.width + (row >> p.page_log2)];
+    const T* ks = reinterpret_cast<const T*>(row_of(K, b, g, t));
+    const T* vs = reinterpret_cast<const T*>(row_of(V, b, g, t));
+    Run<T> ra = load_run(ks + runs.a), rb = load_run(ks + runs.b);
+    const Run<T> va = load_run(vs + runs.a), vb = load_run(vs + runs.b);
+    asm volatile("" ::: "memory");                           // the rows are asked for before it is known that there is a page for them
+    if (turn) {
+        at.take(turns);
+        turn_runs(ra, rb, at, turns.neighbours);
+    }
+    if ((unsigned)page >= (unsigned)p.num_pages) return;
+    const int64_t at_row = (((int64_t)page << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * D;
+    T *kd = reinterpret_cast<T*>(p.K) + at_row, *vd = reinterpret_cast<T*>(p.V) + at_row;
+    store_run(kd + runs.a, ra);
+    store_run(kd + runs.b, rb);
+    store_run(vd + runs.a, va);
+    store_run(vd + runs.b, vb);
 }
 
 // len of every unit, where it stands in the place of start and several workgroups of the append read that
@@ -152,8 +160,10 @@ static Turns turns_of(const zipvl_rope* r, bool inverse) {
 static RowsIn rows_in(const void* p, const int64_t (&s)[3], int e) { return {(const char*)p, s[0] * e, s[1] * e, s[2] * e}; }
 static Rows rows_out(void* p, const int64_t (&s)[3], int e) { return {(char*)p, s[0] * e, s[1] * e, s[2] * e}; }
 
-constexpr int kWalkGrid = 4096;
-static dim3 walk_of(const zipvl_dims& d, int heads, Walk& w) {
+// `apart`: every head has threads of its own; else about kRotateGrid workgroups, each with several heads of its tokens, whose angles it takes once
+// (18432 tokens: 63.1 us; with 2048 64.4, with 16384 70.1).
+constexpr int kRotateGrid = 4096;
+static dim3 walk_of(const zipvl_dims& d, int heads, bool apart, Walk& w) {
     const int rows = 4096 / d.d;                             // of a workgroup, a turn
     w.n = d.n;
     w.total = d.B * d.n;
@@ -161,7 +171,7 @@ static dim3 walk_of(const zipvl_dims& d, int heads, Walk& w) {
     while ((1 << w.tokens_log2) < rows && (1 << w.tokens_log2) < w.total) ++w.tokens_log2;
     const int lanes = rows >> w.tokens_log2, tiles = (w.total + (1 << w.tokens_log2) - 1) >> w.tokens_log2;
     const int most = (heads + lanes - 1) / lanes;
-    const int parts = std::max(1, std::min(most, (kWalkGrid + tiles - 1) / tiles));
+    const int parts = apart ? most : std::min(most, (kRotateGrid + tiles - 1) / tiles);
     w.step = parts * lanes;
     w.inv_n = inverse(d.n);
     return dim3(tiles, parts);
@@ -173,7 +183,7 @@ int launch_rotate(const void* Q, const void* K, const zipvl_dims& d, const int32
     const int e = d.dtype == ZIPVL_BF16 ? 2 : 4;
     const int Hq = Q ? d.Hq : 0, heads = Hq + (K ? d.Hkv : 0);
     Walk w;
-    const dim3 grid = walk_of(d, heads, w);
+    const dim3 grid = walk_of(d, heads, false, w);
     const Turns turns = turns_of(&rope, flags & ZIPVL_ROTATE_INVERSE);
     KernelTimer tm(ZIPVL_K_ROTATE, st);
 #define ZIPVL_ROTATE(T, D)                                                                                                         \
@@ -192,7 +202,7 @@ int launch_paged_append(const void* K, const void* V, const zipvl_dims& d, const
     const int e = d.dtype == ZIPVL_BF16 ? 2 : 4;
     const int heads = d.Hkv + (Q ? d.Hq : 0);
     Walk w;
-    const dim3 grid = walk_of(d, heads, w);
+    const dim3 grid = walk_of(d, heads, true, w);
     const Turns turns = turns_of(rope, false);
     const bool in_place = len == start && d.n > 1;           // one token: the threads that read a start are one wave, and its store comes after
     PagedRows p = {(char*)pages.K, (char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table_pages, table, start, in_place ? nullptr : len,
