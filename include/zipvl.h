@@ -350,7 +350,7 @@ typedef struct zipvl_pages {
  * becomes row start[u] + i of the unit:
  *   K row <- rotate(K[b,g,t]) at pos[:, b, t] (rope NULL: as it is, pos is then not looked at),  V row <- V[b,g,t]
  *   len[u] = min(start[u] + c, table_pages * page)
- * Rows behind the table's end are not written; start is clamped to [0, table_pages * page].  len may be start itself.
+ * Rows behind the table's end are not written; start is clamped to [0, table_pages * page].  len may be start itself; it overlaps no other input.
  * Q (may be NULL; not with idx): Qo[b,h,i] = rotate(Q[b,h,i]) for i < c of the unit of head h; Qo [B,Hq,n,d] contiguous, may be Q; rows from c are left
  * as they are.
  * K, V, Q by dims' strides; start, len [device] int32 [B*Hkv]; flags: 0 or ZIPVL_T_PER_BATCH (idx [B,n], k [B]).  Two units whose new

@@ -58,6 +58,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RowsIn Q, RowsIn K, Rows Qo
     }
 }
 
+constexpr int kHeadsGrid = 32768;     // workgroups on the grid's second axis; an axis has less than 65536
+
 struct PagedRows {
     char *K, *V;
     int num_pages, page_log2, width;                         // width: pages in a unit's row of the table
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, R
     Angles at;
     const bool turn = TURN && runs.first >= 0;
     if (turn && !p.idx) at.ask(turns, runs.first, pos + token, (int64_t)w.total);
-    const int h = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2);
+    const int h = (blockIdx.z * kHeadsGrid + blockIdx.y) * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2);
     if (h >= heads) return;
     const bool query = h >= Hkv;
     const int g = query ? divided(h - Hkv, G, inv_G) : h, u = b * Hkv + g, set = p.per_batch ? b : u;
@@ -178,7 +180,7 @@ static dim3 walk_of(const zipvl_dims& d, int heads, bool apart, Walk& w) {
     const int parts = apart ? most : std::min(most, (kRotateGrid + tiles - 1) / tiles);
     w.step = parts * lanes;
     w.inv_n = inverse(d.n);
-    return dim3(tiles, parts);
+    return dim3(tiles, std::min(parts, kHeadsGrid), (parts + kHeadsGrid - 1) / kHeadsGrid);
 }
 
 int launch_rotate(const void* Q, const void* K, const zipvl_dims& d, const int32_t* pos, const zipvl_rope& rope, int flags, void* Qo, void* Ko,

@@ -467,6 +467,15 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
     if ((reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(rope ? pos : nullptr) |
          reinterpret_cast<uintptr_t>(start) | reinterpret_cast<uintptr_t>(len)) & 3u)
         return set_error(ZIPVL_EALIGN, "%s: idx, k, pos, start or len is not 4-byte aligned", fn);
+    // len is written while other workgroups read the rest
+    const int64_t units = (int64_t)dims->B * dims->Hkv, sets = flags & ZIPVL_T_PER_BATCH ? dims->B : units, tokens = (int64_t)dims->B * dims->n;
+    auto meets = [&](const int32_t* a, int64_t n) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(len);
+        return a && x < y + 4 * units && y < x + 4 * n;
+    };
+    if ((start != len && meets(start, units)) || meets(k, sets) || meets(idx, sets * dims->n) || meets(table, units * table_pages) ||
+        meets(rope ? pos : nullptr, rope ? rope->axes * tokens : 0))
+        return set_error(ZIPVL_EINVAL, "%s: len overlaps start, k, idx, pos or table (it may be start itself)", fn);
     return launch_paged_append(K, V, *dims, idx, k, pos, rope, *pages, table, table_pages, start, len, Q, Qo, flags, (hipStream_t)stream);
 }
 

@@ -305,6 +305,18 @@ def test_paged_append_where_pages_end_or_are_missing(n):
     assert torch.equal(cache.K, want_K) and torch.equal(cache.V, want_V)
 
 
+@pytest.mark.gpu
+def test_paged_append_of_more_heads_than_a_grid_has_rows():
+    heads, n, d = 40000, 64, 64
+    K = torch.arange(heads * n, dtype=torch.int32, device=DEV).view(1, heads, n, 1).expand(1, heads, n, 8).contiguous().view(torch.bfloat16).repeat(1, 1, 1, 4)
+    V = K.flip(1)
+    cache = z.PagedCache(*(torch.zeros((heads, n, d), dtype=torch.bfloat16, device=DEV) for _ in range(2)))
+    table = torch.arange(heads - 1, -1, -1, dtype=torch.int32, device=DEV).view(heads, 1)
+    length, _ = z.zipvl_paged_append(K, V, cache, table, torch.zeros(heads, dtype=torch.int32, device=DEV))
+    assert torch.equal(cache.K.view(torch.int16), K[0].flip(0).view(torch.int16)) and torch.equal(cache.V.view(torch.int16), V[0].flip(0).view(torch.int16))
+    assert (length == n).all()
+
+
 # ---------------------------------------------------------------- attention over pages
 class Batch:
     """A batch in pages whose unused rows and unused pages hold NaN, and its plain result."""
@@ -788,6 +800,17 @@ def test_paged_append_refuses(lib):
     assert call(Q=FAKE, Qo=FAKE, rope=None) == -1
     assert call(dims(q=(8 * 20 * 64, 20 * 64, 128)), Q=FAKE, Qo=FAKE) == -1 and "in the place" in z.zipvl_last_error()
     assert call(flags=1) == -5
+
+
+def test_paged_append_refuses_lengths_in_the_place_of_other_inputs(lib):
+    at = lambda i, off=0: C.c_void_p(0x100000 * i + off)                # arrays a mebibyte apart; B Hkv = 4 units of 10 tokens, tables of 4 pages
+
+    def call(length, rope=True, flags=0):
+        r = z.Rope(frequencies(32))
+        return lib.zipvl_paged_append(at(1), at(2), C.byref(dims()), at(3), at(4), at(5), C.byref(r) if rope else None,
+                                      C.byref(z.Pages(0x1000, 0x1000, 9, 16)), at(6), 4, at(7), length, None, None, flags, None)
+    for length in (at(3), at(3, 156), at(4), at(4, 12), at(4, -12), at(5), at(5, 76), at(6, 60), at(7, 4), at(7, -12)):
+        assert call(length) == -1 and "overlaps" in z.zipvl_last_error()
 
 
 def test_decode_attn_paged_refuses(lib):
