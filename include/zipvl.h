@@ -373,7 +373,7 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
  * q, o [device] [B*Hq, d] contiguous; G = Hq/Hkv <= 32.  Rows that are attended to must be finite.
  * Tables are refused (ZIPVL_ESHAPE) that hold more than 2^24 rows a unit, or in all some 2^35 rows (those of prefixes counted four times for every 128
  * queries begun).
- * Numerics: scores, statistics and sums in fp32; bf16 weights enter the product with V with 16 bits, in two parts; one rounding at the end.  The order of
+ * Numerics: scores, weights, statistics and sums in fp32; one rounding at the end.  The order of
  * all sums follows from the lengths: the same call gives the same bits.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_DECODE_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that
  * overlap on one workspace race).

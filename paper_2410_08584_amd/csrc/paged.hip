@@ -325,42 +325,52 @@ struct WavePart {
     }
 
     // O^T += V^T P^T.  A lane's weights are the operand of P^T as they are: contraction slot t of a lane = its key t.
-    // bf16: the weights as two planes, 16 bits of each: one plane alone is off by 2^-9 of a weight, as much as the output's own rounding where a
-    // few rows have all the weight, and is no faster.
+    // bf16: the weights as three planes, whose sum they are exactly.  With two, 16 bits, a sum that nearly cancels was off by 64 times what fp32 rounds, and 1.9e-3
+    // of the outputs of 16 unshared sequences were not the nearest bf16 numbers (4e-4 with three; 1e-3 of fp32 sums by library calls); 1.3 % less time over 29 calls.
     __device__ __forceinline__ void weighted_rows(const char* vb, const float (&s)[kKeys]) {
         const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
         if constexpr (sizeof(T) == 2) {
             typedef short shortx4 __attribute__((ext_vector_type(4)));
             using lds_ptr = __attribute__((address_space(3))) shortx4*;
-            uintx4 hi[kKeys / 8], lo[kKeys / 8];
-#pragma unroll
-            for (int y = 0; y < kKeys / 8; ++y)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const float a = s[8 * y + 2 * x], b = s[8 * y + 2 * x + 1];
-                    const uint32_t w = pack_bf16x2(a, b);
-                    hi[y][x] = w;
-                    lo[y][x] = pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xFFFF0000u));
-                }
             // Channel l of four keys for every lane l of 16, which give the addresses of four consecutive channels each: lane 4 e + q of key e.
             const int e = (lane >> 2) & 3, q = lane & 3, row = 4 * group() + e;
 #pragma unroll
-            for (int y = 0; y < kKeys / 8; ++y)
+            for (int y = 0; y < kKeys / 8; ++y) {
+                uintx4 plane[3];
 #pragma unroll
-                for (int b = 0; b < kO; ++b) {
-                    const int chunk = COLS == 32 ? 4 * b + 2 * ((lane >> 4) & 1) + (q >> 1) : 2 * b + (q >> 1);
-                    const char* a0 = vb + (row + 16 * y) * C::RB + swz_chunk(chunk, C::v_swizzle(row)) + (q & 1) * 8;
-                    const uintx2 f0 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)a0));
-                    const uintx2 f1 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a0 + (COLS == 32 ? 8 : 16) * C::RB)));
-                    const uintx4 vf = {f0[0], f0[1], f1[0], f1[1]};
-                    if constexpr (COLS == 32) {
-                        o[b] = mma_frag<__bf16>(vf, lo[y], o[b]);
-                        o[b] = mma_frag<__bf16>(vf, hi[y], o[b]);
-                    } else {
-                        o[b] = mma16(vf, lo[y], o[b]);
-                        o[b] = mma16(vf, hi[y], o[b]);
+                for (int x = 0; x < 4; ++x) {
+                    float a = s[8 * y + 2 * x], b = s[8 * y + 2 * x + 1];
+#pragma unroll
+                    for (int z = 0; z < 3; ++z) {
+                        const uint32_t w = pack_bf16x2(a, b);
+                        plane[z][x] = w;
+                        a -= __uint_as_float(w << 16);
+                        b -= __uint_as_float(w & 0xFFFF0000u);
                     }
                 }
+                // 16 columns: four blocks side by side, so that a product does not wait for the one before it (20 sequences of 278 rows 17.3 us, one block
+                // after the other 17.6).  Those of 32 columns last long enough (61 questions about 19382 rows of 64 channels: 60.7 us side by side, 59.9 so).
+                constexpr int kSide = COLS == 16 ? 4 : 1;
+#pragma unroll
+                for (int b0 = 0; b0 < kO; b0 += kSide) {
+                    uintx4 vf[kSide];
+#pragma unroll
+                    for (int x = 0; x < kSide; ++x) {
+                        const int b = b0 + x, chunk = COLS == 32 ? 4 * b + 2 * ((lane >> 4) & 1) + (q >> 1) : 2 * b + (q >> 1);
+                        const char* a0 = vb + (row + 16 * y) * C::RB + swz_chunk(chunk, C::v_swizzle(row)) + (q & 1) * 8;
+                        const uintx2 f0 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)a0));
+                        const uintx2 f1 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a0 + (COLS == 32 ? 8 : 16) * C::RB)));
+                        vf[x] = uintx4{f0[0], f0[1], f1[0], f1[1]};
+                    }
+#pragma unroll
+                    for (int z = 2; z >= 0; --z)
+#pragma unroll
+                        for (int x = 0; x < kSide; ++x) {
+                            if constexpr (COLS == 32) o[b0 + x] = mma_frag<__bf16>(vf[x], plane[z], o[b0 + x]);
+                            else o[b0 + x] = mma16(vf[x], plane[z], o[b0 + x]);
+                        }
+                }
+            }
         } else if constexpr (COLS == 32) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {

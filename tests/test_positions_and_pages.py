@@ -486,6 +486,35 @@ def test_decode_attn_paged_where_one_row_has_all_the_weight(dtype, d, gain, spik
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,Hq,Hkv,groups", [(64, 2, 1, ()), (64, 32, 1, ()), (20, 40, 40, (20,))], ids=["16 columns", "32 columns", "a block of a prefix"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_attn_paged_keeps_all_bits_of_bf16_weights(B, Hq, Hkv, groups, d):
+    """Two rows of weights 1 and w = exp(-a), 0 < a < 0.7, whose values nearly cancel: (w r - v) / (1 + w) with v = w r rounded to bf16.  w is off by 4 u (the scale,
+    the exponent, its power of two: u, u, 2 u), r <= 2 makes 8 u of that, at most six roundings of sums up to 2 are 12 u, and the sum of weights is 1.5 and more:
+    14 u, and half a step of the result.  A weight of 16 bits is off by up to 2^-18, which is 64 u."""
+    say(f"decode_attn_paged weights B={B} Hq={Hq} Hkv={Hkv} d={d}")
+    g = torch.Generator().manual_seed(41)
+    P, page = len(groups), 16
+    units = P * Hkv if P else B * Hkv
+    a = (0.02 + 0.67 * torch.rand((units,), generator=g)).to(torch.bfloat16)
+    w = torch.exp(-a.double())
+    r = (1 + torch.rand((units, d), generator=g)).to(torch.bfloat16)
+    v = (w[:, None] * r.double()).to(torch.bfloat16)
+    K, V = (torch.zeros((units, page, d), dtype=torch.bfloat16) for _ in range(2))
+    K[:, 1, 0], V[:, 0], V[:, 1] = -a, -v, r
+    q = torch.zeros((B * Hq, d), dtype=torch.bfloat16)
+    q[:, 0] = 1.0
+    pages = torch.arange(units, dtype=torch.int32, device=DEV).view(units, 1)
+    two = torch.full((units,), 2, dtype=torch.int32, device=DEV)
+    prefix = dict(prefix_table=pages, prefix_len=two, group_begin=torch.tensor([0, B], dtype=torch.int32, device=DEV)) if P else {}
+    table, length = (torch.zeros((B * Hkv, 1), dtype=torch.int32, device=DEV), torch.zeros((B * Hkv,), dtype=torch.int32, device=DEV)) if P else (pages, two)
+    o = z.zipvl_decode_attn_paged(q.to(DEV), z.PagedCache(K.to(DEV), V.to(DEV)), table, length, 1.0, B=B, Hq=Hq, Hkv=Hkv, **prefix).cpu().double()
+    ref = ((w[:, None] * r.double() - v.double()) / (1 + w[:, None])).view(-1, Hkv, 1, d).expand(B, Hkv, Hq // Hkv, d).reshape(B * Hq, d)
+    err, tol = (o - ref).abs(), 14 * U + half_step(torch.bfloat16) * ref.abs()
+    assert (err <= tol).all(), f"worst {(err - tol).max().item():.3e} over"
+
+
+@pytest.mark.gpu
 def test_decode_attn_paged_without_a_group_and_in_any_partition():
     """Batch elements in front of, between and behind the groups have no prefix; bounds outside the batch are clamped."""
     for begin, groups in (([2, 4, 5], (2, 1)), ([1, 1, 3], (0, 2)), ([-4, 3, 100], (3, 3))):
