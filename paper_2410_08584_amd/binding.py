@@ -581,25 +581,31 @@ def zipvl_rotate(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], pos: torc
 
 
 class PagedCache:
-    """A KV cache in pages: K, V [num_pages, page, d].  Which pages hold the rows of a unit stands in a table, int32 [units, table_pages]."""
+    """A KV cache in pages: K, V [num_pages, page, d].  Which pages hold the rows of a unit stands in a table, int32 [units, table_pages].  K and V may be
+    replaced, as by a pool that has grown: every call takes them as they are then."""
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor):
-        if K.dim() != 3:
-            raise ZipvlError(-2, f"pages of shape {tuple(K.shape)}, expected [num_pages, page, d]")
-        _expect("V", V, K.shape, K.dtype)
-        _dense(K)
-        _dtype_code(K)
         self.K, self.V = K, V
-        if K.device != V.device:
-            raise ZipvlError(-1, f"pages of K on {K.device}, of V on {V.device}")
-        self.num_pages, self.page, self.d = K.shape
+        self.struct()
+
+    num_pages = property(lambda self: self.K.shape[0])
+    page = property(lambda self: self.K.shape[1])
+    d = property(lambda self: self.K.shape[2])
 
     @classmethod
     def empty(cls, num_pages: int, page: int, d: int, dtype: torch.dtype, device) -> "PagedCache":
         return cls(*(torch.empty((num_pages, page, d), dtype=dtype, device=device) for _ in range(2)))
 
     def struct(self) -> Pages:
-        return Pages(self.K.data_ptr(), self.V.data_ptr(), self.num_pages, self.page)
+        K, V = self.K, self.V
+        if K.dim() != 3:
+            raise ZipvlError(-2, f"pages of shape {tuple(K.shape)}, expected [num_pages, page, d]")
+        _expect("V", V, K.shape, K.dtype)
+        _dense(K)
+        _dtype_code(K)
+        if K.device != V.device:
+            raise ZipvlError(-1, f"pages of K on {K.device}, of V on {V.device}")
+        return Pages(K.data_ptr(), V.data_ptr(), K.shape[0], K.shape[1])
 
 
 def zipvl_paged_append(K: torch.Tensor, V: torch.Tensor, cache: PagedCache, table: torch.Tensor, start: torch.Tensor, *,
@@ -616,6 +622,7 @@ def zipvl_paged_append(K: torch.Tensor, V: torch.Tensor, cache: PagedCache, tabl
         return length, Qo if Q is not None else None
     if K.dim() != 4:
         raise ZipvlError(-2, f"zipvl_paged_append: expected K [B,Hkv,n,d], got shape {tuple(K.shape)}")
+    pages = cache.struct()
     B, Hkv, n, d = K.shape
     units = B * Hkv
     _rows_like("V", V, K.shape, K.dtype)
@@ -645,7 +652,6 @@ def zipvl_paged_append(K: torch.Tensor, V: torch.Tensor, cache: PagedCache, tabl
     else:
         Qo = None
     dm = _dims_rows(Q, K, V, B=B, Hq=Hkv if Q is None else Q.shape[1], Hkv=Hkv, n=n, d=d, dtype=_dtype_code(K))
-    pages = cache.struct()
     _on_device(lambda stream: lib.zipvl_paged_append(
         _ptr(K), _ptr(V), C.byref(dm), _ptr(idx), _ptr(k), _ptr(pos), None if rope is None else C.byref(rope), C.byref(pages), _ptr(table),
         table.shape[1], _ptr(start), _ptr(length), _ptr(Q), _ptr(Qo), int(flags), stream), K, V, cache.K, table, start, length, idx, k, pos, Q, Qo)
@@ -667,6 +673,7 @@ def zipvl_decode_attn_paged(q: torch.Tensor, cache: PagedCache, table: torch.Ten
     if o is not None and ws is not None and _called(
             _native.decode_attn_paged(q, cache, table, length, softmax_scale, B, Hq, Hkv, prefix_table, prefix_len, group_begin, o, ws)):
         return o
+    pages = cache.struct()
     d, units = cache.d, B * Hkv
     if table.dim() != 2:
         raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [{units}, table_pages]")
@@ -692,7 +699,6 @@ def zipvl_decode_attn_paged(q: torch.Tensor, cache: PagedCache, table: torch.Ten
         o = torch.empty((B * Hq, d), dtype=q.dtype, device=q.device)
     if ws is None:
         ws = decode_paged_workspace(cache, table, prefix_table, B=B, Hq=Hq, Hkv=Hkv)
-    pages = cache.struct()
     _on_device(lambda stream: lib.zipvl_decode_attn_paged(
         _ptr(q), C.byref(pages), _ptr(table), table.shape[1], _ptr(length), _ptr(prefix_table), 0 if prefix_table is None else prefix_table.shape[1],
         _ptr(prefix_len), _ptr(group_begin), groups, C.byref(dm), float(softmax_scale), _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), stream),

@@ -736,6 +736,46 @@ def test_calls_of_the_extension_module_are_the_general_ones(monkeypatch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("extension", [True, False])
+def test_pools_that_were_replaced(extension, monkeypatch):
+    """A pool that has grown by assignment, and has shrunk: pages are counted as they are at the call, by the extension module and without it."""
+    from paper_2410_08584_amd import binding
+    if not extension:
+        monkeypatch.setattr(binding, "_native", binding._NoExtension())
+    Hkv, n, d, page = 2, 16, 64, 16
+    _, K, V = layer(1, 1, Hkv, n, d, "bf16", "head", 81)
+    cache = pools(4, page, d, "bf16", 82)
+    table = torch.tensor([[7], [3]], dtype=torch.int32, device=DEV)
+    start = torch.zeros((Hkv,), dtype=torch.int32, device=DEV)
+    q = K[0, :, 3].contiguous()
+    o = torch.empty_like(q)
+    ws = z.decode_paged_workspace(cache, table, B=1, Hq=Hkv, Hkv=Hkv)
+
+    def attended(which):
+        length, _ = z.zipvl_paged_append(K, V, cache, table, start, length=torch.empty_like(start))
+        for u in range(Hkv):
+            if which[u]:
+                assert torch.equal(cache.K[int(table[u, 0])], K[0, u]) and torch.equal(cache.V[int(table[u, 0])], V[0, u])
+        for kw in (dict(o=o, ws=ws), {}):
+            got = z.zipvl_decode_attn_paged(q, cache, table, length, 0.125, B=1, Hq=Hkv, Hkv=Hkv, **kw)
+            for u in range(Hkv):
+                k, v = (x[0, u].cpu() if which[u] else x[0, u, :0].cpu() for x in (K, V))
+                ref, bound = attention(q[u:u + 1].cpu(), k, v, 0.125)
+                size = torch.softmax(q[u:u + 1].cpu().double() @ k.double().T * 0.125, dim=1) @ v.double().abs() if which[u] else torch.zeros_like(ref)
+                assert_attention(got[u:u + 1], ref, bound, size)
+
+    small = cache.K, cache.V
+    attended([False, True])
+    cache.K, cache.V = (torch.zeros((9, page, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    attended([True, True])
+    cache.K, cache.V = small
+    attended([False, True])
+    cache.V = torch.zeros((9, page, d), dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(z.ZipvlError, match="V has shape"):
+        attended([False, True])
+
+
+@pytest.mark.gpu
 def test_rows_of_expanded_and_single_axes():
     """Inputs whose axes have stride 0, or one element and torch's own idea of its stride, are taken as they are."""
     d, page = 64, 16
@@ -912,3 +952,21 @@ def test_binding_refuses_what_does_not_fit():
     refused(lambda: attend(prefix_table=i(2, 3), prefix_len=i(2), group_begin=i(3)), "prefix_table")
     refused(lambda: attend(prefix_table=i(4, 3), prefix_len=i(2), group_begin=i(3)), "prefix_len")
     refused(lambda: attend(), "one GPU")
+
+
+def test_pages_are_counted_as_they_are():
+    x = lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype)
+    cache = z.PagedCache(x(4, 16, 64), x(4, 16, 64))
+    cache.K, cache.V = x(9, 32, 128), x(9, 32, 128)
+    pages = cache.struct()
+    assert (pages.K, pages.V, pages.num_pages, pages.page) == (cache.K.data_ptr(), cache.V.data_ptr(), 9, 32)
+    assert (cache.num_pages, cache.page, cache.d) == (9, 32, 128)
+    for V, text in ((x(4, 32, 128), "shape"), (x(9, 32, 128, dtype=torch.bfloat16), "expected"), (x(9, 32, 256)[..., ::2], "contiguous")):
+        cache.V = V
+        with pytest.raises(z.ZipvlError, match=text):
+            cache.struct()
+        i = torch.zeros((4, 1), dtype=torch.int32)
+        with pytest.raises(z.ZipvlError, match=text):
+            z.zipvl_decode_attn_paged(x(8, 128), cache, i, i[:, 0].contiguous(), 0.1, B=2, Hq=4, Hkv=2)
+        with pytest.raises(z.ZipvlError, match=text):
+            z.zipvl_paged_append(x(2, 2, 5, 128), x(2, 2, 5, 128), cache, i, i[:, 0].contiguous())
