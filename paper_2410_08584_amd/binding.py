@@ -699,6 +699,7 @@ def zipvl_decode_attn_paged(q: torch.Tensor, cache: PagedCache, table: torch.Ten
         o = torch.empty((B * Hq, d), dtype=q.dtype, device=q.device)
     if ws is None:
         ws = decode_paged_workspace(cache, table, prefix_table, B=B, Hq=Hq, Hkv=Hkv)
+    _dense(ws)
     _on_device(lambda stream: lib.zipvl_decode_attn_paged(
         _ptr(q), C.byref(pages), _ptr(table), table.shape[1], _ptr(length), _ptr(prefix_table), 0 if prefix_table is None else prefix_table.shape[1],
         _ptr(prefix_len), _ptr(group_begin), groups, C.byref(dm), float(softmax_scale), _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), stream),

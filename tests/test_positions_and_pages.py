@@ -970,3 +970,11 @@ def test_pages_are_counted_as_they_are():
             z.zipvl_decode_attn_paged(x(8, 128), cache, i, i[:, 0].contiguous(), 0.1, B=2, Hq=4, Hkv=2)
         with pytest.raises(z.ZipvlError, match=text):
             z.zipvl_paged_append(x(2, 2, 5, 128), x(2, 2, 5, 128), cache, i, i[:, 0].contiguous())
+
+
+def test_a_workspace_with_gaps_is_refused():
+    x = lambda *shape: torch.zeros(shape)
+    cache, i = z.PagedCache(x(4, 16, 64), x(4, 16, 64)), torch.zeros((4, 1), dtype=torch.int32)
+    for ws in (torch.zeros((1 << 27,), dtype=torch.uint8)[::2], torch.zeros((1,), dtype=torch.uint8).expand(1 << 27)):
+        with pytest.raises(z.ZipvlError, match="contiguous"):
+            z.zipvl_decode_attn_paged(x(8, 64), cache, i, i[:, 0].contiguous(), 0.1, B=2, Hq=4, Hkv=2, o=x(8, 64), ws=ws)
