@@ -366,7 +366,7 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
  *   o[b,h] = softmax( q[b,h] . [Kp ; Ko]^T * softmax_scale ) [Vp ; Vo]
  * with Ko, Vo the first len[u] rows of the unit u = b*Hkv + g by table [B*Hkv, table_pages], and Kp, Vp the first prefix_len[p*Hkv + g] rows
  * by prefix_table [groups*Hkv, prefix_pages] of the group p that b is in.  Group p is the batch elements group_begin[p] .. group_begin[p+1] - 1
- * (group_begin [device] int32 [groups + 1], ascending within [0, B]); elements in no group have no prefix.  The rows of a prefix are
+ * (group_begin [device] int32 [groups + 1], ascending; clamped to [0, B]; where it falls, o is of no meaning); elements in no group have no prefix.  The rows of a prefix are
  * read once for all queries of a group (once for every 128 of them, where there are more).
  * groups = 0: nothing is shared (prefix_table, prefix_len, group_begin are not looked at).  groups <= B.
  * Lengths are clamped to [0, pages of the table * page]; a head without any row gets zeros.  Nothing behind a length is read.

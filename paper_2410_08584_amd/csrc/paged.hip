@@ -65,7 +65,7 @@ struct Parts {
     }
 };
 // On the numbers of pieces: of waves; of a long item; of the first wave, for its whole workgroup.
-constexpr int kByWave = 1 << 30, kLong = 1 << 29, kEntire = 1 << 28, kFlags = kByWave | kLong | kEntire;
+constexpr int kByWave = 1 << 30, kLong = 1 << 29, kEntire = 1 << 28, kNumber = kEntire - 1;
 // A workgroup all of whose piece is of one item joins its four waves' parts if the item is long: more than 16 workgroups' pieces (parts are fewer for the second launch:
 // 13.5 us instead of 15.4 for 3 sequences of 17614 rows), or any item where pieces are 32 tiles and more (its waves then read side by side: 16 unshared
 // sequences 75.0 us instead of 77.5).  For short pieces meeting in LDS costs more than it saves (8 sequences of 811 rows: 16.1 us, 15.2 without).
@@ -785,7 +785,8 @@ __global__ __launch_bounds__(64 * kPartWaves, (PartCfg<T, D>::PER_CU)) void page
     }
 }
 
-// Whose an item's parts are: x .. y, workgroups or waves.  Of a long item: waves from x of the first workgroup (or all four at once), one part of each
+// Whose an item's parts are: x .. y, workgroups or waves, within the workspace whatever stands in `pieces` (nothing, where groups overlap and weigh more than the
+// line holds).  Of a long item: waves from x of the first workgroup (or all four at once), one part of each
 // workgroup between, which has nothing else, and waves up to y of the last (or all four at once).
 struct Span {
     int head, mid, tail;                                     // parts
@@ -800,8 +801,9 @@ struct Span {
 __device__ __forceinline__ Span span_of(const Parts& in, int2 v, int row, int own, int col) {
     static_assert(kPartWaves == 4, "");
     const bool by_wave = v.x & kByWave;
-    const int x = min(v.x & ~kFlags, in.grid * kPartWaves - 1), y = v.y < 0 ? -1 : min(v.y & ~kFlags, in.grid * (by_wave ? kPartWaves : 1) - 1);
-    Span s = {max(0, y - x + 1), 0, 0, x, 0, 0, in.piece(by_wave, 0, 0, col), by_wave ? in.wave_cols : in.cols};
+    const int cols = by_wave ? in.wave_cols : in.cols;
+    const int x = min(v.x & kNumber, in.grid * kPartWaves - 1), y = v.y < 0 ? -1 : min(v.y & kNumber, in.grid * (by_wave ? kPartWaves : 1) - 1);
+    Span s = {max(0, y - x + 1), 0, 0, x, 0, 0, in.piece(by_wave, 0, 0, min(col, cols - 1)), cols};
     if (v.x & kLong && x >> 2 < y >> 2) {
         s.head = v.x & kEntire ? 1 : 4 - (x & 3);
         s.mid = (y >> 2) - (x >> 2) - 1;

@@ -523,6 +523,21 @@ def test_decode_attn_paged_without_a_group_and_in_any_partition():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("junk", [0x00, 0x3F, 0x7F, 0xC0, 0xFF])
+def test_decode_attn_paged_of_groups_that_fall(junk):
+    """Groups that fall may overlap: whatever the workspace holds then, nothing outside it is read, and the next call, with groups that ascend, is right."""
+    say(f"decode_attn_paged groups that fall, workspace of {junk:#x}")
+    batch = Batch(40, 8, 4, 64, "bf16", 16, [20, 0, 50], (25, 15), [100, 31], seed=27)
+    ws = z.decode_paged_workspace(batch.cache, batch.table, batch.prefix_table, B=batch.B, Hq=batch.Hq, Hkv=batch.Hkv).fill_(junk)
+    begin = batch.group_begin.clone()
+    for falling in ([0, 40, 0], [40, 0, 40], [2 ** 31 - 1, -2 ** 31, 7]):
+        batch.group_begin.copy_(torch.tensor(falling))
+        batch.run(ws=ws)
+    batch.group_begin.copy_(begin)
+    batch.check(batch.run(ws=ws))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_decode_attn_paged_skips_rows_without_a_page_and_clamps_lengths(dtype):
     batch = Batch(2, 4, 2, 64, dtype, 16, [64, 64, 64, 64], (2,), [48, 48], seed=25)
