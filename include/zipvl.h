@@ -370,7 +370,8 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
  * read once for all queries of a group (once for every 128 of them, where there are more).
  * groups = 0: nothing is shared (prefix_table, prefix_len, group_begin are not looked at).  groups <= B.
  * Lengths are clamped to [0, pages of the table * page]; a head without any row gets zeros.  Nothing behind a length is read.
- * q, o [device] [B*Hq, d] contiguous; G = Hq/Hkv <= 32.  Rows that are attended to must be finite.
+ * q, o [device] [B*Hq, d] contiguous; G = Hq/Hkv <= 32.  An infinity in a row of V makes its channel infinite, a key of logit -infinity weighs
+ * nothing, as in fp32 products; queries and other logits must be finite.
  * Tables are refused (ZIPVL_ESHAPE) that hold more than 2^24 rows a unit, or in all some 2^35 rows (those of prefixes counted four times for every 128
  * queries begun).
  * Numerics: scores, weights, statistics and sums in fp32; one rounding at the end.  The order of

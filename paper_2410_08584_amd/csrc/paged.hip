@@ -221,7 +221,7 @@ struct WavePart {
         }
     }
 
-    // Rows that are not there take a row that is: its scores are masked, and what weighs nothing must be finite.
+    // Rows that are not there take a row that is: its scores are masked, and its values, which weigh nothing, are finite (or clear_absent takes them).
     template <bool V>
     __device__ static __forceinline__ void fetch(const char* g0, const char* g1, uint32_t rows, unsigned lds) {
         const int lane = threadIdx.x & 63, lr = lane / (C::RB / 16), p = lane % (C::RB / 16);
@@ -325,11 +325,24 @@ struct WavePart {
     }
 
     // O^T += V^T P^T.  A lane's weights are the operand of P^T as they are: contraction slot t of a lane = its key t.
-    // bf16: the weights as three planes, whose sum they are exactly.  With two, 16 bits, a sum that nearly cancels was off by 64 times what fp32 rounds, and 1.9e-3
+    // bf16: the weights as three planes, whose sum they are exactly (PLANES), or one value after the other in fp32 products.  With two planes, 16 bits, a sum that nearly cancels was off by 64 times what fp32 rounds, and 1.9e-3
     // of the outputs of 16 unshared sequences were not the nearest bf16 numbers (4e-4 with three; 1e-3 of fp32 sums by library calls); 1.3 % less time over 29 calls.
+    template <bool PLANES>
     __device__ __forceinline__ void weighted_rows(const char* vb, const float (&s)[kKeys]) {
         const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2 && !PLANES) {
+#pragma unroll
+            for (int r = 0; r < kKeys; ++r) {
+                const int k = key(r);
+#pragma unroll
+                for (int b = 0; b < kO; ++b) {
+                    const int ch = COLS * b + i;
+                    const float v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(vb + k * C::RB + swz_chunk(ch >> 3, C::v_swizzle(k)) + (ch & 7) * 2) << 16);
+                    if constexpr (COLS == 32) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], o[b], 0, 0, 0);
+                    else o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[r], o[b], 0, 0, 0);
+                }
+            }
+        } else if constexpr (sizeof(T) == 2) {
             typedef short shortx4 __attribute__((ext_vector_type(4)));
             using lds_ptr = __attribute__((address_space(3))) shortx4*;
             // Channel l of four keys for every lane l of 16, which give the addresses of four consecutive channels each: lane 4 e + q of key e.
@@ -396,6 +409,15 @@ struct WavePart {
         }
     }
 
+    // Values of rows that are not there become zeros.
+    __device__ static __forceinline__ void clear_absent(char* vb, uint32_t rows) {
+        const int lane = here(), lr = lane / (C::RB / 16);
+#pragma unroll 1
+        for (int q = 0; q < C::NL; ++q)
+            if (!(rows >> (q * C::RPL + lr) & 1)) *reinterpret_cast<uintx4*>(vb + q * 1024 + lane * 16) = uintx4{0, 0, 0, 0};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+
     // The lane's sums to a record of D floats.
     __device__ __forceinline__ void store(float* dst) const {
         const int group = here() / COLS;
@@ -414,7 +436,8 @@ struct WavePart {
 
     // Tiles first, first + step, ... below `end` of an item with `rows` rows and this row of a table.  K of the next tile is requested when K of this one
     // has been read, V of the next when V of this one has: a wave has one tile of each in LDS and one on the way at any time.
-    __device__ __forceinline__ void run(const PagedRead& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine) {
+    template <bool AGAIN>
+    __device__ __forceinline__ void tiles(const PagedRead& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine) {
         first = scalar(first);
         step = scalar(step);
         end = scalar(end);
@@ -473,13 +496,29 @@ struct WavePart {
             weigh(s, cur.rows, c);
             if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::NL) : "memory");   // all but K of the next
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            weighted_rows(vb, s);
+            if (AGAIN && cur.rows != 0xFFFFFFFFu) clear_absent(vb, cur.rows);
+            weighted_rows<!AGAIN>(vb, s);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (more) fetch<true>(nxt.v0, nxt.v1, nxt.rows, vlds);
             cur = nxt;
             have = more;
         }
         l = over_groups<COLS>(l, [](float a, float b) { return a + b; });
+    }
+
+    // The part of the lane's column.  An infinity in V is no number times a plane of 0, or where it stands for a row that is not there: a wave whose sums are not
+    // finite takes its tiles again, without either.  Looking at the sums of each piece: 0.8 % of the time over 29 calls.
+    __device__ __forceinline__ void run(const PagedRead& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine) {
+        tiles<false>(p, table, rows, first, step, end, c, mine);
+        float probe[4] = {};                                 // no number if a sum is not finite
+#pragma unroll
+        for (int b = 0; b < kO; ++b)
+#pragma unroll
+            for (int r = 0; r < kRegs; ++r) probe[r & 3] = fmaf(o[b][r], 0.f, probe[r & 3]);
+        if (__builtin_expect(__any(probe[0] + probe[1] + probe[2] + probe[3] != 0.f), 0)) {
+            reset();
+            tiles<true>(p, table, rows, first, step, end, c, mine);
+        }
     }
 };
 
@@ -666,9 +705,9 @@ __device__ __forceinline__ void shared_piece(const T* __restrict__ q, const Page
     };
     auto record = [&](int col) { return k.whole ? out.whole(row_of(col), k.own) : out.piece(k.by_wave, k.who, k.begins, col); };
     WavePart<T, D, COLS> part;
-    part.reset();
     part.load_queries(q + (int64_t)row_of(k.first_col + max(0, min(part.col(), in_wave - 1))) * D, part.col() < in_wave);
     const int32_t* table = k.own ? p.table + (int64_t)k.unit * p.width : p.prefix_table + (int64_t)k.unit * p.prefix_width;
+    part.reset();
     if (in_wave > 0) part.run(p, table, x.it.rows, x.ta + k.phase, k.phases, x.tb, c, mine);
     if (k.phases == 1) {
         const int i = part.here() & (COLS - 1);

@@ -515,6 +515,60 @@ def test_decode_attn_paged_keeps_all_bits_of_bf16_weights(B, Hq, Hkv, groups, d)
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", [  # B, Hq, Hkv, d, dtype, page, lens, groups, prefix
+    (3, 28, 4, 128, "bf16", 16, [1, 17, 33, 700], (), ()),
+    (2, 8, 4, 64, "bf16", 64, [5, 48, 100, 2000], (), ()),
+    (2, 64, 2, 64, "bf16", 32, [40, 333], (), ()),
+    (5, 40, 2, 128, "bf16", 32, [0], (5,), [50, 900]),
+    (4, 4, 4, 64, "bf16", 16, [3, 20], (3,), [70, 33]),
+    (3, 8, 2, 128, "f32", 16, [1, 17, 33, 500], (), ()),
+    (5, 40, 2, 64, "f32", 32, [0], (5,), [50, 400]),
+], ids=lambda c: f"B{c[0]}Hq{c[1]}Hkv{c[2]}d{c[3]}{c[4]}P{len(c[7])}")
+def test_decode_attn_paged_with_infinities(case):
+    """Of every sequence, or prefix, one row of V has an infinity (the first, the last, a middle one, or the first of the last tile of 32, which others stand in for): its channel
+    is infinite, of its sign, for all heads that see it, and the other channels are as without it.  One key is infinite against queries of the other sign: it weighs nothing."""
+    say(f"decode_attn_paged infinities {case}")
+    batch = Batch(*case, seed=33)
+    page, inf = case[5], math.inf
+    batch.q = batch.q.abs()
+    sign, at = {}, 0
+    units = [(batch.table[u], batch.rows, u) for u in range(len(batch.rows))] + [(batch.prefix_table[u], batch.prefix_rows, u) for u in range(len(batch.prefix_rows))]
+    for table, rows, u in units:
+        k, v = rows[u]
+        n = k.shape[0]
+        if n == 0:
+            continue
+        row = [0, n - 1, n // 2, (n - 1) // 32 * 32][at % 4]
+        channel, value = at % batch.d, inf if at % 3 else -inf
+        at += 1
+        batch.cache.V[int(table[row // page]), row % page, channel] = value
+        v[row, channel] = 0.0
+        sign[id(rows), u] = channel, value
+        if n > 40:                                                       # another row's key; as a row of the plain form it goes
+            gone = row + 1 if row + 1 < n else row - 1
+            batch.cache.K[int(table[gone // page]), gone % page, 1] = -inf
+            keep = torch.arange(n) != gone
+            rows[u] = k[keep], v[keep]
+    o = batch.run()
+    expected, G = {}, batch.Hq // batch.Hkv
+    for b in range(batch.B):
+        for h in range(batch.Hkv):
+            heads = slice(b * batch.Hq + h * G, b * batch.Hq + (h + 1) * G)
+            p = batch.group(b)
+            seen = [sign.get((id(batch.rows), b * batch.Hkv + h))] + ([sign.get((id(batch.prefix_rows), p * batch.Hkv + h))] if p is not None else [])
+            for channel, value in filter(None, seen):
+                assert bool((o[heads, channel] == value).all()), (b, h, channel, value)
+                expected[b, h, channel] = heads
+    for (b, h, channel), heads in expected.items():                      # the other channels: with the infinite ones taken from the plain form
+        k, v = batch.rows[b * batch.Hkv + h]
+        p = batch.group(b)
+        if p is not None:
+            k, v = (torch.cat([x, y]) for x, y in zip(batch.prefix_rows[p * batch.Hkv + h], (k, v)))
+        o[heads, channel] = attention(batch.q[heads].cpu(), k, v, batch.scale)[0][:, channel].to(o.dtype).to(DEV)
+    batch.check(o)
+
+
+@pytest.mark.gpu
 def test_decode_attn_paged_without_a_group_and_in_any_partition():
     """Batch elements in front of, between and behind the groups have no prefix; bounds outside the batch are clamped."""
     for begin, groups in (([2, 4, 5], (2, 1)), ([1, 1, 3], (0, 2)), ([-4, 3, 100], (3, 3))):
