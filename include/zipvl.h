@@ -324,7 +324,7 @@ typedef struct zipvl_rope {
  * The queries and keys of a layer, rotated.  Q [B,Hq,n,d] by dims->q_strides, K [B,Hkv,n,d] by dims->k_strides; one of the two may be NULL
  * (and its output with it).  Qo, Ko are laid out by the q_strides and k_strides of `out` (its other fields are not looked at; NULL = as Q and K):
  * no element twice.  Qo may be Q and Ko may be K (with the same strides); outputs that overlap inputs in any other way are not.
- * pos [device] [axes, B, n] int32 contiguous, any values.  B * n < 2^30.
+ * pos [device] [axes, B, n] int32 contiguous, any values.  B * n < 2^30; one launch for every 2^28 tokens (2^29 for d = 64).
  * Numerics: angles are good to 2e-9 radians plus 1e-9 of a position beyond 2^24 (whole turns are dropped before anything is rounded), sines and
  * cosines to 1e-7, products and sums in fp32, one rounding at the end.
  */
@@ -355,7 +355,7 @@ typedef struct zipvl_pages {
  * as they are.
  * K, V, Q by dims' strides; start, len [device] int32 [B*Hkv]; flags: 0 or ZIPVL_T_PER_BATCH (idx [B,n], k [B]).  Two units whose new
  * rows fall into one page's same rows race.  B * n < 2^30.  Numerics of the rotation as for zipvl_rotate; V and unrotated K are bit copies.
- * One launch; two where len is start and n > 1.
+ * One launch for every 2^28 tokens (2^29 for d = 64); one more where len is start and n > 1.
  */
 int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, const int32_t* idx, const int32_t* k,
                        const int32_t* pos, const zipvl_rope* rope, const zipvl_pages* pages, const int32_t* table, int32_t table_pages,

@@ -20,6 +20,7 @@ template <typename R> __device__ __forceinline__ auto row_of(const R& r, int b, 
 // heads as that leaves, and goes through the heads from its first in steps of `step`.
 struct Walk {
     int n, total, tokens_log2, step;                         // total = B n
+    int base;                                                // the launch's first token
     uint32_t inv_n;
 };
 
@@ -29,7 +30,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RowsIn Q, RowsIn K, Rows Qo
 {
     constexpr int kThreads = D / 16;
     const int slot = threadIdx.x / kThreads, c = threadIdx.x % kThreads;
-    const int token = (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
+    const int token = w.base + (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
     const int first = blockIdx.y * ((256 / kThreads) >> w.tokens_log2) + (slot >> w.tokens_log2);
     if (token >= w.total || first >= heads) return;
     const int b = divided(token, w.n, w.inv_n), t = token - b * w.n;
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(RowsIn K, RowsIn V, R
 {
     constexpr int kThreads = D / 16;
     const int slot = threadIdx.x / kThreads, c = threadIdx.x % kThreads;
-    const int token = (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
+    const int token = w.base + (blockIdx.x << w.tokens_log2) + (slot & ((1 << w.tokens_log2) - 1));
     if (token >= w.total) return;
     const int b = divided(token, w.n, w.inv_n), i = token - b * w.n;         // row i of what a unit brings
     const Runs runs(c, TURN ? turns.pairs : 0, TURN ? turns.neighbours : 0);
@@ -183,6 +184,16 @@ static dim3 walk_of(const zipvl_dims& d, int heads, bool apart, Walk& w) {
     return dim3(tiles, std::min(parts, kHeadsGrid), (parts + kHeadsGrid - 1) / kHeadsGrid);
 }
 
+// An axis of a grid has fewer than 2^32 threads: what goes beyond 2^23 workgroups of tokens is another launch.
+constexpr int kTokenGrid = 1 << 23;
+template <typename F> static void over_tokens(Walk& w, dim3 grid, F&& launch) {
+    const int most = kTokenGrid << w.tokens_log2;
+    for (w.base = 0; w.base < w.total; w.base += most) {
+        grid.x = (std::min(w.total - w.base, most) + (1 << w.tokens_log2) - 1) >> w.tokens_log2;
+        launch(grid);
+    }
+}
+
 int launch_rotate(const void* Q, const void* K, const zipvl_dims& d, const int32_t* pos, const zipvl_rope& rope, int flags, void* Qo, void* Ko,
                   const zipvl_dims& out, hipStream_t st)
 {
@@ -192,12 +203,14 @@ int launch_rotate(const void* Q, const void* K, const zipvl_dims& d, const int32
     const dim3 grid = walk_of(d, heads, false, w);
     const Turns turns = turns_of(&rope, flags & ZIPVL_ROTATE_INVERSE);
     KernelTimer tm(ZIPVL_K_ROTATE, st);
+    over_tokens(w, grid, [&](dim3 grid) {
 #define ZIPVL_ROTATE(T, D)                                                                                                         \
     hipLaunchKernelGGL((rotate_kernel<T, D>), grid, dim3(256), 0, st, rows_in(Q, d.q_strides, e), rows_in(K, d.k_strides, e), \
                        rows_out(Qo, out.q_strides, e), rows_out(Ko, out.k_strides, e), Hq, heads, w, pos, turns)
     if (d.dtype == ZIPVL_BF16) { if (d.d == 128) ZIPVL_ROTATE(__bf16, 128); else ZIPVL_ROTATE(__bf16, 64); }
     else { if (d.d == 128) ZIPVL_ROTATE(float, 128); else ZIPVL_ROTATE(float, 64); }
 #undef ZIPVL_ROTATE
+    });
     return check_launch("rotate");
 }
 
@@ -216,6 +229,7 @@ int launch_paged_append(const void* K, const void* V, const zipvl_dims& d, const
     const int64_t qo[3] = {(int64_t)d.Hq * d.n * d.d, (int64_t)d.n * d.d, d.d};
     {
         KernelTimer tm(ZIPVL_K_PAGED_APPEND, st);
+        over_tokens(w, grid, [&](dim3 grid) {
 #define ZIPVL_APPEND(T, D, TURN)                                                                                                           \
     hipLaunchKernelGGL((paged_append_kernel<T, D, TURN>), grid, dim3(256), 0, st, rows_in(K, d.k_strides, e), rows_in(V, d.v_strides, e),  \
                        rows_in(Q, d.q_strides, e), rows_out(Qo, qo, e), d.Hkv, d.Hq / d.Hkv, inverse(d.Hq / d.Hkv), heads, w, p, pos, turns)
@@ -224,6 +238,7 @@ int launch_paged_append(const void* K, const void* V, const zipvl_dims& d, const
         else { if (d.d == 128) ZIPVL_APPEND_T(float, 128); else ZIPVL_APPEND_T(float, 64); }
 #undef ZIPVL_APPEND_T
 #undef ZIPVL_APPEND
+        });
     }
     const int rc = check_launch("paged_append");
     if (rc || !in_place) return rc;

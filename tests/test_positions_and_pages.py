@@ -317,6 +317,50 @@ def test_paged_append_of_more_heads_than_a_grid_has_rows():
     assert (length == n).all()
 
 
+def needs_memory(gib):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib * 2 ** 30:
+        pytest.skip(f"{gib} GiB of free GPU memory are needed")
+
+
+@pytest.mark.gpu
+def test_paged_append_of_more_tokens_than_one_grid_has_threads():
+    """33 x 2^24 tokens, of which every sequence brings the first few: those of the last are tokens beyond 2^29."""
+    needs_memory(16)
+    B, n, d, page, c = 33, 1 << 24, 128, 16, 5
+    K = torch.zeros((1, 1, n, d), dtype=torch.bfloat16, device=DEV)
+    K[0, 0, :c] = torch.randn((c, d), generator=torch.Generator().manual_seed(91)).to(DEV)
+    wide = K.expand(B, 1, n, d)
+    pos = torch.zeros((1, B, n), dtype=torch.int32, device=DEV)
+    pos[0, :, :c] = positions(1, B, c, 92)[0]
+    f = frequencies(64)
+    cache = pools(B, page, d, "bf16", 93)
+    table = torch.arange(B - 1, -1, -1, dtype=torch.int32, device=DEV).view(B, 1)
+    before = cache.K.clone()
+    length, _ = z.zipvl_paged_append(wide, wide, cache, table, torch.zeros((B,), dtype=torch.int32, device=DEV),
+                                     k=torch.full((B,), c, dtype=torch.int32, device=DEV), pos=pos, rope=z.Rope(f))
+    assert (length == c).all()
+    assert_rotated(cache.K.flip(0)[:, None, :c], K[:, :, :c].expand(B, 1, c, d), pos[:, :, :c], f, [0] * 64, z.ROPE_HALVES)
+    assert torch.equal(cache.V[:, :c], K[0, :, :c].expand(B, c, d)) and torch.equal(cache.K[:, c:], before[:, c:])
+
+
+@pytest.mark.gpu
+def test_rotate_more_tokens_than_one_grid_has_threads():
+    needs_memory(160)
+    B, n, d = 33, 1 << 24, 128
+    K = torch.zeros((B, 1, n, d), dtype=torch.bfloat16, device=DEV)
+    pos = torch.zeros((1, B, n), dtype=torch.int32, device=DEV)
+    spots = [(0, 0), (15, n - 5), (16, 0), (31, n - 5), (32, 0), (32, n // 2 + 3), (32, n - 5)]
+    rows = torch.randn((len(spots), 1, 5, d), generator=torch.Generator().manual_seed(94)).to(torch.bfloat16).to(DEV)
+    at = positions(1, len(spots), 5, 95)
+    for i, (b, t) in enumerate(spots):
+        K[b, 0, t:t + 5], pos[0, b, t:t + 5] = rows[i, 0], at[0, i]
+    f = frequencies(64)
+    z.zipvl_rotate(None, K, pos, z.Rope(f), Ko=K)
+    got = torch.stack([K[b, :, t:t + 5] for b, t in spots])
+    assert_rotated(got, rows, at, f, [0] * 64, z.ROPE_HALVES)
+
+
 # ---------------------------------------------------------------- attention over pages
 class Batch:
     """A batch in pages whose unused rows and unused pages hold NaN, and its plain result."""
