@@ -325,8 +325,8 @@ typedef struct zipvl_rope {
  * (and its output with it).  Qo, Ko are laid out by the q_strides and k_strides of `out` (its other fields are not looked at; NULL = as Q and K):
  * no element twice.  Qo may be Q and Ko may be K (with the same strides); outputs that overlap inputs in any other way are not.
  * pos [device] [axes, B, n] int32 contiguous, any values.  B * n < 2^30; one launch for every 2^28 tokens (2^29 for d = 64).
- * Numerics: angles are good to 2e-9 radians plus 1e-9 of a position beyond 2^24 (whole turns are dropped before anything is rounded), sines and
- * cosines to 1e-7, products and sums in fp32, one rounding at the end.
+ * Numerics: at any position, angles are good to 3.7e-9 radians when whole turns are dropped and what is left, up to an eighth of a turn, is rounded to
+ * fp32; sines and cosines to 2.1e-7, products and sums in fp32, one rounding at the end.
  */
 int zipvl_rotate(const void* Q, const void* K, const zipvl_dims* dims, const int32_t* pos, const zipvl_rope* rope, int flags,
                  void* Qo, void* Ko, const zipvl_dims* out, void* stream);

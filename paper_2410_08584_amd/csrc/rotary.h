@@ -14,9 +14,9 @@ struct Turns {
 
 // sin and cos of pos * freq.  Whole turns must go before anything is rounded: position 60000 of a frequency of 1 is 9549 turns,
 // and a product in fp32 leaves 2^-10 of a turn.  In whole numbers they go by themselves: the low 64 bits of pos * turn are the
-// fraction (a negative position included), off by 2^-32 of a turn at 2^31 and by the 32 bits that are kept: 1.5e-9 radians.  An eighth
-// of a turn to both sides of a quarter is left for the Taylor series (to x^9 / 9! and x^10 / 10!: 2e-9 at pi/4), so that sine and cosine
-// are good to about one rounding of fp32 (6e-8); v_sin_f32 is not.
+// fraction (a negative position included).  A turn is off by up to 3 2^-64, 2.2e-9 radians at 2^31, and the 32 bits that are kept cost 1.5e-9: 3.7e-9 radians at any
+// position.  An eighth of a turn to both sides of a quarter is left for the Taylor series (to x^9 / 9! and x^10 / 10!: 2e-9 at pi/4); rounding that and its
+// factor to fp32 is most of the error, and sine and cosine are within 3.5 2^-24; v_sin_f32 is not.
 __device__ __forceinline__ void turn_of(uint32_t pos, uint64_t turn, uint32_t backwards, float& sn, float& cs) {
     const uint32_t lo = (uint32_t)turn, hi = (uint32_t)(turn >> 32);
     uint32_t f = __umulhi(pos, lo) + pos * hi - ((int32_t)pos < 0 ? lo : 0u);        // in 2^-32 of a turn

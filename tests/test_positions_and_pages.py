@@ -162,6 +162,32 @@ def test_rotate_far_positions(low, high):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotate_at_the_ends_of_int32(inverse):
+    """The fraction of a turn is off by 3.7e-9 radians at most, at any position: turns a position truncated at 3 2^-64 (times 2^31: 2.2e-9) and 32 bits kept (1.5e-9)."""
+    from fractions import Fraction
+    say(f"rotate at the ends inverse={inverse}")
+    n, d, pairs = 40, 128, 64
+    K, _, _ = layer(1, 1, 1, n, d, "f32", "head", 8)
+    pos = positions(1, 1, n, 9, -2 ** 31, 2 ** 31)
+    pos[0, 0, :12] = torch.tensor([-2 ** 31, 2 ** 31 - 1, -2 ** 31 + 1, 2 ** 31 - 2, 2 ** 30, -2 ** 30, 2 ** 24 + 1, 0xFFFF, -1, 0, 1, 2 ** 30 - 1])
+    f = [2 * math.pi, -2 * math.pi, 6.28, -6.2, 5.0, 4.0, 3.9999, -2.0, 1e-300, -1e-12, 0.0] + frequencies(pairs)[11:]
+    _, Ko = z.zipvl_rotate(None, K, pos, z.Rope(f), z.ROTATE_INVERSE if inverse else 0)
+    two_pi = Fraction(314159265358979323846264338327950288419716939937510582097494459, 10 ** 62) * 2
+    angle = torch.empty((n, pairs), dtype=torch.float64)
+    for t in range(n):
+        for i in range(pairs):
+            turns = Fraction(f[i]) * int(pos[0, 0, t]) / two_pi
+            angle[t, i] = float((turns - math.floor(turns)) * two_pi) * (-1 if inverse else 1)
+    c, s = torch.cos(angle), torch.sin(angle)
+    x = K.cpu().double()[0, 0]
+    xa, xb = x[:, :pairs], x[:, pairs:]
+    ref, size = torch.cat([xa * c - xb * s, xa * s + xb * c], dim=-1), (xa.abs() + xb.abs()).repeat(1, 2)
+    err, tol = (Ko.cpu().double()[0, 0] - ref).abs(), (6 * U + 3.7e-9) * size + half_step(torch.float32) * ref.abs()
+    assert (err <= tol).all(), (err - tol).max().item()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layout", [z.ROPE_HALVES, z.ROPE_NEIGHBOURS])
 def test_the_inverse_rotation_is_the_gradient(layout):
     """d/dx of sum(w * rotate(x)) is the inverse rotation of w: against differences of the kernel itself (rotation is linear: any step will do), and
