@@ -303,6 +303,37 @@ def test_paged_append(case, in_place):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", [z.ROPE_HALVES, z.ROPE_NEIGHBOURS])
+@pytest.mark.parametrize("B,Hq,Hkv,n,d,dtype,pairs,k", [(3, 8, 2, 1, 128, "bf16", 64, None), (2, 6, 3, 37, 64, "f32", 24, [[37, 5, 0], [1, 36, 17]]), (4, 28, 4, 130, 128, "bf16", 16, None),
+                                                        (3, 4, 4, 65, 128, "f32", 64, "batch")])
+def test_paged_append_with_queries_in_place(layout, B, Hq, Hkv, n, d, dtype, pairs, k):
+    """Qo in the place of Q, pairs of both layouts: the rows that a head's unit brings are turned, the others stay."""
+    say(f"paged_append in place B={B} n={n} {dtype} layout={layout} k={k}")
+    page, units, axes = 32, B * Hkv, 2
+    Q, K, V = (x.contiguous() for x in layer(B, Hq, Hkv, n, d, dtype, "head", 14))
+    per_batch = k == "batch"
+    counts = [n] * units if k is None else [(7 + 29 * b) % (n + 1) for b in range(B) for _ in range(Hkv)] if per_batch else sum(k, [])
+    k_d = None if k is None else torch.tensor(counts[::Hkv] if per_batch else counts, dtype=torch.int32, device=DEV)
+    pos, f, a = positions(axes, B, n, 15), frequencies(pairs), axes_of(pairs, axes)
+    width = -(-(n + 20) // page)
+    cache, table = pools(units * width, page, d, dtype, 16), random_table(units, width, units * width, 17)
+    start = torch.tensor([u * 5 % 21 for u in range(units)], dtype=torch.int32, device=DEV)
+    want, at = Q.clone(), Q
+    length, got = z.zipvl_paged_append(K, V, cache, table, start, k=k_d, pos=pos, rope=z.Rope(f, a, layout), Q=at, Qo=at, length=torch.empty_like(start),
+                                       flags=z.T_PER_BATCH if per_batch else 0)
+    assert got is at and length.tolist() == [int(start[u]) + counts[u] for u in range(units)]
+    for u in range(units):
+        b, g, m = u // Hkv, u % Hkv, counts[u]
+        heads = slice(g * (Hq // Hkv), (g + 1) * (Hq // Hkv))
+        assert torch.equal(at[b, heads, m:], want[b, heads, m:])
+        if m:
+            assert_rotated(at[b:b + 1, heads, :m], want[b:b + 1, heads, :m], pos[:, b:b + 1, :m], f, a, layout)
+            rows = cache.K[table[u].long()].view(-1, d)[int(start[u]):int(start[u]) + m]
+            assert_rotated(rows[None, None], K[b:b + 1, g:g + 1, :m], pos[:, b:b + 1, :m], f, a, layout)
+            assert torch.equal(cache.V[table[u].long()].view(-1, d)[int(start[u]):int(start[u]) + m], V[b, g, :m])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [1, 70])
 def test_paged_append_where_pages_end_or_are_missing(n):
     """Rows behind the table, and rows whose page is none, are not written; lengths stop at the table's end; starts outside are clamped."""
