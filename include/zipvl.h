@@ -377,7 +377,7 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
  * Numerics: scores, weights, statistics and sums in fp32; one rounding at the end.  The order of
  * all sums follows from the lengths: the same call gives the same bits.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_DECODE_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that
- * overlap on one workspace race).
+ * overlap on one workspace race).  Tables of a few rows need some 100 KB, large ones up to 140 MB (a part of its own for every workgroup).
  */
 int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len,
                             const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len,

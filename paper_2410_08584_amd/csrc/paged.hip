@@ -952,23 +952,29 @@ static PagedLayout paged_layout(const zipvl_dims& d, bool prefixes, int grid) {
     return l;
 }
 
-static int grid_of(const zipvl_dims& d) {
-    if (d.dtype == ZIPVL_BF16) return d.d == 128 ? PartCfg<__bf16, 128>::GRID : PartCfg<__bf16, 64>::GRID;
-    return d.d == 128 ? PartCfg<float, 128>::GRID : PartCfg<float, 64>::GRID;
+// What all lengths at their greatest would weigh, and more.
+static int64_t most_weight(const zipvl_dims& d, int64_t own, int64_t prefix, int groups) {
+    auto tiles = [](int64_t rows) { return (rows + kTileRows - 1) / kTileRows; };
+    const int64_t pre = groups ? ((int64_t)d.B * (d.Hq / d.Hkv) / kBlock + groups) * d.Hkv * (8 * tiles(prefix) + kStartPrefix) : 0;
+    return (int64_t)d.B * d.Hkv * (2 * tiles(own) + kStartWave) + pre;
 }
-size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) { return paged_layout(d, prefix > 0, grid_of(d)).total; }
+// No more workgroups than can have a piece (find_piece).
+static int grid_of(int most, int64_t weight) { return (int)std::max<int64_t>(1, std::min<int64_t>(most, weight / (kLeast / 2))); }
+
+size_t decode_paged_workspace_bytes(const zipvl_dims& d, int own, int prefix) {
+    const int most = d.dtype == ZIPVL_BF16 ? (d.d == 128 ? PartCfg<__bf16, 128>::GRID : PartCfg<__bf16, 64>::GRID) : d.d == 128 ? PartCfg<float, 128>::GRID : PartCfg<float, 64>::GRID;
+    return paged_layout(d, prefix > 0, grid_of(most, most_weight(d, own, prefix, prefix > 0 ? d.B : 0))).total;
+}
 
 template <typename T, int D, int OWN>
 static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, float scale, T* o, char* ws, hipStream_t st) {
     using C = PartCfg<T, D>;
-    const PagedLayout l = paged_layout(d, p.groups > 0, C::GRID);
-    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, l.wave_cols, C::GRID};
-    // what all lengths at their greatest would weigh, and more: positions on the line are below 2^31, and no more workgroups than that
-    const int64_t own = (int64_t)d.B * d.Hkv * (2 * ((((int64_t)p.width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartWave);
-    const int64_t pre = p.groups ? ((int64_t)d.B * p.G / kBlock + p.groups) * d.Hkv * (8 * ((((int64_t)p.prefix_width << p.page_log2) + kTileRows - 1) / kTileRows) + kStartPrefix) : 0;
-    if (own + pre >= (int64_t)1 << 31)
+    const int64_t weight = most_weight(d, (int64_t)p.width << p.page_log2, (int64_t)p.prefix_width << p.page_log2, p.groups);
+    if (weight >= (int64_t)1 << 31)                          // positions on the line are below that
         return set_error(ZIPVL_ESHAPE, "zipvl_decode_attn_paged: tables of %d units and %d prefixes of %d and %d pages hold too many rows (2^35)", d.B * d.Hkv, p.groups * d.Hkv, p.width, p.prefix_width);
-    const int wgs = (int)std::min<int64_t>(C::GRID, own + pre);
+    const int wgs = grid_of(C::GRID, weight);
+    const PagedLayout l = paged_layout(d, p.groups > 0, wgs);
+    const Parts parts = {(float*)(ws + l.o), (float*)(ws + l.ml), (int2*)(ws + l.pieces), d.B * d.Hq, l.cols, l.wave_cols, wgs};
     static std::atomic<uint64_t> lds_set{0};                 // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return set_error(ZIPVL_EHIP, "decode_attn_paged: no current device");

@@ -547,6 +547,23 @@ def test_decode_attn_paged_of_many_items(case):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", DECODE + [(6, 14, 2, 128, "f32", 64, [5000, 40, 0, 1, 2049], (2, 4), [7000, 3001, 1]), (6, 32, 1, 64, "bf16", 16, [9000, 40, 300], (6,), [3000])],
+                         ids=lambda c: f"B{c[0]}Hq{c[1]}Hkv{c[2]}d{c[3]}{c[4]}page{c[5]}P{len(c[7])}")
+def test_decode_attn_paged_stays_in_its_workspace(case):
+    """A workspace of exactly the bytes that the tables need: what follows it is left alone, and the output is the same as with one of wider tables."""
+    say(f"decode_attn_paged workspace {case}")
+    batch = Batch(*case, seed=34)
+    dm = z.dims_of(None, None, None, B=batch.B, Hq=batch.Hq, Hkv=batch.Hkv, n=batch.table.shape[1] * case[5], d=batch.d, dtype=1 if case[4] == "bf16" else 0)
+    need = z.workspace_bytes(z.OP_DECODE_PAGED, dm, batch.prefix_table.shape[1] * case[5] if batch.P else 0)
+    room = torch.full((need + (1 << 20),), 0xA5, dtype=torch.uint8, device=DEV)
+    o = batch.run(ws=room[:need])
+    batch.check(o)
+    assert bool((room[need:] == 0xA5).all())
+    with pytest.raises(z.ZipvlError, match="workspace"):
+        batch.run(ws=room[:need - 1])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("lens", [[1, 0, 16, 17], [0], [0, 0, 0, 0, 0, 0, 5]])
 def test_decode_attn_paged_of_thousands_of_units(lens):
     """More units than are looked at in LDS, most of them short or empty, one long."""
@@ -1148,3 +1165,13 @@ def test_a_workspace_with_gaps_is_refused():
     for ws in (torch.zeros((1 << 27,), dtype=torch.uint8)[::2], torch.zeros((1,), dtype=torch.uint8).expand(1 << 27)):
         with pytest.raises(z.ZipvlError, match="contiguous"):
             z.zipvl_decode_attn_paged(x(8, 64), cache, i, i[:, 0].contiguous(), 0.1, B=2, Hq=4, Hkv=2, o=x(8, 64), ws=ws)
+
+
+def test_workspaces_of_decode_over_pages_go_by_the_tables(lib):
+    size = lambda rows, prefix, **kw: z.workspace_bytes(z.OP_DECODE_PAGED, dims(n=rows, **kw), prefix)
+    for kw in (dict(B=1, Hq=1, Hkv=1, d=128, dtype=1), dict(B=1, Hq=1, Hkv=1, d=64, dtype=0)):
+        assert 0 < size(16, 0, **kw) <= size(16, 16, **kw) < 1 << 20
+    for kw in (dict(), dict(B=64, Hq=32, Hkv=8, d=128), dict(B=40, Hq=32, Hkv=1, d=64, dtype=0)):
+        sizes = [size(rows, prefix, **kw) for rows in (16, 100, 3000, 1 << 24) for prefix in (0, 16, 5000, 1 << 24)]
+        assert all(sizes[4 * r + p] <= sizes[4 * r + p + 1] for r in range(4) for p in range(3)) and all(a <= b for a, b in zip(sizes, sizes[4:]))
+        assert sizes[-1] < 140 << 20
