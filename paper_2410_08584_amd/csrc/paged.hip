@@ -857,45 +857,51 @@ __device__ __forceinline__ Span span_of(const Parts& in, int2 v, int row, int ow
     return s;
 }
 
-// The parts of one query head: those of its group's prefix, then its own -> its output row.  A chain of loads, each for the address of the next:
-// groups, pieces (with the lengths), parts (maxima, sums and the first parts' outputs at once).  WAVES waves have a row: all four where a row
-// may have many parts; one where rows are many, each has a few parts and dispatching
-// a workgroup for it is what lasts (from 1536 rows on: up to 4 % of a call, 32.0 us instead of 33.4 for 49 sequences of 40 heads; always: 1.9 % longer, 22.8 us
-// instead of 19.5 for 8 questions about a video).
-template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts in, T* __restrict__ o) {
-    constexpr int kPer = D / 4, kAt = 64 * WAVES / kPer, kAtOnce = WAVES == 1 ? 4 : 64 / kAt;        // threads per part, parts at a time, loads on the way
-    __shared__ floatx4 sum[256];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = WAVES == 1 ? lane : threadIdx.x;  // among the row's threads
-    const int row = scalar(WAVES == 1 ? (int)blockIdx.x * 4 + w : (int)blockIdx.x);
-    if (row >= in.rows) return;                              // of one wave a row: nobody waits
-    const int b = divided(row, p.Hq, p.inv_Hq), head = row - b * p.Hq, g = divided(head, p.G, p.inv_G), u = b * p.Hkv + g;
-    const int2 own_pieces = in.pieces[piece_own(p, u)];
-    const int own_len = own_rows(p, u);
-    int2 pre = {0, -1}, own = {0, -1};
-    int col = 0;
-    for (int x = 0; x < p.groups; x += 64) {
-        const Group m = x + lane < p.groups ? group_of(p, x + lane) : Group{0, 0};
-        const uint64_t in_it = __ballot(m.begin <= b && b < m.end);
-        if (in_it) {
-            const int who = __builtin_ctzll(in_it), group = x + who, begin = __builtin_amdgcn_readlane(m.begin, who);
-            col = (b - begin) * p.G + head - g * p.G;
-            const int2 pieces = in.pieces[piece_prefix(p, group, begin, col / kBlock, g)];
-            if (prefix_rows(p, group * p.Hkv + g) > 0) pre = pieces;
-            col %= kBlock;
-            break;
+// The parts of one query head: those of its group's prefix, then its own.  Found by a chain of loads, each for the address of the next: groups, pieces (with the lengths).
+struct RowParts {
+    Span pre, own;
+    __device__ __forceinline__ RowParts(const PagedRead& p, const Parts& in, int row) {
+        const int lane = threadIdx.x & 63;
+        const int b = divided(row, p.Hq, p.inv_Hq), head = row - b * p.Hq, g = divided(head, p.G, p.inv_G), u = b * p.Hkv + g;
+        const int2 own_pieces = in.pieces[piece_own(p, u)];
+        const int own_len = own_rows(p, u);
+        int2 of_pre = {0, -1}, of_own = {0, -1};
+        int col = 0;
+        for (int x = 0; x < p.groups; x += 64) {
+            const Group m = x + lane < p.groups ? group_of(p, x + lane) : Group{0, 0};
+            const uint64_t in_it = __ballot(m.begin <= b && b < m.end);
+            if (in_it) {
+                const int who = __builtin_ctzll(in_it), group = x + who, begin = __builtin_amdgcn_readlane(m.begin, who);
+                col = (b - begin) * p.G + head - g * p.G;
+                const int2 pieces = in.pieces[piece_prefix(p, group, begin, col / kBlock, g)];
+                if (prefix_rows(p, group * p.Hkv + g) > 0) of_pre = pieces;
+                col %= kBlock;
+                break;
+            }
         }
+        if (own_len > 0) of_own = own_pieces;
+        pre = span_of(in, of_pre, row, 0, col);
+        own = span_of(in, of_own, row, 1, head - g * p.G);
     }
-    if (own_len > 0) own = own_pieces;
-    const Span a_pre = span_of(in, pre, row, 0, col), a_own = span_of(in, own, row, 1, head - g * p.G);
-    const int n_pre = a_pre.count(), n = n_pre + a_own.count();
-    auto record = [&](int s) { return s < n_pre ? a_pre.record(s) : a_own.record(s - n_pre); };
+    __device__ __forceinline__ int count() const { return pre.count() + own.count(); }
+    __device__ __forceinline__ int record(int i) const {
+        const int n = pre.count();
+        return i < n ? pre.record(i) : own.record(i - n);
+    }
+};
+
+// They are joined by a wave, or by all four of a workgroup (then with a barrier) -> the output row.
+template <typename T, int D, int WAVES>
+__device__ __forceinline__ void join_row(const RowParts& parts, const Parts& in, int row, floatx4 (&sum)[256], T* __restrict__ o) {
+    constexpr int kPer = D / 4, kAt = 64 * WAVES / kPer, kAtOnce = WAVES == 1 ? 4 : 64 / kAt;        // threads per part, parts at a time, loads on the way
+    const int lane = threadIdx.x & 63, tid = WAVES == 1 ? lane : threadIdx.x;                        // among the row's threads
+    const int n = parts.count();
     float M = -INFINITY, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < n; s0 += 64) {                     // 64 parts at a time, every wave all of their maxima and sums
         const int count = min(64, n - s0);
         float2 v = make_float2(-INFINITY, 0.f);
-        const int rec = record(s0 + min(lane, count - 1));
+        const int rec = parts.record(s0 + min(lane, count - 1));
         if (lane < count) v = *reinterpret_cast<const float2*>(in.ml + 2 * (int64_t)rec);
         floatx4 part[kAtOnce];
         auto ask = [&](int y0) {
@@ -934,6 +940,38 @@ __global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts i
         acc *= L > 0.f ? 1.f / L : 0.f;
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uintx2*>(o + (int64_t)row * D + tid * 4) = uintx2{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
         else *reinterpret_cast<floatx4*>(o + (int64_t)row * D + tid * 4) = acc;
+    }
+}
+
+// Four waves a row, or, where rows are many, one: most rows have a few parts then and dispatching a workgroup for each is what lasts (from kManyRows on; 2000 sequences
+// of 40 rows, 8 heads on 1 35.4 us with four, 22.9 with one; 64 questions about 160 rows, 32 heads on 8 18.2, 16.1; always one: 3 % longer over 45 calls, 8 questions about a
+// video 23.6 instead of 20.4).  Rows of more parts than a wave sees at once are joined by the whole workgroup then as well, and the rows of a workgroup are far
+// apart, since the heads of one long item follow each other (one sequence of 60000 rows among 63 of 200, 32 heads on 1: 41.3 us by one wave, 28.7 so, 28.6 with four for
+// all rows; from 32 parts on: two prefixes of 9000 rows, 64 channels 32.6 us instead of 28.0).
+constexpr int kFew = 64, kManyRows = 1536;
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(256, 4) void paged_join_kernel(PagedRead p, Parts in, T* __restrict__ o) {
+    __shared__ floatx4 sum[256];
+    if constexpr (WAVES == 4) {
+        const int row = blockIdx.x;
+        join_row<T, D, 4>(RowParts(p, in, row), in, row, sum, o);
+    } else {
+        __shared__ int many[4];
+        const int w = scalar(threadIdx.x >> 6), row = w * (int)gridDim.x + (int)blockIdx.x;
+        bool mine = false;
+        if (row < in.rows) {
+            const RowParts parts(p, in, row);
+            mine = parts.count() > kFew;
+            if (!mine) join_row<T, D, 1>(parts, in, row, sum, o);
+        }
+        if ((threadIdx.x & 63) == 0) many[w] = mine;
+        __syncthreads();
+        for (int x = 0; x < 4; ++x)
+            if (many[x]) {
+                const int row = x * (int)gridDim.x + (int)blockIdx.x;
+                join_row<T, D, 4>(RowParts(p, in, row), in, row, sum, o);
+                __syncthreads();
+            }
     }
 }
 
@@ -990,7 +1028,7 @@ static int launch_paged_t(const T* q, const PagedRead& p, const zipvl_dims& d, f
         if (rc) return rc;
     }
     KernelTimer tm(ZIPVL_K_PAGED_COMBINE, st);
-    if (parts.rows >= 1536 && (p.groups ? p.groups : d.B) * d.Hkv >= 32) hipLaunchKernelGGL((paged_join_kernel<T, D, 1>), dim3((parts.rows + 3) / 4), dim3(256), 0, st, p, parts, o);
+    if (parts.rows >= kManyRows) hipLaunchKernelGGL((paged_join_kernel<T, D, 1>), dim3((parts.rows + 3) / 4), dim3(256), 0, st, p, parts, o);
     else hipLaunchKernelGGL((paged_join_kernel<T, D, 4>), dim3(parts.rows), dim3(256), 0, st, p, parts, o);
     return check_launch("decode_attn_paged parts");
 }

@@ -594,6 +594,20 @@ def test_decode_attn_paged_of_long_items(case):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", [  # B, Hq, Hkv, d, dtype, page, lens, groups, prefix: many rows, one or two of whose items have most of the parts
+    (64, 32, 1, 128, "bf16", 64, [3, 40, 0, 70] * 8 + [40000] + [5] * 31, (), ()),
+    (53, 31, 1, 64, "bf16", 32, [2] * 50 + [30000, 0, 9000], (), ()),
+    (70, 24, 2, 128, "f32", 16, [1, 7] * 69 + [9000, 12000], (40, 2, 28), [17, 5000, 0, 300, 40, 8]),
+], ids=lambda c: f"B{c[0]}Hq{c[1]}Hkv{c[2]}d{c[3]}{c[4]}P{len(c[7])}")
+def test_decode_attn_paged_of_many_rows_one_of_them_long(case):
+    say(f"decode_attn_paged many rows {case[:6]}")
+    batch = Batch(*case, seed=35)
+    o = batch.run()
+    batch.check(o, which=sorted({0, 1, 2, 31, 32, 33, 40, 41, 42, batch.B - 3, batch.B - 2, batch.B - 1}))
+    assert torch.equal(o, batch.run())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("gain,spike", [(20.0, 0.0), (1.0, 40.0), (1e-3, 0.0)])
 def test_decode_attn_paged_where_one_row_has_all_the_weight(dtype, d, gain, spike):
