@@ -1,6 +1,7 @@
 // Rotary positions of a layer's queries and keys, and the rows that go into a paged cache with the rotation on the way.
-// Both read every row once and write it once: memory, or latency for a few tokens.  Measured: queries and keys of 18432 tokens, bf16, 302 MB, 61 us =
-// 4.9 TB/s; 8192 tokens of a stack into its pages, 1074 MB, 211 us = 5.1 TB/s (a large copy: 4.9 TB/s); one token for each of 8 sequences 3.3 us, a launch.
+// Both read every row once and write it once: memory, or latency for a few tokens.  Measured, in a graph: queries and keys of 18432 tokens, bf16, 302 MB, 62.5 us =
+// 4.8 TB/s (a copy of as many bytes 59.4); 8192 tokens of a stack into its pages, 1074 MB, 211 us = 5.1 TB/s (206); one token for each of 8 sequences 3.2 us, a
+// launch, and 6.7 us a call from Python.
 //
 // D / 16 threads have a row, two runs of eight channels each, so that a pair of channels meets in one thread and a rotated row
 // needs nothing from other lanes.  A thread stays with a token while it goes through heads: angles depend on the token alone.
@@ -73,7 +74,7 @@ __device__ __forceinline__ int paged_len(const PagedRows& p, int start, int coun
 
 // Heads [0, Hkv) are those of K and V, [Hkv, heads) of Q (as many as are given).  A row's way is two round trips to memory: where a unit starts, how
 // much it brings, which token this is and its positions, all at once; then the row, and the page that it goes to, while the angles are taken.
-// Every head has threads of its own: going through heads as rotate_kernel does saves angles and costs 5 to 10 % (64 tokens of 64 sequences: 4.1 us
+// Every head has threads of its own: going through heads as rotate_kernel does saves angles and costs 5 to 10 % (in a graph, 64 tokens of 64 sequences: 4.1 us
 // instead of 3.8, 777 tokens of 5 sequences, fp32 10.5 instead of 10.0, 8192 tokens of a stack 221 instead of 211; only where 0.4 of 18432 tokens
 // are kept it is 8.6 instead of 9.0, since threads of tokens that go are there for nothing).
 template <typename T, int D, bool TURN>
@@ -164,8 +165,8 @@ static RowsIn rows_in(const void* p, const int64_t (&s)[3], int e) { return {(co
 static Rows rows_out(void* p, const int64_t (&s)[3], int e) { return {(char*)p, s[0] * e, s[1] * e, s[2] * e}; }
 
 // `apart`: every head has threads of its own; else about kRotateGrid workgroups, each with several heads of its tokens, whose angles it takes once
-// (18432 tokens: 63.1 us; with 2048 64.4, with 16384 70.1).
-constexpr int kRotateGrid = 4096;
+// (18432 tokens: 62.5 us; with 2048 65.4, with 4096 63.1, with 16384 63.9).
+constexpr int kRotateGrid = 8192;
 static dim3 walk_of(const zipvl_dims& d, int heads, bool apart, Walk& w) {
     const int rows = 4096 / d.d;                             // of a workgroup, a turn
     w.n = d.n;
