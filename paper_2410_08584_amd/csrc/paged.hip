@@ -12,9 +12,11 @@
 // workgroup goes over the B Hkv + groups Hkv lengths by itself, a microsecond.
 // Parts (max, sum, weighted sum of rows) of an item that was cut are joined by a second launch.
 //
-// Measured, bf16, d = 128 (a call, both launches): 64 questions about two videos of 18432 tokens, 437 MB, 103 us = 4.2 TB/s; 16 sequences
-// with nothing shared, 353 MB, 72 us = 4.9 TB/s (reading that much and nothing else: 62 us).  Two questions about one image, fp32: 11.9 us, which is two launches,
+// Measured, in a graph, both launches, bf16, d = 128: 64 questions about four videos of up to 18432 tokens, 437 MB, 107 us = 4.1 TB/s (reading that much and
+// nothing else: 71); 16 sequences with nothing shared, 353 MB, 75 us = 4.7 TB/s (58).  Two questions about one image, fp32: 11.7 us, which is two launches,
 // finding the pieces and one tile after the other, not bytes.
+// The constants below were measured over 29 calls, each in a graph: the listed cases of decode in perf/operators.py and the first 24 that its
+// draw(random.Random(7)) gives of them.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -25,17 +27,17 @@
 namespace zipvl {
 
 constexpr int kTileRows = 32, kCols = 32, kPartWaves = 4, kBlock = kCols * kPartWaves;
-// What starting an item weighs: its queries, its first rows, its part.  Of items that waves cut, bf16: 3; with 6, 95 calls took 0.7 % longer, with 1, 4 %.  fp32
-// tiles last longer and a start is 2 of them (two questions about an image: 11.6 us, with 3 12.8).  Of blocks: 6 or 24 change less than 0.3 %.
+// What starting an item weighs: its queries, its first rows, its part.  Of items that waves cut, bf16: 3; with 6 the 29 calls take 2.0 % longer, with 1 4.3 %.  fp32
+// tiles last longer and a start is 2 of them (two questions about an image: 11.7 us, with 3 12.8).  Of blocks: 12; with 6 2.2 % longer, with 24 0.4 %.
 constexpr int kStartPrefix = 12, kStartWave = 3;
-// Queries up to which waves cut a prefix, as they cut own rows.  Blocks of workgroups for all prefixes: 6 % longer over 95 calls, and twice as long
-// where many prefixes are short (three of 162 rows with 40 KV heads: 24.9 us instead of 11.7).  More than 16 columns would need the wider tile.
+// Queries up to which waves cut a prefix, as they cut own rows.  Blocks of workgroups for all prefixes: the 29 calls take 12 % longer, and those where many prefixes
+// are short twice as long (four of 246 rows with 32 KV heads: 29.9 us instead of 13.3).  More than 16 columns would need the wider tile.
 constexpr int kLight = 16;
 // Weight below which a workgroup is not worth its part; a tile of a block may weigh as much and no piece may be shorter.  fp32 without blocks: half of it, a tile
-// for each wave, since such a tile is 2 us (with 8: 1.7 % longer over 95 calls, 13.0 us instead of 11.6 for two questions about an image); bf16 with 5, 6 or 7: as long.
+// for each wave, since such a tile is 2 us (with 8: 1.1 % longer over the 29 calls, 13.0 us instead of 11.7 for two questions about an image); bf16 with 6: as long.
 constexpr int kLeast = 8;
 constexpr int kCus = 256;
-constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves (0: 0.5 % longer)
+constexpr float kLazy = 8.f;         // how far (log2) a logit may exceed the offset of the exponentials before that moves (0: 0.5 % longer over the 29 calls)
 
 // a wave-uniform number in scalar registers
 __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -67,8 +69,8 @@ struct Parts {
 // On the numbers of pieces: of waves; of a long item; of the first wave, for its whole workgroup.
 constexpr int kByWave = 1 << 30, kLong = 1 << 29, kEntire = 1 << 28, kNumber = kEntire - 1;
 // A workgroup all of whose piece is of one item joins its four waves' parts if the item is long: more than 16 workgroups' pieces (parts are fewer for the second launch:
-// 13.5 us instead of 15.4 for 3 sequences of 17614 rows), or any item where pieces are 32 tiles and more (its waves then read side by side: 16 unshared
-// sequences 75.0 us instead of 77.5).  For short pieces meeting in LDS costs more than it saves (8 sequences of 811 rows: 16.1 us, 15.2 without).
+// one sequence of 60000 rows among 63 of 200, 32 heads on 1, 28.7 us instead of 41.0; from 4 on: 2.1 % longer over the 29 calls), or any item where pieces are 32 tiles
+// and more (its waves then read side by side: 16 unshared sequences 75.9 us instead of 77.9).  For short pieces meeting in LDS costs more than it saves (all items: 3.9 %).
 constexpr int kLongWorkgroups = 16, kLongPiece = 32;
 // Blocks of a prefix are counted from begin G / kBlock + p: no two groups meet, and B G / kBlock + groups + 1 are enough.
 __device__ __forceinline__ int piece_own(const PagedRead& p, int u) { return u; }
@@ -158,7 +160,8 @@ struct PartCfg {
     static constexpr int CH = D / Elem<T>::kPerChunk, ODB = D / 32;
     static_assert(WAVE >= D * kCols * 4, "room for a wave's sums");
     static constexpr int LDS = kPartWaves * WAVE;
-    // workgroups: of bf16 rows of 64 channels two as well, three are up to 10 % slower; one for all: 1.3 % longer over 95 calls, 64 questions 119 us instead of 106
+    // workgroups: of bf16 rows of 64 channels two as well, three take 0.5 % longer over the 29 calls (61 questions about 19382 rows: 63.8 us instead of 60.5); one
+    // for all: 3.6 % longer, 64 questions about videos 125 us instead of 107
     static constexpr int PER_CU = LDS > 80 * 1024 ? 1 : 2;
     static constexpr int GRID = kCus * PER_CU;
     // swizzle of row r's 16-byte chunks: K is read 32 rows at a time at one chunk, V of bf16 by transposing reads
@@ -170,8 +173,8 @@ struct PartCfg {
 };
 
 // A wave's queries, in 32 columns or in 16, against tiles of one item.  With 16 a tile is two of 16x16: half the matrix cycles and half the
-// exponentials, which is what a few tiles on their own last (fp32 products: 2 us a tile of d = 128, 4 with 32 columns; 32 columns for all: 9 % longer over 65
-// calls, two questions about an image 14.4 us instead of 12.6).
+// exponentials, which is what a few tiles on their own last (fp32 products: 2 us a tile of d = 128, 4 with 32 columns; 32 columns for all: 7 % longer over the 29
+// calls, two questions about an image 13.3 us instead of 11.7).
 // Lane l has column l % COLS; the 64 / COLS groups of lanes share its keys and channels.
 template <typename T, int D, int COLS>
 struct WavePart {
@@ -253,8 +256,8 @@ struct WavePart {
         }
     }
 
-    // fp32 sums go in short chains that are added pairwise: with one through all channels the output is off by 3.6e-7 to 1.9e-6 of itself over nine
-    // calls, with these by 2.9e-7 to 6.1e-7, for 1 to 4 % of the time.
+    // fp32 sums go in short chains that are added pairwise: with one through all channels the output is off by 6.2e-7 to 1.2e-6 of itself over the eight calls
+    // of the 29 that are fp32, with these by 2.9e-7 to 5.1e-7, for up to 3 % of the time.
     __device__ __forceinline__ void scores(const char* kb, float (&s)[kKeys]) const {
         const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
         if constexpr (COLS == 32) {
@@ -325,8 +328,9 @@ struct WavePart {
     }
 
     // O^T += V^T P^T.  A lane's weights are the operand of P^T as they are: contraction slot t of a lane = its key t.
-    // bf16: the weights as three planes, whose sum they are exactly (PLANES), or one value after the other in fp32 products.  With two planes, 16 bits, a sum that nearly cancels was off by 64 times what fp32 rounds, and 1.9e-3
-    // of the outputs of 16 unshared sequences were not the nearest bf16 numbers (4e-4 with three; 1e-3 of fp32 sums by library calls); 1.3 % less time over 29 calls.
+    // bf16: the weights as three planes, whose sum they are exactly (PLANES), or one value after the other in fp32 products.  With two planes, 16 bits, a sum that
+    // nearly cancels was off by 64 times what fp32 rounds, and 1.9e-3 of the outputs of 16 unshared sequences were not the nearest bf16 numbers (4e-4 with three;
+    // 1e-3 of fp32 sums by library calls); 1.3 % less time over the 29 calls.
     template <bool PLANES>
     __device__ __forceinline__ void weighted_rows(const char* vb, const float (&s)[kKeys]) {
         const int lane = threadIdx.x & 63, i = lane & (COLS - 1);
@@ -507,7 +511,7 @@ struct WavePart {
     }
 
     // The part of the lane's column.  An infinity in V is no number times a plane of 0, or where it stands for a row that is not there: a wave whose sums are not
-    // finite takes its tiles again, without either.  Looking at the sums of each piece: 0.8 % of the time over 29 calls.
+    // finite takes its tiles again, without either.  Looking at the sums of each piece: 0.8 % of the time over the 29 calls.
     __device__ __forceinline__ void run(const PagedRead& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine) {
         tiles<false>(p, table, rows, first, step, end, c, mine);
         float probe[4] = {};                                 // no number if a sum is not finite
@@ -533,7 +537,7 @@ __device__ __forceinline__ int quotient(int a, int b) {
 // The line of work: the weights of all items follow each other and the workgroups take equal pieces, so that however unequal the lengths, no
 // workgroup has more than another; a long item gets many workgroups and several short ones share one.  First come the blocks of
 // prefixes, which the waves of a workgroup share; then what waves cut, light prefixes and own rows: a workgroup's piece of those is cut again into equal ones for
-// each wave, which then wait for nobody.  (Whole workgroups for every item where items are few: 1.8 % longer over 95 calls.)
+// each wave, which then wait for nobody.
 struct Line {
     int item;                                                // of the workgroup's first position
     int start;                                               // of that item on the line, which is shorter than 2^31
@@ -944,8 +948,8 @@ __device__ __forceinline__ void join_row(const RowParts& parts, const Parts& in,
 }
 
 // Four waves a row, or, where rows are many, one: most rows have a few parts then and dispatching a workgroup for each is what lasts (from kManyRows on; 2000 sequences
-// of 40 rows, 8 heads on 1 35.4 us with four, 22.9 with one; 64 questions about 160 rows, 32 heads on 8 18.2, 16.1; always one: 3 % longer over 45 calls, 8 questions about a
-// video 23.6 instead of 20.4).  Rows of more parts than a wave sees at once are joined by the whole workgroup then as well, and the rows of a workgroup are far
+// of 40 rows, 8 heads on 1 35.4 us with four, 22.9 with one; 64 questions about 160 rows, 32 heads on 8 18.2, 16.1; always one: 8 questions about a video
+// 23.6 instead of 20.4).  Rows of more parts than a wave sees at once are joined by the whole workgroup then as well, and the rows of a workgroup are far
 // apart, since the heads of one long item follow each other (one sequence of 60000 rows among 63 of 200, 32 heads on 1: 41.3 us by one wave, 28.7 so, 28.6 with four for
 // all rows; from 32 parts on: two prefixes of 9000 rows, 64 channels 32.6 us instead of 28.0).
 constexpr int kFew = 64, kManyRows = 1536;
