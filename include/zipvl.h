@@ -362,7 +362,8 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
                        const int32_t* start, int32_t* len, const void* Q, void* Qo, int flags, void* stream);
 
 /*
- * Decode attention (Eq. (5) / Algorithm 2) over pages, for a batch whose elements share long prefixes (questions about one image or video):
+ * Decode attention (Eq. (5) / Algorithm 2) over pages, for a batch whose elements share long prefixes (questions about one image or video),
+ * one new token each (a piece of several tokens, as zipvl_paged_append takes it, has no attention over pages):
  *   o[b,h] = softmax( q[b,h] . [Kp ; Ko]^T * softmax_scale ) [Vp ; Vo]
  * with Ko, Vo the first len[u] rows of the unit u = b*Hkv + g by table [B*Hkv, table_pages], and Kp, Vp the first prefix_len[p*Hkv + g] rows
  * by prefix_table [groups*Hkv, prefix_pages] of the group p that b is in.  Group p is the batch elements group_begin[p] .. group_begin[p+1] - 1
