@@ -367,16 +367,16 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
  *   o[b,h] = softmax( q[b,h] . [Kp ; Ko]^T * softmax_scale ) [Vp ; Vo]
  * with Ko, Vo the first len[u] rows of the unit u = b*Hkv + g by table [B*Hkv, table_pages], and Kp, Vp the first prefix_len[p*Hkv + g] rows
  * by prefix_table [groups*Hkv, prefix_pages] of the group p that b is in.  Group p is the batch elements group_begin[p] .. group_begin[p+1] - 1
- * (group_begin [device] int32 [groups + 1], ascending; clamped to [0, B]; where it falls, o is of no meaning); elements in no group have no prefix.  The rows of a prefix are
- * read once for all queries of a group (once for every 128 of them, where there are more).
+ * (group_begin [device] int32 [groups + 1], ascending; clamped to [0, B]; where it falls, o is of no meaning); elements in no group have no prefix.
+ * The rows of a prefix are read once for all queries of a group (once for every 128 of them, where there are more).
  * groups = 0: nothing is shared (prefix_table, prefix_len, group_begin are not looked at).  groups <= B.
  * Lengths are clamped to [0, pages of the table * page]; a head without any row gets zeros.  Nothing behind a length is read.
  * q, o [device] [B*Hq, d] contiguous; G = Hq/Hkv <= 32.  An infinity in a row of V makes its channel infinite, a key of logit -infinity weighs
  * nothing, as in fp32 products; queries and other logits must be finite.
  * Tables are refused (ZIPVL_ESHAPE) that hold more than 2^24 rows a unit, or in all some 2^35 rows (those of prefixes counted four times for every 128
  * queries begun).
- * Numerics: scores, weights, statistics and sums in fp32; one rounding at the end.  The order of
- * all sums follows from the lengths: the same call gives the same bits.
+ * Numerics: scores, weights, statistics and sums in fp32; one rounding at the end.  The order of all sums follows from the lengths: the same call
+ * gives the same bits.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_DECODE_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that
  * overlap on one workspace race).  Tables of a few rows need some 100 KB, large ones up to 140 MB (a part of its own for every workgroup).
  */
