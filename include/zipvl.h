@@ -57,6 +57,8 @@ extern "C" {
 #define ZIPVL_OP_SCORE_ALL_ROWS 7
 #define ZIPVL_OP_DECODE_STEP    8  /* dims->n = cap */
 #define ZIPVL_OP_DECODE_PAGED   9  /* dims->n = table_pages * page, m = prefix_pages * page (0: no prefixes) */
+#define ZIPVL_OP_CHUNK_PAGED   10  /* dims->n = n of the call, m = (table_pages + prefix_pages) * page */
+#define ZIPVL_OP_PAGED_EVICT   11  /* dims->n = table_pages * page, m = budget */
 
 /* flags of zipvl_sparse_prefill */
 #define ZIPVL_OUT_FULL            0  /* O is [B,Hq,n,d]; rows of dropped tokens are written as zeros */
@@ -363,7 +365,7 @@ int zipvl_paged_append(const void* K, const void* V, const zipvl_dims* dims, con
 
 /*
  * Decode attention (Eq. (5) / Algorithm 2) over pages, for a batch whose elements share long prefixes (questions about one image or video),
- * one new token each (a piece of several tokens, as zipvl_paged_append takes it, has no attention over pages):
+ * one new token each (zipvl_chunk_attn_paged answers pieces of several tokens, as zipvl_paged_append takes them):
  *   o[b,h] = softmax( q[b,h] . [Kp ; Ko]^T * softmax_scale ) [Vp ; Vo]
  * with Ko, Vo the first len[u] rows of the unit u = b*Hkv + g by table [B*Hkv, table_pages], and Kp, Vp the first prefix_len[p*Hkv + g] rows
  * by prefix_table [groups*Hkv, prefix_pages] of the group p that b is in.  Group p is the batch elements group_begin[p] .. group_begin[p+1] - 1
@@ -384,6 +386,59 @@ int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32
                             const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len,
                             const int32_t* group_begin, int32_t groups, const zipvl_dims* dims, float softmax_scale,
                             void* o, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention of several new tokens of every batch element to its pages, causal: pieces of prompts, questions about a cached image, drafted tokens, behind
+ * zipvl_paged_append of the same tokens.  Unit u = b*Hkv + g has c = k[u] of the n tokens (k NULL: all n; clamped to [0, n]); they are the last c of its
+ * len[u] rows.  Query i < c of a head h of unit u sees the rows of the prefix (as in zipvl_decode_attn_paged: prefix_table, prefix_len, group_begin, groups) and
+ * its own rows 0 ... len[u] - c + i:
+ *   O[b,h,i] = softmax( Q[b,h,i] . [Kp ; Ko]^T * softmax_scale ) [Vp ; Vo],   lse[b,h,i] = log sum exp( Q[b,h,i] . [Kp ; Ko]^T * softmax_scale )
+ * A query that sees no row (len[u] < c, pages that are not there) gets zeros and an lse of -infinity.  O and lse of queries from c on are left as they are.
+ * Q [B,Hq,n,d] by dims->q_strides; O by the q_strides of `out` (its other fields are not looked at; NULL = [B,Hq,n,d] contiguous): no element twice, and
+ * overlapping no input.  lse [device] fp32 [B,Hq,n] contiguous, or NULL.  Any Hq / Hkv; n * Hq / Hkv < 2^30.
+ * Lengths are clamped to [0, pages of the table * page].  Nothing behind a length is read.  Inputs that are read must be finite.
+ * Numerics: scores, statistics and sums in fp32, one rounding at the end; where a unit has more than 32 queries (n * Hq / Hkv), the weights of a bf16 call are
+ * rounded to bf16 before they weigh V, and O is divided by the sum of those, lse is of the weights as they were.  The order of all sums follows from the sizes and lengths: the same call
+ * gives the same bits.
+ * ws [device] zipvl_workspace_bytes(ZIPVL_OP_CHUNK_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that overlap on one
+ * workspace race): up to 36 MB.
+ */
+int zipvl_chunk_attn_paged(const void* Q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                           const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin, int32_t groups,
+                           const zipvl_dims* dims, float softmax_scale, void* O, const zipvl_dims* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The attention weight that a unit's rows get from new queries, on top of what they had (for zipvl_paged_evict; the sum of Eq. (6), over the queries of a call and the
+ * heads of a group):
+ *   weight[u,r] = before[u,r] + sum over heads h of the group and queries i < c with r <= len[u] - c + i of exp( Q[b,h,i] . K_r * softmax_scale - lse[b,h,i] )
+ * for r < len[u]; what stands from len[u] on is left as it is.  c, k, len, table and Q as for zipvl_chunk_attn_paged, whose lse this takes (with a prefix the weights
+ * of own rows are what the prefix has left of 1).  Only the last m of a call's queries: Q and lse from there on, n = m, the same len.
+ * lse [device] fp32: query i of head h at lse[(b*Hq + h) * lse_pitch + i], lse_pitch >= n; -infinity: the query weighs nothing.
+ * before, weight [device] fp32 [B*Hkv, table_pages * page] contiguous; before may be weight itself or NULL (zeros); weight overlaps no other input.
+ * Rows in pages that are not there get nothing.  Inputs that are read must be finite (lse apart).
+ * Numerics: fp32; the same call gives the same bits.  pages->V is not looked at.
+ */
+int zipvl_paged_weigh(const void* Q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                      const float* lse, int64_t lse_pitch, const zipvl_dims* dims, float softmax_scale, const float* before, float* weight, void* stream);
+
+/*
+ * Rows leave a paged cache by weight: zipvl_compact_kv for caches that go on growing.  Of unit u stay
+ *   n' = min(len[u], budget, k[u] if k is given)
+ * rows: those of the tokens below `sinks` and of the latest `recent` tokens before all others, then the heaviest; equal weights (and protected rows that are more
+ * than n'): heavier first, then the lower row.  A weight with the sign bit set or that is no number counts as 0.
+ * Keys are cached rotated, so that rows stand in any order: a row below n' that stays is left where it is, and the i-th row from n' on that stays goes to the
+ * i-th row below n' that leaves.  K and V move in place, by the table; a move from or to a row in a page that is not there is left out.
+ *   len_out[u] = n';  weight_out[u,r], tokens_out[u,r] = those of the row that now stands in r for r < n', 0 and -1 for n' <= r < len[u]; from len[u] on both are left.
+ * tokens [device] int32 [B*Hkv, table_pages * page] or NULL (and tokens_out with it): which token each row holds.  Rows with a negative number are new, later than all others in
+ * the order of rows: they get the numbers behind the greatest one there.  (Begin with -1 everywhere; numbers stay below 2^31.)  NULL: row r holds token r, which is true until rows have moved.
+ * weight [device] fp32 [B*Hkv, table_pages * page].  len_out may be len, weight_out weight, tokens_out tokens; outputs overlap no other array.
+ * A page that two units' tables share (or one table holds twice) races.
+ * dims: B, Hkv, d, dtype.  B*Hkv <= 65535.  budget, sinks, recent >= 0.  k [device] int32 [B*Hkv] or NULL, clamped to >= 0.
+ * ws [device] zipvl_workspace_bytes(ZIPVL_OP_PAGED_EVICT, dims, budget) bytes, 16-byte aligned, holds nothing between calls (two calls that overlap on one workspace race).
+ */
+int zipvl_paged_evict(const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const zipvl_dims* dims, const int32_t* len, const int32_t* k,
+                      const float* weight, const int32_t* tokens, int32_t budget, int32_t sinks, int32_t recent,
+                      int32_t* len_out, float* weight_out, int32_t* tokens_out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -46,7 +46,12 @@ extern "C" {
 #define ZIPVL_K_PAGED_ADVANCE  23
 #define ZIPVL_K_PAGED_PARTIAL  24
 #define ZIPVL_K_PAGED_COMBINE  25
-#define ZIPVL_K_COUNT          26
+#define ZIPVL_K_CHUNK_ATTN     26
+#define ZIPVL_K_CHUNK_JOIN     27
+#define ZIPVL_K_PAGED_WEIGH    28
+#define ZIPVL_K_PAGED_EVICT    29
+#define ZIPVL_K_PAGED_MOVE     30
+#define ZIPVL_K_COUNT          31
 int zipvl_timing_enable(int on);
 int zipvl_timing_read(int kernel_id, double* total_ms, int* launches);
 

@@ -18,13 +18,14 @@ OUT_FULL, OUT_COMPACT, KV_ALREADY_COMPACT, T_PER_BATCH = 0, 1, 2, 4
 SCORE_PER_QHEAD = 1
 SELECT_NEGATIVE, SELECT_NONFINITE, SELECT_OVERFLOW = 1, 2, 4
 OP_SCORE, OP_SELECT, OP_SPARSE_PREFILL, OP_DECODE, OP_QUANTIZE_KV, OP_DECODE_Q, OP_SCORE_ALL_ROWS, OP_DECODE_STEP, OP_DECODE_PAGED = 1, 2, 3, 4, 5, 6, 7, 8, 9
+OP_CHUNK_PAGED, OP_PAGED_EVICT = 10, 11
 ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
 ROTATE_INVERSE = 1
 MAX_AXES, MAX_PAIRS = 4, 64
 
 EXPORTS = ("zipvl_version", "zipvl_last_error", "zipvl_workspace_bytes", "zipvl_score", "zipvl_select",
            "zipvl_score_all_rows", "zipvl_share_scores", "zipvl_quantize_kv", "zipvl_decode_attn_q", "zipvl_sparse_prefill", "zipvl_compact_kv", "zipvl_kv_append", "zipvl_decode_attn", "zipvl_decode_attn_static", "zipvl_decode_step",
-           "zipvl_rotate", "zipvl_paged_append", "zipvl_decode_attn_paged",
+           "zipvl_rotate", "zipvl_paged_append", "zipvl_decode_attn_paged", "zipvl_chunk_attn_paged", "zipvl_paged_weigh", "zipvl_paged_evict",
            "zipvl_timing_enable", "zipvl_timing_read", "zipvl_probe_mfma", "zipvl_probe_stream_read")
 
 
@@ -141,7 +142,12 @@ def load_library():
                                        i32p, i32p, vp, vp, C.c_int, vp]
     lib.zipvl_decode_attn_paged.argtypes = [vp, C.POINTER(Pages), i32p, C.c_int32, i32p, i32p, C.c_int32, i32p, i32p, C.c_int32,
                                             C.POINTER(Dims), C.c_float, vp, vp, C.c_size_t, vp]
-    for name in ("zipvl_rotate", "zipvl_paged_append", "zipvl_decode_attn_paged", "zipvl_score", "zipvl_score_all_rows", "zipvl_select", "zipvl_share_scores", "zipvl_quantize_kv",
+    lib.zipvl_chunk_attn_paged.argtypes = [vp, C.POINTER(Pages), i32p, C.c_int32, i32p, i32p, i32p, C.c_int32, i32p, i32p, C.c_int32,
+                                           C.POINTER(Dims), C.c_float, vp, C.POINTER(Dims), f32p, vp, C.c_size_t, vp]
+    lib.zipvl_paged_weigh.argtypes = [vp, C.POINTER(Pages), i32p, C.c_int32, i32p, i32p, f32p, C.c_int64, C.POINTER(Dims), C.c_float, f32p, f32p, vp]
+    lib.zipvl_paged_evict.argtypes = [C.POINTER(Pages), i32p, C.c_int32, C.POINTER(Dims), i32p, i32p, f32p, i32p, C.c_int32, C.c_int32, C.c_int32,
+                                      i32p, f32p, i32p, vp, C.c_size_t, vp]
+    for name in ("zipvl_chunk_attn_paged", "zipvl_paged_weigh", "zipvl_paged_evict", "zipvl_rotate", "zipvl_paged_append", "zipvl_decode_attn_paged", "zipvl_score", "zipvl_score_all_rows", "zipvl_select", "zipvl_share_scores", "zipvl_quantize_kv",
                  "zipvl_decode_attn_q", "zipvl_sparse_prefill", "zipvl_compact_kv", "zipvl_kv_append", "zipvl_decode_attn",
                  "zipvl_decode_step"):
         getattr(lib, name).restype = C.c_int
@@ -707,10 +713,152 @@ def zipvl_decode_attn_paged(q: torch.Tensor, cache: PagedCache, table: torch.Ten
     return o
 
 
+def _queries(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, length: torch.Tensor, k: Optional[torch.Tensor]):
+    """(pages, Hkv) for queries [B,Hq,n,d] against the units of a table."""
+    pages = cache.struct()
+    if Q.dim() != 4:
+        raise ZipvlError(-2, f"expected Q [B,Hq,n,d], got shape {tuple(Q.shape)}")
+    _rows_like("Q", Q, (*Q.shape[:3], cache.d), cache.K.dtype)
+    if table.dim() != 2 or Q.shape[0] == 0 or table.shape[0] == 0 or table.shape[0] % Q.shape[0]:
+        raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [{Q.shape[0]} * Hkv, table_pages]")
+    units = table.shape[0]
+    _expect("table", table, table.shape)
+    _expect("length", length, (units,))
+    if k is not None:
+        _expect("k", k, (units,))
+    return pages, units // Q.shape[0]
+
+
+def _prefix(prefix_table, prefix_len, group_begin, Hkv: int) -> int:
+    """How many groups share a prefix."""
+    given = [t is not None for t in (prefix_table, prefix_len, group_begin)]
+    if not any(given):
+        return 0
+    if not all(given):
+        raise ZipvlError(-1, "prefix_table, prefix_len and group_begin must all be given or all be None")
+    groups = group_begin.numel() - 1
+    if groups < 1:
+        raise ZipvlError(-2, f"group_begin has shape {tuple(group_begin.shape)}, expected [groups + 1]")
+    if prefix_table.dim() != 2:
+        raise ZipvlError(-2, f"prefix_table has shape {tuple(prefix_table.shape)}, expected [{groups * Hkv}, prefix_pages]")
+    _expect("group_begin", group_begin, (groups + 1,))
+    _expect("prefix_table", prefix_table, (groups * Hkv, prefix_table.shape[1]))
+    _expect("prefix_len", prefix_len, (groups * Hkv,))
+    return groups
+
+
+def chunk_paged_workspace(cache: PagedCache, table: torch.Tensor, prefix_table: Optional[torch.Tensor] = None, *, B: int, Hq: int, Hkv: int, n: int) -> torch.Tensor:
+    """A workspace for zipvl_chunk_attn_paged of n tokens over tables of these widths."""
+    dm = dims_of(None, None, None, B=B, Hq=Hq, Hkv=Hkv, n=n, d=cache.d, dtype=_dtype_code(cache.K))
+    rows = (table.shape[1] + (0 if prefix_table is None else prefix_table.shape[1])) * cache.page
+    return _workspace(workspace_bytes(OP_CHUNK_PAGED, dm, rows), cache.K.device)
+
+
+def zipvl_chunk_attn_paged(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, length: torch.Tensor, softmax_scale: float, *,
+                           k: Optional[torch.Tensor] = None, prefix_table: Optional[torch.Tensor] = None, prefix_len: Optional[torch.Tensor] = None,
+                           group_begin: Optional[torch.Tensor] = None, O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                           want_lse: bool = False, ws: Optional[torch.Tensor] = None):
+    """(O [B,Hq,n,d], lse [B,Hq,n] or None): causal attention of the last k[u] (None: n) of the length[u] rows by table [B*Hkv, table_pages], and of the prefix of
+    the batch element's group (as in zipvl_decode_attn_paged).  O may have any strides.  What queries from k[u] on have in O and lse is left as it is."""
+    lib = load_library()
+    pages, Hkv = _queries(Q, cache, table, length, k)
+    B, Hq, n, d = Q.shape
+    groups = _prefix(prefix_table, prefix_len, group_begin, Hkv)
+    if O is None:
+        O = (torch.empty if k is None else torch.zeros)(Q.shape, dtype=Q.dtype, device=Q.device)
+    _rows_like("O", O, Q.shape, Q.dtype)
+    if lse is None and want_lse:
+        lse = (torch.empty if k is None else torch.zeros)((B, Hq, n), dtype=torch.float32, device=Q.device)
+    if lse is not None:
+        _expect("lse", lse, (B, Hq, n), torch.float32)
+    if ws is None:
+        ws = chunk_paged_workspace(cache, table, prefix_table, B=B, Hq=Hq, Hkv=Hkv, n=n)
+    _dense(ws)
+    size = dict(B=B, Hq=Hq, Hkv=Hkv, n=n, d=d, dtype=_dtype_code(Q))
+    dm, out = _dims_rows(Q, None, None, **size), _dims_rows(O, None, None, **size)
+    _on_device(lambda stream: lib.zipvl_chunk_attn_paged(
+        _ptr(Q), C.byref(pages), _ptr(table), table.shape[1], _ptr(length), _ptr(k), _ptr(prefix_table), 0 if prefix_table is None else prefix_table.shape[1],
+        _ptr(prefix_len), _ptr(group_begin), groups, C.byref(dm), float(softmax_scale), _ptr(O), C.byref(out), _ptr(lse), _ptr(ws),
+        ws.numel() * ws.element_size(), stream), Q, cache.K, table, length, k, prefix_table, prefix_len, group_begin, O, lse, ws)
+    return O, lse
+
+
+def zipvl_paged_weigh(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, length: torch.Tensor, lse: torch.Tensor, softmax_scale: float, *,
+                      k: Optional[torch.Tensor] = None, before: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None):
+    """weight [B*Hkv, table_pages * page] fp32: what rows had (before; None: nothing) and get from the queries, whose log sums are lse [B,Hq,n] (of
+    zipvl_chunk_attn_paged; a view of its last tokens together with theirs of Q counts those alone).  weight may be before itself."""
+    lib = load_library()
+    pages, Hkv = _queries(Q, cache, table, length, k)
+    B, Hq, n, d = Q.shape
+    if tuple(lse.shape) != (B, Hq, n):
+        raise ZipvlError(-2, f"lse has shape {tuple(lse.shape)}, expected {(B, Hq, n)}")
+    if lse.dtype != torch.float32:
+        raise ZipvlError(-5, f"lse is {lse.dtype}, expected {torch.float32}")
+    pitch = lse.stride(1) if Hq > 1 else lse.stride(0) if B > 1 else n
+    if (n > 1 and lse.stride(2) != 1) or (B > 1 and lse.stride(0) != Hq * pitch):
+        raise ZipvlError(-1, f"lse of strides {tuple(lse.stride())}: its rows must follow each other at one distance")
+    shape = (table.shape[0], table.shape[1] * cache.page)
+    if weight is None:
+        weight = torch.zeros(shape, dtype=torch.float32, device=Q.device)
+    _expect("weight", weight, shape, torch.float32)
+    if before is not None:
+        _expect("before", before, shape, torch.float32)
+    dm = _dims_rows(Q, None, None, B=B, Hq=Hq, Hkv=Hkv, n=n, d=d, dtype=_dtype_code(Q))
+    _on_device(lambda stream: lib.zipvl_paged_weigh(_ptr(Q), C.byref(pages), _ptr(table), table.shape[1], _ptr(length), _ptr(k), _ptr(lse), int(pitch),
+                                                    C.byref(dm), float(softmax_scale), _ptr(before), _ptr(weight), stream),
+               Q, cache.K, table, length, k, lse, before, weight)
+    return weight
+
+
+def paged_evict_workspace(cache: PagedCache, table: torch.Tensor, budget: int) -> torch.Tensor:
+    """A workspace for zipvl_paged_evict down to `budget` rows by this table."""
+    dm = dims_of(None, None, None, B=table.shape[0], Hq=1, Hkv=1, n=max(1, table.shape[1] * cache.page), d=cache.d, dtype=_dtype_code(cache.K))
+    return _workspace(workspace_bytes(OP_PAGED_EVICT, dm, budget), cache.K.device)
+
+
+def zipvl_paged_evict(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, weight: torch.Tensor, budget: int, *,
+                      k: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None, sinks: int = 0, recent: int = 0,
+                      length_out: Optional[torch.Tensor] = None, weight_out: Optional[torch.Tensor] = None, tokens_out: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None):
+    """length_out: of the length[u] rows by table [units, table_pages], min(length[u], budget, k[u]) stay: the first `sinks` and the last `recent` tokens and
+    the heaviest others; rows that stay move into the places of those that leave.  weight, tokens (which token a row holds, -1: a new one) [units, table_pages * page]
+    move along.  Outputs that are not given are written in place."""
+    lib = load_library()
+    pages = cache.struct()
+    if table.dim() != 2:
+        raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [units, table_pages]")
+    units = table.shape[0]
+    shape = (units, table.shape[1] * cache.page)
+    length_out = length if length_out is None else length_out
+    weight_out = weight if weight_out is None else weight_out
+    if tokens is None and tokens_out is not None:
+        raise ZipvlError(-1, "zipvl_paged_evict: tokens_out is given without tokens")
+    tokens_out = tokens if tokens_out is None else tokens_out
+    _expect("table", table, table.shape)
+    for name, t in (("length", length), ("length_out", length_out), ("k", k)):
+        if t is not None:
+            _expect(name, t, (units,))
+    for name, t, dtype in (("weight", weight, torch.float32), ("weight_out", weight_out, torch.float32), ("tokens", tokens, torch.int32), ("tokens_out", tokens_out, torch.int32)):
+        if t is not None:
+            _expect(name, t, shape, dtype)
+    if not 0 <= budget < 2 ** 31 or not 0 <= sinks < 2 ** 31 or not 0 <= recent < 2 ** 31:
+        raise ZipvlError(-1, f"zipvl_paged_evict: budget, sinks and recent must not be negative (got {budget} {sinks} {recent})")
+    if ws is None:
+        ws = paged_evict_workspace(cache, table, budget)
+    _dense(ws)
+    dm = dims_of(None, None, None, B=units, Hq=1, Hkv=1, n=1, d=cache.d, dtype=_dtype_code(cache.K))
+    _on_device(lambda stream: lib.zipvl_paged_evict(
+        C.byref(pages), _ptr(table), table.shape[1], C.byref(dm), _ptr(length), _ptr(k), _ptr(weight), _ptr(tokens), int(budget), int(sinks), int(recent),
+        _ptr(length_out), _ptr(weight_out), _ptr(tokens_out), _ptr(ws), ws.numel() * ws.element_size(), stream),
+        cache.K, table, length, k, weight, tokens, length_out, weight_out, tokens_out, ws)
+    return length_out
+
+
 KERNELS = ("score_rowstats", "score_colsum", "select", "compact_kv", "kv_append", "zero_fill",
            "pack_kv", "flash_kept", "decode_partial", "decode_combine", "score_rowfinal", "share_scores",
            "token_slots", "quantize_rows", "decode_q_partial", "allrows_lse", "allrows_colsum", "probe_mfma", "probe_read",
-           "decode_step", "select_hist", "rotate", "paged_append", "paged_advance", "paged_partial", "paged_combine")
+           "decode_step", "select_hist", "rotate", "paged_append", "paged_advance", "paged_partial", "paged_combine",
+           "chunk_attn", "chunk_join", "paged_weigh", "paged_evict", "paged_move")
 
 
 def zipvl_probe_peaks(device="cuda:0", iters: int = 4096, read_mib: int = 4096):

@@ -72,6 +72,17 @@ int launch_decode_attn_paged(const void* q, const zipvl_pages& pages, const int3
                              const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin,
                              int32_t groups, const zipvl_dims& d, float scale, void* o, void* ws, hipStream_t st);
 
+size_t chunk_attn_workspace_bytes(const zipvl_dims& d, int64_t keys);                // that a unit's row of the tables and its prefix's can hold
+int launch_chunk_attn_paged(const void* Q, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                            const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin, int32_t groups,
+                            const zipvl_dims& d, float scale, void* O, const int64_t* o_strides, float* lse, void* ws, hipStream_t st);
+int launch_paged_weigh(const void* Q, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                       const float* lse, int64_t lse_pitch, const zipvl_dims& d, float scale, const float* before, float* weight, hipStream_t st);
+size_t paged_evict_workspace_bytes(int64_t units, int64_t rows, int64_t budget);
+int launch_paged_evict(const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const zipvl_dims& d, const int32_t* len, const int32_t* k,
+                       const float* weight, const int32_t* tokens, int32_t budget, int32_t sinks, int32_t recent, int32_t* len_out, float* weight_out,
+                       int32_t* tokens_out, void* ws, hipStream_t st);
+
 int launch_probe_mfma(int iters, int workgroups, float* out, hipStream_t st);
 int launch_probe_read(const void* src, size_t bytes, int workgroups, uint32_t* out, hipStream_t st);
 

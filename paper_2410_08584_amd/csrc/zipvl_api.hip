@@ -117,6 +117,10 @@ size_t zipvl_workspace_bytes(int op, const zipvl_dims* dims, int m) {
         case ZIPVL_OP_DECODE_PAGED:
             if (m < 0) { set_error(ZIPVL_EINVAL, "zipvl_workspace_bytes: m = %d is negative", m); return 0; }
             return decode_paged_workspace_bytes(*dims, dims->n, m);
+        case ZIPVL_OP_CHUNK_PAGED:
+        case ZIPVL_OP_PAGED_EVICT:
+            if (m < 0) { set_error(ZIPVL_EINVAL, "zipvl_workspace_bytes: m = %d is negative", m); return 0; }
+            return op == ZIPVL_OP_CHUNK_PAGED ? chunk_attn_workspace_bytes(*dims, m) : paged_evict_workspace_bytes((int64_t)dims->B * dims->Hkv, dims->n, m);
         default: set_error(ZIPVL_EUNSUPPORTED, "zipvl_workspace_bytes: unknown op %d", op); return 0;
     }
 }
@@ -508,6 +512,105 @@ int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32
     if (!aligned16(ws)) return set_error(ZIPVL_EALIGN, "%s: ws is not 16-byte aligned", fn);
     return launch_decode_attn_paged(q, *pages, table, table_pages, len, prefix_table, prefix_pages, prefix_len, group_begin, groups, d,
                                     softmax_scale, o, ws, (hipStream_t)stream);
+}
+
+// Two arrays of `a` and `b` bytes: apart, or NULL.
+static bool apart(const void* x, int64_t a, const void* y, int64_t b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+    return !x || !y || p + a <= q || q + b <= p;
+}
+
+static int check_chunk(const char* fn, const zipvl_dims* dims, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                       float softmax_scale) {
+    int rc = check_dims(fn, dims, true, false, false);
+    if (rc || (rc = check_tokens(fn, *dims)) || (rc = check_pages(fn, pages)) || (rc = check_table(fn, "table", table, table_pages, pages->page))) return rc;
+    if ((int64_t)dims->n * (dims->Hq / dims->Hkv) >= (1 << 30)) return set_error(ZIPVL_ESHAPE, "%s: n * Hq / Hkv = %lld is not below 2^30", fn, (long long)dims->n * (dims->Hq / dims->Hkv));
+    if (!len) return set_error(ZIPVL_EINVAL, "%s: len is NULL", fn);
+    if ((reinterpret_cast<uintptr_t>(len) | reinterpret_cast<uintptr_t>(k)) & 3u) return set_error(ZIPVL_EALIGN, "%s: len or k is not 4-byte aligned", fn);
+    if (!(softmax_scale > 0.f) || !(softmax_scale < 1e30f)) return set_error(ZIPVL_EINVAL, "%s: softmax_scale must be positive and finite", fn);
+    return ZIPVL_OK;
+}
+
+int zipvl_chunk_attn_paged(const void* Q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                           const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin, int32_t groups,
+                           const zipvl_dims* dims, float softmax_scale, void* O, const zipvl_dims* out, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    const char* fn = "zipvl_chunk_attn_paged";
+    int rc = check_chunk(fn, dims, pages, table, table_pages, len, k, softmax_scale);
+    if (rc) return rc;
+    const zipvl_dims& d = *dims;
+    ZIPVL_REQUIRE_PTR(fn, Q);
+    ZIPVL_REQUIRE_PTR(fn, O);
+    if (groups < 0 || groups > d.B) return set_error(ZIPVL_EINVAL, "%s: %d groups of %d batch elements", fn, groups, d.B);
+    if (groups) {
+        if ((rc = check_table(fn, "prefix_table", prefix_table, prefix_pages, pages->page))) return rc;
+        if (!prefix_len || !group_begin) return set_error(ZIPVL_EINVAL, "%s: prefix_len / group_begin is NULL", fn);
+    } else {
+        prefix_table = prefix_len = group_begin = nullptr;
+        prefix_pages = 0;
+    }
+    if ((reinterpret_cast<uintptr_t>(prefix_len) | reinterpret_cast<uintptr_t>(group_begin) | reinterpret_cast<uintptr_t>(lse)) & 3u)
+        return set_error(ZIPVL_EALIGN, "%s: prefix_len, group_begin or lse is not 4-byte aligned", fn);
+    zipvl_dims o = d;
+    const int64_t dense[3] = {(int64_t)d.Hq * d.n * d.d, (int64_t)d.n * d.d, d.d};
+    std::copy(out ? out->q_strides : dense, (out ? out->q_strides : dense) + 3, o.q_strides);
+    if ((rc = check_dims(fn, &o, true, false, false)) || (rc = check_apart(fn, "O", o.q_strides, {d.B, d.Hq, d.n}, d.d))) return rc;
+    if (O == Q) return set_error(ZIPVL_EINVAL, "%s: O in the place of Q", fn);
+    const size_t need = chunk_attn_workspace_bytes(d, ((int64_t)table_pages + prefix_pages) * pages->page);
+    if (!ws || ws_bytes < need) return set_error(ZIPVL_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+    if (!aligned16(ws)) return set_error(ZIPVL_EALIGN, "%s: ws is not 16-byte aligned", fn);
+    return launch_chunk_attn_paged(Q, *pages, table, table_pages, len, k, prefix_table, prefix_pages, prefix_len, group_begin, groups, d, softmax_scale,
+                                   O, o.q_strides, lse, ws, (hipStream_t)stream);
+}
+
+int zipvl_paged_weigh(const void* Q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
+                      const float* lse, int64_t lse_pitch, const zipvl_dims* dims, float softmax_scale, const float* before, float* weight, void* stream)
+{
+    const char* fn = "zipvl_paged_weigh";
+    const int rc = check_chunk(fn, dims, pages, table, table_pages, len, k, softmax_scale);
+    if (rc) return rc;
+    ZIPVL_REQUIRE_PTR(fn, Q);
+    if (!lse || !weight) return set_error(ZIPVL_EINVAL, "%s: lse / weight is NULL", fn);
+    if (lse_pitch < dims->n) return set_error(ZIPVL_EINVAL, "%s: lse_pitch = %lld is smaller than n = %d", fn, (long long)lse_pitch, dims->n);
+    if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(before) | reinterpret_cast<uintptr_t>(weight)) & 3u)
+        return set_error(ZIPVL_EALIGN, "%s: lse, before or weight is not 4-byte aligned", fn);
+    const int64_t units = (int64_t)dims->B * dims->Hkv, bytes = units * table_pages * pages->page * 4, queries = ((int64_t)dims->B * dims->Hq - 1) * lse_pitch + dims->n;
+    if ((before != weight && !apart(before, bytes, weight, bytes)) || !apart(len, units * 4, weight, bytes) || !apart(k, units * 4, weight, bytes) ||
+        !apart(lse, queries * 4, weight, bytes) || !apart(table, units * table_pages * 4, weight, bytes))
+        return set_error(ZIPVL_EINVAL, "%s: weight overlaps before, len, k, lse or table (it may be before itself)", fn);
+    return launch_paged_weigh(Q, *pages, table, table_pages, len, k, lse, lse_pitch, *dims, softmax_scale, before, weight, (hipStream_t)stream);
+}
+
+int zipvl_paged_evict(const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const zipvl_dims* dims, const int32_t* len, const int32_t* k,
+                      const float* weight, const int32_t* tokens, int32_t budget, int32_t sinks, int32_t recent,
+                      int32_t* len_out, float* weight_out, int32_t* tokens_out, void* ws, size_t ws_bytes, void* stream)
+{
+    const char* fn = "zipvl_paged_evict";
+    zipvl_dims d = dims ? *dims : zipvl_dims{};
+    d.n = 1;                                                 // not looked at
+    d.Hq = d.Hkv;
+    int rc = check_dims(fn, dims ? &d : nullptr, false, false, false);
+    if (rc || (rc = check_pages(fn, pages)) || (rc = check_table(fn, "table", table, table_pages, pages->page))) return rc;
+    if (!len || !weight || !len_out || !weight_out) return set_error(ZIPVL_EINVAL, "%s: len, weight, len_out or weight_out is NULL", fn);
+    if ((tokens == nullptr) != (tokens_out == nullptr)) return set_error(ZIPVL_EINVAL, "%s: tokens and tokens_out must both be given or both be NULL", fn);
+    if (budget < 0 || sinks < 0 || recent < 0) return set_error(ZIPVL_EINVAL, "%s: budget, sinks and recent must not be negative (got %d %d %d)", fn, budget, sinks, recent);
+    for (const void* p : {(const void*)len, (const void*)k, (const void*)weight, (const void*)tokens, (const void*)len_out, (const void*)weight_out, (const void*)tokens_out})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return set_error(ZIPVL_EALIGN, "%s: an array is not 4-byte aligned", fn);
+    const int64_t units = (int64_t)d.B * d.Hkv, room = (int64_t)table_pages * pages->page;
+    struct Span { const void* p; int64_t bytes; };
+    const Span ins[5] = {{len, units * 4}, {weight, units * room * 4}, {tokens, units * room * 4}, {k, units * 4}, {table, units * table_pages * 4}};
+    const Span outs[3] = {{len_out, units * 4}, {weight_out, units * room * 4}, {tokens_out, units * room * 4}};
+    for (int y = 0; y < 3; ++y) {
+        for (int x = 0; x < 5; ++x)
+            if (!(x == y && ins[x].p == outs[y].p) && !apart(ins[x].p, ins[x].bytes, outs[y].p, outs[y].bytes))
+                return set_error(ZIPVL_EINVAL, "%s: an output overlaps another array (len_out may be len, weight_out weight, tokens_out tokens)", fn);
+        for (int x = 0; x < y; ++x)
+            if (!apart(outs[x].p, outs[x].bytes, outs[y].p, outs[y].bytes)) return set_error(ZIPVL_EINVAL, "%s: two outputs overlap", fn);
+    }
+    const size_t need = paged_evict_workspace_bytes(units, room, budget);
+    if (!ws || ws_bytes < need) return set_error(ZIPVL_EWORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+    if (!aligned16(ws)) return set_error(ZIPVL_EALIGN, "%s: ws is not 16-byte aligned", fn);
+    return launch_paged_evict(*pages, table, table_pages, d, len, k, weight, tokens, budget, sinks, recent, len_out, weight_out, tokens_out, ws, (hipStream_t)stream);
 }
 
 int zipvl_probe_mfma(int iters, int workgroups, float* out, void* stream)
