@@ -761,6 +761,9 @@ def zipvl_chunk_attn_paged(Q: torch.Tensor, cache: PagedCache, table: torch.Tens
     """(O [B,Hq,n,d], lse [B,Hq,n] or None): causal attention of the last k[u] (None: n) of the length[u] rows by table [B*Hkv, table_pages], and of the prefix of
     the batch element's group (as in zipvl_decode_attn_paged).  O may have any strides.  What queries from k[u] on have in O and lse is left as it is."""
     lib = load_library()
+    if O is not None and ws is not None and (lse is not None or not want_lse) and _called(
+            _native.chunk_attn_paged(Q, cache, table, length, softmax_scale, k, prefix_table, prefix_len, group_begin, O, lse, ws)):
+        return O, lse
     pages, Hkv = _queries(Q, cache, table, length, k)
     B, Hq, n, d = Q.shape
     groups = _prefix(prefix_table, prefix_len, group_begin, Hkv)
@@ -788,6 +791,8 @@ def zipvl_paged_weigh(Q: torch.Tensor, cache: PagedCache, table: torch.Tensor, l
     """weight [B*Hkv, table_pages * page] fp32: what rows had (before; None: nothing) and get from the queries, whose log sums are lse [B,Hq,n] (of
     zipvl_chunk_attn_paged; a view of its last tokens together with theirs of Q counts those alone).  weight may be before itself."""
     lib = load_library()
+    if weight is not None and _called(_native.paged_weigh(Q, cache, table, length, lse, softmax_scale, k, before, weight)):
+        return weight
     pages, Hkv = _queries(Q, cache, table, length, k)
     B, Hq, n, d = Q.shape
     if tuple(lse.shape) != (B, Hq, n):
@@ -824,16 +829,18 @@ def zipvl_paged_evict(cache: PagedCache, table: torch.Tensor, length: torch.Tens
     the heaviest others; rows that stay move into the places of those that leave.  weight, tokens (which token a row holds, -1: a new one) [units, table_pages * page]
     move along.  Outputs that are not given are written in place."""
     lib = load_library()
-    pages = cache.struct()
-    if table.dim() != 2:
-        raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [units, table_pages]")
-    units = table.shape[0]
-    shape = (units, table.shape[1] * cache.page)
     length_out = length if length_out is None else length_out
     weight_out = weight if weight_out is None else weight_out
     if tokens is None and tokens_out is not None:
         raise ZipvlError(-1, "zipvl_paged_evict: tokens_out is given without tokens")
     tokens_out = tokens if tokens_out is None else tokens_out
+    if ws is not None and _called(_native.paged_evict(cache, table, length, k, weight, tokens, budget, sinks, recent, length_out, weight_out, tokens_out, ws)):
+        return length_out
+    pages = cache.struct()
+    if table.dim() != 2:
+        raise ZipvlError(-2, f"table has shape {tuple(table.shape)}, expected [units, table_pages]")
+    units = table.shape[0]
+    shape = (units, table.shape[1] * cache.page)
     _expect("table", table, table.shape)
     for name, t in (("length", length), ("length_out", length_out), ("k", k)):
         if t is not None:

@@ -197,10 +197,10 @@ __global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel
     auto pass = [&](auto again) {
         constexpr bool AGAIN = decltype(again)::value;
         part.reset();
-        if (t0 < tp) part.template tiles<AGAIN, false>(p, pre, v.prefix_rows, t0 + w, kPartWaves, min(t1, tp), p.c, mine);
+        if (t0 < tp) part.template tiles<AGAIN, false, false>(p, pre, v.prefix_rows, t0 + w, kPartWaves, min(t1, tp), p.c, mine);
         if (t1 > tp) {
             const int first = max(t0 - tp, 0);
-            part.template tiles<AGAIN, true>(p, own, v.len, first + ((w - max(tp - t0, 0)) & 3), kPartWaves, t1 - tp, p.c, mine, last);
+            part.template tiles<AGAIN, true, false>(p, own, v.len, first + ((w - max(tp - t0, 0)) & 3), kPartWaves, t1 - tp, p.c, mine, last);
         }
     };
     pass(std::false_type{});

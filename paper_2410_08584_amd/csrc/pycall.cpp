@@ -459,10 +459,113 @@ PyObject* decode_attn_paged(PyObject*, PyObject* const* a, Py_ssize_t na) {
     });
 }
 
+// Queries [B, H, n, d] against the units of a table: dims with Q's strides, and what stands beside it.
+struct Queries { zipvl_dims d; void *Q, *table, *len, *k; int32_t width; int64_t units, s[4]; PyObject* type; };
+Queries queries(Args& x, const Args::Pool& pool, PyObject* Q, PyObject* table, PyObject* length, PyObject* k) {
+    Queries q = {};
+    x.shape(Q, q.s);
+    q.type = pool.dtype;
+    if (!x.ok || q.s[3] != pool.d || q.s[0] < 1) { x.ok = false; return q; }
+    int64_t t[2] = {};
+    x.shape(table, t);
+    q.units = t[0];
+    if (q.units < 1 || q.units % q.s[0]) x.ok = false;
+    q.d.B = x.narrow(q.s[0]); q.d.Hq = x.narrow(q.s[1]); q.d.n = x.narrow(q.s[2]); q.d.d = x.narrow(q.s[3]);
+    q.d.Hkv = x.ok ? x.narrow(q.units / q.s[0]) : 0;
+    q.d.dtype = q.type == g_bf16;
+    q.Q = x.rows(Q, q.type, q.s[0], q.s[1], q.s[2], q.s[3], q.d.q_strides);
+    q.table = x.table(table, q.units, q.width);
+    q.len = x.ints(length, {q.units});
+    q.k = x.ints_or_null(k, {q.units});
+    return q;
+}
+
+// (Q, cache, table, length, scale, k, prefix_table, prefix_len, group_begin, O, lse, ws)
+PyObject* chunk_attn_paged(PyObject*, PyObject* const* a, Py_ssize_t na) {
+    if (!count_is(na, 12)) return general_way();
+    Args x{a};
+    const Args::Pool pool = x.pool(a[1]);
+    if (!x.ok) return general_way();
+    Queries q = queries(x, pool, a[0], a[2], a[3], a[5]);
+    const float scale = (float)x.real(a[4]);
+    int32_t prefix_width = 0, groups = 0;
+    void *prefix_table = nullptr, *prefix_len = nullptr, *begin = nullptr;
+    if (a[6] != Py_None || a[7] != Py_None || a[8] != Py_None) {
+        int64_t s[1] = {};
+        x.shape(a[8], s);
+        groups = x.narrow(s[0] - 1);
+        if (groups < 1) x.ok = false;
+        prefix_table = x.table(a[6], (int64_t)groups * q.d.Hkv, prefix_width);
+        prefix_len = x.ints(a[7], {(int64_t)groups * q.d.Hkv});
+        begin = x.ints(a[8], {(int64_t)groups + 1});
+    }
+    zipvl_dims out = q.d;
+    void* O = x.rows(a[9], q.type, q.s[0], q.s[1], q.s[2], q.s[3], out.q_strides);
+    void* lse = a[10] == Py_None ? nullptr : x.array(a[10], g_f32, {q.s[0], q.s[1], q.s[2]});
+    x.typed(a[11], g_u8);
+    x.dense(a[11]);
+    void* ws = x.placed(a[11]);
+    const size_t ws_bytes = x.bytes(a[11]);
+    void* st = x.stream_there();
+    return finish(x, [&] {
+        return zipvl_chunk_attn_paged(q.Q, &pool.pages, (int32_t*)q.table, q.width, (int32_t*)q.len, (int32_t*)q.k, (int32_t*)prefix_table, prefix_width, (int32_t*)prefix_len,
+                                      (int32_t*)begin, groups, &q.d, scale, O, &out, (float*)lse, ws, ws_bytes, st);
+    });
+}
+
+// (Q, cache, table, length, lse, scale, k, before, weight)
+PyObject* paged_weigh(PyObject*, PyObject* const* a, Py_ssize_t na) {
+    if (!count_is(na, 9)) return general_way();
+    Args x{a};
+    const Args::Pool pool = x.pool(a[1]);
+    if (!x.ok) return general_way();
+    Queries q = queries(x, pool, a[0], a[2], a[3], a[6]);
+    const float scale = (float)x.real(a[5]);
+    void* lse = x.array(a[4], g_f32, {q.s[0], q.s[1], q.s[2]});          // a view of some of the tokens goes the general way
+    const int64_t room = (int64_t)q.width * pool.pages.page;
+    void* weight = x.array(a[8], g_f32, {q.units, room});
+    void* before = a[7] == Py_None ? nullptr : a[7] == a[8] ? weight : x.array(a[7], g_f32, {q.units, room});
+    void* st = x.stream_there();
+    return finish(x, [&] {
+        return zipvl_paged_weigh(q.Q, &pool.pages, (int32_t*)q.table, q.width, (int32_t*)q.len, (int32_t*)q.k, (float*)lse, q.s[2], &q.d, scale, (float*)before,
+                                 (float*)weight, st);
+    });
+}
+
+// (cache, table, length, k, weight, tokens, budget, sinks, recent, length_out, weight_out, tokens_out, ws)
+PyObject* paged_evict(PyObject*, PyObject* const* a, Py_ssize_t na) {
+    if (!count_is(na, 13)) return general_way();
+    Args x{a};
+    const Args::Pool pool = x.pool(a[0]);
+    int64_t t[2] = {};
+    x.shape(a[1], t);
+    if (!x.ok) return general_way();
+    const int64_t units = t[0], room = t[1] * pool.pages.page;
+    zipvl_dims d = {};
+    d.B = x.narrow(units); d.Hq = d.Hkv = d.n = 1; d.d = x.narrow(pool.d);
+    d.dtype = pool.dtype == g_bf16;
+    int32_t width = 0;
+    void *table = x.table(a[1], units, width), *len = x.ints(a[2], {units}), *k = x.ints_or_null(a[3], {units});
+    void *weight = x.array(a[4], g_f32, {units, room}), *tokens = x.ints_or_null(a[5], {units, room});
+    const int budget = x.int32(a[6]), sinks = x.int32(a[7]), recent = x.int32(a[8]);
+    void* len_out = a[9] == a[2] ? len : x.ints(a[9], {units});
+    void* weight_out = a[10] == a[4] ? weight : x.array(a[10], g_f32, {units, room});
+    void* tokens_out = a[11] == a[5] ? tokens : x.ints_or_null(a[11], {units, room});
+    x.typed(a[12], g_u8);
+    x.dense(a[12]);
+    void* ws = x.placed(a[12]);
+    const size_t ws_bytes = x.bytes(a[12]);
+    void* st = x.stream_there();
+    return finish(x, [&] {
+        return zipvl_paged_evict(&pool.pages, (int32_t*)table, width, &d, (int32_t*)len, (int32_t*)k, (float*)weight, (int32_t*)tokens, budget, sinks, recent,
+                                 (int32_t*)len_out, (float*)weight_out, (int32_t*)tokens_out, ws, ws_bytes, st);
+    });
+}
+
 #define ZIPVL_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ZIPVL_METHOD(score), ZIPVL_METHOD(select), ZIPVL_METHOD(compact_kv), ZIPVL_METHOD(sparse_prefill), ZIPVL_METHOD(kv_append),
                          ZIPVL_METHOD(decode_step), ZIPVL_METHOD(decode_attn_q), ZIPVL_METHOD(rotate), ZIPVL_METHOD(paged_append),
-                         ZIPVL_METHOD(decode_attn_paged), {nullptr, nullptr, 0, nullptr}};
+                         ZIPVL_METHOD(decode_attn_paged), ZIPVL_METHOD(chunk_attn_paged), ZIPVL_METHOD(paged_weigh), ZIPVL_METHOD(paged_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", "Calls of libzipvl.so on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -335,8 +335,8 @@ struct WavePart {
 
     // Tiles first, first + step, ... below `end` of an item with `rows` rows and this row of a table.  K of the next tile is requested when K of this one
     // has been read, V of the next when V of this one has: a wave has one tile of each in LDS and one on the way at any time.
-    // `cache` says where pages are (K, V, num_pages, page_log2).  CAUSAL: the lane's query sees rows up to `last`.
-    template <bool AGAIN, bool CAUSAL, typename Cache>
+    // `cache` says where pages are (K, V, num_pages, page_log2).  CAUSAL: the lane's query sees rows up to `last`.  LAST: no tiles come behind these, sum_groups().
+    template <bool AGAIN, bool CAUSAL, bool LAST, typename Cache>
     __device__ __forceinline__ void tiles(const Cache& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine, int last = 0) {
         first = scalar(first);
         step = scalar(step);
@@ -404,6 +404,7 @@ struct WavePart {
             cur = nxt;
             have = more;
         }
+        if constexpr (LAST) sum_groups();
     }
     __device__ __forceinline__ void sum_groups() { l = over_groups<COLS>(l, [](float a, float b) { return a + b; }); }       // behind the last tile
 
@@ -421,12 +422,11 @@ struct WavePart {
     // finite takes its tiles again, without either.  Looking at the sums of each piece: 0.8 % of the time over the 29 calls.
     template <typename Cache>
     __device__ __forceinline__ void run(const Cache& p, const int32_t* table, int rows, int first, int step, int end, float c, char* mine) {
-        tiles<false, false>(p, table, rows, first, step, end, c, mine);
+        tiles<false, false, true>(p, table, rows, first, step, end, c, mine);
         if (spoilt()) {
             reset();
-            tiles<true, false>(p, table, rows, first, step, end, c, mine);
+            tiles<true, false, true>(p, table, rows, first, step, end, c, mine);
         }
-        sum_groups();
     }
 };
 
