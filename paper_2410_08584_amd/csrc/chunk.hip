@@ -22,6 +22,7 @@ constexpr int kRowsMany = 128;
 constexpr int kLeastMany = 4, kLeastFew = 8;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
 constexpr int kScanUnits = 2048;                             // more units than this go one workgroup a tile of rows, whatever their lengths
 
+// 8-byte fields and pairs of others only: it is read again as a row of 32-bit numbers
 struct Chunk {
     const char *K, *V;
     int num_pages, page_log2;
@@ -256,227 +257,512 @@ struct ChunkCfg {
     static constexpr int BN = sizeof(T) == 2 ? 64 : 32, NBK = BN / 32;          // keys a tile, blocks of 32 of them
     static constexpr int TILE = BN * RB, NL = TILE / 4096, RPL = 1024 / RB;     // loads of 1 KiB per wave and tile, rows per load
     static constexpr int CH = D / Elem<T>::kPerChunk, ODB = D / 32;
-    static constexpr int LDS = 4 * TILE;                     // two tiles of K, two of V
+    static constexpr int LDS = 4 * TILE + 64;                // two tiles of K, two of V, the workgroup's place for the end
     __device__ static __forceinline__ int k_swizzle(int r) { return k_row_swizzle<RB>(r); }
     __device__ static __forceinline__ int v_swizzle(int r) { return PartCfg<T, D>::v_swizzle(r); }
 };
 
-// Where a tile of keys stands: rows of a table from `first`, those that there are as bits, and 64 of the table's entries, one a lane.
-struct KeyTile { int first; bool own; uint64_t rows; };
-struct KeyWindow {
-    int entry, from;                                         // of the table's pages from ... from + 63
-    bool own;
+// Where a tile of keys stands: 16 rows each in row 16 at0 ... of the pages (which hold 16 or more), -1: in no page.  Numbers of their own, in scalar registers: an array that
+// loops walk over would stay in memory.  whole: all rows are there.
+struct KeyTile {
+    int32_t at0, at1, at2, at3;
+    bool whole;
+    __device__ __forceinline__ int32_t at(int x) const { return x == 0 ? at0 : x == 1 ? at1 : x == 2 ? at2 : at3; }
 };
 
+// A tile of rows of one unit against the keys of its piece.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p, ChunkParts out, int wgs, int direct) {
+struct Many {
     using C = ChunkCfg<T, D>;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    static_assert(sizeof(PlaceShared) <= C::LDS, "the lengths' sums stand where tiles come later");
-    Place x;
-    if (!find_place<kRowsMany, C::BN>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastMany, direct, x)) return;
-    const ChunkUnit v = chunk_unit(p, x.u, p.group_begin);
-    const int r0 = x.t * kRowsMany;
-    if (r0 >= v.rows) return;
-    const int tid = threadIdx.x, w = scalar(tid >> 6), lane = tid & 63, i = lane & 31, h = lane >> 5;
-    const int r = r0 + 32 * w + i, r_last = min(r0 + kRowsMany, v.rows) - 1;
-    const RowAt at = row_at(p, v.g, min(r, r_last));
-    const int before = v.len - v.cnt, last = before + at.token;                  // own row that the lane's token stands in
-    const int seen = scalar(between(before + row_at(p, v.g, r_last).token + 1, 0, v.len));         // own rows that a token of the tile sees
-    const int wave_first = scalar(before + row_at(p, v.g, min(r0 + 32 * w, r_last)).token);        // up to this row no lane's mask begins
-    const int tp = scalar((v.prefix_rows + C::BN - 1) / C::BN), all = tp + scalar((seen + C::BN - 1) / C::BN);
-    const int j0 = (int)((int64_t)all * x.piece / x.pieces), j1 = (int)((int64_t)all * (x.piece + 1) / x.pieces);
-    const int32_t *own_table = p.table + (int64_t)x.u * p.width, *pre_table = p.prefix_table + (int64_t)v.prefix * p.prefix_width;
-    const int prefix_rows = scalar(v.prefix_rows);
-
+    static constexpr uint64_t kWhole = C::BN == 64 ? ~0ull : 0xFFFFFFFFull;
+    const char *K, *V;
+    int num_pages, page_log2;
+    float c;
+    char* const smem;
+    const int32_t *own_table, *pre_table;
+    int prefix_rows, seen, tp;                               // rows of the prefix, own rows that a token of the tile sees, tiles of the prefix
+    int wave_first, r_first, r_last, before, G;              // up to this own row no lane's mask begins; of the wave; own rows before the new ones
+    uint32_t inv_G;
+    int w, lane, i, h;
     uintx4 qf[C::CH];
-    {
-        const T* row = query_row<T>(p, v.b, at);
-#pragma unroll
-        for (int cc = 0; cc < C::CH; ++cc) qf[cc] = load16(row + (2 * cc + h) * Elem<T>::kPerFrag);
-    }
     floatx16 o[C::ODB];
-#pragma unroll
-    for (int db = 0; db < C::ODB; ++db) o[db] = floatx16{0};
-    float m = -INFINITY, l = 0.f, l_rounded = 0.f;
+    float m, l, l_rounded;                                   // l: sum of the weights; as V was weighed by them
+    int entry[C::BN / 16];                                   // of the table, for the tile that look() was last called for: asked for a step before they are used
 
-    KeyWindow win = {-1, 0, false};
-    bool empty = true;
-    const int page_mask = (1 << p.page_log2) - 1;
-    auto locate = [&](int j) {
-        KeyTile k;
-        k.own = j >= tp;
-        k.first = (k.own ? j - tp : j) * C::BN;
-        const int left = (k.own ? seen : prefix_rows) - k.first;
-        k.rows = left >= 64 ? ~0ull : (1ull << left) - 1;
-        if (C::BN == 32) k.rows &= 0xFFFFFFFFull;
-        const int a = k.first >> p.page_log2, b = (k.first + min(left, C::BN) - 1) >> p.page_log2;
-        if (empty || win.own != k.own || b >= win.from + 64) {
-            const int width = k.own ? p.width : p.prefix_width;
-            win = {(k.own ? own_table : pre_table)[min(a + lane, width - 1)], a, k.own};
-            empty = false;
-            asm volatile("" : "+v"(win.entry));              // waited for here
-        }
-        for (int e = a; e <= b; ++e)
-            if ((unsigned)__builtin_amdgcn_readlane(win.entry, e - win.from) >= (unsigned)p.num_pages) {
-                const int f0 = max((e << p.page_log2) - k.first, 0), f1 = min(((e + 1) << p.page_log2) - k.first, C::BN);
-                k.rows &= ~((f1 >= 64 ? ~0ull : (1ull << f1) - 1) & ~((1ull << f0) - 1));
-            }
-        return k;
-    };
-    constexpr uint64_t kWhole = C::BN == 64 ? ~0ull : 0xFFFFFFFFull;
-    // a tile of K (V) to LDS; rows that are not there take one that is: they are masked, and their values weigh nothing
-    auto request = [&](const KeyTile& k, auto v_tag, unsigned lds, char* at_lds) {
-        constexpr bool V = decltype(v_tag)::value;
-        const char* pool = V ? p.V : p.K;
-        const int lr = lane / (C::RB / 16), ck = lane % (C::RB / 16);
-        if (k.rows == kWhole) {
+    __device__ __forceinline__ void look(int j) {
+        using scalar_table = const __attribute__((address_space(4))) int32_t*;
+        const bool own = j >= tp;
+        const int first = (own ? j - tp : j) * C::BN, end = own ? seen : prefix_rows;
+        const scalar_table table = (scalar_table)(own ? own_table : pre_table);
 #pragma unroll
-            for (int q = 0; q < C::NL; ++q) {
-                const int row = (q * 4 + w) * C::RPL, key = k.first + row;
-                const int64_t e = __builtin_amdgcn_readlane(win.entry, (key >> p.page_log2) - win.from);
-                const char* base = scalar_ptr(pool + ((e << p.page_log2) + (key & page_mask)) * C::RB);
-                load_kib_to_lds(base, lr * C::RB + ((ck ^ (V ? C::v_swizzle(row + lr) : C::k_swizzle(row + lr))) << 4), lds + (q * 4 + w) * 1024);
-            }
-        } else if (k.rows == 0) {
-            for (int q = 0; q < C::NL; ++q) *reinterpret_cast<uintx4*>(at_lds + (q * 4 + w) * 1024 + lane * 16) = uintx4{0, 0, 0, 0};
+        for (int x = 0; x < C::BN / 16; ++x) entry[x] = table[min(first + 16 * x, end - 1) >> page_log2];
+    }
+    __device__ __forceinline__ bool own(int j) const { return j >= tp; }
+    __device__ __forceinline__ int first(int j) const { return (own(j) ? j - tp : j) * C::BN; }
+    __device__ __forceinline__ int left(int j) const { return (own(j) ? seen : prefix_rows) - first(j); }
+    __device__ __forceinline__ KeyTile locate(int j) const {
+        KeyTile k = {0, 0, 0, 0, left(j) >= C::BN};
+        const int row = first(j);
+        auto where = [&](int x) {
+            const bool there = (unsigned)entry[x] < (unsigned)num_pages;
+            k.whole = k.whole && there;
+            return there ? (entry[x] << (page_log2 - 4)) + (((row + 16 * x) & ((1 << page_log2) - 1)) >> 4) : -1;
+        };
+        k.at0 = where(0);
+        k.at1 = where(1);
+        if constexpr (C::BN == 64) {
+            k.at2 = where(2);
+            k.at3 = where(3);
+        }
+        return k;
+    }
+    // Own tiles that all tokens of the workgroup's rows see whole.
+    __device__ __forceinline__ int clean_own() const { return between(before + divided(r_first - 32 * w, G, inv_G) + 1, 0, seen) / C::BN; }
+    // Whether some of the rows of tiles j0 ... j1 - 1 are in no page.
+    __device__ __forceinline__ bool lacks_pages(int j0, int j1) const {
+        bool lacks = false;
+        auto table = [&](const int32_t* t, int a, int b) {   // rows a ... b - 1
+            if (a < b)
+                for (int e = (a >> page_log2) + lane; e <= (b - 1) >> page_log2; e += 64) lacks |= (unsigned)t[e] >= (unsigned)num_pages;
+        };
+        table(pre_table, min(j0 * C::BN, prefix_rows), min(j1 * C::BN, prefix_rows));
+        table(own_table, max(j0 - tp, 0) * C::BN, min(max(j1 - tp, 0) * C::BN, seen));
+        return __any(lacks);
+    }
+    // the rows that there are, as bits
+    __device__ __forceinline__ uint64_t rows(const KeyTile& k, int j) const {
+        uint64_t x = left(j) >= C::BN ? kWhole : (1ull << left(j)) - 1;
+        if (k.at0 < 0) x &= ~0xFFFFull;
+        if (k.at1 < 0) x &= ~(0xFFFFull << 16);
+        if (k.at2 < 0) x &= ~(0xFFFFull << 32);
+        if (k.at3 < 0) x &= ~(0xFFFFull << 48);
+        return x;
+    }
+
+    // Load q of the wave of a whole tile of K (V): a lane's offset is the same in all of them, but for the row of the pages.
+    template <bool IS_V>
+    __device__ __forceinline__ int lane_offset() const {
+        const int lr = lane / (C::RB / 16), row = w * C::RPL + lr;
+        return (row & 15) * C::RB + (((lane % (C::RB / 16)) ^ (IS_V ? C::v_swizzle(row) : C::k_swizzle(row))) << 4);
+    }
+    template <bool IS_V>
+    __device__ __forceinline__ const char* load_base(const KeyTile& k, int q) const {
+        constexpr int kRows = 4 * C::RPL;                    // of the four waves' loads together: 8, 16 or 32
+        const int32_t at = kRows == 16 ? k.at(q) : kRows == 32 ? (w < 2 ? k.at(2 * q) : k.at(2 * q + 1)) : k.at(q / 2);
+        return scalar_ptr((IS_V ? V : K) + ((int64_t)at * 16 + (kRows == 8 ? q % 2 * 8 : 0)) * C::RB);
+    }
+    __device__ __forceinline__ char* buffer(bool v, int buf) const { return smem + (v ? 2 * C::TILE : 0) + buf * C::TILE; }
+
+    // A tile of K (V) to LDS; rows that are not there take one that is: they are masked, and their values weigh nothing
+    template <bool IS_V>
+    __device__ __forceinline__ void request(const KeyTile& k, int j, int buf) const {
+        char* const to = buffer(IS_V, buf) + w * 1024;
+        if (k.whole) {
+            const int off = lane_offset<IS_V>();
+#pragma unroll
+            for (int q = 0; q < C::NL; ++q) load_kib_to_lds(load_base<IS_V>(k, q), C::RPL == 2 && q % 2 ? off ^ 128 : off, lds_address(to) + q * 4096);      // rows of 512 bytes: the swizzle of 8 rows on
+        } else if (const uint64_t there = rows(k, j); there == 0) {
+            for (int q = 0; q < C::NL; ++q) *reinterpret_cast<uintx4*>(to + q * 4096 + lane * 16) = uintx4{0, 0, 0, 0};
         } else {
-            const int safe = __builtin_ctzll(k.rows);
+            const int safe = __builtin_ctzll(there), ck = lane % (C::RB / 16);
 #pragma unroll 1
             for (int q = 0; q < C::NL; ++q) {
-                const int row = (q * 4 + w) * C::RPL + lr, there = k.rows >> row & 1 ? row : safe, key = k.first + there;
-                const int64_t e = __shfl(win.entry, (key >> p.page_log2) - win.from);
-                load_kib_to_lds_at(pool + ((e << p.page_log2) + (key & page_mask)) * C::RB + ((ck ^ (V ? C::v_swizzle(row) : C::k_swizzle(row))) << 4),
-                                   lds + (q * 4 + w) * 1024);
+                const int row = (q * 4 + w) * C::RPL + lane / (C::RB / 16), from = there >> row & 1 ? row : safe;
+                load_kib_to_lds_at((IS_V ? V : K) + ((int64_t)k.at(from >> 4) * 16 + (from & 15)) * C::RB + ((ck ^ (IS_V ? C::v_swizzle(row) : C::k_swizzle(row))) << 4), lds_address(to) + q * 4096);
             }
         }
-    };
-    char *const kbuf = smem, *const vbuf = smem + 2 * C::TILE;
-    auto request_both = [&](const KeyTile& k, int buf) {
-        request(k, std::false_type{}, lds_address(kbuf) + buf * C::TILE, kbuf + buf * C::TILE);
-        request(k, std::true_type{}, lds_address(vbuf) + buf * C::TILE, vbuf + buf * C::TILE);
-    };
-
-    KeyTile cur = {}, nxt = {};
-    if (j0 < j1) {
-        cur = locate(j0);
-        request_both(cur, 0);
     }
-    for (int j = j0, buf = 0; j < j1; ++j, buf ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __syncthreads();                                     // the tile is there for all waves, and all have read the one before
-        if (j + 1 < j1) {
-            nxt = locate(j + 1);
-            request_both(nxt, buf ^ 1);
-        }
-        const char *kb = kbuf + buf * C::TILE, *vb = vbuf + buf * C::TILE;
-        floatx16 s[C::NBK];
+
+    __device__ __forceinline__ void reset() {
+#pragma unroll
+        for (int db = 0; db < C::ODB; ++db) o[db] = floatx16{0};
+        m = -INFINITY;
+        l = l_rounded = 0.f;
+    }
+    using Scores = floatx16[C::NBK];
+    __device__ __forceinline__ void scores(const char* kb, Scores& s) const {
 #pragma unroll
         for (int blk = 0; blk < C::NBK; ++blk) {
             s[blk] = floatx16{0};
 #pragma unroll
             for (int cc = 0; cc < C::CH; ++cc) {
-                const uintx4 kf = *reinterpret_cast<const uintx4*>(kb + (32 * blk + i) * C::RB + swz_chunk(2 * cc + h, C::k_swizzle(32 * blk + i)));
+                const uintx4 kf = *reinterpret_cast<const uintx4*>(kb + (32 * blk + i) * C::RB + swz_chunk(2 * cc + h, C::k_swizzle(i)));
                 s[blk] = mma_frag<T>(kf, qf[cc], s[blk]);
+                if (sizeof(T) == 2 && cc & 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (cur.rows != kWhole) {
+    }
+    __device__ __forceinline__ void mask(const KeyTile& k, int j, Scores& s) const {
+        if (!k.whole) {
+            const uint64_t there = rows(k, j) >> 4 * h;
 #pragma unroll
             for (int blk = 0; blk < C::NBK; ++blk)
 #pragma unroll
-                for (int y = 0; y < 16; ++y)
-                    if (!(cur.rows >> (32 * blk + acc_row(y, h)) & 1)) s[blk][y] = -INFINITY;
+                for (int y = 0; y < 16; ++y) {
+                    if (!(there >> (32 * blk + acc_row(y, 0)) & 1)) s[blk][y] = -INFINITY;
+                    __builtin_amdgcn_sched_barrier(0);       // one condition at a time: all 32 at once are 64 scalar registers
+                }
         }
-        if (cur.own && cur.first + C::BN - 1 > wave_first) {
+        if (own(j) && first(j) + C::BN - 1 > wave_first) {
+            int tid = threadIdx.x;                           // the lane's own row, said anew: it is not kept for this
+            asm volatile("" : "+v"(tid));
+            const int upto = before + divided(min(r_first + (tid & 31), r_last), G, inv_G) - first(j) - 4 * (tid >> 5 & 1);        // against numbers that the lane does not come into: those would be kept in registers
 #pragma unroll
             for (int blk = 0; blk < C::NBK; ++blk)
 #pragma unroll
-                for (int y = 0; y < 16; ++y)
-                    if (cur.first + 32 * blk + acc_row(y, h) > last) s[blk][y] = -INFINITY;
+                for (int y = 0; y < 16; ++y) {
+                    if (32 * blk + acc_row(y, 0) > upto) s[blk][y] = -INFINITY;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
         }
-        // the offset of the exponentials follows the running maximum lazily
+    }
+    __device__ __forceinline__ float largest(const Scores& s) const {
         float mx = s[0][0];
 #pragma unroll
         for (int blk = 0; blk < C::NBK; ++blk)
 #pragma unroll
             for (int y = 0; y < 16; ++y) mx = fmaxf(mx, s[blk][y]);
-        mx *= p.c;
-        if (__any(mx > m + kLazy)) {
-            mx = over_groups<32>(mx, [](float a, float b) { return fmaxf(a, b); });
-            const float m_new = fmaxf(m, mx), a = m_new > -INFINITY ? fast_exp2(m - m_new) : 1.f;
-            l *= a;
-            l_rounded *= a;
-#pragma unroll
-            for (int db = 0; db < C::ODB; ++db)
-#pragma unroll
-                for (int y = 0; y < 16; ++y) o[db][y] *= a;
-            m = m_new;
-        }
-        const float ms = m > -INFINITY ? m : 0.f;
-#pragma unroll
-        for (int blk = 0; blk < C::NBK; ++blk) {
-#pragma unroll
-            for (int y = 0; y < 16; ++y) {
-                s[blk][y] = fast_exp2(fmaf(s[blk][y], p.c, -ms));
-                l += s[blk][y];
+        return mx * c;
+    }
+    // Where a lane's address of V stands in a tile: channels 32 db ... of key 4 h + e, for the transposing reads
+    __device__ __forceinline__ int v_lane(int db) const {
+        const int e = (lane >> 2) & 3, q = lane & 3, row = 4 * h + e;
+        return row * C::RB + swz_chunk(4 * db + 2 * ((lane >> 4) & 1) + (q >> 1), C::v_swizzle(row)) + (q & 1) * 8;
+    }
+    __device__ static __forceinline__ uintx4 v_frag(const char* a0) {
+        typedef short shortx4 __attribute__((ext_vector_type(4)));
+        using lds_ptr = __attribute__((address_space(3))) shortx4*;
+        const uintx2 f0 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)a0));
+        const uintx2 f1 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a0 + 8 * C::RB)));
+        return uintx4{f0[0], f0[1], f1[0], f1[1]};
+    }
+
+    // Tiles j0 ... j1 - 1, one after the other, the offset of the exponentials behind the running maximum: any tiles, any logits
+    __device__ __forceinline__ void plain(int j0, int j1) {
+        if (j0 >= j1) return;
+        look(j0);
+        KeyTile cur = locate(j0), nxt = cur;
+        request<false>(cur, j0, 0);
+        request<true>(cur, j0, 0);
+        if (j0 + 1 < j1) look(j0 + 1);
+        for (int j = j0, buf = 0; j < j1; ++j, buf ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __syncthreads();                                 // the tile is there for all waves, and all have read the one before
+            if (j + 1 < j1) {
+                nxt = locate(j + 1);
+                request<false>(nxt, j + 1, buf ^ 1);
+                request<true>(nxt, j + 1, buf ^ 1);
+                if (j + 2 < j1) look(j + 2);
             }
-            if constexpr (sizeof(T) == 2) {
-                typedef short shortx4 __attribute__((ext_vector_type(4)));
-                using lds_ptr = __attribute__((address_space(3))) shortx4*;
-                const int e = (lane >> 2) & 3, q = lane & 3, row = 4 * h + e;
+            const char* vb = buffer(true, buf);
+            Scores s;
+            scores(buffer(false, buf), s);
+            mask(cur, j, s);
+            float mx = largest(s);
+            if (__any(mx > m + kLazy)) {
+                mx = over_groups<32>(mx, [](float a, float b) { return fmaxf(a, b); });
+                const float m_new = fmaxf(m, mx), a = m_new > -INFINITY ? fast_exp2(m - m_new) : 1.f;
+                l *= a;
+                l_rounded *= a;
 #pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    uintx4 pf;
+                for (int db = 0; db < C::ODB; ++db)
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        pf[y] = pack_bf16x2(s[blk][8 * s2 + 2 * y], s[blk][8 * s2 + 2 * y + 1]);
-                        l_rounded = add_bf16x2(pf[y], l_rounded);
-                    }
+                    for (int y = 0; y < 16; ++y) o[db][y] *= a;
+                m = m_new;
+            }
+            const float ms = m > -INFINITY ? m : 0.f;
 #pragma unroll
-                    for (int db = 0; db < C::ODB; ++db) {
-                        const char* a0 = vb + (32 * blk + 16 * s2 + row) * C::RB + swz_chunk(4 * db + 2 * ((lane >> 4) & 1) + (q >> 1), C::v_swizzle(row)) + (q & 1) * 8;
-                        const uintx2 f0 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)a0));
-                        const uintx2 f1 = __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(a0 + 8 * C::RB)));
-                        o[db] = mma_frag<__bf16>(uintx4{f0[0], f0[1], f1[0], f1[1]}, pf, o[db]);
-                    }
-                }
-            } else {
+            for (int blk = 0; blk < C::NBK; ++blk) {
 #pragma unroll
                 for (int y = 0; y < 16; ++y) {
-                    const int k = 32 * blk + acc_row(y, h);
+                    s[blk][y] = fast_exp2(fmaf(s[blk][y], c, -ms));
+                    l += s[blk][y];
+                }
+                if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                    for (int db = 0; db < C::ODB; ++db) {
-                        const float vv = *reinterpret_cast<const float*>(vb + k * C::RB + swz_chunk(8 * db + (i >> 2), C::v_swizzle(k)) + (i & 3) * 4);
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv, s[blk][y], o[db], 0, 0, 0);
+                    for (int s2 = 0; s2 < 2; ++s2) {
+                        uintx4 pf;
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            pf[y] = pack_bf16x2(s[blk][8 * s2 + 2 * y], s[blk][8 * s2 + 2 * y + 1]);
+                            l_rounded = add_bf16x2(pf[y], l_rounded);
+                        }
+#pragma unroll
+                        for (int db = 0; db < C::ODB; ++db) o[db] = mma_frag<__bf16>(v_frag(vb + v_lane(db) + (32 * blk + 16 * s2) * C::RB), pf, o[db]);
+                    }
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) {
+                        const int k = 32 * blk + acc_row(y, h);
+#pragma unroll
+                        for (int db = 0; db < C::ODB; ++db) {
+                            const float vv = *reinterpret_cast<const float*>(vb + k * C::RB + swz_chunk(8 * db + (i >> 2), C::v_swizzle(k)) + (i & 3) * 4);
+                            o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv, s[blk][y], o[db], 0, 0, 0);
+                        }
                     }
                 }
             }
+            cur = nxt;
         }
-        cur = nxt;
+        __syncthreads();
+    }
+
+    // bf16: n tiles from j0, an even number of 4 or more, all rows of which are there and seen by all queries, three tiles deep.  A step multiplies P V of tile t - 1 and takes half
+    // of the exponentials of tile t in its first half, multiplies K Q^T of tile t + 1 and takes the other half in its second: nothing in a step waits for anything
+    // else in it, and the order of instructions is written out - behind every product its share of the vector work, in front of it the reads of an operand three products
+    // ahead, the requests (K of tile t + 2, V of t + 1) one at a time.  The offset of the exponentials stays, or is the first tile's maximum if there was no
+    // tile before: right as long as no sum leaves the middle of the fp32 range, which the caller looks at.
+    // The steps are a loop of their own without any other way through them: with one for tiles that lack rows beside it, operands spilled in both.
+    static constexpr int kAhead = 3;
+    __device__ __forceinline__ void piped(int j0, int n) {
+        static_assert(sizeof(T) == 2, "");
+        using Probs = uintx4[2][2];
+        const int koff = lane_offset<false>(), voff = lane_offset<true>(), vl = v_lane(0);      // V of channel block db: the swizzle takes its number by exclusive or
+        Scores sa, sb;
+        Probs pa, pb;
+        auto exps = [&](int blk, Scores& sc, Probs& pc) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float e0 = fast_exp2(fmaf(sc[blk][r], c, -m)), e1 = fast_exp2(fmaf(sc[blk][r + 1], c, -m));
+                const uint32_t pk = pack_bf16x2(e0, e1);
+                pc[blk][r >> 3][(r & 7) >> 1] = pk;
+                l_rounded = add_bf16x2(pk, l_rounded);
+                l += e0 + e1;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto weighted = [&](const char* vb, Probs& pp) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < 4 * C::ODB; ++j) {
+                o[j % C::ODB] = mma_frag<__bf16>(v_frag(vb + (vl ^ (j % C::ODB) << 6) + (32 * (j / (2 * C::ODB)) + 16 * (j / C::ODB & 1)) * C::RB), pp[j / (2 * C::ODB)][j / C::ODB & 1], o[j % C::ODB]);
+                if (j & 1) __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto all_there = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); __syncthreads(); };
+        auto look_or_last = [&](int t) { look(j0 + min(t, n - 1)); };                // behind the last tile that again, unread
+        look(j0);
+        KeyTile next, after;                                 // tiles t + 1, t + 2 of step t
+        {
+            const KeyTile c0 = locate(j0);
+            look(j0 + 1);
+            const KeyTile c1 = locate(j0 + 1);
+            look(j0 + 2);
+            request<false>(c0, j0, 0);
+            request<false>(c1, j0 + 1, 1);
+            request<true>(c0, j0, 0);
+            all_there();
+            scores(buffer(false, 0), sa);
+            if (__any(m == -INFINITY)) {
+                const float mx = over_groups<32>(largest(sa), [](float a, float b) { return fmaxf(a, b); });
+                if (m == -INFINITY) m = mx;                  // of lanes that have met none: no sums yet
+            }
+            exps(0, sa, pb);
+            exps(1, sa, pb);
+            scores(buffer(false, 1), sb);
+            all_there();                                     // K of both has been read by all
+            next = locate(j0 + 2);
+            request<false>(next, j0 + 2, 0);
+            request<true>(c1, j0 + 1, 1);
+            look_or_last(3);
+        }
+        auto half = [&](auto half_tag, const char* src, Scores& sc, Scores& sn, Probs& pp, Probs& pc, const KeyTile& k, unsigned to) __attribute__((always_inline)) {
+            constexpr int HALF = decltype(half_tag)::value, NM = HALF == 0 ? 4 * C::ODB : 2 * C::CH, PPM = 16 / NM;
+            uintx4 frag[NM];
+            float e[16];
+            auto read = [&](int j) __attribute__((always_inline)) {
+                if constexpr (HALF == 0) frag[j] = v_frag(src + (vl ^ (j % C::ODB) << 6) + (32 * (j / (2 * C::ODB)) + 16 * (j / C::ODB & 1)) * C::RB);
+                else frag[j] = *reinterpret_cast<const uintx4*>(src + (32 * (j & 1) + i) * C::RB + swz_chunk(2 * (j >> 1) + h, C::k_swizzle(i)));
+            };
+            auto vector = [&](int q) __attribute__((always_inline)) {       // 16 pieces: half a pair of keys each
+                const int r = q & ~1;
+                if ((q & 1) == 0) {
+                    e[r] = fast_exp2(fmaf(sc[HALF][r], c, -m));
+                    e[r + 1] = fmaf(sc[HALF][r + 1], c, -m);
+                } else {
+                    e[r + 1] = fast_exp2(e[r + 1]);
+#pragma unroll
+                    for (int L = 0; L < C::NL; ++L)
+                        if (q == (((2 * L + 1) * 16 / (2 * C::NL)) | 1)) {
+                            unsigned pin = __float_as_uint(e[r + 1]);
+                            load_kib_to_lds_pinned(load_base<HALF == 1>(k, L), HALF == 0 ? koff : voff, to + L * 4096, pin);
+                            e[r + 1] = __uint_as_float(pin);
+                        }
+                    const uint32_t pk = pack_bf16x2(e[r], e[r + 1]);
+                    pc[HALF][r >> 3][(r & 7) >> 1] = pk;
+                    l_rounded = add_bf16x2(pk, l_rounded);
+                    l += e[r] + e[r + 1];
+                }
+            };
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) read(j);
+#pragma unroll
+            for (int j = 0; j < NM; ++j) {
+                if (j + kAhead < NM) read(j + kAhead);
+                if constexpr (HALF == 0) o[j % C::ODB] = mma_frag<__bf16>(frag[j], pp[j / (2 * C::ODB)][j / C::ODB & 1], o[j % C::ODB]);
+                else sn[j & 1] = mma_frag<__bf16>(frag[j], qf[j >> 1], j < 2 ? floatx16{0} : sn[j & 1]);
+#pragma unroll
+                for (int q = 0; q < PPM; ++q) vector(j * PPM + q);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto wait = [&]() __attribute__((always_inline)) {   // all but the last two requests of tiles have landed, and the wave's LDS reads
+            __builtin_amdgcn_s_waitcnt(0x0070 | ((2 * C::NL) & 15) | (((2 * C::NL) >> 4) << 14));
+            __syncthreads();
+        };
+        // V of tile t - 1, K of tile t + 1 are there or on their way, V of tile t behind them; ODD: t is
+        auto step = [&](auto odd_tag, int t, Scores& sc, Scores& sn, Probs& pp, Probs& pc) __attribute__((always_inline)) {
+            constexpr int ODD = decltype(odd_tag)::value;
+            after = locate(j0 + min(t + 2, n - 1));
+            look_or_last(t + 3);
+            half(std::integral_constant<int, 0>{}, buffer(true, !ODD), sc, sn, pp, pc, after, lds_address(buffer(false, ODD)) + w * 1024);
+            wait();                                          // K of tile t + 1 is there
+            half(std::integral_constant<int, 1>{}, buffer(false, !ODD), sc, sn, pp, pc, next, lds_address(buffer(true, !ODD)) + w * 1024);
+            wait();                                          // V of tile t is there
+            next = after;
+        };
+        for (int t = 1; t < n - 1; t += 2) {
+            step(std::integral_constant<int, 1>{}, t, sb, sa, pb, pa);
+            step(std::integral_constant<int, 0>{}, t + 1, sa, sb, pa, pb);
+        }
+        weighted(buffer(true, 0), pb);                       // tile n - 2
+        all_there();
+        exps(0, sb, pa);
+        exps(1, sb, pa);
+        weighted(buffer(true, 1), pa);
+        __syncthreads();
+    }
+};
+
+// Sums of the offset that stays, outside which the tiles are repeated with running maxima.
+constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p64f;
+
+// The kernel's arguments, read again: kept in scalar registers through the tiles they spilled.
+template <typename A>
+__device__ __forceinline__ A read_again(int offset) {
+    typedef const __attribute__((address_space(4))) char* const_ptr;
+    const_ptr at = (const_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    A x;
+    static_assert(sizeof(A) % 4 == 0, "");
+    uint32_t* to = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(A) / 4; ++i) to[i] = reinterpret_cast<const __attribute__((address_space(4))) uint32_t*>(at + offset)[i];
+    return x;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts out_, int wgs, int direct) {
+    using C = ChunkCfg<T, D>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    // of the workgroup, for the end; behind the tiles, which then begin where LDS does: their addresses fit an instruction's offset
+    struct Held { Place x; int b, g, rows, j0, j1, sees_from, again; };
+    static_assert(sizeof(Held) <= 64, "");
+    Held& held = *reinterpret_cast<Held*>(smem + 4 * C::TILE);
+    static_assert(sizeof(PlaceShared) <= 4 * C::TILE, "the lengths' sums stand where tiles come later");
+    Many<T, D> many = {p_.K, p_.V, p_.num_pages, p_.page_log2, p_.c, smem};
+    int j0, j1, r0;
+    {
+        const Chunk p = read_again<Chunk>(0);
+        const ChunkParts out = read_again<ChunkParts>(sizeof(Chunk));
+        Place x;
+        if (!find_place<kRowsMany, C::BN>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastMany, direct, x)) return;
+        const ChunkUnit v = chunk_unit(p, x.u, p.group_begin);
+        r0 = x.t * kRowsMany;
+        if (r0 >= v.rows) return;
+        const int tid = threadIdx.x;
+        many.w = scalar(tid >> 6);
+        many.lane = tid & 63;
+        many.i = tid & 31;
+        many.h = tid >> 5 & 1;
+        many.r_first = r0 + 32 * many.w;
+        many.r_last = scalar(min(r0 + kRowsMany, v.rows) - 1);
+        many.before = scalar(v.len - v.cnt);
+        many.G = p.G;
+        many.inv_G = p.inv_G;
+        many.own_table = p.table + (int64_t)x.u * p.width;
+        many.pre_table = p.prefix_table + (int64_t)scalar(v.prefix) * p.prefix_width;
+        many.prefix_rows = scalar(v.prefix_rows);
+        many.seen = scalar(between(many.before + divided(many.r_last, p.G, p.inv_G) + 1, 0, v.len));
+        many.tp = scalar((v.prefix_rows + C::BN - 1) / C::BN);
+        many.wave_first = scalar(many.before + divided(min(many.r_first, many.r_last), p.G, p.inv_G));
+        const int all = many.tp + scalar((many.seen + C::BN - 1) / C::BN);
+        j0 = scalar((int)((int64_t)all * x.piece / x.pieces));
+        j1 = scalar((int)((int64_t)all * (x.piece + 1) / x.pieces));
+        if (tid == 0) held = {x, v.b, v.g, v.rows, j0, j1, j0 < j1 ? j0 < many.tp ? INT32_MIN : (j0 - many.tp) * C::BN : INT32_MAX, 0};
+        __syncthreads();
+        const T* row = query_row<T>(p, v.b, row_at(p, v.g, min(many.r_first + many.i, many.r_last)));
+#pragma unroll
+        for (int cc = 0; cc < C::CH; ++cc) many.qf[cc] = load16(row + (2 * cc + many.h) * Elem<T>::kPerFrag);
     }
     auto both = [](float a) { return over_groups<32>(a, [](float p, float q) { return p + q; }); };
-    l = both(l);
-    const float weight = sizeof(T) == 2 ? both(l_rounded) : l;       // what V was weighed by
-    if (r > r_last) return;
-    if (x.pieces == 1) {
+    // What follows the tiles goes by numbers read and said anew: registers are scarce among them.
+    struct End { Place x; int b, g, i, h, r, r_last, token; };
+    auto end = [&](const Chunk& p) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        End e;
+        e.x = held.x;
+        e.b = held.b;
+        e.g = held.g;
+        e.i = tid & 31;
+        e.h = tid >> 5 & 1;
+        e.r = held.x.t * kRowsMany + 32 * (tid >> 6) + e.i;
+        e.r_last = min((held.x.t + 1) * kRowsMany, held.rows) - 1;
+        e.token = divided(min(e.r, e.r_last), p.G, p.inv_G);
+        return e;
+    };
+    float l;
+    if constexpr (sizeof(T) == 2) {
+        for (bool safe = many.lacks_pages(j0, j1);; safe = true) {
+            many.reset();
+            int j = j0;
+#pragma unroll 1
+            for (int own = 0; own < 2; ++own) {              // the prefix, then the unit's rows: first the tiles that have all rows and are seen by all, then others up to the next such
+                const int clean = own ? max(j, many.tp + many.clean_own()) : many.prefix_rows / C::BN, n = max(0, min(clean, j1) - j) & ~1;
+                if (!safe && n >= 4) {
+                    many.piped(j, n);
+                    j += n;
+                }
+                const int upto = own ? j1 : min(j1, max(j, many.tp));
+                many.plain(j, upto);
+                j = upto;
+            }
+            l = both(many.l);
+            if (safe) break;
+            const bool sees = many.before + end(read_again<Chunk>(0)).token >= held.sees_from;      // a key of the piece
+            if (__any(sees && !(l >= kSumLow && l <= kSumHigh)) && threadIdx.x % 64 == 0) held.again = 1;
+            __syncthreads();
+            if (!scalar(held.again)) break;
+        }
+    } else {
+        many.reset();
+        many.plain(j0, j1);
+        l = both(many.l);
+    }
+    const Chunk p = read_again<Chunk>(0);
+    const float m = many.m, weight = sizeof(T) == 2 ? both(many.l_rounded) : l;      // what V was weighed by
+    const End e = end(p);
+    if (e.r > e.r_last) return;
+    const RowAt at = {e.token, e.g * p.G + e.r - e.token * p.G};
+    auto four = [&](int db, int a) { return floatx4{many.o[db][4 * a], many.o[db][4 * a + 1], many.o[db][4 * a + 2], many.o[db][4 * a + 3]}; };
+    if (e.x.pieces == 1) {
         const float inv = weight > 0.f ? 1.f / weight : 0.f;
-        T* row = out_row<T>(p, v.b, at);
+        T* row = out_row<T>(p, e.b, at);
 #pragma unroll
         for (int db = 0; db < C::ODB; ++db)
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
-                store4(row + 32 * db + 8 * a + 4 * h, floatx4{o[db][4 * a], o[db][4 * a + 1], o[db][4 * a + 2], o[db][4 * a + 3]} * inv);
-        if (p.lse && h == 0) *lse_at(p, v.b, at) = log_sum(m, l);
+            for (int a = 0; a < 4; ++a) store4(row + 32 * db + 8 * a + 4 * e.h, four(db, a) * inv);
+        if (p.lse && e.h == 0) *lse_at(p, e.b, at) = log_sum(m, l);
     } else {
         // the sums to the part's own unrounded one, so that parts are joined by one number
+        const ChunkParts out = read_again<ChunkParts>(sizeof(Chunk));
         const float f = weight > 0.f ? l / weight : 0.f;
-        const int64_t rec = (int64_t)(x.record + x.piece * x.tiles + x.t) * kRowsMany + 32 * w + i;
+        const int64_t rec = (int64_t)(e.x.record + e.x.piece * e.x.tiles + e.x.t) * kRowsMany + e.r % kRowsMany;
 #pragma unroll
         for (int db = 0; db < C::ODB; ++db)
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
-                *reinterpret_cast<floatx4*>(out.o + rec * D + 32 * db + 8 * a + 4 * h) = floatx4{o[db][4 * a], o[db][4 * a + 1], o[db][4 * a + 2], o[db][4 * a + 3]} * f;
-        if (h == 0) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(m, l);
+            for (int a = 0; a < 4; ++a) *reinterpret_cast<floatx4*>(out.o + rec * D + 32 * db + 8 * a + 4 * e.h) = four(db, a) * f;
+        if (e.h == 0) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(l > 0.f ? m : -INFINITY, l);
     }
 }
 
