@@ -56,6 +56,13 @@ __device__ __forceinline__ void load_dwords_to_lds(const char* gbase, int goff, 
                  :: "s"(m0v), "v"(goff), "s"(gbase) : "memory", "m0");
 }
 
+// The same with a 64-bit address per lane.
+__device__ __forceinline__ void load_dwords_to_lds_at(const char* lane_ptr, unsigned lds_base) {
+    const unsigned m0v = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                 :: "s"(m0v), "v"(lane_ptr) : "memory", "m0");
+}
+
 // The first load, placed by data flow instead of by program order: it is tied to a register (`pin`, passed
 // through unchanged) so that it issues after the instruction that produced `pin` and before the one that
 // consumes it, without ordering the surrounding LDS reads the way a statement with side effects would.

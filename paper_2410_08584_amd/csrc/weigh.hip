@@ -1,9 +1,14 @@
 // The attention weight that cached rows get from new queries: weight[u, r] = before[u, r] + sum over heads and tokens of exp(scale q.k - lse).
 //
-// Keys stay, queries come: a wave has 32 keys in registers, S = K Q^T on matrix tiles gives a lane one query and 16 keys, whose exponentials it
-// adds up over all queries; the 32 lanes meet once, at the end.  No sum crosses workgroups, so no order of arrival changes a result.
-// Few queries (a decode step): the read of K.  Many: products, and exponentials at a quarter of the vector rate.
+// Keys stay, queries come: a wave has 32 or 64 keys in registers, S = K Q^T on matrix tiles gives a lane one query and 16 keys of each 32, whose exponentials it
+// adds up over all queries; the 32 lanes, and the waves that share keys, meet once, at the end.  No sum crosses workgroups and no wave waits for another before that, so no order of
+// arrival changes a result.  Queries come from L1 and L2 straight into registers, a tile of 32 ahead.
+// fp32 numbers go as three planes of bf16 (planes.h): six products instead of one that takes sixteen times as long.
+// Few queries (a decode step) are bound by the read of K, many by products and by exponentials at a quarter of the vector rate.
+#include <atomic>
+
 #include "launch.h"
+#include "planes.h"
 #include "wavepart.h"
 
 namespace zipvl {
@@ -20,91 +25,309 @@ struct Weigh {
     float scale;
 };
 
-template <typename T, int D>
+// Operands of 16 channels of 32 rows, a row a lane (halves of the wave: 8 channels each).
+template <typename T> struct Rows;
+template <> struct Rows<__bf16> {
+    using Raw = uintx4;
+    using Frag = uintx4;
+    __device__ static __forceinline__ Frag split(const Raw& x) { return x; }
+    __device__ static __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 acc) { return mma_frag<__bf16>(a, b, acc); }
+    __device__ static __forceinline__ float largest(const Raw&, float most) { return most; }
+    __device__ static __forceinline__ Raw load(const char* row, int cc, int h) { return load16(row + 32 * cc + 16 * h); }
+    template <int RB> __device__ static __forceinline__ Raw from_lds(const char* row, int r, int cc, int h) { return load16(row + swz_chunk(2 * cc + h, k_row_swizzle<RB>(r))); }
+};
+template <> struct Rows<float> {
+    struct Raw { uintx4 a, b; };
+    using Frag = Planes;
+    __device__ static __forceinline__ Frag split(const Raw& x) { return split8(x.a, x.b); }
+    __device__ static __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 acc) { return mma_planes(a, b, acc); }
+    __device__ static __forceinline__ float largest(const Raw& x, float most) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(most) : "v"(x.a[e]), "v"(x.b[e]));
+        return most;
+    }
+    __device__ static __forceinline__ Raw load(const char* row, int cc, int h) { return {load16(row + 64 * cc + 32 * h), load16(row + 64 * cc + 32 * h + 16)}; }
+    template <int RB> __device__ static __forceinline__ Raw from_lds(const char* row, int r, int cc, int h) {
+        const int sw = k_row_swizzle<RB>(r);
+        return {load16(row + swz_chunk(4 * cc + 2 * h, sw)), load16(row + swz_chunk(4 * cc + 2 * h + 1, sw))};
+    }
+};
+// Planes are off by 2^-134 where a number is small (planes.h): nothing in a logit as long as what it is multiplied by is below this.  A wave that meets larger
+// numbers takes its tiles in fp32 products.
+constexpr float kPlaneHigh = 0x1p100f;
+
+// 32 KB keys a wave.  QW = 1: the four waves have keys of their own and share tiles of queries; 4: they have the same keys and take every fourth tile, each from LDS of its own.
+// A tile is of queries that follow each other head by head, token by token, or, WIDE, of tokens of one head: its rows are then at one distance and asked for without a
+// vector instruction, and n is long enough that a last tile with few tokens is no loss.  FEW: of queries, so that short tiles of them will do.
+template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
 struct WeighCfg {
-    static constexpr int RB = D * (int)sizeof(T), QT = sizeof(T) == 2 ? 64 : 32;        // queries a tile
-    static constexpr int TILE = QT * RB, NL = TILE / 4096, RPL = 1024 / RB, CH = D / Elem<T>::kPerChunk;
+    static constexpr int RB = D * (int)sizeof(T), CH = D / 16, KEYS = 32 * KB * (4 / QW);
+    static constexpr int QT = QW == 1 && sizeof(T) == 2 && !FEW ? 64 : 32, SHARE = 4 / QW;       // queries a tile, waves that share it
+    static constexpr int TILE = QT * RB, NL = TILE / 1024 / SHARE, RPL = 1024 / RB;  // loads of 1 KiB a wave, rows a load
+    static constexpr int BUF = TILE + 256 * SHARE;                                   // a tile, and each wave's copy of its lse
+    // Tiles on the way, beside the one that is read.  A wave that has its tiles to itself takes one into registers and asks for the next into its place, where
+    // there are registers for it (511 tokens of three prompts, fp32: 55.3 us, with two buffers 57.3).
+    static constexpr int AHEAD = QW > 1 && RB <= 256 ? 0 : QW > 1 || FEW ? 1 : 2;
+    static constexpr int LDS = (AHEAD + 1) * BUF * QW;
 };
 
-template <typename T, int D>
+template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
 __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
-    using C = WeighCfg<T, D>;
-    __shared__ __attribute__((aligned(16))) char tile[2 * C::TILE];
-    const int u = blockIdx.y, k0 = blockIdx.x * 128, room = p.width << p.page_log2;
-    const int len = scalar(max(0, min(p.len[u], room)));
-    if (k0 >= len) return;
+    using R = Rows<T>;
+    using C = WeighCfg<T, D, KB, QW, WIDE, FEW>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ float meet[4][32 * KB];
+    const int u = blockIdx.y, k0 = blockIdx.x * C::KEYS, room = p.width << p.page_log2;
     const int tid = threadIdx.x, w = scalar(tid >> 6), lane = tid & 63, i = lane & 31, h = lane >> 5;
-    const int b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv;
-    const int cnt = p.cnt ? scalar(max(0, min(p.cnt[u], p.n))) : p.n, rows = cnt * p.G, first = len - cnt;     // token i stands in row first + i
-    const int key0 = k0 + 32 * w, key = min(key0 + i, len - 1);
-    const int entry = p.table[(int64_t)u * p.width + (key >> p.page_log2)];
-    const bool there = (unsigned)entry < (unsigned)p.num_pages;
-    uintx4 kf[C::CH];
-    {
-        const char* row = p.K + (((int64_t)(there ? entry : 0) << p.page_log2) + (key & ((1 << p.page_log2) - 1))) * C::RB;
+    const int key0 = k0 + 32 * KB * (w / QW), qw = w % QW;
+    // All that a workgroup goes by is asked for at once: the table's entries also of rows behind the length, if it has room for them.
+    const int len_there = p.len[u], cnt_there = p.cnt ? p.cnt[u] : p.n;
+    int entry[KB];
 #pragma unroll
-        for (int cc = 0; cc < C::CH; ++cc) kf[cc] = load16(row + (2 * cc + h) * 16);
+    for (int kb = 0; kb < KB; ++kb) entry[kb] = p.table[(int64_t)u * p.width + (min(key0 + 32 * kb + i, room - 1) >> p.page_log2)];
+    const int64_t at0 = (int64_t)u * room + key0;
+    float was[KB] = {};                                      // of row lane of the wave (64 at a time)
+    if (p.before && qw == 0)
+#pragma unroll
+        for (int x = 0; x < (KB + 1) / 2; ++x)
+            if (64 * x + lane < 32 * KB && key0 + 64 * x + lane < room) was[x] = p.before[at0 + 64 * x + lane];
+    const int len = scalar(max(0, min(len_there, room))), cnt = scalar(max(0, min(cnt_there, p.n)));
+    if (k0 >= len) return;
+    const int b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv, rows = cnt * p.G, first = len - cnt;        // token i stands in row first + i
+    // Rows of the wave's keys.  Rows that are not there read row 0 of the pages and get nothing.
+    const char* key_row[KB];
+    bool there[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        const int key = key0 + 32 * kb + i;
+        there[kb] = key < len && (unsigned)entry[kb] < (unsigned)p.num_pages;
+        key_row[kb] = p.K + (there[kb] ? ((int64_t)entry[kb] << p.page_log2) + (key & ((1 << p.page_log2) - 1)) : 0) * C::RB;
     }
-    float sum[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sum[r] = 0.f;
-    // row r: token r / G, head r % G; the first token that sees a key of the workgroup
-    const int r_first = max(0, k0 - first) * p.G, t0 = r_first / C::QT, t1 = (rows + C::QT - 1) / C::QT;
+    const char* const queries = p.Q + (b * p.q[0] + (int64_t)g * p.G * p.q[1]) * (int64_t)sizeof(T);
+    const char* const lses = reinterpret_cast<const char*>(p.lse + ((int64_t)b * p.Hq + g * p.G) * p.lse_pitch);
+    const int64_t token_bytes = p.q[2] * (int64_t)sizeof(T), head_bytes = p.q[1] * (int64_t)sizeof(T), pitch = p.lse_pitch * 4;
+    char* const ring = smem + (QW == 1 ? 0 : w * (C::AHEAD + 1) * C::BUF);
+    const int part = QW == 1 ? w : 0;                        // of a shared tile
+    // Tiles from the first token that sees a key of those that share them, qw tiles on for each wave of the same keys.
+    const int skipped = max(0, (QW == 1 ? k0 : key0) - first);
+    const int t0 = (WIDE ? skipped / C::QT * p.G : skipped * p.G / C::QT) + qw, t1 = WIDE ? (cnt + C::QT - 1) / C::QT * p.G : (rows + C::QT - 1) / C::QT;
+    // !WIDE: row r: token r / G, head r % G.  The rows that a lane asks for, one in each load and one lse, are QT QW rows on with every tile, which is `tokens` tokens and
+    // `heads` heads, and where those run over a token more: sums, since products of numbers of 64 bits took as long as the tile's own.
+    const int tokens = C::QT * QW / p.G, heads = C::QT * QW - tokens * p.G;
+    const int64_t row_step = tokens * token_bytes + heads * head_bytes, row_carry = token_bytes - p.G * head_bytes;
+    const int64_t lse_step = tokens * 4 + heads * pitch, lse_carry = 4 - p.G * pitch;
+    struct Walk { const char* at; int r, head; };
+    Walk row[WIDE ? 1 : C::NL], number;
+    auto begin = [&](Walk& x, int r, const char* from, int64_t token_step, int64_t head_step) {
+        const int token = divided(r, p.G, p.inv_G);
+        x.r = r;
+        x.head = r - token * p.G;
+        x.at = from + token * token_step + x.head * head_step;
+    };
+    auto walk = [&](Walk& x, const char* from, int64_t step, int64_t carry) {        // where it stands, in the first row for rows that are not there; and on
+        const char* at = x.r < rows ? x.at : from;
+        x.r += C::QT * QW;
+        x.head += heads;
+        x.at += step;
+        if (x.head >= p.G) {
+            x.head -= p.G;
+            x.at += carry;
+        }
+        return at;
+    };
+    auto in_tile = [&](int x) { return (x * C::SHARE + part) * C::RPL + lane / (C::RB / 16); };  // the lane's row of load x
+    auto chunk = [&](int x) { return swz_chunk(lane % (C::RB / 16), k_row_swizzle<C::RB>(in_tile(x))); };
     auto request = [&](int t, int buf) {
+        const unsigned to = lds_address(ring) + buf * C::BUF;
+        if constexpr (WIDE) {
+            const int block = divided(t, p.G, p.inv_G), head = t - block * p.G, token = block * C::QT, left = cnt - 1 - token;
+            const char* from = scalar_ptr(queries + head * head_bytes + token * token_bytes);
+            const char* numbers = scalar_ptr(lses + head * pitch + token * 4);
 #pragma unroll
-        for (int q = 0; q < C::NL; ++q) {
-            const int at = (q * 4 + w) * C::RPL + lane / (C::RB / 16), r = min(t * C::QT + at, rows - 1), token = divided(r, p.G, p.inv_G);
-            const T* row = reinterpret_cast<const T*>(p.Q) + b * p.q[0] + (g * p.G + r - token * p.G) * p.q[1] + token * p.q[2];
-            load_kib_to_lds_at(reinterpret_cast<const char*>(row) + swz_chunk(lane % (C::RB / 16), k_row_swizzle<C::RB>(at)),
-                               lds_address(tile) + buf * C::TILE + (q * 4 + w) * 1024);
+            for (int x = 0; x < C::NL; ++x) {
+                const int at = left >= C::QT - 1 ? in_tile(x) : min(in_tile(x), left);
+                load_kib_to_lds(from, at * (int)token_bytes + chunk(x), to + (x * C::SHARE + part) * 1024);
+            }
+            load_dwords_to_lds(numbers, 4 * min(C::QT == 64 ? lane : i, left), to + C::TILE + part * 256);
+        } else {
+#pragma unroll
+            for (int x = 0; x < C::NL; ++x) load_kib_to_lds_at(walk(row[x], queries, row_step, row_carry) + chunk(x), to + (x * C::SHARE + part) * 1024);
+            load_dwords_to_lds_at(walk(number, lses, lse_step, lse_carry), to + C::TILE + part * 256);
         }
     };
-    if (t0 < t1) request(t0, 0);
-    for (int t = t0, buf = 0; t < t1; ++t, buf ^= 1) {
-        float lse[C::QT / 32];
-        int last[C::QT / 32];
+    const float c = p.scale * kLog2e;
+    float sum[KB][16];
+    // exp(x - lse) = 2^(x log2 e - whole) * 2^(whole - lse log2 e), with a whole number near lse log2 e: the second factor is one a query, and no logit loses bits to lse.
+    struct Base { float whole, factor; };
+    auto base_of = [&](float lse) {
+        const float whole = rintf(lse * kLog2e);
+        Base x = {whole, fast_exp2(fmaf(-lse, kLog2e, whole))};
+        if (__builtin_isinf(lse)) x = {1e9f, 0.f};           // a query that sees nothing weighs nothing
+        return x;
+    };
+    auto add = [&](int kb, const floatx16& s, const Base& base, auto whole, int last) __attribute__((always_inline)) {
+        const int upto = last - key0 - 32 * kb - 4 * h;
 #pragma unroll
-        for (int x = 0; x < C::QT / 32; ++x) {
-            const int r = t * C::QT + 32 * x + i, rr = min(r, rows - 1), token = divided(rr, p.G, p.inv_G);
-            lse[x] = p.lse[((int64_t)b * p.Hq + g * p.G + rr - token * p.G) * p.lse_pitch + token];
-            if (lse[x] == -INFINITY) lse[x] = INFINITY;      // a query that sees nothing
-            last[x] = r < rows ? first + token : -1;
+        for (int r = 0; r < 16; ++r) {
+            float e = fast_exp2(fmaf(s[r], c, -base.whole));
+            if (!decltype(whole)::value && acc_row(r, 0) > upto) e = 0.f;
+            sum[kb][r] = fmaf(e, base.factor, sum[kb][r]);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (t + 1 < t1) request(t + 1, buf ^ 1);
-        const bool whole = first + divided(t * C::QT, p.G, p.inv_G) >= key0 + 31 && (t + 1) * C::QT <= rows;       // every query sees every key of the wave
+    };
+    // the token of query `at` of a tile, cnt or more where there is none
+    auto token_of = [&](int t, int at) {
+        if constexpr (WIDE) return divided(t, p.G, p.inv_G) * C::QT + at;
+        else return t * C::QT + at < rows ? divided(t * C::QT + at, p.G, p.inv_G) : cnt;
+    };
+    auto last_of = [&](int token) { return token < cnt ? first + token : -1; };      // own row that a token stands in
+    auto clear = [&]() {
 #pragma unroll
-        for (int x = 0; x < C::QT / 32; ++x) {
-            floatx16 s = {0};
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[kb][r] = 0.f;
+    };
+    float most = 0.f;
+    clear();
+    if (t0 < t1) {
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int x = 0; x < C::NL; ++x) begin(row[x], t0 * C::QT + in_tile(x), queries, token_bytes, head_bytes);
+            begin(number, t0 * C::QT + (C::QT == 64 ? lane : i), lses, 4, pitch);
+        }
+#pragma unroll
+        for (int x = 0; x < max(C::AHEAD, 1); ++x)
+            if (t0 + x * QW < t1) request(t0 + x * QW, x);
+        typename R::Frag kf[KB][C::CH];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int cc = 0; cc < C::CH; ++cc) {
-                const uintx4 qf = *reinterpret_cast<const uintx4*>(tile + buf * C::TILE + (32 * x + i) * C::RB + swz_chunk(2 * cc + h, k_row_swizzle<C::RB>(32 * x + i)));
-                s = mma_frag<T>(kf[cc], qf, s);
+                const typename R::Raw x = R::load(key_row[kb], cc, h);
+                if (there[kb]) most = R::largest(x, most);
+                kf[kb][cc] = R::split(x);
             }
+        int buf = 0;
+        for (int t = t0; t < t1; t += QW) {
+            if (C::AHEAD > 1 && t + QW < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::NL + 1) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if constexpr (QW == 1) __syncthreads();          // the tile is there for all waves, and all have read the one before
+            else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            const char* tile = ring + buf * C::BUF;
+            typename R::Raw held[C::AHEAD ? 1 : C::CH];
+            float held_lse = 0.f;
+            if constexpr (C::AHEAD > 0) {
+                if (t + C::AHEAD * QW < t1) request(t + C::AHEAD * QW, buf == 0 ? C::AHEAD : buf - 1);
+            } else {
+                static_assert(C::AHEAD || C::QT == 32, "");
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float e = fast_exp2(fmaf(s[r], p.scale, -lse[x]) * kLog2e);
-                if (!whole && key0 + acc_row(r, h) > last[x]) e = 0.f;
-                sum[r] += e;
+                for (int cc = 0; cc < C::CH; ++cc) held[cc] = R::template from_lds<C::RB>(tile + i * C::RB, i, cc, h);
+                held_lse = *reinterpret_cast<const float*>(tile + C::TILE + part * 256 + i * 4);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (t + QW < t1) request(t + QW, 0);
+            }
+            auto weigh_tile = [&](auto whole) __attribute__((always_inline)) {
+#pragma unroll
+                for (int x = 0; x < C::QT / 32; ++x) {
+                    const int r = 32 * x + i;
+                    const Base base = base_of(C::AHEAD ? *reinterpret_cast<const float*>(tile + C::TILE + part * 256 + r * 4) : held_lse);
+                    floatx16 s[KB];
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) s[kb] = floatx16{0};
+#pragma unroll
+                    for (int cc = 0; cc < C::CH; ++cc) {
+                        typename R::Raw raw;
+                        if constexpr (C::AHEAD > 0) raw = R::template from_lds<C::RB>(tile + r * C::RB, i, cc, h);
+                        else raw = held[cc];
+                        most = R::largest(raw, most);
+                        const typename R::Frag qf = R::split(raw);
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb) s[kb] = R::mma(kf[kb][cc], qf, s[kb]);
+                    }
+                    const int last = decltype(whole)::value ? 0 : last_of(token_of(t, r));
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) add(kb, s[kb], base, whole, last);
+                    if (KB * C::CH >= 8) __builtin_amdgcn_sched_barrier(0);          // one after the other: side by side they took 60 registers more, and a workgroup of a CU
+                }
+            };
+            // whether every query of the tile sees every key of the wave
+            if (first + token_of(t, 0) >= key0 + 32 * KB - 1 && token_of(t, C::QT - 1) < cnt) weigh_tile(std::true_type{});
+            else weigh_tile(std::false_type{});
+            buf = buf == C::AHEAD ? 0 : buf + 1;
+        }
+        if constexpr (sizeof(T) == 4) {
+            if (__any(!(most < kPlaneHigh))) {
+                clear();
+                for (int t = t0; t < t1; t += QW)
+                    for (int x = 0; x < C::QT; x += 32) {
+                        const int token = token_of(t, x + i), safe = min(token, cnt - 1);
+                        const int head = WIDE ? t - divided(t, p.G, p.inv_G) * p.G : min(t * C::QT + x + i, rows - 1) - safe * p.G;
+                        const char* q = queries + head * head_bytes + safe * token_bytes;
+                        const Base base = base_of(*reinterpret_cast<const float*>(lses + head * pitch + safe * 4));
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb) {
+                            floatx16 s = {0};
+#pragma unroll 1
+                            for (int cc = 0; cc < D / 8; ++cc) s = mma_frag<float>(load16(key_row[kb] + (8 * cc + 4 * h) * 4), load16(q + (8 * cc + 4 * h) * 4), s);
+                            add(kb, s, base, std::false_type{}, last_of(token));
+                        }
+                    }
             }
         }
     }
-    // over the 32 lanes of a half; lane r of it keeps key acc_row(r, h)
-    float mine = 0.f;
+    // Over the 32 lanes of a half, half as many numbers a step: lane i ends with number i / 2.
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        float v = sum[r];
+    for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) v += __shfl_xor(v, off);
-        if ((lane & 15) == r) mine = v;
+        for (int off = 16, n = 8; n; off >>= 1, n >>= 1)
+#pragma unroll
+            for (int r = 0; r < n; ++r) {
+                const float low = sum[kb][r], high = sum[kb][r + n];
+                sum[kb][r] = (i & off ? high : low) + __shfl_xor(i & off ? low : high, off);
+            }
+        float mine = sum[kb][0] + __shfl_xor(sum[kb][0], 1);
+        const int at = acc_row(i >> 1, h);
+        if (!__shfl((int)there[kb], at)) mine = 0.f;
+        if ((i & 1) == 0) meet[w][32 * kb + at] = mine;
     }
-    const int at = acc_row(lane & 15, h);
-    const bool key_there = __shfl((int)there, at) != 0;
-    if (i < 16 && key0 + at < len) {
-        const int64_t x = (int64_t)u * room + key0 + at;
-        p.weight[x] = (p.before ? p.before[x] : 0.f) + (key_there ? mine : 0.f);
+    if (QW > 1) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (qw == 0)
+#pragma unroll
+        for (int x = 0; x < (KB + 1) / 2; ++x) {
+            const int r = 64 * x + lane;
+            if (r < 32 * KB && key0 + r < len) {
+                float v = 0.f;
+#pragma unroll
+                for (int y = 0; y < QW; ++y) v += meet[w + y][r];
+                p.weight[at0 + r] = was[x] + v;
+            }
+        }
+}
+
+template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
+static void launch_weigh_as(const Weigh& p, int units, hipStream_t st) {
+    using C = WeighCfg<T, D, KB, QW, WIDE, FEW>;
+    static std::atomic<uint64_t> set{0};                     // more than 64 KB of LDS has to be asked for, on every device
+    int dev = 0;
+    if (C::LDS + 1024 > 64 * 1024 && hipGetDevice(&dev) == hipSuccess && (dev > 63 || !(set.load(std::memory_order_relaxed) >> dev & 1))) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_weigh_kernel<T, D, KB, QW, WIDE, FEW>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) == hipSuccess && dev <= 63)
+            set.fetch_or(1ull << dev, std::memory_order_relaxed);        // the launch says so if it was refused
     }
+    const dim3 grid((unsigned)((((int64_t)p.width << p.page_log2) + C::KEYS - 1) / C::KEYS), units);
+    hipLaunchKernelGGL((paged_weigh_kernel<T, D, KB, QW, WIDE, FEW>), grid, dim3(256), C::LDS, st, p);
+}
+template <typename T, int D>
+static int launch_weigh_t(const Weigh& p, int units, hipStream_t st) {
+    constexpr int kWide = sizeof(T) == 4 ? 1 : 2;            // planes of 64 keys are too many registers
+    const int64_t tiles = ((int64_t)p.n * p.G + 31) / 32, keys = (int64_t)units * p.width << p.page_log2;
+    const bool wide = p.n >= 64 && p.q[2] * (int64_t)sizeof(T) < 1 << 24;            // offsets of a tile's rows fit 32 bits
+    KernelTimer tm(ZIPVL_K_PAGED_WEIGH, st);
+    if (tiles < 8) launch_weigh_as<T, D, 1, 1, false, true>(p, units, st);
+    else if (!wide) launch_weigh_as<T, D, 1, 1, false, false>(p, units, st);
+    else if (keys / (32 * kWide) >= 4096) launch_weigh_as<T, D, kWide, 1, true, false>(p, units, st);
+    else if (keys / 32 >= 2048) launch_weigh_as<T, D, 1, 1, true, false>(p, units, st);
+    else launch_weigh_as<T, D, 1, 4, true, false>(p, units, st);
+    return check_launch("paged_weigh");
 }
 
 int launch_paged_weigh(const void* Q, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
@@ -113,16 +336,8 @@ int launch_paged_weigh(const void* Q, const zipvl_pages& pages, const int32_t* t
     const int G = d.Hq / d.Hkv;
     const Weigh p = {(const char*)pages.K, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len, k, (const char*)Q,
                      {d.q_strides[0], d.q_strides[1], d.q_strides[2]}, lse, lse_pitch, before, weight, d.Hq, d.Hkv, G, d.n, inverse(d.Hkv), inverse(G), scale};
-    const dim3 grid((unsigned)(((int64_t)table_pages * pages.page + 127) / 128), d.B * d.Hkv);
-    KernelTimer tm(ZIPVL_K_PAGED_WEIGH, st);
-    if (d.dtype == ZIPVL_BF16) {
-        if (d.d == 128) hipLaunchKernelGGL((paged_weigh_kernel<__bf16, 128>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((paged_weigh_kernel<__bf16, 64>), grid, dim3(256), 0, st, p);
-    } else {
-        if (d.d == 128) hipLaunchKernelGGL((paged_weigh_kernel<float, 128>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((paged_weigh_kernel<float, 64>), grid, dim3(256), 0, st, p);
-    }
-    return check_launch("paged_weigh");
+    if (d.dtype == ZIPVL_BF16) return d.d == 128 ? launch_weigh_t<__bf16, 128>(p, d.B * d.Hkv, st) : launch_weigh_t<__bf16, 64>(p, d.B * d.Hkv, st);
+    return d.d == 128 ? launch_weigh_t<float, 128>(p, d.B * d.Hkv, st) : launch_weigh_t<float, 64>(p, d.B * d.Hkv, st);
 }
 
 }  // namespace zipvl
