@@ -431,7 +431,7 @@ int zipvl_paged_weigh(const void* Q, const zipvl_pages* pages, const int32_t* ta
  *   len_out[u] = n';  weight_out[u,r], tokens_out[u,r] = those of the row that now stands in r for r < n', 0 and -1 for n' <= r < len[u]; from len[u] on both are left.
  * tokens [device] int32 [B*Hkv, table_pages * page] or NULL (and tokens_out with it): which token each row holds.  Rows with a negative number are new, later than all others in
  * the order of rows: they get the numbers behind the greatest one there.  (Begin with -1 everywhere; numbers stay below 2^31.)  NULL: row r holds token r, which is true until rows have moved.
- * weight [device] fp32 [B*Hkv, table_pages * page].  len_out may be len, weight_out weight, tokens_out tokens; outputs overlap no other array.
+ * weight [device] fp32 [B*Hkv, table_pages * page], as tokens and both outputs 16-byte aligned.  len_out may be len, weight_out weight, tokens_out tokens; outputs overlap no other array.
  * A page that two units' tables share (or one table holds twice) races.
  * dims: B, Hkv, d, dtype.  B*Hkv <= 65535.  budget, sinks, recent >= 0.  k [device] int32 [B*Hkv] or NULL, clamped to >= 0.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_PAGED_EVICT, dims, budget) bytes, 16-byte aligned, holds nothing between calls (two calls that overlap on one workspace race).

@@ -8,6 +8,7 @@
 //   move     K and V of the rows on the lists; where a unit can have few, the first kernel's workgroup does it
 // Bounded by the latency of a chain of steps over a unit's weights, then by the bytes that move.
 #include <algorithm>
+#include <atomic>
 
 #include "launch.h"
 #include "wavepart.h"
@@ -34,13 +35,14 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
     return b > 0x7F800000u ? 0u : b;
 }
 
-// Moves j = first, first + step, ... below `end` of a unit, RB / 16 threads each.
-template <int RB>
-__device__ __forceinline__ void move_rows(char* K, char* V, int num_pages, int page_log2, const int32_t* table, const int32_t* gap, const Late* late, int first, int step, int end) {
+// Moves j = first, first + step, ... below `end` of a unit, RB / 16 threads each; move(j): to which row, from which.
+template <int RB, typename F>
+__device__ __forceinline__ void move_rows(char* K, char* V, int num_pages, int page_log2, const int32_t* table, int first, int step, int end, F&& move) {
     const int c = threadIdx.x % (RB / 16) * 16, page = (1 << page_log2) - 1;
 #pragma unroll 4
     for (int j = first; j < end; j += step) {
-        const int to = gap[j], from = late[j].row;
+        const int2 m = move(j);
+        const int to = m.x, from = m.y;
         const int pt = table[to >> page_log2], pf = table[from >> page_log2];
         if ((unsigned)pt >= (unsigned)num_pages || (unsigned)pf >= (unsigned)num_pages) continue;
         const int64_t x = (((int64_t)pt << page_log2) + (to & page)) * RB + c, y = (((int64_t)pf << page_log2) + (from & page)) * RB + c;
@@ -52,10 +54,10 @@ __device__ __forceinline__ void move_rows(char* K, char* V, int num_pages, int p
 
 template <int WAVES>
 struct EvictShared {
-    uint32_t hist[kDigits];
+    __attribute__((aligned(16))) uint32_t hist[kDigits + 256];
     int sums[WAVES];
-    uint32_t digit, equal;
-    int above, newest;
+    uint32_t digit, key;
+    int above, equal, found_above, found_equal, newest;
 };
 
 // Exclusive sum over the workgroup's threads, and the total.
@@ -77,23 +79,29 @@ __device__ __forceinline__ int block_scan_of(int v, int (&sums)[WAVES], int& tot
 }
 
 // The digit at which rows counted from the largest key on reach k, of a histogram of `digits` (sh.hist): sh.digit, sh.above (rows above it), sh.equal (rows with it).
+// By one wave, between two barriers: all waves took three and four times as long.
 template <int WAVES>
 __device__ __forceinline__ void crossing_digit(EvictShared<WAVES>& sh, int digits, int above, int k) {
-    constexpr int kPer = kDigits / (64 * WAVES);
-    uint32_t mine[kPer];
-    int sum = 0, total;
-    const int top = digits - 1 - (int)threadIdx.x * kPer;    // thread t has the digits from there down
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x, per = digits / 64, top = digits - per * lane;      // lane l has the digits from `top` down
+        int sum = 0;
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) sum += mine[x] = top - x >= 0 ? sh.hist[top - x] : 0;
-    int before = above + block_scan_of<WAVES>(sum, sh.sums, total);
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-        if (before < k && k <= before + (int)mine[x]) {
-            sh.digit = top - x;
-            sh.above = before;
-            sh.equal = mine[x];
+        for (int x = 0; x < kDigits / 64; x += 4)
+            if (x < per) {
+                // lanes stand 128 bytes apart: each begins at another sixteen, or they would meet in the same banks
+                const uintx4 four = *reinterpret_cast<const uintx4*>(sh.hist + top - per + ((x + 4 * lane) & (per - 1)));
+                sum += four[0] + four[1] + four[2] + four[3];
+            }
+        const int upto = above + wave_scan(sum);
+        const int at = __builtin_ctzll(__ballot(upto >= k) | 1ull << 63);                // the lane with the digit
+        const int from = digits - per * at, before = __builtin_amdgcn_readlane(upto - sum, at);
+        const int n = lane < per ? (int)sh.hist[from - 1 - lane] : 0, till = before + wave_scan(n);
+        if (till - n < k && k <= till) {
+            sh.digit = from - 1 - lane;
+            sh.above = till - n;
+            sh.equal = n;
         }
-        before += mine[x];
     }
     __syncthreads();
 }
@@ -113,123 +121,206 @@ __device__ __forceinline__ EvictUnit evict_unit(const Evict& p, int u) {
     return x;
 }
 
-// Behind the list of moves: the moved rows' weights and tokens, and where moves are done here, their K and V.
+// evict_sweep_kernel, behind the list of moves: the moved rows' weights and tokens, and where moves are done here, their K and V.
 template <int RB>
 __device__ __forceinline__ void finish_unit(const Evict& p, const EvictUnit& x, int u, int moves, int threads) {
     __syncthreads();
+#pragma unroll 4
     for (int j = threadIdx.x; j < moves; j += threads) {
         const int r = x.gap[j];
         const Late from = x.late[j];
         x.weight_out[r] = from.weight;
         if (x.tokens) x.tokens_out[r] = from.token;
     }
-    if (p.here) move_rows<RB>(p.K, p.V, p.num_pages, p.page_log2, p.table + (int64_t)u * p.width, x.gap, x.late, threadIdx.x / (RB / 16), threads / (RB / 16), moves);
+    if (p.here) move_rows<RB>(p.K, p.V, p.num_pages, p.page_log2, p.table + (int64_t)u * p.width, threadIdx.x / (RB / 16), threads / (RB / 16), moves, [&](int j) { return int2{x.gap[j], x.late[j].row}; });
     if (threadIdx.x == 0) {
         p.count[u] = moves;
         p.len_out[u] = x.k;
     }
 }
 
-// Up to KPT rows a thread, their keys in registers: row c 64 WAVES + t is thread t's c-th.  Ranks in the order of rows come from ballots: the counts of
-// (c, wave) stand in LDS and one scan adds them up, two barriers for all rows of a kind.
-template <int WAVES, int KPT, int RB>
+// Units whose keys fit LDS.  A round is four rows a thread, which follow each other; their weights and tokens stay in registers, their keys in LDS.  Ranks in the order of rows are
+// sums over the threads before in the wave, and over the counts of (round, wave) before, which stand in LDS.  One CU has a unit, and it is bound by the instructions of
+// its sweeps and some twenty barriers.  4 units of 18432 rows, 7200 to stay, this kernel alone: 27 us (41 with keys in registers, a row a thread and round, ranks by ballots; 30 with the
+// weights and tokens read a second time); 256 units of 2304 rows with their few moves: 10 us (12, with the k-th key's digit found by lanes that meet in LDS banks).
+constexpr int kRoundsMost = 9;                               // of 4096 rows: 147 KB of keys
+constexpr int kFewKeys = 256;                                // that have the first digits of the k-th are looked at one by one, instead of two more digits
+template <int WAVES, int ROUNDS, int RB>
 __global__ __launch_bounds__(64 * WAVES) void evict_select_kernel(Evict p) {
-    constexpr int kThreads = 64 * WAVES, kCells = KPT * WAVES, kPer = (kCells + kThreads - 1) / kThreads;
+    constexpr int kThreads = 64 * WAVES;
+    extern __shared__ __attribute__((aligned(16))) uint32_t keys[];
     __shared__ EvictShared<WAVES> sh;
-    __shared__ int cells[KPT][WAVES];
+    __shared__ int cells[ROUNDS * WAVES + 1];
+    int* const gaps = reinterpret_cast<int*>(keys);          // the rows that others move to, when the keys are done with
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = scalar(tid >> 6);
+    auto first_row = [&](int c) { return (c * kThreads + tid) * 4; };
+    uintx4 weight[ROUNDS], token[ROUNDS];                    // all asked for at once, with the length
+    {
+        const uint32_t* const from = reinterpret_cast<const uint32_t*>(p.weight) + (int64_t)u * p.room;
+        const uint32_t* const tokens = reinterpret_cast<const uint32_t*>(p.tokens) + (int64_t)u * p.room;
+#pragma unroll
+        for (int c = 0; c < ROUNDS; ++c) {
+            weight[c] = uintx4{0, 0, 0, 0};
+            token[c] = uintx4{(uint32_t)first_row(c), (uint32_t)first_row(c) + 1, (uint32_t)first_row(c) + 2, (uint32_t)first_row(c) + 3};
+            if (first_row(c) < p.room) {                     // a multiple of four
+                if (p.tokens) token[c] = load16(tokens + first_row(c));
+                weight[c] = load16(from + first_row(c));
+            }
+        }
+    }
+    for (int y = tid; y < kDigits; y += kThreads) sh.hist[y] = 0;
+    if (tid == 0) sh.newest = -1;
     const EvictUnit x = evict_unit(p, u);
-    int len = scalar(x.len);
-    const int k = scalar(x.k), rounds = (len + kThreads - 1) / kThreads;
-    auto row = [&](int c) { return c * kThreads + tid; };
-    // Said anew before each loop over the rows: which of them there are (two scalar registers a row) is not kept from one for the next (it spilled).
-    auto afresh = [&]() { asm volatile("" : "+s"(len)); };
-    // cells -> what all cells before hold; the total
+    const int len = scalar(x.len), k = scalar(x.k), rounds = (len + 4 * kThreads - 1) / (4 * kThreads);
+    auto held = [&](int c) -> uintx4& { return *reinterpret_cast<uintx4*>(keys + first_row(c)); };
+    // f(round) of rounds with rows
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < ROUNDS; ++c)
+            if (c < rounds) f(c);
+    };
+    // cells -> what all cells before hold; the total.  By one wave.
     auto scan_cells = [&]() {
         __syncthreads();
-        int v[kPer], sum = 0, total;
+        if (tid < 64) {
+            constexpr int kPer = (ROUNDS * WAVES + 63) / 64;
+            int v[kPer], sum = 0;
 #pragma unroll
-        for (int y = 0; y < kPer; ++y) {
-            const int cell = tid * kPer + y;
-            sum += v[y] = cell < rounds * WAVES ? (&cells[0][0])[cell] : 0;
-        }
-        int before = block_scan_of<WAVES>(sum, sh.sums, total);
+            for (int y = 0; y < kPer; ++y) {
+                const int cell = lane * kPer + y;
+                sum += v[y] = cell < rounds * WAVES ? cells[cell] : 0;
+            }
+            const int upto = wave_scan(sum);
+            int before = upto - sum;
 #pragma unroll
-        for (int y = 0; y < kPer; ++y) {
-            const int cell = tid * kPer + y;
-            if (cell < rounds * WAVES) (&cells[0][0])[cell] = before;
-            before += v[y];
+            for (int y = 0; y < kPer; ++y) {
+                const int cell = lane * kPer + y;
+                if (cell < rounds * WAVES) cells[cell] = before;
+                before += v[y];
+            }
+            if (lane == 63) cells[ROUNDS * WAVES] = upto;
         }
         __syncthreads();
-        return total;
+        return cells[ROUNDS * WAVES];
     };
-    auto below = [&](uint64_t bits) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0)); };
-
-    uint64_t sure = 0;                                       // bit c: row c is protected
+    // a thread's count of a round -> what the threads before in the wave have; the wave's to its cell
+    auto in_wave = [&](int count) { return wave_scan(count) - count; };
+    auto to_cell = [&](int c, int count) {
+        const int upto = wave_scan(count);
+        if (lane == 63) cells[c * WAVES + w] = upto;
+    };
+    // One more of a digit, in lanes where there is one.  Those that have the first lane's go at once: thousands of equal weights would queue for one number.
+    auto count = [&](uint32_t digit, bool there) {
+        const uint64_t lanes = __ballot(there);
+        if (!lanes) return;
+        const int leader = __builtin_ctzll(lanes);
+        const uint32_t common = __builtin_amdgcn_readlane(digit, leader);
+        const uint64_t same = __ballot(there && digit == common);
+        if (lane == leader) atomicAdd(&sh.hist[common], (uint32_t)__popcll(same));
+        if (there && digit != common) atomicAdd(&sh.hist[digit], 1u);
+    };
+    int last = len - 1;
+    __syncthreads();
     if (x.tokens) {
         // the newest token: rows without one (negative) are new and follow each other behind it
-        int32_t token[KPT];
+        auto fresh_of = [&](int c) {                         // new rows of four, as bits
+            int f = 0;
 #pragma unroll
-        for (int c = 0; c < KPT; ++c) {
-            token[c] = 0;
-            if (c < rounds && row(c) < len) token[c] = x.tokens[row(c)];
-        }
-        if (tid == 0) sh.newest = -1;
+            for (int e = 0; e < 4; ++e) f |= ((int)token[c][e] < 0 && first_row(c) + e < len) << e;
+            return f;
+        };
         int newest = -1;
-        afresh();
+        each([&](int c) {
 #pragma unroll
-        for (int c = 0; c < KPT; ++c)
-            if (c < rounds) {
-                if (row(c) < len) newest = max(newest, token[c]);
-                const uint64_t fresh = __ballot(token[c] < 0);
-                if (lane == 0) cells[c][w] = __popcll(fresh);
-            }
-        __syncthreads();
+            for (int e = 0; e < 4; ++e)
+                if (first_row(c) + e < len) newest = max(newest, (int)token[c][e]);
+            to_cell(c, __popc(fresh_of(c)));
+        });
         newest = wave_reduce(newest, -1, [](int a, int b) { return max(a, b); });
         if (lane == 0) atomicMax(&sh.newest, newest);
-        const int fresh = scan_cells();
+        last = scan_cells() + sh.newest;
         newest = sh.newest;
-        const int last = newest + fresh;
+        each([&](int c) {
+            const int fresh = fresh_of(c);
+            if (__any(fresh)) {
+                int number = newest + 1 + cells[c * WAVES + w] + in_wave(__popc(fresh));
 #pragma unroll
-        for (int c = 0; c < KPT; ++c)
-            if (c < rounds) {
-                const int rank = below(__ballot(token[c] < 0));
-                if (token[c] < 0) {
-                    token[c] = newest + 1 + cells[c][w] + rank;
-                    x.tokens_out[row(c)] = token[c];         // where it is looked up again below
-                }
-                sure |= (uint64_t)(token[c] < p.sinks || token[c] > last - p.recent) << c;
+                for (int e = 0; e < 4; ++e)
+                    if (fresh >> e & 1) token[c][e] = number++;
             }
-        __syncthreads();
+        });
     }
-    uint32_t key[KPT];
-    {
-        float weight[KPT];
-        afresh();
+    // keys, and the histogram of their first digit
+    const int recent_from = last - p.recent;
+    each([&](int c) {
+        const int r = first_row(c);
+        uintx4 key;
 #pragma unroll
-        for (int c = 0; c < KPT; ++c) {
-            weight[c] = 0.f;
-            if (c < rounds && row(c) < len) weight[c] = x.weight[row(c)];
+        for (int e = 0; e < 4; ++e) {
+            key[e] = weight_key(__uint_as_float(weight[c][e]));
+            if ((int)token[c][e] < p.sinks || (int)token[c][e] > recent_from) key[e] |= 0x80000000u;
+            if (r + e >= len) key[e] = 0;
+            count(key[e] >> (32 - kDigit), r + e < len);
         }
-#pragma unroll
-        for (int c = 0; c < KPT; ++c) {
-            const bool first = x.tokens ? sure >> c & 1 : row(c) < p.sinks || row(c) > len - 1 - p.recent;
-            key[c] = weight_key(weight[c]) | (first ? 0x80000000u : 0u);
-        }
-    }
+        held(c) = key;
+    });
     // the k-th largest key, how many rows have a larger one and how many have it
-    uint32_t prefix = 0, mask = 0;
+    uint32_t prefix = 0;
     int above = 0, equal = 0;
-    if (k > 0 && k < len)
+    const bool all = k == len, some = k > 0 && k < len;
+    if (some) {
+        uint32_t mask = 0;
         for (int shift : {32 - kDigit, 32 - 2 * kDigit, 0}) {
             const uint32_t digits = shift ? kDigits : 1u << (32 - 2 * kDigit);
-            for (int y = tid; y < kDigits; y += kThreads) sh.hist[y] = 0;
-            __syncthreads();
-            afresh();
+            if (mask && equal <= kFewKeys) {
+                // Few rows have the first digits of the k-th key: each looks how many of the others are larger, and how many as large.
+                if (tid == 0) sh.digit = 0;
+                __syncthreads();
+                each([&](int c) {
+                    const uintx4 key = held(c);
 #pragma unroll
-            for (int c = 0; c < KPT; ++c)
-                if (c < rounds && row(c) < len && (key[c] & mask) == prefix) atomicAdd(&sh.hist[key[c] >> shift & (digits - 1)], 1u);
-            __syncthreads();
+                    for (int e = 0; e < 4; ++e)
+                        if ((key[e] & mask) == prefix && first_row(c) + e < len) sh.hist[atomicAdd(&sh.digit, 1u) & (kDigits - 1)] = key[e];
+                });
+                __syncthreads();
+                constexpr int kParts = kThreads / kFewKeys;  // threads to a key, next to each other
+                const uint32_t mine = sh.hist[tid / kParts];
+                int larger = 0, as_large = 0;
+                if (tid / kParts < equal) {
+                    for (int y = tid % kParts * 4; y < equal; y += 4 * kParts) {
+                        const uintx4 others = *reinterpret_cast<const uintx4*>(sh.hist + y);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            larger += y + e < equal && others[e] > mine;
+                            as_large += y + e < equal && others[e] == mine;
+                        }
+                    }
+#pragma unroll
+                    for (int part = 1; part < kParts; part *= 2) {
+                        larger += __shfl_xor(larger, part);
+                        as_large += __shfl_xor(as_large, part);
+                    }
+                    if (above + larger < k && k <= above + larger + as_large) {      // all that are as large write the same
+                        sh.key = mine;
+                        sh.found_above = above + larger;
+                        sh.found_equal = as_large;
+                    }
+                }
+                __syncthreads();
+                prefix = sh.key;
+                above = sh.found_above;
+                equal = sh.found_equal;
+                break;
+            }
+            if (mask) {
+                for (int y = tid; y < kDigits; y += kThreads) sh.hist[y] = 0;
+                __syncthreads();
+                each([&](int c) {
+                    const uintx4 key = held(c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) count(key[e] >> shift & (digits - 1), (key[e] & mask) == prefix && first_row(c) + e < len);
+                });
+            }
             crossing_digit<WAVES>(sh, (int)digits, above, k);
             prefix |= sh.digit << shift;
             mask |= (digits - 1) << shift;
@@ -237,77 +328,108 @@ __global__ __launch_bounds__(64 * WAVES) void evict_select_kernel(Evict p) {
             equal = sh.equal;
             __syncthreads();
         }
+    } else __syncthreads();
     const int ties = k - above;                              // of the rows with that key, the first ones stay
-    // 0 leaves, 1 stays, of rows with the k-th key those that come first
-    const bool all = k == len, some = k > 0 && k < len, count_ties = some && ties < equal;
-    if (count_ties) {
-        afresh();
+    const bool count_ties = some && ties < equal;
+    auto tied_of = [&](const uintx4& key) {
+        int t = 0;
 #pragma unroll
-        for (int c = 0; c < KPT; ++c)
-            if (c < rounds) {
-                const uint64_t tie = __ballot(row(c) < len && key[c] == prefix);
-                if (lane == 0) cells[c][w] = __popcll(tie);
-            }
+        for (int e = 0; e < 4; ++e) t |= (key[e] == prefix) << e;
+        return t;                                            // rows behind the length among them, behind all others
+    };
+    if (count_ties) {
+        each([&](int c) { to_cell(c, __popc(tied_of(held(c)))); });
         scan_cells();
     }
-    uint64_t stays = 0;                                      // bit c: of row c
-    afresh();
+    // Rows that stay, as bits; moves: rows below k that leave, rows from k on that stay, both kinds counted in one number.
+    auto first = [](int n) { return (1 << max(0, min(n, 4))) - 1; };        // of four rows, those with n left
+    uint64_t in_all = 0;                                     // four bits a round
+    static_assert(ROUNDS <= 16, "");
+    each([&](int c) {
+        const int r = first_row(c);
+        const uintx4 key = held(c);
+        int in = 0;
 #pragma unroll
-    for (int c = 0; c < KPT; ++c)
-        if (c < rounds) {
-            const bool there = row(c) < len, tie = there && some && key[c] == prefix;
-            bool in = there && (all || (some && key[c] >= prefix));
-            if (count_ties) {
-                const int rank = cells[c][w] + below(__ballot(tie));
-                if (tie) in = rank < ties;
+        for (int e = 0; e < 4; ++e) in |= (all || (some && key[e] >= prefix)) << e;
+        if (count_ties) {
+            const int tied = tied_of(key);
+            if (__any(tied)) {
+                int rank = cells[c * WAVES + w] + in_wave(__popc(tied));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (tied >> e & 1 && rank++ >= ties) in &= ~(1 << e);
             }
-            stays |= (uint64_t)in << c;
         }
-    static_assert(KPT <= 64, "a bit for each row of a thread");
-    __syncthreads();
-    // moves: rows below k that leave, rows from k on that stay; both kinds counted in one number
-    afresh();
-#pragma unroll
-    for (int c = 0; c < KPT; ++c)
-        if (c < rounds) {
-            const bool in = stays >> c & 1, there = row(c) < len;
-            const uint64_t out = __ballot(there && row(c) < k && !in), come = __ballot(row(c) >= k && in);
-            if (lane == 0) cells[c][w] = __popcll(out) | __popcll(come) << 16;
-        }
-    static_assert(KPT * 64 * WAVES < 1 << 17, "at most half of the rows are of either kind: 16 bits each");
+        in_all |= (uint64_t)(in & first(len - r)) << 4 * c;
+    });
+    auto in_of = [&](int c) { return (int)(in_all >> 4 * c) & 15; };
+    __syncthreads();                                         // cells and keys have been read
+    each([&](int c) {
+        const int in = in_of(c), low = first(k - first_row(c));
+        to_cell(c, __popc(low & ~in) | __popc(in & ~low) << 16);
+    });
+    static_assert(ROUNDS * kThreads * 4 < 1 << 17, "at most half of the rows are of either kind: 16 bits each");
     const int total = scan_cells();
     const int moves = (int)min<int64_t>(min(total & 0xFFFF, (int)((uint32_t)total >> 16)), p.most);
-    afresh();
+    const bool copied = x.weight_out != x.weight || x.tokens_out != x.tokens;         // else old rows that stay where they are stand there already
+    // The rows that others move to, and those that move; a moved row's weight and token have to wait for the first.
+    each([&](int c) {
+        if (c * kThreads * 4 + 256 * w >= k) return;         // of the wave
+        const int leave = first(k - first_row(c)) & ~in_of(c);
+        int rank = (cells[c * WAVES + w] + in_wave(__popc(leave))) & 0xFFFF;
 #pragma unroll
-    for (int c = 0; c < KPT; ++c)
-        if (c < rounds) {
-            const int r = row(c);
-            const bool in = stays >> c & 1, there = r < len, out = there && r < k && !in, come = r >= k && in;
-            const uint32_t base = cells[c][w];
-            const int gap_rank = (base & 0xFFFF) + below(__ballot(out)), late_rank = (base >> 16) + below(__ballot(come));
-            if (there && in) {
-                const float weight = x.weight[r];
-                int token = r;
-                if (x.tokens) {
-                    token = x.tokens[r];
-                    if (token < 0) token = x.tokens_out[r];
+        for (int e = 0; e < 4; ++e)
+            if (leave >> e & 1) gaps[rank++] = first_row(c) + e;
+    });
+    __syncthreads();
+    each([&](int c) {
+        const int r = first_row(c), in = in_of(c), low = first(k - r), there = first(len - r), come = in & ~low;
+        if (__any(come)) {
+            int rank = (int)((uint32_t)cells[c * WAVES + w] >> 16) + in_wave(__popc(come));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (come >> e & 1 && rank < moves) {
+                    const int to = gaps[rank];
+                    x.weight_out[to] = __uint_as_float(weight[c][e]);
+                    if (x.tokens) x.tokens_out[to] = (int)token[c][e];
+                    gaps[moves + rank++] = r + e;
                 }
-                if (come && late_rank < p.most) x.late[late_rank] = {r, token, weight, 0};
-                if (r < k) {
-                    x.weight_out[r] = weight;
-                    if (x.tokens) x.tokens_out[r] = token;
-                }
-            }
-            if (out && gap_rank < p.most) x.gap[gap_rank] = r;
-            if (there && r >= k) {
-                x.weight_out[r] = 0.f;
-                if (x.tokens) x.tokens_out[r] = -1;
-            }
         }
-    finish_unit<RB>(p, x, u, moves, kThreads);
+        const int put = (in & low) | (there & ~low);         // rows that are written down; in place, weights that stay and old tokens could be left, but most rounds have some new ones
+        if (!copied && !x.tokens && put == (in & low)) return;
+        uintx4 v = weight[c], t = token[c];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!(low >> e & 1)) {
+                v[e] = 0;
+                t[e] = -1;
+            }
+        if (put == 15) {
+            store16(reinterpret_cast<uint32_t*>(x.weight_out) + r, v);
+            if (x.tokens) store16(reinterpret_cast<uint32_t*>(x.tokens_out) + r, t);
+        } else if (put) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (put >> e & 1) {
+                    x.weight_out[r + e] = __uint_as_float(v[e]);
+                    if (x.tokens) x.tokens_out[r + e] = (int)t[e];
+                }
+        }
+    });
+    __syncthreads();
+    if (p.here) move_rows<RB>(p.K, p.V, p.num_pages, p.page_log2, p.table + (int64_t)u * p.width, tid / (RB / 16), kThreads / (RB / 16), moves, [&](int j) { return int2{gaps[j], gaps[moves + j]}; });
+    else
+        for (int j = tid; j < moves; j += kThreads) {
+            x.gap[j] = gaps[j];
+            x.late[j].row = gaps[moves + j];
+        }
+    if (tid == 0) {
+        p.count[u] = moves;
+        p.len_out[u] = k;
+    }
 }
 
-// Units of any length, whose keys do not stay in registers: the same, in sweeps over the rows, 1024 at a time.
+// Units of any length, whose keys do not fit LDS: the same, in sweeps over the rows, 1024 at a time.
 template <int RB>
 __global__ __launch_bounds__(1024) void evict_sweep_kernel(Evict p) {
     constexpr int kWaves = 16, kThreads = 1024;
@@ -389,8 +511,10 @@ template <int RB>
 __global__ __launch_bounds__(256) void evict_move_kernel(Evict p) {
     const int u = blockIdx.y, moves = p.count[u], j0 = blockIdx.x * kMoveRows;
     if (j0 >= moves) return;
-    move_rows<RB>(p.K, p.V, p.num_pages, p.page_log2, p.table + (int64_t)u * p.width, p.gap + u * p.most, p.late + u * p.most, j0 + threadIdx.x / (RB / 16), 256 / (RB / 16),
-                  min(j0 + kMoveRows, moves));
+    const int32_t* gap = p.gap + u * p.most;
+    const Late* late = p.late + u * p.most;
+    move_rows<RB>(p.K, p.V, p.num_pages, p.page_log2, p.table + (int64_t)u * p.width, j0 + threadIdx.x / (RB / 16), 256 / (RB / 16), min(j0 + kMoveRows, moves),
+                  [&](int j) { return int2{gap[j], late[j].row}; });
 }
 
 // Moves of a unit: no more than rows that stay, nor than rows that leave.  given: k may ask for fewer than the budget
@@ -403,10 +527,21 @@ template <int RB>
 static int launch_evict_t(const Evict& p, int units, hipStream_t st) {
     {
         KernelTimer tm(ZIPVL_K_PAGED_EVICT, st);
-        if (p.room <= 1024) hipLaunchKernelGGL((evict_select_kernel<4, 4, RB>), dim3(units), dim3(256), 0, st, p);
-        else if (p.room <= 4096) hipLaunchKernelGGL((evict_select_kernel<16, 4, RB>), dim3(units), dim3(1024), 0, st, p);
-        else if (p.room <= 36 * 1024) hipLaunchKernelGGL((evict_select_kernel<16, 36, RB>), dim3(units), dim3(1024), 0, st, p);
-        else hipLaunchKernelGGL((evict_sweep_kernel<RB>), dim3(units), dim3(1024), 0, st, p);
+        if (p.room <= 1024) hipLaunchKernelGGL((evict_select_kernel<4, 1, RB>), dim3(units), dim3(256), 1024 * 4, st, p);
+        else if (p.room <= 4096) hipLaunchKernelGGL((evict_select_kernel<16, 1, RB>), dim3(units), dim3(1024), 4096 * 4, st, p);
+        else if (p.room <= kRoundsMost * 4096) {
+            const bool five = p.room <= 5 * 4096;
+            auto kernel = five ? &evict_select_kernel<16, 5, RB> : &evict_select_kernel<16, kRoundsMost, RB>;
+            static std::atomic<uint64_t> set[2];             // more than 64 KB of LDS has to be asked for, on every device
+            int dev = 0;
+            if (hipGetDevice(&dev) != hipSuccess) return set_error(ZIPVL_EHIP, "paged_evict: no current device");
+            if (dev > 63 || !(set[five].load(std::memory_order_relaxed) >> dev & 1)) {
+                const int most = (five ? 5 : kRoundsMost) * 4096 * 4;
+                if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess) return set_error(ZIPVL_EHIP, "paged_evict: %d bytes of LDS are refused", most);
+                if (dev <= 63) set[five].fetch_or(1ull << dev, std::memory_order_relaxed);
+            }
+            hipLaunchKernelGGL(kernel, dim3(units), dim3(1024), (p.room + 4095) / 4096 * 4096 * 4, st, p);
+        } else hipLaunchKernelGGL((evict_sweep_kernel<RB>), dim3(units), dim3(1024), 0, st, p);
         const int rc = check_launch("paged_evict");
         if (rc || p.here) return rc;
     }

@@ -596,6 +596,8 @@ int zipvl_paged_evict(const zipvl_pages* pages, const int32_t* table, int32_t ta
     if (budget < 0 || sinks < 0 || recent < 0) return set_error(ZIPVL_EINVAL, "%s: budget, sinks and recent must not be negative (got %d %d %d)", fn, budget, sinks, recent);
     for (const void* p : {(const void*)len, (const void*)k, (const void*)weight, (const void*)tokens, (const void*)len_out, (const void*)weight_out, (const void*)tokens_out})
         if (reinterpret_cast<uintptr_t>(p) & 3u) return set_error(ZIPVL_EALIGN, "%s: an array is not 4-byte aligned", fn);
+    for (const void* p : {(const void*)weight, (const void*)tokens, (const void*)weight_out, (const void*)tokens_out})
+        if (!aligned16(p)) return set_error(ZIPVL_EALIGN, "%s: weight, tokens, weight_out or tokens_out is not 16-byte aligned", fn);
     const int64_t units = (int64_t)d.B * d.Hkv, room = (int64_t)table_pages * pages->page;
     struct Span { const void* p; int64_t bytes; };
     const Span ins[5] = {{len, units * 4}, {weight, units * room * 4}, {tokens, units * room * 4}, {k, units * 4}, {table, units * table_pages * 4}};

@@ -714,8 +714,10 @@ def test_paged_evict_refuses(lib):
     assert call(budget=-1) == -1 and call(sinks=-1) == -1 and call(recent=-1) == -1
     for name in ("length", "weight", "tokens", "k", "length_out", "weight_out", "tokens_out"):
         assert call(**{name: 0x5000002}) == -3
+    for name in ("weight", "tokens", "weight_out", "tokens_out"):        # read and written by four rows
+        assert call(**{name: 0x5000008}) == -3
     size = 4 * 4 * 16 * 4
-    assert call(weight_out=far[2] + 4) == -1 and "overlaps" in z.zipvl_last_error() and call(tokens_out=far[2]) == -1 and call(weight_out=far[3] - size + 4) == -1
+    assert call(weight_out=far[2] + 16) == -1 and "overlaps" in z.zipvl_last_error() and call(tokens_out=far[2]) == -1 and call(weight_out=far[3] - size + 16) == -1
     assert call(length_out=far[2]) == -1 and call(length_out=far[0]) == -1 and call(weight_out=far[6] + 16) == -1 and "two outputs" in z.zipvl_last_error()
     assert call(k=far[1], length=far[1], length_out=far[1]) == -1
     need = z.workspace_bytes(z.OP_PAGED_EVICT, dims(n=64), 10)
