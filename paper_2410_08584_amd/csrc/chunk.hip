@@ -19,8 +19,8 @@
 namespace zipvl {
 
 constexpr int kRowsMany = 128;
-constexpr int kLeastMany = 4, kLeastFew = 8;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
-constexpr int kScanUnits = 2048;                             // more units than this go one workgroup a tile of rows, whatever their lengths
+constexpr int kLeastMany = 4, kLeastFew = 4;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
+constexpr int kScanItems = 2048;                             // more tiles of rows than this get a workgroup each, whatever their keys
 
 // 8-byte fields and pairs of others only: it is read again as a row of 32-bit numbers
 struct Chunk {
@@ -36,7 +36,7 @@ struct Chunk {
     float c;                                                 // scale log2(e)
 };
 
-// Parts of tiles of rows that were cut: `rows` rows of D sums and (offset, sum) each.  pieces: the first record of a unit and into how many its keys were cut.
+// Parts of tiles of rows that were cut: `rows` rows of D sums and (offset, sum) each.  pieces: a tile's first record and into how many its keys were cut.
 struct ChunkParts { float* o; float* ml; int2* pieces; };
 
 __device__ __forceinline__ int between(int v, int low, int high) { return max(low, min(v, high)); }
@@ -54,7 +54,8 @@ __device__ __forceinline__ int group_with(const int32_t* begin, int groups, int 
 
 struct ChunkUnit {
     int b, g, rows, cnt, len, prefix, prefix_rows;           // rows of queries; prefix: row of prefix_table
-    __device__ __forceinline__ int tiles(int bn) const { return (len + bn - 1) / bn + (prefix_rows + bn - 1) / bn; }
+    // own rows that the last token of rows of queries up to r sees
+    __device__ __forceinline__ int seen(const Chunk& p, int r) const { return between(len - cnt + divided(min(r, rows - 1), p.G, p.inv_G) + 1, 0, len); }
 };
 __device__ __forceinline__ ChunkUnit chunk_unit(const Chunk& p, int u, const int32_t* begin) {
     ChunkUnit x;
@@ -74,80 +75,82 @@ __device__ __forceinline__ ChunkUnit chunk_unit(const Chunk& p, int u, const int
     return x;
 }
 
-// What a workgroup has: keys `piece` of `pieces` of tile t of `tiles` of unit u's rows; its record, if pieces > 1.
-struct Place { int u, t, tiles, piece, pieces, record; };
+// What a workgroup has: keys `piece` of `pieces` of tile t of unit u's rows; its record, if pieces > 1.
+struct Place { int u, t, piece, pieces, record; };
 struct PlaceShared {
-    int32_t begin[kScanUnits + 1];
+    int32_t begin[kScanItems + 1], keys[kScanItems];
     unsigned long long total;
     int2 sums[4];
     Place place;
 };
 
-// BM rows of queries and BN keys a tile.  Workgroups of one unit that have the same keys follow each other on one XCD (workgroups go to the eight in turn).
+// BM rows of queries and BN keys a tile.  Workgroups that have neighbouring tiles of rows, and so the same keys, follow each other on one XCD (workgroups go to the eight in turn).
 template <int BM, int BN>
 __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, const ChunkParts& out, int wgs, int least, int direct, Place& x) {
     const int tid = threadIdx.x, lane = tid & 63, w = scalar(tid >> 6);
+    const int most = (p.n * p.G + BM - 1) / BM, items = p.units * most;      // tiles of rows of a unit, of all
     if (direct) {
-        const int per = gridDim.x / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3), most = (p.n * p.G + BM - 1) / BM;
-        if (id >= p.units * most) return false;
-        x = {id / most, most - 1 - id % most, 0, 0, 1, 0};
+        const int per = gridDim.x / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+        if (id >= items) return false;
+        x = {id / most, most - 1 - id % most, 0, 1, 0};
         return true;
     }
     for (int i = tid; i <= p.groups && p.groups; i += 256) sh.begin[i] = p.group_begin[i];
     if (tid == 0) { sh.total = 0; sh.place.pieces = 0; }
     __syncthreads();
-    int T = 0, N = 0;
+    // tiles of keys of each: tile of rows `most` - 1 first, the longest; -1: the unit has fewer rows
     unsigned long long mine = 0;
-    auto sizes = [&](int u) {
-        T = N = 0;
-        if (u < p.units) {
-            const ChunkUnit v = chunk_unit(p, u, sh.begin);
-            T = (v.rows + BM - 1) / BM;
-            N = v.tiles(BN);
+    for (int e = tid; e < items; e += 256) {
+        const int u = e / most, r0 = (most - 1 - e % most) * BM;
+        const ChunkUnit v = chunk_unit(p, u, sh.begin);
+        int N = -1;
+        if (r0 < v.rows) {
+            N = (v.seen(p, r0 + BM - 1) + BN - 1) / BN + (v.prefix_rows + BN - 1) / BN;
+            mine += N;
         }
-    };
-    for (int u0 = 0; u0 < p.units; u0 += 256) {
-        sizes(u0 + tid);
-        mine += (unsigned long long)T * N;
+        sh.keys[e] = N;
     }
     if (mine) atomicAdd(&sh.total, mine);
     __syncthreads();
     // A tile of rows is cut into as many pieces as it has average loads, rounded down: then all pieces fit the chip at once
     const int q = max(least, (int)min((unsigned long long)INT32_MAX, (sh.total + wgs - 1) / wgs));
-    // how many workgroups all tiles take, first; then whose unit this one's is
-    int used = 0, own = 0;
-    for (int round = 0; round < 2; ++round) {
-        int at = 0, record = 0;
-        for (int u0 = 0; u0 < p.units; u0 += 256) {
-            if (p.units > 256) sizes(u0 + tid);
-            const int s = max(1, N / q), a = T * s, r = s > 1 ? a : 0;
-            const int a_upto = wave_scan(a), r_upto = wave_scan(r);
-            __syncthreads();
-            if (lane == 63) sh.sums[w] = make_int2(a_upto, r_upto);
-            __syncthreads();
-            int a0 = at + a_upto - a, r0 = record + r_upto - r;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int2 v = sh.sums[y];
-                if (y < w) { a0 += v.x; r0 += v.y; }
-                at += v.x;
-                record += v.y;
-            }
-            if (round && a0 <= own && own < a0 + a) {
-                const int rest = own - a0;
-                sh.place = {u0 + tid, T - 1 - rest % T, T, rest / T, s, r0};
-                if (rest == 0) out.pieces[u0 + tid] = make_int2(r0, s);
-            }
-        }
-        if (round) break;
-        used = scalar(at);
-        const int per = (used + 7) / 8;
-        own = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-        if ((int)(blockIdx.x >> 3) >= per || own >= used) return false;
+    // how many workgroups all tiles take; then whose tile this one's is: each thread has some that follow each other
+    const int some = (items + 255) / 256, e0 = tid * some, e1 = min(items, e0 + some);
+    auto pieces = [&](int e) { const int N = sh.keys[e]; return N < 0 ? 0 : max(1, N / q); };
+    int a = 0, records = 0;
+    for (int e = e0; e < e1; ++e) {
+        const int s = pieces(e);
+        a += s;
+        records += s > 1 ? s : 0;
     }
+    const int a_upto = wave_scan(a), r_upto = wave_scan(records);
+    if (lane == 63) sh.sums[w] = make_int2(a_upto, r_upto);
+    __syncthreads();
+    int a0 = a_upto - a, r0 = r_upto - records, used = 0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const int2 v = sh.sums[y];
+        if (y < w) { a0 += v.x; r0 += v.y; }
+        used += v.x;
+    }
+    used = scalar(used);
+    const int per = (used + 7) / 8, own = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || own >= used) return false;
+    if (a0 <= own && own < a0 + a)
+        for (int e = e0; e < e1; ++e) {
+            const int s = pieces(e);
+            if (own < a0 + s) {
+                const int u = e / most, t = most - 1 - e % most;
+                sh.place = {u, t, own - a0, s, r0 + (own - a0)};
+                if (own == a0) out.pieces[u * most + t] = make_int2(r0, s);
+                break;
+            }
+            a0 += s;
+            r0 += s > 1 ? s : 0;
+        }
     __syncthreads();
     x = sh.place;
-    x.u = scalar(x.u); x.t = scalar(x.t); x.tiles = scalar(x.tiles); x.piece = scalar(x.piece); x.pieces = scalar(x.pieces); x.record = scalar(x.record);
+    x.u = scalar(x.u); x.t = scalar(x.t); x.piece = scalar(x.piece); x.pieces = scalar(x.pieces); x.record = scalar(x.record);
     __syncthreads();
     return x.pieces > 0;
 }
@@ -179,15 +182,15 @@ template <typename T, int D, int COLS>
 __global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel(Chunk p, ChunkParts out, int wgs, int direct) {
     using C = PartCfg<T, D>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ PlaceShared sh;
+    static_assert(sizeof(PlaceShared) <= C::LDS, "the keys' numbers stand where tiles come later");
     __shared__ float2 ml[kPartWaves][kCols];
     Place x;
-    if (!find_place<COLS, kTileRows>(p, sh, out, wgs, kLeastFew, direct, x)) return;
+    if (!find_place<COLS, kTileRows>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastFew, direct, x)) return;
     const ChunkUnit v = chunk_unit(p, x.u, p.group_begin);
     if (v.rows == 0) return;
     const int w = scalar(threadIdx.x >> 6);
     char* const mine = smem + w * C::WAVE;
-    const int tp = (v.prefix_rows + kTileRows - 1) / kTileRows, all = v.tiles(kTileRows);
+    const int tp = (v.prefix_rows + kTileRows - 1) / kTileRows, all = tp + (v.len + kTileRows - 1) / kTileRows;
     const int t0 = (int)((int64_t)all * x.piece / x.pieces), t1 = (int)((int64_t)all * (x.piece + 1) / x.pieces);
     WavePart<T, D, COLS> part;
     const int col = part.col();
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel
             store4(out_row<T>(p, v.b, to) + ch, s);
             if (p.lse && ch == 0) *lse_at(p, v.b, to) = log_sum(top, L);
         } else {
-            const int64_t rec = (int64_t)(x.record + x.piece) * COLS + r;
+            const int64_t rec = (int64_t)x.record * COLS + r;
             *reinterpret_cast<floatx4*>(out.o + rec * D + ch) = s;
             if (ch == 0) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(top, L);
         }
@@ -658,7 +661,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
     struct Held { Place x; int b, g, rows, j0, j1, sees_from, again; };
     static_assert(sizeof(Held) <= 64, "");
     Held& held = *reinterpret_cast<Held*>(smem + 4 * C::TILE);
-    static_assert(sizeof(PlaceShared) <= 4 * C::TILE, "the lengths' sums stand where tiles come later");
+    static_assert(sizeof(PlaceShared) <= 4 * C::TILE, "the keys' numbers stand where tiles come later");
     Many<T, D> many = {p_.K, p_.V, p_.num_pages, p_.page_log2, p_.c, smem};
     int j0, j1, r0;
     {
@@ -682,7 +685,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         many.own_table = p.table + (int64_t)x.u * p.width;
         many.pre_table = p.prefix_table + (int64_t)scalar(v.prefix) * p.prefix_width;
         many.prefix_rows = scalar(v.prefix_rows);
-        many.seen = scalar(between(many.before + divided(many.r_last, p.G, p.inv_G) + 1, 0, v.len));
+        many.seen = scalar(v.seen(p, many.r_last));
         many.tp = scalar((v.prefix_rows + C::BN - 1) / C::BN);
         many.wave_first = scalar(many.before + divided(min(many.r_first, many.r_last), p.G, p.inv_G));
         const int all = many.tp + scalar((many.seen + C::BN - 1) / C::BN);
@@ -757,7 +760,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         // the sums to the part's own unrounded one, so that parts are joined by one number
         const ChunkParts out = read_again<ChunkParts>(sizeof(Chunk));
         const float f = weight > 0.f ? l / weight : 0.f;
-        const int64_t rec = (int64_t)(e.x.record + e.x.piece * e.x.tiles + e.x.t) * kRowsMany + e.r % kRowsMany;
+        const int64_t rec = (int64_t)e.x.record * kRowsMany + e.r % kRowsMany;
 #pragma unroll
         for (int db = 0; db < C::ODB; ++db)
 #pragma unroll
@@ -767,33 +770,48 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
 }
 
 // ---------------------------------------------------------------- parts of cut rows -> rows
-// 1024 / D rows at a time, D / 4 lanes a row; `per` rows a workgroup.
+// 1024 / D rows at a time, D / 4 lanes a row; `per` rows a workgroup.  Parts are asked for eight at a time: a row is a chain of few loads, not of as many as it has parts.
 template <typename T, int D, int BM>
 __global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in, int per, int records) {
-    const int u = blockIdx.y;
-    const ChunkUnit v = chunk_unit(p, u, p.group_begin);
-    const int2 piece = in.pieces[u];
-    const int s = piece.y, tiles = (v.rows + BM - 1) / BM, r_end = min(v.rows, ((int)blockIdx.x + 1) * per);
-    if (v.rows == 0 || s <= 1 || piece.x < 0 || piece.x + tiles * s > records) return;
+    constexpr int kAtOnce = 8;
+    const int u = blockIdx.y, b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv, rows = (p.cnt ? between(p.cnt[u], 0, p.n) : p.n) * p.G;
+    const int most = (p.n * p.G + BM - 1) / BM, r_end = min(rows, ((int)blockIdx.x + 1) * per);
     const int ch = threadIdx.x % (D / 4) * 4;
     for (int r = blockIdx.x * per + threadIdx.x / (D / 4); r < r_end; r += 1024 / D) {
-        const int64_t rec0 = (int64_t)(piece.x + r / BM) * BM + r % BM, step = (int64_t)tiles * BM;
+        const int2 piece = in.pieces[u * most + r / BM];
+        const int s = piece.y;
+        if (s <= 1 || piece.x < 0 || s > records - piece.x) continue;
+        const int64_t rec0 = (int64_t)piece.x * BM + r % BM;
         float M = -INFINITY, L = 0.f;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int y = 0; y < s; ++y) M = fmaxf(M, in.ml[2 * (rec0 + y * step)]);
-        if (M > -INFINITY) {
-#pragma unroll 4
-            for (int y = 0; y < s; ++y) {
-                const float2 ml = *reinterpret_cast<const float2*>(in.ml + 2 * (rec0 + y * step));
-                const float a = fast_exp2(ml.x - M);
-                L += a * ml.y;
-                acc += a * *reinterpret_cast<const floatx4*>(in.o + (rec0 + y * step) * D + ch);
+        for (int y0 = 0; y0 < s; y0 += kAtOnce) {
+            float2 ml[kAtOnce];
+            floatx4 o[kAtOnce];
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const int64_t rec = rec0 + (int64_t)min(y0 + y, s - 1) * BM;
+                ml[y] = *reinterpret_cast<const float2*>(in.ml + 2 * rec);
+                o[y] = *reinterpret_cast<const floatx4*>(in.o + rec * D + ch);
             }
+            float top = M;
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) top = fmaxf(top, ml[y].x);
+            if (top == -INFINITY) continue;
+            const float f = fast_exp2(M - top);
+            L *= f;
+            acc *= f;
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const float a = y0 + y < s ? fast_exp2(ml[y].x - top) : 0.f;
+                L += a * ml[y].y;
+                acc += a * o[y];
+            }
+            M = top;
         }
-        const RowAt at = row_at(p, v.g, r);
+        const RowAt at = row_at(p, g, r);
         acc *= L > 0.f ? 1.f / L : 0.f;
-        store4(out_row<T>(p, v.b, at) + ch, acc);
-        if (p.lse && ch == 0) *lse_at(p, v.b, at) = log_sum(M, L);
+        store4(out_row<T>(p, b, at) + ch, acc);
+        if (p.lse && ch == 0) *lse_at(p, b, at) = log_sum(M, L);
     }
 }
 
@@ -810,13 +828,13 @@ static ChunkPlan chunk_plan(const zipvl_dims& d, int64_t keys) {
     const int64_t tiles = (keys + bn - 1) / bn + 1, items = units * ((rows + x.bm - 1) / x.bm);
     x.wgs = x.few && d.dtype == ZIPVL_F32 && d.d == 128 ? kCus : 2 * kCus;
     const int64_t least = x.few ? kLeastFew : kLeastMany;
-    x.direct = units > kScanUnits || tiles < 2 * least;      // nothing can be cut
+    x.direct = items > kScanItems || d.B > kScanItems || tiles < 2 * least;      // the last: nothing can be cut
     x.join = !x.direct;
     x.grid = (x.direct ? items : items + x.wgs) / 8 * 8 + 8;
     x.records = x.direct ? 0 : x.wgs;
     x.ml = (size_t)x.records * x.bm * d.d * sizeof(float);
     x.pieces = x.ml + (size_t)x.records * x.bm * 2 * sizeof(float);
-    x.total = x.pieces + (x.direct ? 0 : units * sizeof(int2));
+    x.total = x.pieces + (x.direct ? 0 : items * sizeof(int2));
     return x;
 }
 

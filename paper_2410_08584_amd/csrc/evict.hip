@@ -142,7 +142,7 @@ __device__ __forceinline__ void finish_unit(const Evict& p, const EvictUnit& x, 
 // Units whose keys fit LDS.  A round is four rows a thread, which follow each other; their weights and tokens stay in registers, their keys in LDS.  Ranks in the order of rows are
 // sums over the threads before in the wave, and over the counts of (round, wave) before, which stand in LDS.  One CU has a unit, and it is bound by the instructions of
 // its sweeps and some twenty barriers.  4 units of 18432 rows, 7200 to stay, this kernel alone: 27 us (41 with keys in registers, a row a thread and round, ranks by ballots; 30 with the
-// weights and tokens read a second time); 256 units of 2304 rows with their few moves: 10 us (12, with the k-th key's digit found by lanes that meet in LDS banks).
+// weights and tokens read a second time); 256 units of 2064 rows with 16 to leave: 10 us (12, with the k-th key's digit found by lanes that meet in LDS banks).
 constexpr int kRoundsMost = 9;                               // of 4096 rows: 147 KB of keys
 constexpr int kFewKeys = 256;                                // that have the first digits of the k-th are looked at one by one, instead of two more digits
 template <int WAVES, int ROUNDS, int RB>
