@@ -19,7 +19,7 @@
 namespace zipvl {
 
 constexpr int kRowsMany = 128;
-constexpr int kLeastMany = 4, kLeastFew = 4;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
+constexpr int kLeastMany = 4, kLeastPacked = 4, kLeastFew = 4;      // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
 constexpr int kScanItems = 2048;                             // more tiles of rows than this get a workgroup each, whatever their keys
 
 // 8-byte fields and pairs of others only: it is read again as a row of 32-bit numbers
@@ -34,10 +34,12 @@ struct Chunk {
     char* O; int64_t o[3];
     float* lse;
     float c;                                                 // scale log2(e)
+    int slots;                                               // packed: tiles of rows that a KV head's groups may have; 0: rows are not packed
 };
 
-// Parts of tiles of rows that were cut: `rows` rows of D sums and (offset, sum) each.  pieces: a tile's first record and into how many its keys were cut.
-struct ChunkParts { float* o; float* ml; int2* pieces; };
+// Parts of tiles of rows that were cut: rows of D sums and (offset, sum) each.  pieces: of a tile (those of packed rows first), its first row here and into how many its keys were
+// cut; shared: of a unit, the first tile of its group's packed rows (-1: none) and its first row among them.
+struct ChunkParts { float* o; float* ml; int2* pieces; int2* shared; int rows; };
 
 __device__ __forceinline__ int between(int v, int low, int high) { return max(low, min(v, high)); }
 
@@ -53,61 +55,108 @@ __device__ __forceinline__ int group_with(const int32_t* begin, int groups, int 
 }
 
 struct ChunkUnit {
-    int b, g, rows, cnt, len, prefix, prefix_rows;           // rows of queries; prefix: row of prefix_table
+    int b, g, rows, cnt, len, group, prefix, prefix_rows;    // rows of queries; prefix: row of prefix_table
     // own rows that the last token of rows of queries up to r sees
     __device__ __forceinline__ int seen(const Chunk& p, int r) const { return between(len - cnt + divided(min(r, rows - 1), p.G, p.inv_G) + 1, 0, len); }
 };
+__device__ __forceinline__ int tokens_of(const Chunk& p, int u) { return p.cnt ? between(p.cnt[u], 0, p.n) : p.n; }
+__device__ __forceinline__ int prefix_rows_of(const Chunk& p, int prefix) { return between(p.prefix_len[prefix], 0, p.prefix_width << p.page_log2); }
 __device__ __forceinline__ ChunkUnit chunk_unit(const Chunk& p, int u, const int32_t* begin) {
     ChunkUnit x;
     x.b = divided(u, p.Hkv, p.inv_Hkv);
     x.g = u - x.b * p.Hkv;
-    x.cnt = p.cnt ? between(p.cnt[u], 0, p.n) : p.n;
+    x.cnt = tokens_of(p, u);
     x.rows = x.cnt * p.G;
     x.len = between(p.len[u], 0, p.width << p.page_log2);
     x.prefix = x.prefix_rows = 0;
+    x.group = -1;
     if (p.groups) {
-        const int group = group_with(begin, p.groups, p.B, x.b);
-        if (group >= 0) {
-            x.prefix = group * p.Hkv + x.g;
-            x.prefix_rows = between(p.prefix_len[x.prefix], 0, p.prefix_width << p.page_log2);
+        x.group = group_with(begin, p.groups, p.B, x.b);
+        if (x.group >= 0) {
+            x.prefix = x.group * p.Hkv + x.g;
+            x.prefix_rows = prefix_rows_of(p, x.prefix);
         }
     }
     return x;
 }
 
-// What a workgroup has: keys `piece` of `pieces` of tile t of unit u's rows; its record, if pieces > 1.
-struct Place { int u, t, piece, pieces, record; };
+// What a workgroup has: keys `piece` of `pieces` of tile t of unit u's rows, or of the rows of KV head u that group `group` has packed (-1: a unit's).  record: its first row among the
+// parts, -1: it has all that its rows see.
+struct Place { int u, t, piece, pieces, record, group; };
 struct PlaceShared {
-    int32_t begin[kScanItems + 1], keys[kScanItems];
+    int32_t begin[kScanItems + 1], keys[kScanItems], before[kScanItems];        // before: packed rows of the unit's group in front of its own
     unsigned long long total;
     int2 sums[4];
     Place place;
 };
 
+// Packed rows: those of all units of a group and KV head follow each other, so that a prefix meets as few tiles as can.  Tile 0 of a group's is item first_slot() of the head's.
+template <int BM>
+__device__ __forceinline__ int first_slot(const Chunk& p, const int32_t* begin, int group) { return between(begin[group], 0, p.B) * (p.n * p.G) / BM + group; }
+struct Packed { int group, tile, rows; };
+template <int BM>
+__device__ __forceinline__ Packed packed_tile(const Chunk& p, const PlaceShared& sh, int g, int slot) {
+    int lo = 0, hi = p.groups - 1;
+    while (lo < hi) {                                        // the last group that begins there or before
+        const int mid = (lo + hi + 1) >> 1;
+        if (first_slot<BM>(p, sh.begin, mid) <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    const int b0 = between(sh.begin[lo], 0, p.B), b1 = between(sh.begin[lo + 1], 0, p.B) - 1;
+    return {lo, slot - first_slot<BM>(p, sh.begin, lo), b1 < b0 ? 0 : sh.before[b1 * p.Hkv + g] + tokens_of(p, b1 * p.Hkv + g) * p.G};
+}
+// the unit and its row that packed row r of a group and head is
+__device__ __forceinline__ int2 packed_row(const Chunk& p, const PlaceShared& sh, int group, int g, int r) {
+    int lo = between(sh.begin[group], 0, p.B), hi = max(lo, between(sh.begin[group + 1], 0, p.B) - 1);
+    while (lo < hi) {                                        // the last element whose rows begin there or before; those without rows have the one behind them
+        const int mid = (lo + hi + 1) >> 1;
+        if (sh.before[mid * p.Hkv + g] <= r) lo = mid;
+        else hi = mid - 1;
+    }
+    return make_int2(lo, between(r - sh.before[lo * p.Hkv + g], 0, p.n * p.G - 1));
+}
+
 // BM rows of queries and BN keys a tile.  Workgroups that have neighbouring tiles of rows, and so the same keys, follow each other on one XCD (workgroups go to the eight in turn).
-template <int BM, int BN>
+template <int BM, int BN, bool PACKS>
 __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, const ChunkParts& out, int wgs, int least, int direct, Place& x) {
-    const int tid = threadIdx.x, lane = tid & 63, w = scalar(tid >> 6);
-    const int most = (p.n * p.G + BM - 1) / BM, items = p.units * most;      // tiles of rows of a unit, of all
+    const int tid = threadIdx.x, lane = tid & 63, w = scalar(tid >> 6), rows = p.n * p.G;
+    const int most = (rows + BM - 1) / BM, packed = PACKS ? p.Hkv * p.slots : 0, items = packed + p.units * most;        // tiles of rows of a unit, of packed rows, all
     if (direct) {
         const int per = gridDim.x / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
         if (id >= items) return false;
-        x = {id / most, most - 1 - id % most, 0, 1, 0};
+        x = {id / most, most - 1 - id % most, 0, 1, -1, -1};
         return true;
     }
     for (int i = tid; i <= p.groups && p.groups; i += 256) sh.begin[i] = p.group_begin[i];
     if (tid == 0) { sh.total = 0; sh.place.pieces = 0; }
     __syncthreads();
-    // tiles of keys of each: tile of rows `most` - 1 first, the longest; -1: the unit has fewer rows
+    if (packed) {
+        for (int u = tid; u < p.units; u += 256) {
+            const int b = divided(u, p.Hkv, p.inv_Hkv), group = group_with(sh.begin, p.groups, p.B, b);
+            int before = 0;
+            if (group >= 0) {
+#pragma unroll 8
+                for (int y = between(sh.begin[group], 0, p.B); y < b; ++y) before += tokens_of(p, y * p.Hkv + u - b * p.Hkv);
+            }
+            sh.before[u] = before * p.G;
+        }
+        __syncthreads();
+    }
+    // tiles of keys of each: packed rows first, and a unit's tile of rows `most` - 1, the longest; -1: there are fewer rows
     unsigned long long mine = 0;
     for (int e = tid; e < items; e += 256) {
-        const int u = e / most, r0 = (most - 1 - e % most) * BM;
-        const ChunkUnit v = chunk_unit(p, u, sh.begin);
         int N = -1;
-        if (r0 < v.rows) {
-            N = (v.seen(p, r0 + BM - 1) + BN - 1) / BN + (v.prefix_rows + BN - 1) / BN;
-            mine += N;
+        if (e < packed) {
+            const int g = e / p.slots;
+            const Packed x = packed_tile<BM>(p, sh, g, e - g * p.slots);
+            if (x.tile >= 0 && x.tile * BM < x.rows) N = (prefix_rows_of(p, x.group * p.Hkv + g) + BN - 1) / BN;
+            if (N == 0) N = -1;
+        } else {
+            const int u = (e - packed) / most, r0 = (most - 1 - (e - packed) % most) * BM;
+            const ChunkUnit v = chunk_unit(p, u, sh.begin);
+            if (r0 < v.rows) N = (v.seen(p, r0 + BM - 1) + BN - 1) / BN + (packed ? 0 : (v.prefix_rows + BN - 1) / BN);
         }
+        mine += max(N, 0);
         sh.keys[e] = N;
     }
     if (mine) atomicAdd(&sh.total, mine);
@@ -117,11 +166,15 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
     // how many workgroups all tiles take; then whose tile this one's is: each thread has some that follow each other
     const int some = (items + 255) / 256, e0 = tid * some, e1 = min(items, e0 + some);
     auto pieces = [&](int e) { const int N = sh.keys[e]; return N < 0 ? 0 : max(1, N / q); };
+    // A piece's part has so many rows.  Of tiles that are not cut, those of packed rows have one, and of packed prefixes those of the units' rows (also of units without such a prefix,
+    // which leave theirs).
+    const int part = min(rows, BM);
+    auto parts = [&](int e, int s) { return e < packed ? s * BM : s > 1 || packed ? s * part : 0; };
     int a = 0, records = 0;
     for (int e = e0; e < e1; ++e) {
         const int s = pieces(e);
         a += s;
-        records += s > 1 ? s : 0;
+        records += parts(e, s);
     }
     const int a_upto = wave_scan(a), r_upto = wave_scan(records);
     if (lane == 63) sh.sums[w] = make_int2(a_upto, r_upto);
@@ -140,17 +193,30 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
         for (int e = e0; e < e1; ++e) {
             const int s = pieces(e);
             if (own < a0 + s) {
-                const int u = e / most, t = most - 1 - e % most;
-                sh.place = {u, t, own - a0, s, r0 + (own - a0)};
-                if (own == a0) out.pieces[u * most + t] = make_int2(r0, s);
+                const int piece = own - a0;
+                if (e < packed) {
+                    const int g = e / p.slots;
+                    const Packed x = packed_tile<BM>(p, sh, g, e - g * p.slots);
+                    sh.place = {g, x.tile, piece, s, r0 + piece * BM, x.group};
+                } else {
+                    const int u = (e - packed) / most, t = most - 1 - (e - packed) % most;
+                    bool whole = s == 1;
+                    if (packed) {
+                        const ChunkUnit v = chunk_unit(p, u, sh.begin);
+                        if (v.prefix_rows) whole = false;
+                        if (piece == 0) out.shared[u] = v.prefix_rows ? make_int2(v.g * p.slots + first_slot<BM>(p, sh.begin, v.group), sh.before[u]) : make_int2(-1, 0);
+                    }
+                    sh.place = {u, t, piece, s, whole ? -1 : r0 + piece * part, -1};
+                }
+                if (piece == 0) out.pieces[e < packed ? e : packed + (e - packed) / most * most + sh.place.t] = make_int2(sh.place.record, s);
                 break;
             }
             a0 += s;
-            r0 += s > 1 ? s : 0;
+            r0 += parts(e, s);
         }
     __syncthreads();
     x = sh.place;
-    x.u = scalar(x.u); x.t = scalar(x.t); x.piece = scalar(x.piece); x.pieces = scalar(x.pieces); x.record = scalar(x.record);
+    x.u = scalar(x.u); x.t = scalar(x.t); x.piece = scalar(x.piece); x.pieces = scalar(x.pieces); x.record = scalar(x.record); x.group = scalar(x.group);
     __syncthreads();
     return x.pieces > 0;
 }
@@ -185,7 +251,7 @@ __global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel
     static_assert(sizeof(PlaceShared) <= C::LDS, "the keys' numbers stand where tiles come later");
     __shared__ float2 ml[kPartWaves][kCols];
     Place x;
-    if (!find_place<COLS, kTileRows>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastFew, direct, x)) return;
+    if (!find_place<COLS, kTileRows, false>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastFew, direct, x)) return;
     const ChunkUnit v = chunk_unit(p, x.u, p.group_begin);
     if (v.rows == 0) return;
     const int w = scalar(threadIdx.x >> 6);
@@ -240,13 +306,13 @@ __global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[e] += base[y * (C::WAVE / 4) + (ch + e) * kCols + (r ^ ((ch + e) & 31))];
         }
-        if (x.pieces == 1) {
+        if (x.record < 0) {
             const RowAt to = row_at(p, v.g, r);
             s *= L > 0.f ? 1.f / L : 0.f;
             store4(out_row<T>(p, v.b, to) + ch, s);
             if (p.lse && ch == 0) *lse_at(p, v.b, to) = log_sum(top, L);
         } else {
-            const int64_t rec = (int64_t)x.record * COLS + r;
+            const int64_t rec = x.record + r;
             *reinterpret_cast<floatx4*>(out.o + rec * D + ch) = s;
             if (ch == 0) *reinterpret_cast<float2*>(out.ml + 2 * rec) = make_float2(top, L);
         }
@@ -668,8 +734,16 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         const Chunk p = read_again<Chunk>(0);
         const ChunkParts out = read_again<ChunkParts>(sizeof(Chunk));
         Place x;
-        if (!find_place<kRowsMany, C::BN>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastMany, direct, x)) return;
-        const ChunkUnit v = chunk_unit(p, x.u, p.group_begin);
+        PlaceShared& sh = *reinterpret_cast<PlaceShared*>(smem);
+        if (!find_place<kRowsMany, C::BN, true>(p, sh, out, wgs, p.slots ? kLeastPacked : kLeastMany, direct, x)) return;
+        ChunkUnit v;
+        if (x.group >= 0) {                                  // packed rows, which see all of their prefix and nothing else
+            v = {0, x.u, packed_tile<kRowsMany>(p, sh, x.u, first_slot<kRowsMany>(p, sh.begin, x.group)).rows, 0, 0, x.group, x.group * p.Hkv + x.u, 0};
+            v.prefix_rows = prefix_rows_of(p, v.prefix);
+        } else {
+            v = chunk_unit(p, x.u, p.group_begin);
+            if (p.slots) v.prefix_rows = 0;
+        }
         r0 = x.t * kRowsMany;
         if (r0 >= v.rows) return;
         const int tid = threadIdx.x;
@@ -682,7 +756,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         many.before = scalar(v.len - v.cnt);
         many.G = p.G;
         many.inv_G = p.inv_G;
-        many.own_table = p.table + (int64_t)x.u * p.width;
+        many.own_table = p.table + (int64_t)(x.group >= 0 ? 0 : x.u) * p.width;
         many.pre_table = p.prefix_table + (int64_t)scalar(v.prefix) * p.prefix_width;
         many.prefix_rows = scalar(v.prefix_rows);
         many.seen = scalar(v.seen(p, many.r_last));
@@ -692,8 +766,14 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         j0 = scalar((int)((int64_t)all * x.piece / x.pieces));
         j1 = scalar((int)((int64_t)all * (x.piece + 1) / x.pieces));
         if (tid == 0) held = {x, v.b, v.g, v.rows, j0, j1, j0 < j1 ? j0 < many.tp ? INT32_MIN : (j0 - many.tp) * C::BN : INT32_MAX, 0};
-        __syncthreads();
-        const T* row = query_row<T>(p, v.b, row_at(p, v.g, min(many.r_first + many.i, many.r_last)));
+        int r = min(many.r_first + many.i, many.r_last);
+        if (x.group >= 0) {
+            const int2 at = packed_row(p, sh, x.group, v.g, r);
+            v.b = at.x;
+            r = at.y;
+        }
+        __syncthreads();                                     // `before` has been read: tiles may come there
+        const T* row = query_row<T>(p, v.b, row_at(p, v.g, r));
 #pragma unroll
         for (int cc = 0; cc < C::CH; ++cc) many.qf[cc] = load16(row + (2 * cc + many.h) * Elem<T>::kPerFrag);
     }
@@ -748,7 +828,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
     if (e.r > e.r_last) return;
     const RowAt at = {e.token, e.g * p.G + e.r - e.token * p.G};
     auto four = [&](int db, int a) { return floatx4{many.o[db][4 * a], many.o[db][4 * a + 1], many.o[db][4 * a + 2], many.o[db][4 * a + 3]}; };
-    if (e.x.pieces == 1) {
+    if (e.x.record < 0) {
         const float inv = weight > 0.f ? 1.f / weight : 0.f;
         T* row = out_row<T>(p, e.b, at);
 #pragma unroll
@@ -760,7 +840,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         // the sums to the part's own unrounded one, so that parts are joined by one number
         const ChunkParts out = read_again<ChunkParts>(sizeof(Chunk));
         const float f = weight > 0.f ? l / weight : 0.f;
-        const int64_t rec = (int64_t)e.x.record * kRowsMany + e.r % kRowsMany;
+        const int64_t rec = e.x.record + e.r % kRowsMany;
 #pragma unroll
         for (int db = 0; db < C::ODB; ++db)
 #pragma unroll
@@ -772,16 +852,20 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
 // ---------------------------------------------------------------- parts of cut rows -> rows
 // 1024 / D rows at a time, D / 4 lanes a row; `per` rows a workgroup.  Parts are asked for eight at a time: a row is a chain of few loads, not of as many as it has parts.
 template <typename T, int D, int BM>
-__global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in, int per, int records) {
+__global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in, int per) {
     constexpr int kAtOnce = 8;
-    const int u = blockIdx.y, b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv, rows = (p.cnt ? between(p.cnt[u], 0, p.n) : p.n) * p.G;
-    const int most = (p.n * p.G + BM - 1) / BM, r_end = min(rows, ((int)blockIdx.x + 1) * per);
+    const int u = blockIdx.y, b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv, rows = tokens_of(p, u) * p.G;
+    const int most = (p.n * p.G + BM - 1) / BM, part = min(p.n * p.G, BM), packed = p.Hkv * p.slots, r_end = min(rows, ((int)blockIdx.x + 1) * per);
     const int ch = threadIdx.x % (D / 4) * 4;
     for (int r = blockIdx.x * per + threadIdx.x / (D / 4); r < r_end; r += 1024 / D) {
-        const int2 piece = in.pieces[u * most + r / BM];
-        const int s = piece.y;
-        if (s <= 1 || piece.x < 0 || s > records - piece.x) continue;
-        const int64_t rec0 = (int64_t)piece.x * BM + r % BM;
+        const int2 own = in.pieces[packed + u * most + r / BM], shared = packed ? in.shared[u] : make_int2(-1, 0);
+        if (own.x < 0 || own.y < 1 || own.x + own.y * part > in.rows) continue;          // nothing to join
+        int2 first = {0, 0};
+        const int packed_r = shared.y + r;
+        if (shared.x >= 0 && shared.x + packed_r / BM < packed) first = in.pieces[shared.x + packed_r / BM];
+        if (first.x < 0 || first.y < 0 || first.x + first.y * BM > in.rows) continue;
+        const int s = first.y + own.y;                       // parts
+        auto record = [&](int y) { return (int64_t)(y < first.y ? first.x + y * BM + packed_r % BM : own.x + (y - first.y) * part + r % BM); };
         float M = -INFINITY, L = 0.f;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int y0 = 0; y0 < s; y0 += kAtOnce) {
@@ -789,7 +873,7 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in,
             floatx4 o[kAtOnce];
 #pragma unroll
             for (int y = 0; y < kAtOnce; ++y) {
-                const int64_t rec = rec0 + (int64_t)min(y0 + y, s - 1) * BM;
+                const int64_t rec = record(min(y0 + y, s - 1));
                 ml[y] = *reinterpret_cast<const float2*>(in.ml + 2 * rec);
                 o[y] = *reinterpret_cast<const floatx4*>(in.o + rec * D + ch);
             }
@@ -817,28 +901,45 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in,
 
 // ---------------------------------------------------------------- host
 constexpr int kFewRows = 32;
-struct ChunkPlan { int few, direct, wgs, records, bm, join; int64_t grid; size_t ml, pieces, total; };
+constexpr int kRowsPacked = 4 * kRowsMany;                   // of a unit, up to which rows of a group are packed: tiles that are not full are then a part of all that counts
+struct ChunkPlan { int few, direct, wgs, rows, bm, slots; int64_t grid; size_t ml, pieces, shared, total; };
 // keys: that the tables of a unit and its prefix can hold
-static ChunkPlan chunk_plan(const zipvl_dims& d, int64_t keys) {
+static ChunkPlan chunk_plan(const zipvl_dims& d, int64_t keys, int groups) {
     ChunkPlan x;
     const int64_t rows = (int64_t)d.n * (d.Hq / d.Hkv), units = (int64_t)d.B * d.Hkv;
     x.few = rows <= kFewRows;
+    x.slots = 0;
+    int64_t items = 0;
+    if (groups > 0 && 2 * groups <= d.B && rows <= kRowsPacked && rows * d.B / groups > kFewRows) {
+        const int64_t slots = d.B * rows / kRowsMany + groups + 1;
+        items = units * ((rows + kRowsMany - 1) / kRowsMany) + d.Hkv * slots;
+        if (items <= kScanItems) {
+            x.slots = (int)slots;
+            x.few = 0;
+        }
+    }
     x.bm = x.few ? (rows <= 16 ? 16 : 32) : kRowsMany;
     const int bn = x.few || d.dtype == ZIPVL_F32 ? 32 : 64;
-    const int64_t tiles = (keys + bn - 1) / bn + 1, items = units * ((rows + x.bm - 1) / x.bm);
+    const int64_t tiles = (keys + bn - 1) / bn + 1;
+    if (!x.slots) items = units * ((rows + x.bm - 1) / x.bm);
     x.wgs = x.few && d.dtype == ZIPVL_F32 && d.d == 128 ? kCus : 2 * kCus;
-    const int64_t least = x.few ? kLeastFew : kLeastMany;
-    x.direct = items > kScanItems || d.B > kScanItems || tiles < 2 * least;      // the last: nothing can be cut
-    x.join = !x.direct;
+    const int64_t least = x.few ? kLeastFew : kLeastMany, part = std::min<int64_t>(rows, x.bm);
+    x.direct = !x.slots && (items > kScanItems || tiles < 2 * least);      // the last: nothing can be cut
     x.grid = (x.direct ? items : items + x.wgs) / 8 * 8 + 8;
-    x.records = x.direct ? 0 : x.wgs;
-    x.ml = (size_t)x.records * x.bm * d.d * sizeof(float);
-    x.pieces = x.ml + (size_t)x.records * x.bm * 2 * sizeof(float);
-    x.total = x.pieces + (x.direct ? 0 : items * sizeof(int2));
+    x.rows = x.direct ? 0 : x.slots ? (int)(x.wgs * x.bm + units * ((rows + x.bm - 1) / x.bm) * part + (int64_t)d.Hkv * x.slots * x.bm) : (int)(x.wgs * part);
+    x.ml = (size_t)x.rows * d.d * sizeof(float);
+    x.pieces = x.ml + (size_t)x.rows * 2 * sizeof(float);
+    x.shared = x.pieces + (x.direct ? 0 : items * sizeof(int2));
+    x.total = x.shared + (x.slots ? units * sizeof(int2) : 0);
     return x;
 }
 
-size_t chunk_attn_workspace_bytes(const zipvl_dims& d, int64_t keys) { return std::max<size_t>(16, chunk_plan(d, keys).total); }
+// For any number of groups: of those whose rows are packed, the most take most.
+size_t chunk_attn_workspace_bytes(const zipvl_dims& d, int64_t keys) {
+    const int64_t rows = (int64_t)d.n * (d.Hq / d.Hkv), left = (kScanItems - (int64_t)d.B * d.Hkv * ((rows + kRowsMany - 1) / kRowsMany)) / d.Hkv - d.B * rows / kRowsMany - 1;
+    const int64_t groups = std::min<int64_t>(std::min<int64_t>(d.B / 2, left), d.B * rows / (kFewRows + 1));
+    return std::max<size_t>(std::max<size_t>(16, chunk_plan(d, keys, 0).total), groups > 0 ? chunk_plan(d, keys, (int)groups).total : 0);
+}
 
 template <typename Kernel>
 static int allow_lds(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
@@ -858,7 +959,7 @@ static int launch_join(const Chunk& p, const ChunkParts& parts, const ChunkPlan&
     int64_t per = step;                                      // about 2048 workgroups at most
     while (p.units * ((rows + per - 1) / per) > 2048 && per < rows) per *= 2;
     KernelTimer tm(ZIPVL_K_CHUNK_JOIN, st);
-    hipLaunchKernelGGL((chunk_join_kernel<T, D, BM>), dim3((unsigned)((rows + per - 1) / per), p.units), dim3(256), 0, st, p, parts, (int)per, x.records);
+    hipLaunchKernelGGL((chunk_join_kernel<T, D, BM>), dim3((unsigned)((rows + per - 1) / per), p.units), dim3(256), 0, st, p, parts, (int)per);
     return check_launch("chunk_attn_paged parts");
 }
 
@@ -872,7 +973,7 @@ static int launch_few(const Chunk& p, const ChunkParts& parts, const ChunkPlan& 
         hipLaunchKernelGGL((chunk_few_kernel<T, D, COLS>), dim3((unsigned)x.grid), dim3(256), (PartCfg<T, D>::LDS), st, p, parts, x.wgs, x.direct);
         if ((rc = check_launch("chunk_attn_paged"))) return rc;
     }
-    return x.join ? launch_join<T, D, COLS>(p, parts, x, st) : ZIPVL_OK;
+    return !x.direct ? launch_join<T, D, COLS>(p, parts, x, st) : ZIPVL_OK;
 }
 
 template <typename T, int D>
@@ -886,7 +987,7 @@ static int launch_chunk_t(const Chunk& p, const ChunkParts& parts, const ChunkPl
         hipLaunchKernelGGL((chunk_many_kernel<T, D>), dim3((unsigned)x.grid), dim3(256), (ChunkCfg<T, D>::LDS), st, p, parts, x.wgs, x.direct);
         if ((rc = check_launch("chunk_attn_paged"))) return rc;
     }
-    return x.join ? launch_join<T, D, kRowsMany>(p, parts, x, st) : ZIPVL_OK;
+    return !x.direct ? launch_join<T, D, kRowsMany>(p, parts, x, st) : ZIPVL_OK;
 }
 
 int launch_chunk_attn_paged(const void* Q, const zipvl_pages& pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
@@ -894,12 +995,13 @@ int launch_chunk_attn_paged(const void* Q, const zipvl_pages& pages, const int32
                             const zipvl_dims& d, float scale, void* O, const int64_t* o_strides, float* lse, void* ws, hipStream_t st)
 {
     const int G = d.Hq / d.Hkv;
-    const Chunk p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len, k,
+    Chunk p = {(const char*)pages.K, (const char*)pages.V, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len, k,
                      prefix_table, prefix_pages, prefix_len, group_begin, groups, d.B, d.Hq, d.Hkv, G, d.n, d.B * d.Hkv, inverse(d.Hkv), inverse(G),
-                     (const char*)Q, {d.q_strides[0], d.q_strides[1], d.q_strides[2]}, (char*)O, {o_strides[0], o_strides[1], o_strides[2]}, lse, scale * kLog2e};
-    const ChunkPlan x = chunk_plan(d, ((int64_t)table_pages + prefix_pages) * pages.page);
+                     (const char*)Q, {d.q_strides[0], d.q_strides[1], d.q_strides[2]}, (char*)O, {o_strides[0], o_strides[1], o_strides[2]}, lse, scale * kLog2e, 0};
+    const ChunkPlan x = chunk_plan(d, ((int64_t)table_pages + prefix_pages) * pages.page, groups);
+    p.slots = x.slots;
     if (x.grid >= 1 << 24) return set_error(ZIPVL_ESHAPE, "zipvl_chunk_attn_paged: %lld tiles of queries are more than one grid takes", (long long)x.grid);
-    const ChunkParts parts = {(float*)ws, (float*)((char*)ws + x.ml), (int2*)((char*)ws + x.pieces)};
+    const ChunkParts parts = {(float*)ws, (float*)((char*)ws + x.ml), (int2*)((char*)ws + x.pieces), (int2*)((char*)ws + x.shared), x.rows};
     if (d.dtype == ZIPVL_BF16) return d.d == 128 ? launch_chunk_t<__bf16, 128>(p, parts, x, st) : launch_chunk_t<__bf16, 64>(p, parts, x, st);
     return d.d == 128 ? launch_chunk_t<float, 128>(p, parts, x, st) : launch_chunk_t<float, 64>(p, parts, x, st);
 }

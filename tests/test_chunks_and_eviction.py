@@ -129,7 +129,9 @@ class Setting:
         w = torch.exp(logits - torch.where(lse > -math.inf, lse, torch.zeros_like(lse))[..., None])
         big = float((q.abs() @ K.abs().T * seen[None]).max()) * self.scale if K.shape[0] and c else 0.0
         off = (self.d + 4) * U * big + (K.shape[0] + 64) * U
-        rounded = half_step(torch.bfloat16) if self.dtype == torch.bfloat16 and self.n * self.G > 32 else 0.0
+        groups = len(self.begin) - 1
+        packed = groups > 0 and 2 * groups <= self.B and self.n * self.G * self.B // groups > 32       # a group's rows of queries in tiles together
+        rounded = half_step(torch.bfloat16) if self.dtype == torch.bfloat16 and (self.n * self.G > 32 or packed) else 0.0
         return w @ V, lse, 2 * (off + rounded) * (w @ V.abs()), off + 4 * U * (lse.abs().nan_to_num(0, 0, 0) + big), w[..., first:], big
 
 
@@ -170,6 +172,12 @@ CHUNK = [  # B, Hq, Hkv, n, d, dtype, page, lens, k, groups, pre, order
     (1, 7, 1, 70, 128, "f32", 64, [700], None, (0, 1), (97,), "token"),
     (2, 5, 1, 13, 128, "f32", 256, [13, 270], None, (1, 2), (31,), "head"),
     (5, 16, 8, 33, 64, "bf16", 16, [33, 40, 1030, 0, 12, 77, 64], [33, 32, 0, 5], (0, 1, 4), (1025, 64, 17), "token"),
+    (6, 28, 4, 2, 128, "bf16", 64, [2, 65, 1, 0, 900], [2, 1, 0], (0, 4, 6), (700, 0, 65, 1300, 100), "token"),
+    (9, 4, 1, 10, 64, "f32", 16, [10, 50, 100], [10, 3, 0, 7], (0, 2, 2, 7), (129, 64, 0), "head"),
+    (16, 7, 1, 18, 128, "bf16", 16, [18, 300, 0, 40], [18, 0, 0, 5, 17], (0, 16), (2000,), "token"),
+    (4, 2, 2, 256, 64, "bf16", 32, [256, 700, 300], [256, 255, 1], (0, 4), (333, 1), "head"),
+    (8, 40, 2, 1, 128, "f32", 16, [1, 30, 0], None, (2, 6), (500, 77), "token"),
+    (40, 1, 1, 1, 64, "bf16", 16, [1, 2, 90], [1, 1, 0], (0, 40), (640,), "head"),
 ]
 
 
