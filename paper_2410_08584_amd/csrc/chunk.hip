@@ -19,7 +19,7 @@
 namespace zipvl {
 
 constexpr int kRowsMany = 128;
-constexpr int kLeastMany = 4, kLeastPacked = 4, kLeastFew = 4;      // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
+constexpr int kLeastMany = 4, kLeastFew = 4;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
 constexpr int kScanItems = 2048;                             // more tiles of rows than this get a workgroup each, whatever their keys
 
 // 8-byte fields and pairs of others only: it is read again as a row of 32-bit numbers
@@ -85,7 +85,7 @@ __device__ __forceinline__ ChunkUnit chunk_unit(const Chunk& p, int u, const int
 struct Place { int u, t, piece, pieces, record, group; };
 struct PlaceShared {
     int32_t begin[kScanItems + 1], keys[kScanItems], before[kScanItems];        // before: packed rows of the unit's group in front of its own
-    unsigned long long total;
+    unsigned long long total[4];
     int2 sums[4];
     Place place;
 };
@@ -118,7 +118,7 @@ __device__ __forceinline__ int2 packed_row(const Chunk& p, const PlaceShared& sh
 
 // BM rows of queries and BN keys a tile.  Workgroups that have neighbouring tiles of rows, and so the same keys, follow each other on one XCD (workgroups go to the eight in turn).
 template <int BM, int BN, bool PACKS>
-__device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, const ChunkParts& out, int wgs, int least, int direct, Place& x) {
+__device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, const ChunkParts& out, int log2_wgs, int least, int direct, Place& x) {
     const int tid = threadIdx.x, lane = tid & 63, w = scalar(tid >> 6), rows = p.n * p.G;
     const int most = (rows + BM - 1) / BM, packed = PACKS ? p.Hkv * p.slots : 0, items = packed + p.units * most;        // tiles of rows of a unit, of packed rows, all
     if (direct) {
@@ -128,7 +128,7 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
         return true;
     }
     for (int i = tid; i <= p.groups && p.groups; i += 256) sh.begin[i] = p.group_begin[i];
-    if (tid == 0) { sh.total = 0; sh.place.pieces = 0; }
+    if (tid == 0) sh.place.pieces = 0;
     __syncthreads();
     if (packed) {
         for (int u = tid; u < p.units; u += 256) {
@@ -143,7 +143,7 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
         __syncthreads();
     }
     // tiles of keys of each: packed rows first, and a unit's tile of rows `most` - 1, the longest; -1: there are fewer rows
-    unsigned long long mine = 0;
+    int mine = 0;                                            // of 8 items at most
     for (int e = tid; e < items; e += 256) {
         int N = -1;
         if (e < packed) {
@@ -159,10 +159,14 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
         mine += max(N, 0);
         sh.keys[e] = N;
     }
-    if (mine) atomicAdd(&sh.total, mine);
+    {
+        // 32 bits may not hold the sum of all: high and low halves apart
+        const int low = wave_sum(mine & 0xFFFF), high = wave_sum(mine >> 16);
+        if (lane == 0) sh.total[w] = ((unsigned long long)high << 16) + low;
+    }
     __syncthreads();
     // A tile of rows is cut into as many pieces as it has average loads, rounded down: then all pieces fit the chip at once
-    const int q = max(least, (int)min((unsigned long long)INT32_MAX, (sh.total + wgs - 1) / wgs));
+    const int q = max(least, (int)min((unsigned long long)INT32_MAX, (sh.total[0] + sh.total[1] + sh.total[2] + sh.total[3] + (1 << log2_wgs) - 1) >> log2_wgs));
     // how many workgroups all tiles take; then whose tile this one's is: each thread has some that follow each other
     const int some = (items + 255) / 256, e0 = tid * some, e1 = min(items, e0 + some);
     auto pieces = [&](int e) { const int N = sh.keys[e]; return N < 0 ? 0 : max(1, N / q); };
@@ -245,13 +249,13 @@ __device__ __forceinline__ float* lse_at(const Chunk& p, int b, RowAt x) { retur
 
 // ---------------------------------------------------------------- few rows
 template <typename T, int D, int COLS>
-__global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel(Chunk p, ChunkParts out, int wgs, int direct) {
+__global__ __launch_bounds__(256, (PartCfg<T, D>::PER_CU)) void chunk_few_kernel(Chunk p, ChunkParts out, int log2_wgs, int direct) {
     using C = PartCfg<T, D>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     static_assert(sizeof(PlaceShared) <= C::LDS, "the keys' numbers stand where tiles come later");
     __shared__ float2 ml[kPartWaves][kCols];
     Place x;
-    if (!find_place<COLS, kTileRows, false>(p, *reinterpret_cast<PlaceShared*>(smem), out, wgs, kLeastFew, direct, x)) return;
+    if (!find_place<COLS, kTileRows, false>(p, *reinterpret_cast<PlaceShared*>(smem), out, log2_wgs, kLeastFew, direct, x)) return;
     const ChunkUnit v = chunk_unit(p, x.u, p.group_begin);
     if (v.rows == 0) return;
     const int w = scalar(threadIdx.x >> 6);
@@ -720,7 +724,7 @@ __device__ __forceinline__ A read_again(int offset) {
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts out_, int wgs, int direct) {
+__global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts out_, int log2_wgs, int direct) {
     using C = ChunkCfg<T, D>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     // of the workgroup, for the end; behind the tiles, which then begin where LDS does: their addresses fit an instruction's offset
@@ -735,7 +739,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         const ChunkParts out = read_again<ChunkParts>(sizeof(Chunk));
         Place x;
         PlaceShared& sh = *reinterpret_cast<PlaceShared*>(smem);
-        if (!find_place<kRowsMany, C::BN, true>(p, sh, out, wgs, p.slots ? kLeastPacked : kLeastMany, direct, x)) return;
+        if (!find_place<kRowsMany, C::BN, true>(p, sh, out, log2_wgs, kLeastMany, direct, x)) return;
         ChunkUnit v;
         if (x.group >= 0) {                                  // packed rows, which see all of their prefix and nothing else
             v = {0, x.u, packed_tile<kRowsMany>(p, sh, x.u, first_slot<kRowsMany>(p, sh.begin, x.group)).rows, 0, 0, x.group, x.group * p.Hkv + x.u, 0};
@@ -970,7 +974,7 @@ static int launch_few(const Chunk& p, const ChunkParts& parts, const ChunkPlan& 
     if (rc) return rc;
     {
         KernelTimer tm(ZIPVL_K_CHUNK_ATTN, st);
-        hipLaunchKernelGGL((chunk_few_kernel<T, D, COLS>), dim3((unsigned)x.grid), dim3(256), (PartCfg<T, D>::LDS), st, p, parts, x.wgs, x.direct);
+        hipLaunchKernelGGL((chunk_few_kernel<T, D, COLS>), dim3((unsigned)x.grid), dim3(256), (PartCfg<T, D>::LDS), st, p, parts, __builtin_ctz(x.wgs), x.direct);
         if ((rc = check_launch("chunk_attn_paged"))) return rc;
     }
     return !x.direct ? launch_join<T, D, COLS>(p, parts, x, st) : ZIPVL_OK;
@@ -984,7 +988,7 @@ static int launch_chunk_t(const Chunk& p, const ChunkParts& parts, const ChunkPl
     if (rc) return rc;
     {
         KernelTimer tm(ZIPVL_K_CHUNK_ATTN, st);
-        hipLaunchKernelGGL((chunk_many_kernel<T, D>), dim3((unsigned)x.grid), dim3(256), (ChunkCfg<T, D>::LDS), st, p, parts, x.wgs, x.direct);
+        hipLaunchKernelGGL((chunk_many_kernel<T, D>), dim3((unsigned)x.grid), dim3(256), (ChunkCfg<T, D>::LDS), st, p, parts, __builtin_ctz(x.wgs), x.direct);
         if ((rc = check_launch("chunk_attn_paged"))) return rc;
     }
     return !x.direct ? launch_join<T, D, kRowsMany>(p, parts, x, st) : ZIPVL_OK;
