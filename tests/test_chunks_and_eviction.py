@@ -363,6 +363,34 @@ def test_paged_weigh_of_the_last_queries(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("spare", [100, 300])
+def test_paged_weigh_where_tables_are_wide(dtype, d, spare):
+    """Many rows may be there, so that a wave has more of them: few are."""
+    say(f"weigh {dtype} {d} {spare} spare pages")
+    s = Setting(2, 6, 2, 70, d, dtype, 256, [700, 90, 64, 1], [70, 33, 64, 65], order="token", seed=19, spare=spare)
+    s.table[1, 0] = -1
+    cache = s.cache()
+    _, lse = chunk(s, cache)
+    weight = torch.full((4, s.table.shape[1] * s.page), 7.0, device=DEV)
+    z.zipvl_paged_weigh(s.Q, cache, s.table.to(DEV), s.ints(s.lens), lse, s.scale, k=s.ints(s.k), weight=weight)
+    assert_weights(s, weight, lse, None, fill=7.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [3, 70])
+@pytest.mark.parametrize("of_queries", [2.0 ** 101, 2.0 ** -101])
+def test_paged_weigh_of_huge_numbers(n, of_queries):
+    """fp32 whose products fit, with queries or keys that the planes of bf16 do not hold in full range: the same weights as of their like of ordinary size."""
+    s = Setting(1, 4, 2, n, 64, "f32", 16, [200, 100], None, seed=20)
+    _, lse = chunk(s)
+    s.Q.mul_(of_queries)
+    s.K.mul_(1 / of_queries)
+    w = z.zipvl_paged_weigh(s.Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale)
+    assert_weights(s, w, lse, None)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [1, 4, 50])
 def test_paged_weigh_skips_rows_without_a_page_and_clamps_lengths(n):
     s = Setting(2, 4, 2, n, 128, "bf16", 16, [200, 77, 150, 64], None, seed=18)
@@ -413,6 +441,10 @@ EVICT = [  # B, Hkv, d, dtype, page, lens, budget, sinks, recent, tokens, weight
     (1, 4, 64, "bf16", 16, [900, 800, 700, 600], 10 ** 9, 0, 0, True, "random", [100, -1, 2 ** 31 - 1, 0]),
     (1, 2, 128, "bf16", 64, [34000, 20000], 12345, 4, 100, True, "ties", None),
     (70, 2, 64, "bf16", 16, [40, 33, 48], 32, 1, 4, False, "random", None),
+    (1, 2, 64, "bf16", 128, [16000, 9000], 7000, 4, 100, True, "zeros", None),
+    (1, 2, 64, "bf16", 256, [40000, 36900], 11111, 4, 100, True, "odd", None),
+    (1, 2, 64, "f32", 16, [40000, 39970], 39960, 4, 100, True, "random", None),
+    (2, 2, 128, "f32", 64, [4097, 8192, 4096, 20479], 4096, 0, 1, False, "ties", None),
 ]
 
 
@@ -642,6 +674,76 @@ def test_steps_as_a_graph_and_on_another_stream(n):
             busy = torch.randn(1000, device=DEV).sum()
             assert math.isfinite(float(busy))
             assert all(torch.equal(a, b) for a, b in zip(seen(y), want[i])), f"replay {i}"
+
+
+@pytest.mark.gpu
+def test_calls_of_the_extension_module_are_the_general_ones(monkeypatch):
+    """The three calls through _pycall and through ctypes: the same bits; and tensors that it does not take are refused all the same."""
+    from paper_2410_08584_amd import binding
+    s = Setting(4, 8, 4, 20, 64, "bf16", 16, [20, 90, 300], [20, 3, 0], (0, 3, 4), (40, 77), order="token", seed=41)
+    taken = []
+
+    class Watched:
+        def __init__(self, inner):
+            self.inner = inner
+
+        def __getattr__(self, name):
+            def call(*args):
+                taken.append((name, getattr(self.inner, name)(*args)))
+                return taken[-1][1]
+            return call
+
+    table, a = s.table.to(DEV), s.args()
+
+    def everything():
+        cache, length = s.cache(), s.ints(s.lens)
+        O, lse = torch.zeros((s.B, s.Hq, s.n, s.d), dtype=s.dtype, device=DEV), torch.zeros((s.B, s.Hq, s.n), device=DEV)
+        z.zipvl_chunk_attn_paged(s.Q, cache, table, length, s.scale, O=O, lse=lse, ws=z.chunk_paged_workspace(cache, table, a["prefix_table"], B=s.B, Hq=s.Hq, Hkv=s.Hkv, n=s.n), **a)
+        weight = torch.zeros((s.B * s.Hkv, s.table.shape[1] * s.page), device=DEV)
+        z.zipvl_paged_weigh(s.Q, cache, table, length, lse, s.scale, k=a["k"], before=weight, weight=weight)
+        tokens = torch.full(weight.shape, -1, dtype=torch.int32, device=DEV)
+        out = dict(length_out=torch.zeros_like(length), weight_out=torch.zeros_like(weight), tokens_out=torch.zeros_like(tokens))
+        z.zipvl_paged_evict(cache, table, length, weight, 60, tokens=tokens, sinks=2, recent=5, ws=z.paged_evict_workspace(cache, table, 60), **out)
+        return O, lse, weight, *out.values(), cache.K, cache.V
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_native", Watched(binding._native))
+        fast = everything()
+        assert taken == [("chunk_attn_paged", 0), ("paged_weigh", 0), ("paged_evict", 0)]
+        cache, length, lse = s.cache(), s.ints(s.lens), torch.zeros((s.B, s.Hq, s.n), device=DEV)
+        weight = torch.zeros((s.B * s.Hkv, s.table.shape[1] * s.page), device=DEV)
+        for call in (lambda: z.zipvl_chunk_attn_paged(s.Q, cache, table, length.cpu(), s.scale, O=torch.zeros_like(s.Q), lse=lse, **a),
+                     lambda: z.zipvl_paged_weigh(s.Q, cache, table, length, lse.double(), s.scale, weight=weight),
+                     lambda: z.zipvl_paged_evict(cache, table, length, weight[:, :-1], 60)):
+            with pytest.raises(z.ZipvlError):
+                call()
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_native", binding._NoExtension())
+        general = everything()
+    assert all(torch.equal(x, y) for x, y in zip(fast, general))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,Hq,Hkv,n,d,dtype,lens,groups,pre", [(6, 28, 4, 9, 128, "bf16", [900, 9, 40], (0, 6), (1500,)), (2, 8, 8, 300, 64, "f32", [2000, 300], (), ()),
+                                                                (7, 4, 2, 5, 64, "bf16", [5000, 5], (), ()), (5, 2, 1, 40, 128, "f32", [40, 100], (1, 3, 5), (700, 64))])
+def test_workspaces_are_kept_to(B, Hq, Hkv, n, d, dtype, lens, groups, pre):
+    """Nothing behind the bytes that were asked for is written, and what they held does not matter."""
+    s = Setting(B, Hq, Hkv, n, d, dtype, 16, lens, None, groups, pre, seed=42)
+    cache, table, a = s.cache(), s.table.to(DEV), s.args()
+
+    def guarded(ws):
+        x = torch.full((ws.numel() + 4096,), 0xFF, dtype=torch.uint8, device=DEV)
+        return x[:ws.numel()], x[ws.numel():]
+
+    ws, guard = guarded(z.chunk_paged_workspace(cache, table, a["prefix_table"], B=B, Hq=Hq, Hkv=Hkv, n=n))
+    O, lse = chunk(s, cache, ws=ws)
+    assert (guard == 0xFF).all()
+    assert_chunk(s, O, lse)
+    weight = torch.rand((B * Hkv, s.table.shape[1] * 16), device=DEV)
+    ws, guard = guarded(z.paged_evict_workspace(cache, table, 100))
+    length = s.ints(s.lens)
+    z.zipvl_paged_evict(cache, table, length, weight, 100, ws=ws)
+    assert (guard == 0xFF).all() and length.tolist() == [min(x, 100) for x in s.lens]
 
 
 # ---------------------------------------------------------------- refusals, on the CPU
