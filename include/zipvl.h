@@ -397,11 +397,11 @@ int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32
  * Q [B,Hq,n,d] by dims->q_strides; O by the q_strides of `out` (its other fields are not looked at; NULL = [B,Hq,n,d] contiguous): no element twice, and
  * overlapping no input.  lse [device] fp32 [B,Hq,n] contiguous, or NULL.  Any Hq / Hkv; n * Hq / Hkv < 2^30.
  * Lengths are clamped to [0, pages of the table * page].  Nothing behind a length is read.  Inputs that are read must be finite.
- * Numerics: scores, statistics and sums in fp32, one rounding at the end; where a unit has more than 32 queries (n * Hq / Hkv), the weights of a bf16 call are
- * rounded to bf16 before they weigh V, and O is divided by the sum of those, lse is of the weights as they were.  The order of all sums follows from the sizes and lengths: the same call
+ * Numerics: scores, statistics and sums in fp32, one rounding at the end; where a unit has more than 32 queries (n * Hq / Hkv), or the units of a group, which are two or more on
+ * average, have together (B / groups times as many), the weights of a bf16 call are rounded to bf16 before they weigh V, and O is divided by the sum of those, lse is of the weights as they were.  The order of all sums follows from the sizes and lengths: the same call
  * gives the same bits.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_CHUNK_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that overlap on one
- * workspace race): up to 36 MB.
+ * workspace race): for any number of groups, up to 36 MB, and up to 172 MB where a group's queries may be put together (B >= 2, up to 512 queries a unit).
  */
 int zipvl_chunk_attn_paged(const void* Q, const zipvl_pages* pages, const int32_t* table, int32_t table_pages, const int32_t* len, const int32_t* k,
                            const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_len, const int32_t* group_begin, int32_t groups,

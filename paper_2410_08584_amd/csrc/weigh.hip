@@ -2,7 +2,7 @@
 //
 // Keys stay, queries come: a wave has 32 or 64 keys in registers, S = K Q^T on matrix tiles gives a lane one query and 16 keys of each 32, whose exponentials it
 // adds up over all queries; the 32 lanes, and the waves that share keys, meet once, at the end.  No sum crosses workgroups and no wave waits for another before that, so no order of
-// arrival changes a result.  Queries come from L1 and L2 straight into registers, a tile of 32 ahead.
+// arrival changes a result.  Queries come through LDS, tiles ahead.
 // fp32 numbers go as three planes of bf16 (planes.h): six products instead of one that takes sixteen times as long.
 // Few queries (a decode step) are bound by the read of K, many by products and by exponentials at a quarter of the vector rate.
 #include <atomic>
@@ -23,6 +23,7 @@ struct Weigh {
     int Hq, Hkv, G, n;
     uint32_t inv_Hkv, inv_G;
     float scale;
+    int units, blocks; uint32_t inv_blocks;                  // blocks: workgroups of a unit; 0: the grid's x, and the units its y
 };
 
 // Operands of 16 channels of 32 rows, a row a lane (halves of the wave: 8 channels each).
@@ -71,13 +72,46 @@ struct WeighCfg {
     static constexpr int LDS = (AHEAD + 1) * BUF * QW;
 };
 
+// The unit and the block of a workgroup where the queries of all are more than the L2s hold.  Workgroups go to the eight XCDs in turn, and all of a unit's read the same queries: eight
+// units at a time have an XCD's L2 each, then, of those that are left, four at a time two XCDs each, two four, one eight.
+// bf16, 3091 tokens of 3392 rows: 16 units of 4 heads (50 MB of queries) 157 us and not 383, 8 (25 MB) 95 and not 203.  But unequal units load XCDs unequally, which costs where L2 is no bound:
+// 14 units of 7 heads, fp32, 511 tokens (13 MB) 131 us and not 94.
+constexpr int64_t kQueriesAlone = 24 << 20;
+__device__ __forceinline__ bool place_of(const Weigh& p, int& u, int& block) {
+    const int xcd = block & 7, whole = (p.units >> 3) * p.blocks;
+    int j = block >> 3;
+    if (j < whole) {
+        const int at = divided(j, p.blocks, p.inv_blocks);
+        u = at * 8 + xcd;
+        block = j - at * p.blocks;
+        return true;
+    }
+    j -= whole;
+    u = p.units & ~7;
+#pragma unroll
+    for (int log2 = 2; log2 >= 0; --log2)
+        if (p.units >> log2 & 1) {
+            const int n = (p.blocks + (8 >> log2) - 1) >> (3 - log2);
+            if (j < n) {
+                u += xcd & ((1 << log2) - 1);
+                block = (j << (3 - log2)) + (xcd >> log2);
+                return block < p.blocks;
+            }
+            j -= n;
+            u += 1 << log2;
+        }
+    return false;
+}
+
 template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
 __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
     using R = Rows<T>;
     using C = WeighCfg<T, D, KB, QW, WIDE, FEW>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ float meet[4][32 * KB];
-    const int u = blockIdx.y, k0 = blockIdx.x * C::KEYS, room = p.width << p.page_log2;
+    int u = blockIdx.y, block = blockIdx.x;
+    if (p.blocks && !place_of(p, u, block)) return;
+    const int k0 = block * C::KEYS, room = p.width << p.page_log2;
     const int tid = threadIdx.x, w = scalar(tid >> 6), lane = tid & 63, i = lane & 31, h = lane >> 5;
     const int key0 = k0 + 32 * KB * (w / QW), qw = w % QW;
     // All that a workgroup goes by is asked for at once: the table's entries also of rows behind the length, if it has room for them.
@@ -305,7 +339,7 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
 }
 
 template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
-static void launch_weigh_as(const Weigh& p, int units, hipStream_t st) {
+static void launch_weigh_as(Weigh p, int units, hipStream_t st) {
     using C = WeighCfg<T, D, KB, QW, WIDE, FEW>;
     static std::atomic<uint64_t> set{0};                     // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
@@ -313,7 +347,17 @@ static void launch_weigh_as(const Weigh& p, int units, hipStream_t st) {
         if (hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_weigh_kernel<T, D, KB, QW, WIDE, FEW>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) == hipSuccess && dev <= 63)
             set.fetch_or(1ull << dev, std::memory_order_relaxed);        // the launch says so if it was refused
     }
-    const dim3 grid((unsigned)((((int64_t)p.width << p.page_log2) + C::KEYS - 1) / C::KEYS), units);
+    const int64_t blocks = (((int64_t)p.width << p.page_log2) + C::KEYS - 1) / C::KEYS;
+    dim3 grid((unsigned)blocks, units);
+    if ((int64_t)units * p.G * p.n * C::RB >= kQueriesAlone && units * blocks < 1 << 23) {       // 2^32 threads
+        p.units = units;
+        p.blocks = (int)blocks;
+        p.inv_blocks = inverse(p.blocks);
+        int64_t rounds = units / 8 * blocks;
+        for (int log2 = 2; log2 >= 0; --log2)
+            if (units >> log2 & 1) rounds += (blocks + (8 >> log2) - 1) >> (3 - log2);
+        grid = dim3((unsigned)(8 * rounds));
+    }
     hipLaunchKernelGGL((paged_weigh_kernel<T, D, KB, QW, WIDE, FEW>), grid, dim3(256), C::LDS, st, p);
 }
 template <typename T, int D>
@@ -335,7 +379,7 @@ int launch_paged_weigh(const void* Q, const zipvl_pages& pages, const int32_t* t
 {
     const int G = d.Hq / d.Hkv;
     const Weigh p = {(const char*)pages.K, pages.num_pages, __builtin_ctz(pages.page), table, table_pages, len, k, (const char*)Q,
-                     {d.q_strides[0], d.q_strides[1], d.q_strides[2]}, lse, lse_pitch, before, weight, d.Hq, d.Hkv, G, d.n, inverse(d.Hkv), inverse(G), scale};
+                     {d.q_strides[0], d.q_strides[1], d.q_strides[2]}, lse, lse_pitch, before, weight, d.Hq, d.Hkv, G, d.n, inverse(d.Hkv), inverse(G), scale, 0, 0, 0};
     if (d.dtype == ZIPVL_BF16) return d.d == 128 ? launch_weigh_t<__bf16, 128>(p, d.B * d.Hkv, st) : launch_weigh_t<__bf16, 64>(p, d.B * d.Hkv, st);
     return d.d == 128 ? launch_weigh_t<float, 128>(p, d.B * d.Hkv, st) : launch_weigh_t<float, 64>(p, d.B * d.Hkv, st);
 }

@@ -378,6 +378,17 @@ def test_paged_weigh_where_tables_are_wide(dtype, d, spare):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,Hkv,n,dtype", [(3, 5, 3500, "f32"), (1, 1, 26000, "f32"), (9, 1, 11500, "bf16"), (2, 3, 8300, "bf16")])
+def test_paged_weigh_of_many_queries(B, Hkv, n, dtype):
+    """More queries than the caches hold: units are dealt out another way.  Rows of the last tokens and the first, against the plain form."""
+    say(f"weigh {B} {Hkv} {n} {dtype}")
+    s = Setting(B, 2 * Hkv, Hkv, n, 64 if B > 2 else 128, dtype, 64, [90, 300, 33, 1], [n, n - 5, 40, n], seed=21)
+    _, lse = chunk(s)
+    w = z.zipvl_paged_weigh(s.Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale, k=s.ints(s.k))
+    assert_weights(s, w, lse, None)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [3, 70])
 @pytest.mark.parametrize("of_queries", [2.0 ** 101, 2.0 ** -101])
 def test_paged_weigh_of_huge_numbers(n, of_queries):
