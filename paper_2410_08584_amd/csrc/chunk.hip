@@ -4,12 +4,17 @@
 // A unit (batch element, KV head) has c G rows of queries, the G heads of its group token by token, so that a key that is met serves all heads of the group.
 // They go in tiles of rows against the prefix of the unit's group and then its own rows, up to the row that the tile's last token stands in.
 // Two forms:
-//   few     up to 32 rows a unit: memory-bound.  Each wave has all of them and tiles of 32 keys of its own (wavepart.h, as decode).
-//   many    128 rows a workgroup, 32 a wave; tiles of keys in LDS, double-buffered, are shared by the four waves.
+//   few     up to 32 rows a unit: memory-bound.  Each wave has all of them and tiles of 32 keys of its own (wavepart.h, as decode).  Four tokens each of 16 conversations of up to 33 000
+//           rows, bf16: 78 us for 341 MB, 4.4 TB/s.
+//   many    128 rows a workgroup, 32 a wave; tiles of keys in LDS are shared by the four waves, two deep, or three where whole tiles of bf16 follow each other (piped).  2048 tokens of 28
+//           heads on 4 behind 16 384, bf16: 492 us, 1.0 PFLOP/s, the matrix units busy 54 % of the time, of a large product 1.14; two deep throughout 680.
 // S^T = K Q^T and O^T += V^T P^T on matrix tiles, so that a lane has one row of queries and its statistics are scalars.
 //
-// How the keys are cut up is decided on the device, where the lengths are (find_place): every workgroup adds up what all units
-// weigh and takes a piece; a tile of rows whose keys are many gets several workgroups, and their parts are joined by a second launch.
+// The rows of a group's units may go together against its prefix (packed rows): eight questions of 6 tokens of 7 heads about 7200 rows 33 us and not 38 a unit at a time, 55 tokens 75 and not 88.
+//
+// How the keys are cut up is decided on the device, where the lengths are (find_place): every workgroup adds up the tiles of keys that all tiles of rows see
+// and takes a piece; a tile of rows whose keys are many gets several workgroups, and their parts are joined by a second launch.  To know its place takes a workgroup 4 us of a chain of
+// loads and barriers; that all see how long each is, and not only its unit, took five prompts of unequal length from 65 to 46 us.
 #include <algorithm>
 #include <atomic>
 
@@ -19,7 +24,7 @@
 namespace zipvl {
 
 constexpr int kRowsMany = 128;
-constexpr int kLeastMany = 4, kLeastFew = 4;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least
+constexpr int kLeastMany = 4, kLeastFew = 4;                 // tiles of keys (64, or 32 of fp32; 32) that a piece has at least: packed rows with 4, 8, 12, 16 took 28, 33, 37, 43 us (94 rows, 4964 keys), few rows of 616 keys with 4, 8 13.3, 14.7
 constexpr int kScanItems = 2048;                             // more tiles of rows than this get a workgroup each, whatever their keys
 
 // 8-byte fields and pairs of others only: it is read again as a row of 32-bit numbers
@@ -86,7 +91,7 @@ struct Place { int u, t, piece, pieces, record, group; };
 struct PlaceShared {
     int32_t begin[kScanItems + 1], keys[kScanItems], before[kScanItems];        // before: packed rows of the unit's group in front of its own
     unsigned long long total[4];
-    int2 sums[4];
+    int4 sums[4];
     Place place;
 };
 
@@ -165,8 +170,11 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
         if (lane == 0) sh.total[w] = ((unsigned long long)high << 16) + low;
     }
     __syncthreads();
-    // A tile of rows is cut into as many pieces as it has average loads, rounded down: then all pieces fit the chip at once
-    const int q = max(least, (int)min((unsigned long long)INT32_MAX, (sh.total[0] + sh.total[1] + sh.total[2] + sh.total[3] + (1 << log2_wgs) - 1) >> log2_wgs));
+    // A tile of rows is cut into as many pieces as it has loads q, rounded down.  With the average load all pieces fit the chip at once, but for tiles that have less than one: where they
+    // are many, loads are made larger, until the workgroups suffice (14 go to waste: two kinds of pieces are dealt to eight XCDs).  A workgroup for every piece that there might be
+    // would find nothing to do most of the time, and look for it as long as others: 8 units' 1022 packed rows took 210 us so, and 156 now.
+    const int limit = gridDim.x - 14;
+    int q = max(least, (int)min((unsigned long long)INT32_MAX, (sh.total[0] + sh.total[1] + sh.total[2] + sh.total[3] + (1 << log2_wgs) - 1) >> log2_wgs));
     // how many workgroups all tiles take; then whose tile this one's is: each thread has some that follow each other
     const int some = (items + 255) / 256, e0 = tid * some, e1 = min(items, e0 + some);
     auto pieces = [&](int e) { const int N = sh.keys[e]; return N < 0 ? 0 : max(1, N / q); };
@@ -174,25 +182,40 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
     // which leave theirs).
     const int part = min(rows, BM);
     auto parts = [&](int e, int s) { return e < packed ? s * BM : s > 1 || packed ? s * part : 0; };
-    int a = 0, records = 0;
-    for (int e = e0; e < e1; ++e) {
-        const int s = pieces(e);
-        a += s;
-        records += parts(e, s);
-    }
-    const int a_upto = wave_scan(a), r_upto = wave_scan(records);
-    if (lane == 63) sh.sums[w] = make_int2(a_upto, r_upto);
-    __syncthreads();
-    int a0 = a_upto - a, r0 = r_upto - records, used = 0;
+    int a, a0, r0, used, first;                              // first: pieces of packed rows
+    for (int round = 0;; ++round) {
+        int records = 0, of_packed = 0;
+        a = 0;
+        for (int e = e0; e < e1; ++e) {
+            const int s = pieces(e);
+            a += s;
+            records += parts(e, s);
+            if (e < packed) of_packed += s;
+        }
+        const int a_upto = wave_scan(a), r_upto = wave_scan(records);
+        if (PACKS) of_packed = wave_sum(of_packed);
+        if (lane == 63) sh.sums[w] = int4{a_upto, r_upto, of_packed, 0};
+        __syncthreads();
+        a0 = a_upto - a;
+        r0 = r_upto - records;
+        used = first = 0;
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        const int2 v = sh.sums[y];
-        if (y < w) { a0 += v.x; r0 += v.y; }
-        used += v.x;
+        for (int y = 0; y < 4; ++y) {
+            const int4 v = sh.sums[y];
+            if (y < w) { a0 += v.x; r0 += v.y; }
+            used += v.x;
+            first += v.z;
+        }
+        used = scalar(used);
+        first = PACKS ? scalar(first) : 0;
+        if (used <= limit || round == 4) break;
+        q = round < 3 ? (int)((float)q * used / limit) + 1 : INT32_MAX;      // the last: one piece a tile
+        __syncthreads();
     }
-    used = scalar(used);
-    const int per = (used + 7) / 8, own = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || own >= used) return false;
+    // each XCD has its share of the packed rows' and of the units' pieces, which are shorter
+    const int per = (first + 7) / 8, rest = (used - first + 7) / 8, at = blockIdx.x >> 3, xcd = blockIdx.x & 7;
+    const int own = at < per ? xcd * per + at : first + xcd * rest + at - per;
+    if (at < per ? own >= first : at - per >= rest || own >= used) return false;
     if (a0 <= own && own < a0 + a)
         for (int e = e0; e < e1; ++e) {
             const int s = pieces(e);
@@ -905,7 +928,9 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in,
 
 // ---------------------------------------------------------------- host
 constexpr int kFewRows = 32;
-constexpr int kRowsPacked = 4 * kRowsMany;                   // of a unit, up to which rows of a group are packed: tiles that are not full are then a part of all that counts
+// Rows of a unit up to which those of a group are packed, where tiles that are not full are a part of all that counts.  Eight units, 7200 shared rows, us, packed and not: 42 rows 33, 38; 168
+// rows 48, 56 (two a group); 259 rows 64, 73; 385 rows 75, 88; 511 rows 90, 89.  Not for groups whose rows fit a wave: 28 rows in two units are read twice, from L2.
+constexpr int kRowsPacked = 4 * kRowsMany;
 struct ChunkPlan { int few, direct, wgs, rows, bm, slots; int64_t grid; size_t ml, pieces, shared, total; };
 // keys: that the tables of a unit and its prefix can hold
 static ChunkPlan chunk_plan(const zipvl_dims& d, int64_t keys, int groups) {
@@ -929,7 +954,7 @@ static ChunkPlan chunk_plan(const zipvl_dims& d, int64_t keys, int groups) {
     x.wgs = x.few && d.dtype == ZIPVL_F32 && d.d == 128 ? kCus : 2 * kCus;
     const int64_t least = x.few ? kLeastFew : kLeastMany, part = std::min<int64_t>(rows, x.bm);
     x.direct = !x.slots && (items > kScanItems || tiles < 2 * least);      // the last: nothing can be cut
-    x.grid = (x.direct ? items : items + x.wgs) / 8 * 8 + 8;
+    x.grid = x.direct ? items / 8 * 8 + 8 : std::max<int64_t>(x.wgs + 64, (items + 21) / 8 * 8);
     x.rows = x.direct ? 0 : x.slots ? (int)(x.wgs * x.bm + units * ((rows + x.bm - 1) / x.bm) * part + (int64_t)d.Hkv * x.slots * x.bm) : (int)(x.wgs * part);
     x.ml = (size_t)x.rows * d.d * sizeof(float);
     x.pieces = x.ml + (size_t)x.rows * 2 * sizeof(float);
