@@ -7,7 +7,7 @@
 //   few     up to 32 rows a unit: memory-bound.  Each wave has all of them and tiles of 32 keys of its own (wavepart.h, as decode).  Four tokens each of 16 conversations of up to 33 000
 //           rows, bf16: 78 us for 341 MB, 4.4 TB/s.
 //   many    128 rows a workgroup, 32 a wave; tiles of keys in LDS are shared by the four waves, two deep, or three where whole tiles of bf16 follow each other (piped).  2048 tokens of 28
-//           heads on 4 behind 16 384, bf16: 492 us, 1.0 PFLOP/s, the matrix units busy 54 % of the time, of a large product 1.14; two deep throughout 680.
+//           heads on 4 behind 16 384, bf16: 492 us, 1.0 PFLOP/s, the matrix units busy 54 % of the time, of a large product 1.14 (543 us two deep throughout, 506 with the third).
 // S^T = K Q^T and O^T += V^T P^T on matrix tiles, so that a lane has one row of queries and its statistics are scalars.
 //
 // The rows of a group's units may go together against its prefix (packed rows): eight questions of 6 tokens of 7 heads about 7200 rows 33 us and not 38 a unit at a time, 55 tokens 75 and not 88.
@@ -209,7 +209,7 @@ __device__ __forceinline__ bool find_place(const Chunk& p, PlaceShared& sh, cons
         used = scalar(used);
         first = PACKS ? scalar(first) : 0;
         if (used <= limit || round == 4) break;
-        q = round < 3 ? (int)((float)q * used / limit) + 1 : INT32_MAX;      // the last: one piece a tile
+        q = round < 3 ? (int)fminf((float)q * used / limit, 1e9f) + 1 : INT32_MAX;      // the last: one piece a tile
         __syncthreads();
     }
     // each XCD has its share of the packed rows' and of the units' pieces, which are shorter
