@@ -377,7 +377,7 @@ struct Many {
     char* const smem;
     const int32_t *own_table, *pre_table;
     int prefix_rows, seen, tp;                               // rows of the prefix, own rows that a token of the tile sees, tiles of the prefix
-    int wave_first, r_first, r_last, before, G;              // up to this own row no lane's mask begins; of the wave; own rows before the new ones
+    int wave_first, wave_last, r_first, r_last, before, G;   // the own rows that the wave's first and last row of queries see up to (-2: the wave has none); own rows before the new ones
     uint32_t inv_G;
     int w, lane, i, h;
     uintx4 qf[C::CH];
@@ -550,10 +550,13 @@ struct Many {
                 request<true>(nxt, j + 1, buf ^ 1);
                 if (j + 2 < j1) look(j + 2);
             }
+            const KeyTile here = cur;
+            cur = nxt;
+            if (wave_last < (own(j) ? first(j) : -1)) continue;      // nothing that the wave's rows see, or no rows
             const char* vb = buffer(true, buf);
             Scores s;
             scores(buffer(false, buf), s);
-            mask(cur, j, s);
+            mask(here, j, s);
             float mx = largest(s);
             if (__any(mx > m + kLazy)) {
                 mx = over_groups<32>(mx, [](float a, float b) { return fmaxf(a, b); });
@@ -598,7 +601,6 @@ struct Many {
                     }
                 }
             }
-            cur = nxt;
         }
         __syncthreads();
     }
@@ -789,6 +791,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         many.seen = scalar(v.seen(p, many.r_last));
         many.tp = scalar((v.prefix_rows + C::BN - 1) / C::BN);
         many.wave_first = scalar(many.before + divided(min(many.r_first, many.r_last), p.G, p.inv_G));
+        many.wave_last = many.r_first > many.r_last ? -2 : max(-1, scalar(many.before + divided(min(many.r_first + 31, many.r_last), p.G, p.inv_G)));
         const int all = many.tp + scalar((many.seen + C::BN - 1) / C::BN);
         j0 = scalar((int)((int64_t)all * x.piece / x.pieces));
         j1 = scalar((int)((int64_t)all * (x.piece + 1) / x.pieces));
@@ -839,7 +842,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
             }
             l = both(many.l);
             if (safe) break;
-            const bool sees = many.before + end(read_again<Chunk>(0)).token >= held.sees_from;      // a key of the piece
+            const bool sees = many.wave_last != -2 && many.before + end(read_again<Chunk>(0)).token >= held.sees_from;      // a key of the piece
             if (__any(sees && !(l >= kSumLow && l <= kSumHigh)) && threadIdx.x % 64 == 0) held.again = 1;
             __syncthreads();
             if (!scalar(held.again)) break;

@@ -253,6 +253,25 @@ def test_chunk_attn_paged_of_large_and_small_logits(dtype, n, gain):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("gain", [40.0, 1.0])
+def test_chunk_attn_paged_of_groups_with_large_logits_and_missing_pages(dtype, d, gain):
+    """A group's queries together: sums that leave the middle of fp32's range, rows of the prefix without a page, counts and lengths beyond what there is."""
+    say(f"groups {dtype} {d} {gain}")
+    s = Setting(7, 14, 2, 12, d, dtype, 64, [300, 12, 5, 0], [12, 1, 0, 7, 12], (0, 4, 7), (900, 640, 1500, 63), seed=23, gain=gain)
+    if gain == 1.0:
+        pages = s.K.shape[0]
+        s.prefix_table[0, 1:3] = pages
+        s.prefix_table[1, :] = -1
+        s.prefix_table[2, 20] = NONE
+        s.pre[2] = 2 ** 31 - 1
+        s.k[3], s.k[8] = 2 ** 31 - 1, -4
+        s.lens[2] = 10 ** 9
+    s.spoil()
+    assert_chunk(s, *chunk(s))
+
+
+@pytest.mark.gpu
 def test_chunk_attn_paged_of_one_token_is_decode():
     s = Setting(4, 28, 4, 1, 128, "bf16", 64, [500, 1, 70, 1300], None, (0, 3, 4), (300, 41), seed=10)
     cache = s.cache()
