@@ -19,6 +19,7 @@
 #include <atomic>
 
 #include "launch.h"
+#include "planes.h"
 #include "wavepart.h"
 
 namespace zipvl {
@@ -353,7 +354,9 @@ struct ChunkCfg {
     static constexpr int BN = sizeof(T) == 2 ? 64 : 32, NBK = BN / 32;          // keys a tile, blocks of 32 of them
     static constexpr int TILE = BN * RB, NL = TILE / 4096, RPL = 1024 / RB;     // loads of 1 KiB per wave and tile, rows per load
     static constexpr int CH = D / Elem<T>::kPerChunk, ODB = D / 32;
-    static constexpr int LDS = 4 * TILE + 64;                // two tiles of K, two of V, the workgroup's place for the end
+    static constexpr int CHP = sizeof(T) == 4 ? D / 16 : 1;  // operands of three planes of a row of queries
+    static constexpr bool KEPT = D == 64;                    // planes of queries are kept; of longer rows they are made for every tile, or operands spill
+    static constexpr int LDS = 4 * TILE + 64 + (sizeof(T) == 4 ? 8 * kRowsMany : 0);     // two tiles of K, two of V, the workgroup's place for the end, of fp32 where the rows of queries are
     __device__ static __forceinline__ int k_swizzle(int r) { return k_row_swizzle<RB>(r); }
     __device__ static __forceinline__ int v_swizzle(int r) { return PartCfg<T, D>::v_swizzle(r); }
 };
@@ -381,8 +384,10 @@ struct Many {
     uint32_t inv_G;
     int w, lane, i, h;
     uintx4 qf[C::CH];
+    Planes qp[C::KEPT ? C::CHP : 1];                         // fp32, instead
     floatx16 o[C::ODB];
     float m, l, l_rounded;                                   // l: sum of the weights; as V was weighed by them
+    float most;                                              // fp32: the largest number, at least, that went into planes
     int entry[C::BN / 16];                                   // of the table, for the tile that look() was last called for: asked for a step before they are used
 
     __device__ __forceinline__ void look(int j) {
@@ -475,7 +480,58 @@ struct Many {
         m = -INFINITY;
         l = l_rounded = 0.f;
     }
+    // fp32 numbers go as three planes of bf16, six products for one that takes sixteen times as long, where none is too large for them (kPlaneHigh).  Five pieces of up to 777 tokens, d = 64:
+    // 38.6 us, 43.4 in fp32 products; 8 units of 168 rows about 7200 shared ones, d = 128: 196 and 213 (planes of queries kept, 54 registers spilled: 270).
+    __device__ __forceinline__ Planes split(const uintx4& a, const uintx4& b) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(most) : "v"(a[e]), "v"(b[e]));
+        return split8(a, b);
+    }
+    __device__ __forceinline__ void load_planes(const T* row) {
+        most = 0.f;
+#pragma unroll
+        for (int cc = 0; cc < C::CHP; ++cc) {
+            const uintx4 a = load16(row + 16 * cc + 8 * h), b = load16(row + 16 * cc + 8 * h + 4);
+            if constexpr (C::KEPT) qp[cc] = split(a, b);
+            else {
+                qf[2 * cc] = a;
+                qf[2 * cc + 1] = b;
+            }
+        }
+    }
+    __device__ __forceinline__ void load_queries(const T* row) {
+#pragma unroll
+        for (int cc = 0; cc < C::CH; ++cc) qf[cc] = load16(row + (2 * cc + h) * Elem<T>::kPerFrag);
+    }
     using Scores = floatx16[C::NBK];
+    __device__ __forceinline__ void plane_scores(const char* kb, Scores& s) {
+        int at = lane;
+        if constexpr (!C::KEPT) asm volatile("" : "+v"(at));  // nor are addresses through all tiles
+        const int i = at & 31, h = at >> 5;
+        const char* const row = kb + i * C::RB;
+        s[0] = floatx16{0};
+#pragma unroll
+        for (int cc = 0; cc < C::CHP; ++cc) {
+            const Planes k = split(load16(row + swz_chunk(4 * cc + 2 * h, C::k_swizzle(i))), load16(row + swz_chunk(4 * cc + 2 * h + 1, C::k_swizzle(i))));
+            if constexpr (C::KEPT) s[0] = mma_planes(k, qp[cc], s[0]);
+            else {
+                uintx4 a = qf[2 * cc], b = qf[2 * cc + 1];
+                asm volatile("" : "+v"(a), "+v"(b));         // not made once for all tiles
+                s[0] = mma_planes(k, split(a, b), s[0]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    // channels 32 db ... of eight keys, a channel a lane
+    __device__ __forceinline__ Planes v_planes(const char* vb, int s2, int db) {
+        uintx4 x[2];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+            const int k = acc_row(8 * s2 + y, h);
+            x[y / 4][y % 4] = *reinterpret_cast<const uint32_t*>(vb + k * C::RB + swz_chunk(8 * db + (i >> 2), C::v_swizzle(k)) + (i & 3) * 4);
+        }
+        return split(x[0], x[1]);
+    }
     __device__ __forceinline__ void scores(const char* kb, Scores& s) const {
 #pragma unroll
         for (int blk = 0; blk < C::NBK; ++blk) {
@@ -534,6 +590,7 @@ struct Many {
     }
 
     // Tiles j0 ... j1 - 1, one after the other, the offset of the exponentials behind the running maximum: any tiles, any logits
+    template <bool PLANES>
     __device__ __forceinline__ void plain(int j0, int j1) {
         if (j0 >= j1) return;
         look(j0);
@@ -555,7 +612,8 @@ struct Many {
             if (wave_last < (own(j) ? first(j) : -1)) continue;      // nothing that the wave's rows see, or no rows
             const char* vb = buffer(true, buf);
             Scores s;
-            scores(buffer(false, buf), s);
+            if constexpr (PLANES) plane_scores(buffer(false, buf), s);
+            else scores(buffer(false, buf), s);
             mask(here, j, s);
             float mx = largest(s);
             if (__any(mx > m + kLazy)) {
@@ -588,6 +646,19 @@ struct Many {
                         }
 #pragma unroll
                         for (int db = 0; db < C::ODB; ++db) o[db] = mma_frag<__bf16>(v_frag(vb + v_lane(db) + (32 * blk + 16 * s2) * C::RB), pf, o[db]);
+                    }
+                } else if constexpr (PLANES) {
+#pragma unroll
+                    for (int s2 = 0; s2 < 2; ++s2) {
+                        uintx4 x[2];
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) x[y / 4][y % 4] = __float_as_uint(s[0][8 * s2 + y]);
+                        const Planes weights = split8(x[0], x[1]);
+#pragma unroll
+                        for (int db = 0; db < C::ODB; ++db) {
+                            o[db] = mma_planes(v_planes(vb, s2, db), weights, o[db]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -731,6 +802,8 @@ struct Many {
     }
 };
 
+// Planes are off by 2^-134 where a number is small: nothing in a logit or a sum as long as what it is multiplied by is below this.  A piece that meets larger numbers is done again.
+constexpr float kPlaneHigh = 0x1p100f;
 // Sums of the offset that stays, outside which the tiles are repeated with running maxima.
 constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p64f;
 
@@ -757,6 +830,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
     static_assert(sizeof(Held) <= 64, "");
     Held& held = *reinterpret_cast<Held*>(smem + 4 * C::TILE);
     static_assert(sizeof(PlaceShared) <= 4 * C::TILE, "the keys' numbers stand where tiles come later");
+    const T** const query_at = reinterpret_cast<const T**>(smem + 4 * C::TILE + 64);
     Many<T, D> many = {p_.K, p_.V, p_.num_pages, p_.page_log2, p_.c, smem};
     int j0, j1, r0;
     {
@@ -804,8 +878,10 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         }
         __syncthreads();                                     // `before` has been read: tiles may come there
         const T* row = query_row<T>(p, v.b, row_at(p, v.g, r));
-#pragma unroll
-        for (int cc = 0; cc < C::CH; ++cc) many.qf[cc] = load16(row + (2 * cc + many.h) * Elem<T>::kPerFrag);
+        if constexpr (sizeof(T) == 4) {
+            many.load_planes(row);
+            if (many.h == 0) query_at[32 * many.w + many.i] = row;
+        } else many.load_queries(row);
     }
     auto both = [](float a) { return over_groups<32>(a, [](float p, float q) { return p + q; }); };
     // What follows the tiles goes by numbers read and said anew: registers are scarce among them.
@@ -837,7 +913,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
                     j += n;
                 }
                 const int upto = own ? j1 : min(j1, max(j, many.tp));
-                many.plain(j, upto);
+                many.template plain<false>(j, upto);
                 j = upto;
             }
             l = both(many.l);
@@ -849,7 +925,14 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         }
     } else {
         many.reset();
-        many.plain(j0, j1);
+        many.template plain<true>(j0, j1);
+        if (__any(!(many.most < kPlaneHigh)) && threadIdx.x % 64 == 0) held.again = 1;
+        __syncthreads();
+        if (scalar(held.again)) {                            // in fp32 products
+            many.load_queries(query_at[threadIdx.x / 64 * 32 + threadIdx.x % 32]);
+            many.reset();
+            many.template plain<false>(j0, j1);
+        }
         l = both(many.l);
     }
     const Chunk p = read_again<Chunk>(0);

@@ -253,6 +253,19 @@ def test_chunk_attn_paged_of_large_and_small_logits(dtype, n, gain):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,n", [(64, 3), (64, 70), (128, 70)])
+@pytest.mark.parametrize("of_queries,of_values", [(2.0 ** 101, 1.0), (2.0 ** -101, 1.0), (1.0, 2.0 ** 115), (1.0, 2.0 ** -100)])
+def test_chunk_attn_paged_of_huge_and_small_numbers(d, n, of_queries, of_values):
+    """fp32 whose products fit, with numbers that planes of bf16 do not hold in full range: the output of their like of ordinary size, times what values were."""
+    say(f"huge {d} {n} {of_queries} {of_values}")
+    s = Setting(2, 4, 2, n, d, "f32", 16, [200, 100, 80, 75], None, seed=24)
+    s.Q.mul_(of_queries)
+    s.K.mul_(1 / of_queries)
+    s.V.mul_(of_values)
+    assert_chunk(s, *chunk(s))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 @pytest.mark.parametrize("gain", [40.0, 1.0])
 def test_chunk_attn_paged_of_groups_with_large_logits_and_missing_pages(dtype, d, gain):
