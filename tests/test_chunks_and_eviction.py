@@ -297,7 +297,7 @@ def test_chunk_attn_paged_of_one_token_is_decode():
 
 @pytest.mark.gpu
 def test_over_more_than_4_gib():
-    """Pages, queries and weights behind 4 GiB."""
+    """Pages behind 4 GiB."""
     page, d, n = 256, 128, 3
     pages = (5 << 30) // (page * d * 2)
     K = torch.empty((pages, page, d), dtype=torch.bfloat16, device=DEV)
@@ -321,6 +321,23 @@ def test_over_more_than_4_gib():
         got = cache.K[table[u].long()].view(-1, d)[:290].cpu()
         want, _ = s.rows(s.K, s.table, u, s.lens[u])
         assert torch.equal(got.double(), want[source[u]])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 70])
+def test_queries_and_outputs_far_apart(dtype, n):
+    """Heads and batch elements of Q and O more than 2^31 elements from each other."""
+    s = Setting(2, 2, 1, n, 64, dtype, 16, [200, 90], None, seed=26)
+    strides = (2 ** 31 + 2 ** 20, 2 ** 31 - 2 ** 19 + 64, 64, 1)
+    size = sum(x * (k - 1) for x, k in zip(strides, (2, 2, n, 64))) + 1
+    Q, O = (torch.empty(size, dtype=s.dtype, device=DEV).as_strided((2, 2, n, 64), strides) for _ in range(2))
+    Q.copy_(s.Q)
+    cache, table, length = s.cache(), s.table.to(DEV), s.ints(s.lens)
+    got, lse = z.zipvl_chunk_attn_paged(Q, cache, table, length, s.scale, O=O, want_lse=True)
+    assert got is O
+    assert_chunk(s, O, lse)
+    assert_weights(s, z.zipvl_paged_weigh(Q, cache, table, length, lse, s.scale), lse, None)
 
 
 # ---------------------------------------------------------------- weights
