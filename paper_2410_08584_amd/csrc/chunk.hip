@@ -963,10 +963,9 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
 }
 
 // ---------------------------------------------------------------- parts of cut rows -> rows
-// 1024 / D rows at a time, D / 4 lanes a row; `per` rows a workgroup.  Parts are asked for eight at a time: a row is a chain of few loads, not of as many as it has parts.
+// 1024 / D rows at a time, D / 4 lanes a row; `per` rows a workgroup.  Parts are asked for eight or sixteen at a time: a row is a chain of few loads, not of as many as it has parts.
 template <typename T, int D, int BM>
 __global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in, int per) {
-    constexpr int kAtOnce = 8;
     const int u = blockIdx.y, b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv, rows = tokens_of(p, u) * p.G;
     const int most = (p.n * p.G + BM - 1) / BM, part = min(p.n * p.G, BM), packed = p.Hkv * p.slots, r_end = min(rows, ((int)blockIdx.x + 1) * per);
     const int ch = threadIdx.x % (D / 4) * 4;
@@ -981,30 +980,34 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(Chunk p, ChunkParts in,
         auto record = [&](int y) { return (int64_t)(y < first.y ? first.x + y * BM + packed_r % BM : own.x + (y - first.y) * part + r % BM); };
         float M = -INFINITY, L = 0.f;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int y0 = 0; y0 < s; y0 += kAtOnce) {
-            float2 ml[kAtOnce];
-            floatx4 o[kAtOnce];
+        auto parts = [&](auto at_once, int y0) __attribute__((always_inline)) {
+            constexpr int N = decltype(at_once)::value;
+            float2 ml[N];
+            floatx4 o[N];
 #pragma unroll
-            for (int y = 0; y < kAtOnce; ++y) {
+            for (int y = 0; y < N; ++y) {
                 const int64_t rec = record(min(y0 + y, s - 1));
                 ml[y] = *reinterpret_cast<const float2*>(in.ml + 2 * rec);
                 o[y] = *reinterpret_cast<const floatx4*>(in.o + rec * D + ch);
             }
             float top = M;
 #pragma unroll
-            for (int y = 0; y < kAtOnce; ++y) top = fmaxf(top, ml[y].x);
-            if (top == -INFINITY) continue;
+            for (int y = 0; y < N; ++y) top = fmaxf(top, ml[y].x);
+            if (top == -INFINITY) return;
             const float f = fast_exp2(M - top);
             L *= f;
             acc *= f;
 #pragma unroll
-            for (int y = 0; y < kAtOnce; ++y) {
+            for (int y = 0; y < N; ++y) {
                 const float a = y0 + y < s ? fast_exp2(ml[y].x - top) : 0.f;
                 L += a * ml[y].y;
                 acc += a * o[y];
             }
             M = top;
-        }
+        };
+        int y0 = 0;
+        for (; s - y0 > 8; y0 += 16) parts(std::integral_constant<int, 16>{}, y0);
+        if (y0 < s) parts(std::integral_constant<int, 8>{}, y0);
         const RowAt at = row_at(p, g, r);
         acc *= L > 0.f ? 1.f / L : 0.f;
         store4(out_row<T>(p, b, at) + ch, acc);
