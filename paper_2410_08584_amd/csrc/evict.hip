@@ -16,7 +16,9 @@
 namespace zipvl {
 
 constexpr int kDigit = 11, kDigits = 1 << kDigit;            // a key of 32 bits goes in digits of 11, 11 and 10
-constexpr int kMovesHere = 64;                               // moves of a unit up to which the first kernel does them
+// Moves of a unit up to which the first kernel does them.  256 units of bf16, d = 128, us, here and by a second launch: 16 moves 11, 13; 128 15, 18; 256 20, 23; eight units: 128 10.5, 12.5; 256 10.7, 11.1;
+// 1000 15.7, 12.5.
+constexpr int kMovesHere = 256;
 
 struct Late { int row, token; float weight; int unused; };   // a row at or behind k that stays
 struct Evict {
@@ -527,6 +529,7 @@ template <int RB>
 static int launch_evict_t(const Evict& p, int units, hipStream_t st) {
     {
         KernelTimer tm(ZIPVL_K_PAGED_EVICT, st);
+        // four waves for short units, of which a CU then has several: 3200 units of 500 rows 25 us, 79 with 16 waves; 256 units as long
         if (p.room <= 1024) hipLaunchKernelGGL((evict_select_kernel<4, 1, RB>), dim3(units), dim3(256), 1024 * 4, st, p);
         else if (p.room <= 4096) hipLaunchKernelGGL((evict_select_kernel<16, 1, RB>), dim3(units), dim3(1024), 4096 * 4, st, p);
         else if (p.room <= kRoundsMost * 4096) {

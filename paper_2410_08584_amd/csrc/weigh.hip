@@ -57,18 +57,18 @@ template <> struct Rows<float> {
 // numbers takes its tiles in fp32 products.
 constexpr float kPlaneHigh = 0x1p100f;
 
-// 32 KB keys a wave.  QW = 1: the four waves have keys of their own and share tiles of queries; 4: they have the same keys and take every fourth tile, each from LDS of its own.
+// 32 keys a wave.  QW = 1: the four waves have keys of their own and share tiles of queries; 4: they have the same keys and take every fourth tile, each from LDS of its own.
 // A tile is of queries that follow each other head by head, token by token, or, WIDE, of tokens of one head: its rows are then at one distance and asked for without a
-// vector instruction, and n is long enough that a last tile with few tokens is no loss.  FEW: of queries, so that short tiles of them will do.
-template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
+// vector instruction, and n is long enough that a last tile with few tokens is no loss.
+template <typename T, int D, int QW, bool WIDE>
 struct WeighCfg {
-    static constexpr int RB = D * (int)sizeof(T), CH = D / 16, KEYS = 32 * KB * (4 / QW);
-    static constexpr int QT = QW == 1 && sizeof(T) == 2 && !FEW ? 64 : 32, SHARE = 4 / QW;       // queries a tile, waves that share it
+    static constexpr int RB = D * (int)sizeof(T), CH = D / 16, KEYS = 32 * (4 / QW);
+    static constexpr int QT = QW == 1 && sizeof(T) == 2 ? 64 : 32, SHARE = 4 / QW;       // queries a tile, waves that share it
     static constexpr int TILE = QT * RB, NL = TILE / 1024 / SHARE, RPL = 1024 / RB;  // loads of 1 KiB a wave, rows a load
     static constexpr int BUF = TILE + 256 * SHARE;                                   // a tile, and each wave's copy of its lse
     // Tiles on the way, beside the one that is read.  A wave that has its tiles to itself takes one into registers and asks for the next into its place, where
     // there are registers for it (511 tokens of three prompts, fp32: 55.3 us, with two buffers 57.3).
-    static constexpr int AHEAD = QW > 1 && RB <= 256 ? 0 : QW > 1 || FEW ? 1 : 2;
+    static constexpr int AHEAD = QW > 1 && RB <= 256 ? 0 : QW > 1 ? 1 : 2;
     static constexpr int LDS = (AHEAD + 1) * BUF * QW;
 };
 
@@ -103,40 +103,29 @@ __device__ __forceinline__ bool place_of(const Weigh& p, int& u, int& block) {
     return false;
 }
 
-template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
+template <typename T, int D, int QW, bool WIDE>
 __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
     using R = Rows<T>;
-    using C = WeighCfg<T, D, KB, QW, WIDE, FEW>;
+    using C = WeighCfg<T, D, QW, WIDE>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ float meet[4][32 * KB];
+    __shared__ float meet[4][32];
     int u = blockIdx.y, block = blockIdx.x;
     if (p.blocks && !place_of(p, u, block)) return;
     const int k0 = block * C::KEYS, room = p.width << p.page_log2;
     const int tid = threadIdx.x, w = scalar(tid >> 6), lane = tid & 63, i = lane & 31, h = lane >> 5;
-    const int key0 = k0 + 32 * KB * (w / QW), qw = w % QW;
+    const int key0 = k0 + 32 * (w / QW), qw = w % QW;
     // All that a workgroup goes by is asked for at once: the table's entries also of rows behind the length, if it has room for them.
     const int len_there = p.len[u], cnt_there = p.cnt ? p.cnt[u] : p.n;
-    int entry[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) entry[kb] = p.table[(int64_t)u * p.width + (min(key0 + 32 * kb + i, room - 1) >> p.page_log2)];
+    const int entry = p.table[(int64_t)u * p.width + (min(key0 + i, room - 1) >> p.page_log2)];
     const int64_t at0 = (int64_t)u * room + key0;
-    float was[KB] = {};                                      // of row lane of the wave (64 at a time)
-    if (p.before && qw == 0)
-#pragma unroll
-        for (int x = 0; x < (KB + 1) / 2; ++x)
-            if (64 * x + lane < 32 * KB && key0 + 64 * x + lane < room) was[x] = p.before[at0 + 64 * x + lane];
+    const float was = p.before && qw == 0 && lane < 32 && key0 + lane < room ? p.before[at0 + lane] : 0.f;        // of row lane of the wave
     const int len = scalar(max(0, min(len_there, room))), cnt = scalar(max(0, min(cnt_there, p.n)));
     if (k0 >= len) return;
     const int b = divided(u, p.Hkv, p.inv_Hkv), g = u - b * p.Hkv, rows = cnt * p.G, first = len - cnt;        // token i stands in row first + i
-    // Rows of the wave's keys.  Rows that are not there read row 0 of the pages and get nothing.
-    const char* key_row[KB];
-    bool there[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-        const int key = key0 + 32 * kb + i;
-        there[kb] = key < len && (unsigned)entry[kb] < (unsigned)p.num_pages;
-        key_row[kb] = p.K + (there[kb] ? ((int64_t)entry[kb] << p.page_log2) + (key & ((1 << p.page_log2) - 1)) : 0) * C::RB;
-    }
+    // The lane's row of keys.  One that is not there reads row 0 of the pages and gets nothing.
+    const int key = key0 + i;
+    const bool there = key < len && (unsigned)entry < (unsigned)p.num_pages;
+    const char* const key_row = p.K + (there ? ((int64_t)entry << p.page_log2) + (key & ((1 << p.page_log2) - 1)) : 0) * C::RB;
     const char* const queries = p.Q + (b * p.q[0] + (int64_t)g * p.G * p.q[1]) * (int64_t)sizeof(T);
     const char* const lses = reinterpret_cast<const char*>(p.lse + ((int64_t)b * p.Hq + g * p.G) * p.lse_pitch);
     const int64_t token_bytes = p.q[2] * (int64_t)sizeof(T), head_bytes = p.q[1] * (int64_t)sizeof(T), pitch = p.lse_pitch * 4;
@@ -190,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
         }
     };
     const float c = p.scale * kLog2e;
-    float sum[KB][16];
+    float sum[16];
     // exp(x - lse) = 2^(x log2 e - whole) * 2^(whole - lse log2 e), with a whole number near lse log2 e: the second factor is one a query, and no logit loses bits to lse.
     struct Base { float whole, factor; };
     auto base_of = [&](float lse) {
@@ -199,13 +188,13 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
         if (__builtin_isinf(lse)) x = {1e9f, 0.f};           // a query that sees nothing weighs nothing
         return x;
     };
-    auto add = [&](int kb, const floatx16& s, const Base& base, auto whole, int last) __attribute__((always_inline)) {
-        const int upto = last - key0 - 32 * kb - 4 * h;
+    auto add = [&](const floatx16& s, const Base& base, auto whole, int last) __attribute__((always_inline)) {
+        const int upto = last - key0 - 4 * h;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             float e = fast_exp2(fmaf(s[r], c, -base.whole));
             if (!decltype(whole)::value && acc_row(r, 0) > upto) e = 0.f;
-            sum[kb][r] = fmaf(e, base.factor, sum[kb][r]);
+            sum[r] = fmaf(e, base.factor, sum[r]);
         }
     };
     // the token of query `at` of a tile, cnt or more where there is none
@@ -216,9 +205,7 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
     auto last_of = [&](int token) { return token < cnt ? first + token : -1; };      // own row that a token stands in
     auto clear = [&]() {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum[kb][r] = 0.f;
+        for (int r = 0; r < 16; ++r) sum[r] = 0.f;
     };
     float most = 0.f;
     clear();
@@ -231,15 +218,13 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
 #pragma unroll
         for (int x = 0; x < max(C::AHEAD, 1); ++x)
             if (t0 + x * QW < t1) request(t0 + x * QW, x);
-        typename R::Frag kf[KB][C::CH];
+        typename R::Frag kf[C::CH];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int cc = 0; cc < C::CH; ++cc) {
-                const typename R::Raw x = R::load(key_row[kb], cc, h);
-                if (there[kb]) most = R::largest(x, most);
-                kf[kb][cc] = R::split(x);
-            }
+        for (int cc = 0; cc < C::CH; ++cc) {
+            const typename R::Raw x = R::load(key_row, cc, h);
+            if (there) most = R::largest(x, most);
+            kf[cc] = R::split(x);
+        }
         int buf = 0;
         for (int t = t0; t < t1; t += QW) {
             if (C::AHEAD > 1 && t + QW < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(C::NL + 1) : "memory");
@@ -262,11 +247,10 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
             auto weigh_tile = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
                 for (int x = 0; x < C::QT / 32; ++x) {
+                    if (!WIDE && x && t * C::QT + 32 * x >= rows) break;             // of few queries
                     const int r = 32 * x + i;
                     const Base base = base_of(C::AHEAD ? *reinterpret_cast<const float*>(tile + C::TILE + part * 256 + r * 4) : held_lse);
-                    floatx16 s[KB];
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) s[kb] = floatx16{0};
+                    floatx16 s = {0};
 #pragma unroll
                     for (int cc = 0; cc < C::CH; ++cc) {
                         typename R::Raw raw;
@@ -274,17 +258,15 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
                         else raw = held[cc];
                         most = R::largest(raw, most);
                         const typename R::Frag qf = R::split(raw);
-#pragma unroll
-                        for (int kb = 0; kb < KB; ++kb) s[kb] = R::mma(kf[kb][cc], qf, s[kb]);
+                        s = R::mma(kf[cc], qf, s);
                     }
                     const int last = decltype(whole)::value ? 0 : last_of(token_of(t, r));
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) add(kb, s[kb], base, whole, last);
-                    if (KB * C::CH >= 8) __builtin_amdgcn_sched_barrier(0);          // one after the other: side by side they took 60 registers more, and a workgroup of a CU
+                    add(s, base, whole, last);
+                    if (C::CH >= 8) __builtin_amdgcn_sched_barrier(0);          // one after the other: side by side they took 60 registers more, and a workgroup of a CU
                 }
             };
             // whether every query of the tile sees every key of the wave
-            if (first + token_of(t, 0) >= key0 + 32 * KB - 1 && token_of(t, C::QT - 1) < cnt) weigh_tile(std::true_type{});
+            if (first + token_of(t, 0) >= key0 + 31 && token_of(t, C::QT - 1) < cnt) weigh_tile(std::true_type{});
             else weigh_tile(std::false_type{});
             buf = buf == C::AHEAD ? 0 : buf + 1;
         }
@@ -297,54 +279,43 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
                         const int head = WIDE ? t - divided(t, p.G, p.inv_G) * p.G : min(t * C::QT + x + i, rows - 1) - safe * p.G;
                         const char* q = queries + head * head_bytes + safe * token_bytes;
                         const Base base = base_of(*reinterpret_cast<const float*>(lses + head * pitch + safe * 4));
-#pragma unroll
-                        for (int kb = 0; kb < KB; ++kb) {
-                            floatx16 s = {0};
+                        floatx16 s = {0};
 #pragma unroll 1
-                            for (int cc = 0; cc < D / 8; ++cc) s = mma_frag<float>(load16(key_row[kb] + (8 * cc + 4 * h) * 4), load16(q + (8 * cc + 4 * h) * 4), s);
-                            add(kb, s, base, std::false_type{}, last_of(token));
-                        }
+                        for (int cc = 0; cc < D / 8; ++cc) s = mma_frag<float>(load16(key_row + (8 * cc + 4 * h) * 4), load16(q + (8 * cc + 4 * h) * 4), s);
+                        add(s, base, std::false_type{}, last_of(token));
                     }
             }
         }
     }
     // Over the 32 lanes of a half, half as many numbers a step: lane i ends with number i / 2.
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int off = 16, n = 8; n; off >>= 1, n >>= 1)
 #pragma unroll
-        for (int off = 16, n = 8; n; off >>= 1, n >>= 1)
-#pragma unroll
-            for (int r = 0; r < n; ++r) {
-                const float low = sum[kb][r], high = sum[kb][r + n];
-                sum[kb][r] = (i & off ? high : low) + __shfl_xor(i & off ? low : high, off);
-            }
-        float mine = sum[kb][0] + __shfl_xor(sum[kb][0], 1);
-        const int at = acc_row(i >> 1, h);
-        if (!__shfl((int)there[kb], at)) mine = 0.f;
-        if ((i & 1) == 0) meet[w][32 * kb + at] = mine;
-    }
+        for (int r = 0; r < n; ++r) {
+            const float low = sum[r], high = sum[r + n];
+            sum[r] = (i & off ? high : low) + __shfl_xor(i & off ? low : high, off);
+        }
+    float mine = sum[0] + __shfl_xor(sum[0], 1);
+    const int at = acc_row(i >> 1, h);
+    if (!__shfl((int)there, at)) mine = 0.f;
+    if ((i & 1) == 0) meet[w][at] = mine;
     if (QW > 1) __syncthreads();
     else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (qw == 0)
+    if (qw == 0 && lane < 32 && key0 + lane < len) {
+        float v = 0.f;
 #pragma unroll
-        for (int x = 0; x < (KB + 1) / 2; ++x) {
-            const int r = 64 * x + lane;
-            if (r < 32 * KB && key0 + r < len) {
-                float v = 0.f;
-#pragma unroll
-                for (int y = 0; y < QW; ++y) v += meet[w + y][r];
-                p.weight[at0 + r] = was[x] + v;
-            }
-        }
+        for (int y = 0; y < QW; ++y) v += meet[w + y][lane];
+        p.weight[at0 + lane] = was + v;
+    }
 }
 
-template <typename T, int D, int KB, int QW, bool WIDE, bool FEW>
+template <typename T, int D, int QW, bool WIDE>
 static void launch_weigh_as(Weigh p, int units, hipStream_t st) {
-    using C = WeighCfg<T, D, KB, QW, WIDE, FEW>;
+    using C = WeighCfg<T, D, QW, WIDE>;
     static std::atomic<uint64_t> set{0};                     // more than 64 KB of LDS has to be asked for, on every device
     int dev = 0;
     if (C::LDS + 1024 > 64 * 1024 && hipGetDevice(&dev) == hipSuccess && (dev > 63 || !(set.load(std::memory_order_relaxed) >> dev & 1))) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_weigh_kernel<T, D, KB, QW, WIDE, FEW>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) == hipSuccess && dev <= 63)
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_weigh_kernel<T, D, QW, WIDE>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) == hipSuccess && dev <= 63)
             set.fetch_or(1ull << dev, std::memory_order_relaxed);        // the launch says so if it was refused
     }
     const int64_t blocks = (((int64_t)p.width << p.page_log2) + C::KEYS - 1) / C::KEYS;
@@ -358,19 +329,20 @@ static void launch_weigh_as(Weigh p, int units, hipStream_t st) {
             if (units >> log2 & 1) rounds += (blocks + (8 >> log2) - 1) >> (3 - log2);
         grid = dim3((unsigned)(8 * rounds));
     }
-    hipLaunchKernelGGL((paged_weigh_kernel<T, D, KB, QW, WIDE, FEW>), grid, dim3(256), C::LDS, st, p);
+    hipLaunchKernelGGL((paged_weigh_kernel<T, D, QW, WIDE>), grid, dim3(256), C::LDS, st, p);
 }
 template <typename T, int D>
 static int launch_weigh_t(const Weigh& p, int units, hipStream_t st) {
-    constexpr int kWide = sizeof(T) == 4 ? 1 : 2;            // planes of 64 keys are too many registers
-    const int64_t tiles = ((int64_t)p.n * p.G + 31) / 32, keys = (int64_t)units * p.width << p.page_log2;
+    const int64_t keys = (int64_t)units * p.width << p.page_log2;
+    constexpr int kTile = WeighCfg<T, D, 1, true>::QT;
     const bool wide = p.n >= 64 && p.q[2] * (int64_t)sizeof(T) < 1 << 24;            // offsets of a tile's rows fit 32 bits
     KernelTimer tm(ZIPVL_K_PAGED_WEIGH, st);
-    if (tiles < 8) launch_weigh_as<T, D, 1, 1, false, true>(p, units, st);
-    else if (!wide) launch_weigh_as<T, D, 1, 1, false, false>(p, units, st);
-    else if (keys / (32 * kWide) >= 4096) launch_weigh_as<T, D, kWide, 1, true, false>(p, units, st);
-    else if (keys / 32 >= 2048) launch_weigh_as<T, D, 1, 1, true, false>(p, units, st);
-    else launch_weigh_as<T, D, 1, 4, true, false>(p, units, st);
+    // Four waves on the same keys where waves of 32 keys each would leave the chip idle or unequal work to the last of them.  bf16, d = 128, us, four and one: 53 000 keys, 3091 tokens 157, 241;
+    // 37 000, 256 tokens 23, 27; 74 000, 64 tokens 28, 20; 110 000, 512 tokens 92, 71.
+    if (wide && keys / 32 < 2048) launch_weigh_as<T, D, 4, true>(p, units, st);
+    // Tiles of one head where their last ones are nearly full.  131 000 keys of groups of 7, us, of one head and of all: 64 tokens 24, 27; 100 (of 128 that two tiles have) 34, 30; 160 (of 192) 46, 44.
+    else if (wide && (p.n + kTile - 1) / kTile * kTile <= p.n + p.n / 8) launch_weigh_as<T, D, 1, true>(p, units, st);
+    else launch_weigh_as<T, D, 1, false>(p, units, st);
     return check_launch("paged_weigh");
 }
 
