@@ -369,6 +369,9 @@ struct KeyTile {
     __device__ __forceinline__ int32_t at(int x) const { return x == 0 ? at0 : x == 1 ? at1 : x == 2 ? at2 : at3; }
 };
 
+// Sums of the offset that stays, outside which the tiles are repeated with running maxima.
+constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p64f;
+
 // A tile of rows of one unit against the keys of its piece.
 template <typename T, int D>
 struct Many {
@@ -680,7 +683,7 @@ struct Many {
     // of the exponentials of tile t in its first half, multiplies K Q^T of tile t + 1 and takes the other half in its second: nothing in a step waits for anything
     // else in it, and the order of instructions is written out - behind every product its share of the vector work, in front of it the reads of an operand three products
     // ahead, the requests (K of tile t + 2, V of t + 1) one at a time.  The offset of the exponentials stays, or is the first tile's maximum if there was no
-    // tile before: right as long as no sum leaves the middle of the fp32 range, which the caller looks at.
+    // tile before: right as long as no sum leaves the middle of the fp32 range, which the caller asks strayed() about.
     // The steps are a loop of their own without any other way through them: with one for tiles that lack rows beside it, operands spilled in both.
     static constexpr int kAhead = 3;
     __device__ __forceinline__ void piped(int j0, int n) {
@@ -800,12 +803,21 @@ struct Many {
         weighted(buffer(true, 1), pa);
         __syncthreads();
     }
+    // Right behind piped(), before a running maximum scales the sums: whether one of the wave's is no number, infinite, or of weights that are far from 1.  Sums of V leave the range
+    // before those of the weights where V is large.
+    __device__ __forceinline__ bool strayed() const {
+        float probe[4] = {fmaf(l_rounded, 0.f, 0.f), 0.f, 0.f, 0.f};                 // no number if a sum is not finite
+#pragma unroll
+        for (int db = 0; db < C::ODB; ++db)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) probe[y & 3] = fmaf(o[db][y], 0.f, probe[y & 3]);
+        const float weights = over_groups<32>(l, [](float a, float b) { return a + b; });
+        return __any(!(weights >= kSumLow && weights <= kSumHigh) || probe[0] + probe[1] + probe[2] + probe[3] != 0.f);
+    }
 };
 
 // Planes are off by 2^-134 where a number is small: nothing in a logit or a sum as long as what it is multiplied by is below this.  A piece that meets larger numbers is done again.
 constexpr float kPlaneHigh = 0x1p100f;
-// Sums of the offset that stays, outside which the tiles are repeated with running maxima.
-constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p64f;
 
 // The kernel's arguments, read again: kept in scalar registers through the tiles they spilled.
 template <typename A>
@@ -826,7 +838,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
     using C = ChunkCfg<T, D>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     // of the workgroup, for the end; behind the tiles, which then begin where LDS does: their addresses fit an instruction's offset
-    struct Held { Place x; int b, g, rows, j0, j1, sees_from, again; };
+    struct Held { Place x; int b, g, rows, again; };
     static_assert(sizeof(Held) <= 64, "");
     Held& held = *reinterpret_cast<Held*>(smem + 4 * C::TILE);
     static_assert(sizeof(PlaceShared) <= 4 * C::TILE, "the keys' numbers stand where tiles come later");
@@ -869,7 +881,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         const int all = many.tp + scalar((many.seen + C::BN - 1) / C::BN);
         j0 = scalar((int)((int64_t)all * x.piece / x.pieces));
         j1 = scalar((int)((int64_t)all * (x.piece + 1) / x.pieces));
-        if (tid == 0) held = {x, v.b, v.g, v.rows, j0, j1, j0 < j1 ? j0 < many.tp ? INT32_MIN : (j0 - many.tp) * C::BN : INT32_MAX, 0};
+        if (tid == 0) held = {x, v.b, v.g, v.rows, 0};
         int r = min(many.r_first + many.i, many.r_last);
         if (x.group >= 0) {
             const int2 at = packed_row(p, sh, x.group, v.g, r);
@@ -900,7 +912,6 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
         e.token = divided(min(e.r, e.r_last), p.G, p.inv_G);
         return e;
     };
-    float l;
     if constexpr (sizeof(T) == 2) {
         for (bool safe = many.lacks_pages(j0, j1);; safe = true) {
             many.reset();
@@ -910,16 +921,14 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
                 const int clean = own ? max(j, many.tp + many.clean_own()) : many.prefix_rows / C::BN, n = max(0, min(clean, j1) - j) & ~1;
                 if (!safe && n >= 4) {
                     many.piped(j, n);
+                    if (many.wave_last != -2 && many.strayed() && threadIdx.x % 64 == 0) held.again = 1;       // of waves that have rows
                     j += n;
                 }
                 const int upto = own ? j1 : min(j1, max(j, many.tp));
                 many.template plain<false>(j, upto);
                 j = upto;
             }
-            l = both(many.l);
             if (safe) break;
-            const bool sees = many.wave_last != -2 && many.before + end(read_again<Chunk>(0)).token >= held.sees_from;      // a key of the piece
-            if (__any(sees && !(l >= kSumLow && l <= kSumHigh)) && threadIdx.x % 64 == 0) held.again = 1;
             __syncthreads();
             if (!scalar(held.again)) break;
         }
@@ -933,10 +942,9 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
             many.reset();
             many.template plain<false>(j0, j1);
         }
-        l = both(many.l);
     }
     const Chunk p = read_again<Chunk>(0);
-    const float m = many.m, weight = sizeof(T) == 2 ? both(many.l_rounded) : l;      // what V was weighed by
+    const float m = many.m, l = both(many.l), weight = sizeof(T) == 2 ? both(many.l_rounded) : l;      // what V was weighed by
     const End e = end(p);
     if (e.r > e.r_last) return;
     const RowAt at = {e.token, e.g * p.G + e.r - e.token * p.G};

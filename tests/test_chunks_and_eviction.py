@@ -285,6 +285,31 @@ def test_chunk_attn_paged_of_groups_with_large_logits_and_missing_pages(dtype, d
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hot,late,values", [(43.75, 41.5, 8.0), (43.75, 41.5, 1000.0), (17.5, 0.0, 2.0 ** 80), (60.0, 55.0, 1.0)])
+@pytest.mark.parametrize("where", ["own", "prefix", "packed"])
+def test_chunk_attn_paged_of_keys_far_above_the_first(where, hot, late, values, d):
+    """Tiles of 64 keys whose first has logits near 0 and a later one a logit of 2 `hot`, then new tokens' keys of 2 `late`: whatever the sums are by the first maximum, the outputs
+    are those of the formula.  In powers of two 17.5, 41.5 and 43.75 are 50, 120 and 126."""
+    say(f"hot {where} {hot} {late} {values} {d}")
+    n = 70
+    if where == "own":
+        s = Setting(1, 1, 1, n, d, "bf16", 16, [384], seed=51, spare=0)
+    else:
+        B = 1 if where == "prefix" else 2
+        s = Setting(B, 1, 1, n, d, "bf16", 16, [96], None, (0, B), (256,), seed=51, spare=0)
+    tab, at = (s.table, 150) if where == "own" else (s.prefix_table, 150)
+    s.V.mul_(values)
+    s.Q[..., 0] = 2.0 * math.sqrt(d)                          # times the scale: 2
+    s.K[..., 0] = 0.0
+    s.K[int(tab[0, at // 16]), at % 16, 0] = hot
+    for u, L in enumerate(s.lens):
+        for r in range(L - n, L):
+            s.K[int(s.table[u, r // 16]), r % 16, 0] = late
+    assert_chunk(s, *chunk(s))
+
+
+@pytest.mark.gpu
 def test_chunk_attn_paged_of_one_token_is_decode():
     s = Setting(4, 28, 4, 1, 128, "bf16", 64, [500, 1, 70, 1300], None, (0, 3, 4), (300, 41), seed=10)
     cache = s.cache()
