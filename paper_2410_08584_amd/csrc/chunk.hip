@@ -369,6 +369,10 @@ struct KeyTile {
     __device__ __forceinline__ int32_t at(int x) const { return x == 0 ? at0 : x == 1 ? at1 : x == 2 ? at2 : at3; }
 };
 
+// Planes are off by 2^-134 where a number is small.  In a logit that is nothing as long as what the number is multiplied by is below kPlaneHigh.  In an output, times the sum of its
+// weights, it is nothing beside kOutLow, where values are off, and beside kOutLowOfMost times the largest value, where weights are.  A piece that meets larger numbers or has smaller
+// outputs is done again.
+constexpr float kPlaneHigh = 0x1p100f, kOutLow = 0x1p-80f, kOutLowOfMost = 0x1p-90f;
 // Sums of the offset that stays, outside which the tiles are repeated with running maxima.
 constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p64f;
 
@@ -814,10 +818,17 @@ struct Many {
         const float weights = over_groups<32>(l, [](float a, float b) { return a + b; });
         return __any(!(weights >= kSumLow && weights <= kSumHigh) || probe[0] + probe[1] + probe[2] + probe[3] != 0.f);
     }
+    // fp32, behind plain<true>(): whether numbers were larger, or outputs are smaller, than planes hold with all bits.  Outputs of 0 pass: of values that are 0.
+    __device__ __forceinline__ bool exceeds_planes() const {
+        Least least;
+#pragma unroll
+        for (int db = 0; db < C::ODB; ++db)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) least.add(__float_as_uint(o[db][y]));
+        const float weights = over_groups<32>(l, [](float a, float b) { return a + b; });
+        return __any(!(most < kPlaneHigh) || least.below(fmaxf(kOutLow, kOutLowOfMost * wave_max(most)) * fmaxf(weights, 1.f)));
+    }
 };
-
-// Planes are off by 2^-134 where a number is small: nothing in a logit or a sum as long as what it is multiplied by is below this.  A piece that meets larger numbers is done again.
-constexpr float kPlaneHigh = 0x1p100f;
 
 // The kernel's arguments, read again: kept in scalar registers through the tiles they spilled.
 template <typename A>
@@ -935,7 +946,7 @@ __global__ __launch_bounds__(256, 2) void chunk_many_kernel(Chunk p_, ChunkParts
     } else {
         many.reset();
         many.template plain<true>(j0, j1);
-        if (__any(!(many.most < kPlaneHigh)) && threadIdx.x % 64 == 0) held.again = 1;
+        if (many.exceeds_planes() && threadIdx.x % 64 == 0) held.again = 1;
         __syncthreads();
         if (scalar(held.again)) {                            // in fp32 products
             many.load_queries(query_at[threadIdx.x / 64 * 32 + threadIdx.x % 32]);

@@ -266,6 +266,18 @@ def test_chunk_attn_paged_of_huge_and_small_numbers(d, n, of_queries, of_values)
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,groups", [(3, ()), (70, ()), (70, (0, 2))])
+@pytest.mark.parametrize("of_values", [2.0 ** -110, 2.0 ** -122])
+def test_chunk_attn_paged_of_values_near_the_smallest(d, n, groups, of_values):
+    """fp32 values whose third plane of bf16 would end below bf16's smallest number: the outputs have all their bits."""
+    say(f"small values {d} {n} {groups} {of_values}")
+    s = Setting(2, 4, 2, n, d, "f32", 16, [200, 100, 80, 75], None, groups, (300, 70), seed=52)
+    s.V.mul_(of_values)
+    assert_chunk(s, *chunk(s))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 @pytest.mark.parametrize("gain", [40.0, 1.0])
 def test_chunk_attn_paged_of_groups_with_large_logits_and_missing_pages(dtype, d, gain):
