@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
     auto base_of = [&](float lse) {
         const float whole = rintf(lse * kLog2e);
         Base x = {whole, fast_exp2(fmaf(-lse, kLog2e, whole))};
-        if (__builtin_isinf(lse)) x = {1e9f, 0.f};           // a query that sees nothing weighs nothing
+        if (__builtin_isinf(lse)) x = {INFINITY, 0.f};       // a query that sees nothing weighs nothing, whatever its logits are
         return x;
     };
     auto add = [&](const floatx16& s, const Base& base, auto whole, int last) __attribute__((always_inline)) {
@@ -270,34 +270,41 @@ __global__ __launch_bounds__(256, 2) void paged_weigh_kernel(Weigh p) {
             else weigh_tile(std::false_type{});
             buf = buf == C::AHEAD ? 0 : buf + 1;
         }
-        if constexpr (sizeof(T) == 4) {
-            if (__any(!(most < kPlaneHigh))) {
-                clear();
-                for (int t = t0; t < t1; t += QW)
-                    for (int x = 0; x < C::QT; x += 32) {
-                        const int token = token_of(t, x + i), safe = min(token, cnt - 1);
-                        const int head = WIDE ? t - divided(t, p.G, p.inv_G) * p.G : min(t * C::QT + x + i, rows - 1) - safe * p.G;
-                        const char* q = queries + head * head_bytes + safe * token_bytes;
-                        const Base base = base_of(*reinterpret_cast<const float*>(lses + head * pitch + safe * 4));
-                        floatx16 s = {0};
-#pragma unroll 1
-                        for (int cc = 0; cc < D / 8; ++cc) s = mma_frag<float>(load16(key_row + (8 * cc + 4 * h) * 4), load16(q + (8 * cc + 4 * h) * 4), s);
-                        add(s, base, std::false_type{}, last_of(token));
-                    }
-            }
-        }
     }
-    // Over the 32 lanes of a half, half as many numbers a step: lane i ends with number i / 2.
+    const int at = acc_row(i >> 1, h);                       // the row whose sum the lane ends with
+    float mine;
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+        if (again) {
+            clear();
+            for (int t = t0; t < t1; t += QW)
+                for (int x = 0; x < C::QT; x += 32) {
+                    const int token = token_of(t, x + i), safe = min(token, cnt - 1);
+                    const int head = WIDE ? t - divided(t, p.G, p.inv_G) * p.G : min(t * C::QT + x + i, rows - 1) - safe * p.G;
+                    const char* q = queries + head * head_bytes + safe * token_bytes;
+                    const Base base = base_of(*reinterpret_cast<const float*>(lses + head * pitch + safe * 4));
+                    floatx16 s = {0};
+#pragma unroll 1
+                    for (int c16 = 16 * h; c16 < C::RB; c16 += 32) s = mma_frag<T>(load16(key_row + c16), load16(q + c16), s);
 #pragma unroll
-    for (int off = 16, n = 8; n; off >>= 1, n >>= 1)
-#pragma unroll
-        for (int r = 0; r < n; ++r) {
-            const float low = sum[r], high = sum[r + n];
-            sum[r] = (i & off ? high : low) + __shfl_xor(i & off ? low : high, off);
+                    for (int r = 0; r < 16; ++r) s[r] = base.factor == 0.f ? 0.f : s[r];
+                    add(s, base, std::false_type{}, last_of(token));
+                }
         }
-    float mine = sum[0] + __shfl_xor(sum[0], 1);
-    const int at = acc_row(i >> 1, h);
-    if (!__shfl((int)there, at)) mine = 0.f;
+        // Over the 32 lanes of a half, half as many numbers a step: lane i ends with number i / 2.
+#pragma unroll
+        for (int off = 16, n = 8; n; off >>= 1, n >>= 1)
+#pragma unroll
+            for (int r = 0; r < n; ++r) {
+                const float low = sum[r], high = sum[r + n];
+                sum[r] = (i & off ? high : low) + __shfl_xor(i & off ? low : high, off);
+            }
+        mine = sum[0] + __shfl_xor(sum[0], 1);
+        if (!__shfl((int)there, at)) mine = 0.f;
+        // Once more, with operands from memory: numbers that planes do not hold, in fp32 products; and a sum that is not finite, since a query that weighs nothing may have logits that are
+        // not, and 0 times their exponentials is no number.
+        if (again || !__any(!(most < kPlaneHigh) || mine * 0.f != 0.f)) break;
+    }
     if ((i & 1) == 0) meet[w][at] = mine;
     if (QW > 1) __syncthreads();
     else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

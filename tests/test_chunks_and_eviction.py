@@ -488,6 +488,23 @@ def test_paged_weigh_of_huge_numbers(n, of_queries):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("n,spare", [(3, 1), (70, 1), (64, 300), (70, 300)])
+@pytest.mark.parametrize("size", [1e10, 1e30, 3e38])
+def test_paged_weigh_of_queries_that_weigh_nothing(dtype, d, n, spare, size):
+    """An lse of -infinity leaves a query out, however large its (finite) numbers are."""
+    say(f"weigh nothing {dtype} {d} {n} {spare} {size}")
+    s = Setting(1, 4, 2, n, d, dtype, 256, [300, 90], None, seed=53, spare=spare)
+    _, lse = chunk(s)
+    out = (torch.arange(n) % 3 == 1).to(DEV)
+    lse[:, 1:3, out] = -math.inf
+    Q = s.Q.clone()
+    Q[:, 1:3, out] = torch.where(Q[:, 1:3, out] < 0, -size, size).to(s.dtype)
+    w = z.zipvl_paged_weigh(Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale)
+    assert_weights(s, w, lse, None)                           # which gives such queries' weights as 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [1, 4, 50])
 def test_paged_weigh_skips_rows_without_a_page_and_clamps_lengths(n):
     s = Setting(2, 4, 2, n, 128, "bf16", 16, [200, 77, 150, 64], None, seed=18)
