@@ -224,6 +224,34 @@ def test_chunk_attn_paged_of_thousands_of_units(n, lens):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,n,B,tile,wgs,groups", [("bf16", 64, 40, 540, 64, 512, ()), ("bf16", 128, 40, 400, 64, 512, ()), ("bf16", 64, 40, 300, 64, 512, ()), ("f32", 64, 36, 520, 32, 512, ()),
+                                                         ("bf16", 64, 2, 540, 32, 512, ()), ("f32", 128, 3, 300, 32, 256, ()), ("bf16", 64, 4, 400, 64, 512, (0, 40, 400)),
+                                                         ("f32", 64, 4, 500, 32, 512, (0, 200, 500))])
+def test_chunk_attn_paged_of_many_short_units_and_few_long_ones(dtype, d, n, B, tile, wgs, groups):
+    """Hundreds of tiles of rows that have a workgroup each leave too few for the pieces of the long ones: pieces are made larger, in one case after another."""
+    say(f"short and long {dtype} {d} {n} {B} {groups}")
+    s = Setting(B, 1, 1, n, d, dtype, 16, [n, n + 5, n + 14], None, groups, (70, 33), seed=54, spare=0)
+    width = 400 * tile // 16
+    s.table = torch.randint(0, s.K.shape[0], (B, width), generator=torch.Generator().manual_seed(55)).to(torch.int32)
+    long = [3, B // 2, B // 2 + 1, B - 1]
+    for u in long:
+        s.lens[u] = 400 * tile - u % 7
+    # the pieces, as the device counts them: a tile of rows is cut into its tiles of keys / q, at least one
+    loads = [-(-L // tile) for L in s.lens]
+    items = B
+    if groups:
+        P = len(groups) - 1
+        for p in range(P):
+            packed = n * (groups[p + 1] - groups[p])
+            loads += [-(-s.pre[p] // tile)] * -(-packed // 128)
+        items += B * n // 128 + P + 1
+    limit = max(wgs + 64, (items + 21) // 8 * 8) - 14
+    q = max(4, -(-sum(loads) // wgs))
+    assert items <= 2048 and sum(max(1, x // q) for x in loads) > limit
+    assert_chunk(s, *chunk(s))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [1, 4, 50])
 def test_chunk_attn_paged_skips_rows_without_a_page_and_clamps_lengths(dtype, n):
@@ -471,6 +499,48 @@ def test_paged_weigh_of_many_queries(B, Hkv, n, dtype):
     s = Setting(B, 2 * Hkv, Hkv, n, 64 if B > 2 else 128, dtype, 64, [90, 300, 33, 1], [n, n - 5, 40, n], seed=21)
     _, lse = chunk(s)
     w = z.zipvl_paged_weigh(s.Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale, k=s.ints(s.k))
+    assert_weights(s, w, lse, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,n", [("bf16", 128, 64), ("bf16", 128, 127), ("bf16", 64, 128), ("bf16", 64, 180), ("f32", 128, 64), ("f32", 128, 95), ("f32", 64, 96), ("f32", 64, 90)])
+def test_paged_weigh_of_tiles_of_one_head(dtype, d, n):
+    """Room for many rows, and tokens that nearly fill their last tile: waves share tiles of one head."""
+    say(f"weigh one head {dtype} {d} {n}")
+    s = Setting(2, 6, 2, n, d, dtype, 256, [700, 90, n, 300], [n, 33, n - 1, 1], order="token", seed=56, spare=64)
+    tile = 64 if dtype == "bf16" else 32
+    assert s.table.numel() * s.page // 32 >= 2048 and -(-n // tile) * tile <= n + n // 8
+    s.table[0, 1] = -1
+    _, lse = chunk(s)
+    s.spoil()
+    weight = torch.full((4, s.table.shape[1] * s.page), 7.0, device=DEV)
+    z.zipvl_paged_weigh(s.Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale, k=s.ints(s.k), weight=weight)
+    assert_weights(s, weight, lse, None, fill=7.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,G,n,d,dtype", [(13, 2, 7680, 64, "bf16"), (7, 4, 1760, 128, "f32")])
+def test_paged_weigh_of_many_queries_in_tiles_of_one_head(B, G, n, d, dtype):
+    """As before, with more queries than the caches hold, so that units are dealt out another way: eight, four, two and one at a time."""
+    say(f"weigh many queries, one head {B} {G} {n} {d} {dtype}")
+    s = Setting(B, G, 1, n, d, dtype, 64, [90, 300, 33, 1], [n, n - 5, 40, n], seed=57, spare=148)
+    tile = 64 if dtype == "bf16" else 32
+    assert s.table.numel() * s.page // 32 >= 2048 and -(-n // tile) * tile <= n + n // 8 and s.Q.numel() * s.Q.element_size() >= 24 << 20
+    _, lse = chunk(s)
+    w = z.zipvl_paged_weigh(s.Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale, k=s.ints(s.k))
+    assert_weights(s, w, lse, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n", [(64, 64), (128, 96)])
+@pytest.mark.parametrize("of_queries", [2.0 ** 101, 2.0 ** -101])
+def test_paged_weigh_of_huge_numbers_in_tiles_of_one_head(d, n, of_queries):
+    s = Setting(1, 4, 2, n, d, "f32", 256, [200, 100], None, seed=58, spare=128)
+    assert s.table.numel() * s.page // 32 >= 2048
+    _, lse = chunk(s)
+    s.Q.mul_(of_queries)
+    s.K.mul_(1 / of_queries)
+    w = z.zipvl_paged_weigh(s.Q, s.cache(), s.table.to(DEV), s.ints(s.lens), lse, s.scale)
     assert_weights(s, w, lse, None)
 
 
