@@ -190,7 +190,8 @@ int zipvl_share_scores(const float* mass, const float* rank, int B, int Hkv, int
  * 2^-26 of it; a workgroup with a query element outside [2^-100, 2^90] or an output below 2^-80 (0 apart), where parts would
  * be cut short, repeats its keys in fp32 products.  Logits of any finite magnitude are handled: rows whose scaled logits all lie within about
  * +-44 of zero are exponentiated without an offset, a workgroup with any other row repeats its keys with running
- * maxima (twice the time for that workgroup, up to three times for fp32; the same result up to rounding).  Inputs must be finite.
+ * maxima (twice the time for that workgroup, up to three times for fp32; the same result up to rounding).  Inputs must be finite, and values of a
+ * bf16 call that are not 0 between 2^-60 and 2^60: where exponentials have no offset, they are weighed by up to 2^64 and from 2^-64 on before they are divided.
  */
 int zipvl_sparse_prefill(const void* Q, const void* K, const void* V, const zipvl_dims* dims,
                          const int32_t* idx, const int32_t* k, float softmax_scale, int flags,
@@ -398,8 +399,9 @@ int zipvl_decode_attn_paged(const void* q, const zipvl_pages* pages, const int32
  * overlapping no input.  lse [device] fp32 [B,Hq,n] contiguous, or NULL.  Any Hq / Hkv; n * Hq / Hkv < 2^30.
  * Lengths are clamped to [0, pages of the table * page].  Nothing behind a length is read.  Inputs that are read must be finite.
  * Numerics: scores, statistics and sums in fp32, one rounding at the end; where a unit has more than 32 queries (n * Hq / Hkv), or the units of a group, which are two or more on
- * average, have together (B / groups times as many), the weights of a bf16 call are rounded to bf16 before they weigh V, and O is divided by the sum of those, lse is of the weights as they were.  The order of all sums follows from the sizes and lengths: the same call
- * gives the same bits.
+ * average, have together (B / groups times as many), the weights of a bf16 call are rounded to bf16 before they weigh V, and O is divided by the sum of those, lse is of the weights as they were
+ * (so groups change how a call of fewer queries rounds).  V is summed undivided, by weights of up to 2^8: 2^8 times a query's rows times the largest value must stay below 2^128.  fp32 values below
+ * 2^-126 may count as 0.  The order of all sums follows from the sizes and lengths: the same call gives the same bits.
  * ws [device] zipvl_workspace_bytes(ZIPVL_OP_CHUNK_PAGED, dims, m) bytes, 16-byte aligned, holds nothing between calls (two calls that overlap on one
  * workspace race): for any number of groups, up to 36 MB, and up to 172 MB where a group's queries may be put together (B >= 2, up to 512 queries a unit).
  */
@@ -413,7 +415,8 @@ int zipvl_chunk_attn_paged(const void* Q, const zipvl_pages* pages, const int32_
  *   weight[u,r] = before[u,r] + sum over heads h of the group and queries i < c with r <= len[u] - c + i of exp( Q[b,h,i] . K_r * softmax_scale - lse[b,h,i] )
  * for r < len[u]; what stands from len[u] on is left as it is.  c, k, len, table and Q as for zipvl_chunk_attn_paged, whose lse this takes (with a prefix the weights
  * of own rows are what the prefix has left of 1).  Only the last m of a call's queries: Q and lse from there on, n = m, the same len.
- * lse [device] fp32: query i of head h at lse[(b*Hq + h) * lse_pitch + i], lse_pitch >= n; -infinity: the query weighs nothing.
+ * Rows of a prefix get no weights: queries of many units see them, and all of them see all, which is not the end that own rows have.
+ * lse [device] fp32: query i of head h at lse[(b*Hq + h) * lse_pitch + i], lse_pitch >= n; infinite: the query weighs nothing.
  * before, weight [device] fp32 [B*Hkv, table_pages * page] contiguous; before may be weight itself or NULL (zeros); weight overlaps no other input.
  * Rows in pages that are not there get nothing.  Inputs that are read must be finite (lse apart).
  * Numerics: fp32; the same call gives the same bits.  pages->V is not looked at.

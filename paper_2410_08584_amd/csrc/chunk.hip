@@ -4,7 +4,7 @@
 // A unit (batch element, KV head) has c G rows of queries, the G heads of its group token by token, so that a key that is met serves all heads of the group.
 // They go in tiles of rows against the prefix of the unit's group and then its own rows, up to the row that the tile's last token stands in.
 // Two forms:
-//   few     up to 32 rows a unit: memory-bound.  Each wave has all of them and tiles of 32 keys of its own (wavepart.h, as decode).  Four tokens each of 16 conversations of up to 33 000
+//   few     up to 32 rows a unit, not packed: memory-bound.  Each wave has all of them and tiles of 32 keys of its own (wavepart.h, as decode).  Four tokens each of 16 conversations of up to 33 000
 //           rows, bf16: 78 us for 341 MB, 4.4 TB/s.
 //   many    128 rows a workgroup, 32 a wave; tiles of keys in LDS are shared by the four waves, two deep, or three where whole tiles of bf16 follow each other (piped).  2048 tokens of 28
 //           heads on 4 behind 16 384, bf16: 492 us, 1.0 PFLOP/s, the matrix units busy 54 % of the time, of a large product 1.14 (543 us two deep throughout, 506 with the third).
@@ -369,10 +369,9 @@ struct KeyTile {
     __device__ __forceinline__ int32_t at(int x) const { return x == 0 ? at0 : x == 1 ? at1 : x == 2 ? at2 : at3; }
 };
 
-// Planes are off by 2^-134 where a number is small.  In a logit that is nothing as long as what the number is multiplied by is below kPlaneHigh.  In an output, times the sum of its
-// weights, it is nothing beside kOutLow, where values are off, and beside kOutLowOfMost times the largest value, where weights are.  A piece that meets larger numbers or has smaller
-// outputs is done again.
-constexpr float kPlaneHigh = 0x1p100f, kOutLow = 0x1p-80f, kOutLowOfMost = 0x1p-90f;
+// What planes are off by where a number is small (planes.h), 2^-134, is nothing in an output, times the sum of its weights, beside kOutLow, where values are off, and beside
+// kOutLowOfMost times the largest value, where weights are.  A piece with smaller outputs is done again.
+constexpr float kOutLow = 0x1p-80f, kOutLowOfMost = 0x1p-90f;
 // Sums of the offset that stays, outside which the tiles are repeated with running maxima.
 constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p64f;
 
@@ -643,6 +642,8 @@ struct Many {
                     l += s[blk][y];
                 }
                 if constexpr (sizeof(T) == 2) {
+                    // Rounded to bf16, and what they are divided by is the sum of the rounded ones: three planes, as few queries have them, would be four products where these are two.  Of an output
+                    // the weights' roundings leave 0.7e-3 to 1.4e-3 (2-norm), its own 1.67e-3.
 #pragma unroll
                     for (int s2 = 0; s2 < 2; ++s2) {
                         uintx4 pf;

@@ -20,7 +20,7 @@ constexpr int kDigit = 11, kDigits = 1 << kDigit;            // a key of 32 bits
 // 1000 15.7, 12.5.
 constexpr int kMovesHere = 256;
 
-struct Late { int row, token; float weight; int unused; };   // a row at or behind k that stays
+struct Late { int row, token; float weight; int unused; };   // a row at or behind k that stays; token and weight: of evict_sweep_kernel, whose second look at them would be another sweep
 struct Evict {
     const int32_t* len; const int32_t* k;
     const float* weight; const int32_t* tokens;
@@ -431,7 +431,8 @@ __global__ __launch_bounds__(64 * WAVES) void evict_select_kernel(Evict p) {
     }
 }
 
-// Units of any length, whose keys do not fit LDS: the same, in sweeps over the rows, 1024 at a time.
+// Units of any length, whose keys do not fit LDS: the same, in sweeps over the rows, 1024 at a time.  4 units of 36 928 rows, 8192 to stay, with the moves 176 us (36 864 in the form before: 52), of
+// 131 072, 16 384 to stay, 593.
 template <int RB>
 __global__ __launch_bounds__(1024) void evict_sweep_kernel(Evict p) {
     constexpr int kWaves = 16, kThreads = 1024;
@@ -529,7 +530,8 @@ template <int RB>
 static int launch_evict_t(const Evict& p, int units, hipStream_t st) {
     {
         KernelTimer tm(ZIPVL_K_PAGED_EVICT, st);
-        // four waves for short units, of which a CU then has several: 3200 units of 500 rows 25 us, 79 with 16 waves; 256 units as long
+        // By the tables' width, which the host knows: 256 units of 2064 rows, 16 to leave, take 9 us where tables hold 2112 rows, 19 at 4096 (a second launch moves), 35 at 36 864, 31 behind.
+        // Four waves for short units, of which a CU then has several: 3200 units of 500 rows 25 us, 79 with 16 waves; 256 units as long
         if (p.room <= 1024) hipLaunchKernelGGL((evict_select_kernel<4, 1, RB>), dim3(units), dim3(256), 1024 * 4, st, p);
         else if (p.room <= 4096) hipLaunchKernelGGL((evict_select_kernel<16, 1, RB>), dim3(units), dim3(1024), 4096 * 4, st, p);
         else if (p.room <= kRoundsMost * 4096) {

@@ -14,6 +14,9 @@ struct Least {
     __device__ __forceinline__ void add(uint32_t x) { key = min(key, 2 * x - 1); }
     __device__ __forceinline__ bool below(float x) const { return key < 2 * __float_as_uint(x) - 1; }        // x > 0
 };
+// Planes are off by 2^-134 where a number is small: nothing in a logit as long as what the number is multiplied by is below this.  Tiles that meet larger numbers are taken again, in fp32
+// products.
+constexpr float kPlaneHigh = 0x1p100f;
 // x - the low (high) half of a packed pair, in one instruction
 // (the factors through a register: as a constant 0xBF800000 is taken for the float -1)
 __device__ __forceinline__ float less_half(float x, uint32_t pair, uint32_t factors) {

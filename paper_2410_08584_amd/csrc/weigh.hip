@@ -1,10 +1,11 @@
 // The attention weight that cached rows get from new queries: weight[u, r] = before[u, r] + sum over heads and tokens of exp(scale q.k - lse).
 //
-// Keys stay, queries come: a wave has 32 or 64 keys in registers, S = K Q^T on matrix tiles gives a lane one query and 16 keys of each 32, whose exponentials it
+// Keys stay, queries come: a wave has 32 keys in registers, S = K Q^T on matrix tiles gives a lane one query and 16 keys of each 32, whose exponentials it
 // adds up over all queries; the 32 lanes, and the waves that share keys, meet once, at the end.  No sum crosses workgroups and no wave waits for another before that, so no order of
 // arrival changes a result.  Queries come through LDS, tiles ahead.
 // fp32 numbers go as three planes of bf16 (planes.h): six products instead of one that takes sixteen times as long.
-// Few queries (a decode step) are bound by the read of K, many by products and by exponentials at a quarter of the vector rate.
+// Few queries (a decode step) are bound by the read of K, many by products, the exponentials between them (64 queries over a video's cache, bf16: the matrix units are busy 23 % of 20 us, the exponentials and
+// their sums take 5 us of vector instructions) and the rest by a barrier a tile and by workgroups that are not a whole number a CU.
 #include <atomic>
 
 #include "launch.h"
@@ -53,10 +54,6 @@ template <> struct Rows<float> {
         return {load16(row + swz_chunk(4 * cc + 2 * h, sw)), load16(row + swz_chunk(4 * cc + 2 * h + 1, sw))};
     }
 };
-// Planes are off by 2^-134 where a number is small (planes.h): nothing in a logit as long as what it is multiplied by is below this.  A wave that meets larger
-// numbers takes its tiles in fp32 products.
-constexpr float kPlaneHigh = 0x1p100f;
-
 // 32 keys a wave.  QW = 1: the four waves have keys of their own and share tiles of queries; 4: they have the same keys and take every fourth tile, each from LDS of its own.
 // A tile is of queries that follow each other head by head, token by token, or, WIDE, of tokens of one head: its rows are then at one distance and asked for without a
 // vector instruction, and n is long enough that a last tile with few tokens is no loss.
